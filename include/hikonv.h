@@ -440,6 +440,85 @@ typedef enum {
 int hikonv_pipe_rate(int kind, int iters, uint32_t *d_scratch_word, double *h_ops_per_second,
                      double *h_lanes_per_clock_per_sm, void *stream);
 
+/*
+ * hikonv_quantize_rows - rows of floats to signed or unsigned codes with one scale per row.
+ *   x: [M][K] of x_type (hikonv_out_type: F32, F16 or BF16), row r starting at element r * x_row_stride (0 when all rows
+ *      are one); columns are contiguous, elements naturally aligned.
+ *   signed:   scale[r] = max_k |x[r][k]| / (2^(bits-1) - 1), bits in 2..8
+ *   unsigned: scale[r] = max(0, max_k x[r][k]) / (2^bits - 1), bits in 1..8
+ *   codes[r][k] = clamp(round(x[r][k] / scale[r]), lo, hi), divisions in 32 bits, rounded to nearest, ties to even.
+ * Codes are stored one per byte, rows without gaps; scales are float.  A row of zeros (unsigned: without a positive value)
+ * has scale 0 and codes 0.  A row with a NaN has scale NaN; a row whose largest magnitude is infinite has scale infinity; a
+ * quotient that is NaN has code 0 (so what is computed from such a row is NaN, as 0 times its scale is).  Subnormal
+ * inputs and scales are kept.  Codes and scales must not overlap x.  M == 0 launches nothing; K >= 1.
+ */
+typedef enum {
+    HIKONV_OUT_SUMS = 0,  /* exact int32 sums                                       */
+    HIKONV_OUT_CODES = 1, /* requantised codes, one per byte                        */
+    HIKONV_OUT_F32 = 2,
+    HIKONV_OUT_F16 = 3,
+    HIKONV_OUT_BF16 = 4
+} hikonv_out_type;
+
+typedef enum {
+    HIKONV_ACT_NONE = 0,
+    HIKONV_ACT_RELU = 1, /* max(v, 0)                         */
+    HIKONV_ACT_SILU = 2, /* v / (1 + exp(-v))                 */
+    HIKONV_ACT_GELU = 3  /* v (1 + erf(v / sqrt(2))) / 2      */
+} hikonv_activation;
+
+int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, int M, int K, int bits, int is_signed,
+                         int8_t *d_codes, float *d_scale, void *stream);
+
+/*
+ * hikonv_linear - matrix product of codes with everything that follows it in the same launch.
+ * (The paper's layers are convolutions; a fully connected layer is the 1x1 convolution of one pixel per row.  Its depth is
+ * long and nothing overlaps, so the products run on byte dot products and tensor cores instead of packed words.)
+ *   sum[m][n] = sum_k x[m][k] w[n][k], exact
+ *   SUMS:            out = sum                                                       (int32)
+ *   CODES:           out = clamp((sum + bias[n]) >> shift, lo, hi), arithmetic shift, bias int32 or NULL; the addition does
+ *                    not wrap; 0 <= shift <= 31, -128 <= lo <= hi <= 255            (one byte)
+ *   F32, F16, BF16:  out = act(sum x_scale[m] w_scale[n] + bias[n]) + residual[m][n] (32-bit arithmetic, rounded once)
+ *                    x_scale, w_scale, bias: float or NULL (1, 1, 0); residual: of the output's type, or NULL
+ *   x: [M][K] codes of p bits, one per byte, row m starting x_row_stride bytes after row m - 1 (>= K).
+ *   w: [N][K] codes of q bits, rows without gaps: w_store_bits 8 (one per byte), or q in {1, 2, 4} (dense: 8 / q codes per byte, the
+ *      first in the lowest bits, two's complement when signed; K q a multiple of 8, else HIKONV_ERR_UNSUPPORTED).
+ *   out, residual: [M][N], rows out_row_stride / residual_row_stride elements apart (>= N).
+ * Arguments that belong to another output type must be NULL or 0, else HIKONV_ERR_INVALID_ARG.
+ * Depth: K max|x| W <= 2^31 - 1 with W = 128 for signed weights (dense ones are multiplied as the upper bits of a byte) and
+ * 2^q - 1 for unsigned ones, else HIKONV_ERR_NO_FIT.
+ * out must not overlap any input, except that it may be the residual itself (same address and stride), else
+ * HIKONV_ERR_INVALID_ARG.  M == 0 launches nothing; N, K >= 1.  Any alignment of codes is accepted; rows of x and w that
+ * start on 16-byte boundaries are read fastest.  No workspace is needed.
+ */
+typedef struct {
+    int out_type;                   /* hikonv_out_type                                             */
+    int activation;                 /* hikonv_activation; F32, F16, BF16 only                      */
+    const float *d_x_scale;         /* [M]                                                         */
+    const float *d_w_scale;         /* [N] (grouped: [E][N])                                       */
+    const void *d_bias;             /* [N] (grouped: [E][N]), float; CODES: int32                  */
+    const void *d_residual;         /* [M][N] of the output's type                                 */
+    long long residual_row_stride;  /* in elements                                                 */
+    int shift, lo, hi;              /* CODES                                                       */
+} hikonv_epilogue_t;
+
+int hikonv_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, int M, int N, int K, int p, int q,
+                  int x_signed, int w_signed, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream);
+
+/*
+ * hikonv_grouped_linear - hikonv_linear with one matrix of weights per group of rows (the experts of a mixture).
+ *   x: [T][K]; w: [E][N][K]; rows offsets[e] .. offsets[e + 1] - 1 of x, residual and out belong to matrix e.
+ *   offsets: E + 1 int32 on the DEVICE, not decreasing, within 0 .. T; the host never reads them, so a call can be captured
+ *   into a graph and replayed with other groups.  Rows in front of offsets[0] and behind offsets[E] - 1 are left as they
+ *   were.  Offsets outside 0 .. T are taken as the nearest bound, and a group that ends before it begins as empty: no
+ *   memory outside the tensors is touched, but rows that two groups claim are undefined.
+ *   1 <= E <= HIKONV_MAX_GROUPS, T == 0 launches nothing.  Everything else as for hikonv_linear with M = T.
+ */
+#define HIKONV_MAX_GROUPS 1024
+int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, const int32_t *d_offsets, int E,
+                          int T, int N, int K, int p, int q, int x_signed, int w_signed, void *d_out, long long out_row_stride,
+                          const hikonv_epilogue_t *epilogue, void *stream);
+
 const char *hikonv_status_string(int status);
 
 #ifdef __cplusplus

@@ -4,7 +4,7 @@ PyTorch is used for device memory and streams; every arithmetic step runs in the
 library.  Loading fails loudly when the library has not been built: there is no fallback.
 
 The calls of every step (``conv1d``, ``conv1d_dense``, ``pack``, ``conv2d``, ``conv2d_dense`` without tuning record and
-explicit stream) go through the extension module ``_fast`` first, which makes the same checks on the tensors natively and
+explicit stream, ``quantize_rows``, ``linear`` and ``grouped_linear`` without explicit stream) go through the extension module ``_fast`` first, which makes the same checks on the tensors natively and
 returns None where anything is amiss; the Python code below then raises the error.
 """
 from __future__ import annotations
@@ -23,6 +23,9 @@ STATIC_SCRATCH_BYTES = 4 << 20
 ALGO_PACKED32, ALGO_PACKED64EMU, ALGO_UNPACKED_IMAD, ALGO_DP4A = 0, 1, 2, 3
 FORM_TWO_LAUNCHES, FORM_ONE_LAUNCH, FORM_FILTERS, FORM_UNPACKED = 0, 1, 2, 3
 GB_SINGLE, GB_1D, GB_DNN = 0, 1, 2
+OUT_SUMS, OUT_CODES, OUT_F32, OUT_F16, OUT_BF16 = range(5)
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
+MAX_GROUPS = 1024
 PIPE_KINDS = {"mad_wide_u32": 0, "mad_wide_s32": 1, "mad_lo_s32": 2, "logic": 3, "shift": 4, "prmt": 5,
               "mad_wide_with_logic": 6, "fma_f64": 7}
 
@@ -50,10 +53,16 @@ class Conv2dFormT(ctypes.Structure):
                 + [(n, ctypes.c_double) for n in ("multiplies", "double_multiplies")])
 
 
+class EpilogueT(ctypes.Structure):
+    _fields_ = [("out_type", ctypes.c_int), ("activation", ctypes.c_int), ("d_x_scale", ctypes.c_void_p), ("d_w_scale", ctypes.c_void_p),
+                ("d_bias", ctypes.c_void_p), ("d_residual", ctypes.c_void_p), ("residual_row_stride", ctypes.c_longlong),
+                ("shift", ctypes.c_int), ("lo", ctypes.c_int), ("hi", ctypes.c_int)]
+
+
 _lib = None
 _fast = None          # the extension module, its entry points bound to the library's
 
-_vp, _sz, _i, _d = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_double
+_vp, _sz, _i, _d, _ll = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_double, ctypes.c_longlong
 
 _SIGNATURES = {
     "hikonv_plan": (_i, [_i] * 7 + [ctypes.POINTER(PlanT)]),
@@ -87,12 +96,15 @@ _SIGNATURES = {
     "hikonv_conv2d_multiplies": (_d, [_i] * 12 + [ctypes.POINTER(TuningT)]),
     "hikonv_conv2d_layout": (_i, [_i] * 11 + [ctypes.POINTER(TuningT), ctypes.POINTER(LayoutT), ctypes.POINTER(_i)]),
     "hikonv_pipe_rate": (_i, [_i, _i, _vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
+    "hikonv_quantize_rows": (_i, [_vp, _i, _ll, _i, _i, _i, _i, _vp, _vp, _vp]),
+    "hikonv_linear": (_i, [_vp, _ll, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
+    "hikonv_grouped_linear": (_i, [_vp, _ll, _vp, _i, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
     "hikonv_status_string": (ctypes.c_char_p, [_i]),
 }
 
 
 _FAST_ENTRY_POINTS = ("hikonv_conv1d", "hikonv_conv1d_dense", "hikonv_pack", "hikonv_conv2d", "hikonv_conv2d_dense",
-                      "hikonv_conv2d_workspace_bytes")
+                      "hikonv_conv2d_workspace_bytes", "hikonv_quantize_rows", "hikonv_linear", "hikonv_grouped_linear")
 
 
 def exported_names():
@@ -476,6 +488,149 @@ def conv1d_multiplies(n, K, p, q, f_signed, g_signed, algo=ALGO_PACKED32, tune=N
 
 def conv2d_multiplies(B, Ci, H, W, Co, K, pad, p, q, x_signed, w_signed, algo=ALGO_PACKED32, tune=None) -> float:
     return float(lib().hikonv_conv2d_multiplies(B, Ci, H, W, Co, K, pad, p, q, int(x_signed), int(w_signed), algo, _tune(tune)))
+
+
+# ------------------------------------------------------------------ linear layers
+
+_FLOAT_TYPES = {torch.float32: OUT_F32, torch.float16: OUT_F16, torch.bfloat16: OUT_BF16}
+
+
+def _rows(t: torch.Tensor, name: str, dtypes, like: Optional[torch.Tensor] = None, shape=None) -> int:
+    """Checks a matrix whose rows may lie apart; returns the elements from one row to the next."""
+    if not getattr(t, "is_cuda", False) or t.layout != torch.strided or t.dim() != 2:
+        raise ValueError("%s must be a CUDA matrix" % name)
+    if t.dtype not in dtypes:
+        raise ValueError("%s must have dtype %s, not %s" % (name, " or ".join(str(d) for d in dtypes), t.dtype))
+    if like is not None and t.device != like.device:
+        raise ValueError("%s is on %s, x is on %s" % (name, t.device, like.device))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, the call needs %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t: Optional[torch.Tensor], name: str, dtype, shape, like: torch.Tensor):
+    """Checks a contiguous tensor of scales, biases or offsets; returns its address, None for None."""
+    if t is None:
+        return None
+    if not getattr(t, "is_cuda", False) or t.device != like.device or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor on %s" % (name, dtype, like.device))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, the call needs %s" % (name, tuple(t.shape), tuple(shape)))
+    return t.data_ptr()
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    """The given stream, or the current one of the tensor's device."""
+    return _raw_stream(t.device.index) if stream is None else int(stream.cuda_stream)
+
+
+def quantize_rows(x: torch.Tensor, bits: int, is_signed: bool = True, codes: Optional[torch.Tensor] = None,
+                  scale: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """Codes of ``bits`` bits, one per byte, and one float scale per row of the matrix ``x`` (float32, float16 or bfloat16; its rows
+    may lie apart, or be one): ``x`` is ``codes * scale`` up to half a step.  Signed codes use the range symmetric around zero,
+    unsigned ones leave out what is negative.  Returns (codes, scale)."""
+    if stream is None:
+        done = (_fast or _load_fast()).quantize_rows(x, bits, is_signed, codes, scale)
+        if done is not None:
+            return done
+    if getattr(x, "dtype", None) not in _FLOAT_TYPES:
+        raise ValueError("x must be a float32, float16 or bfloat16 matrix")
+    x_row = _rows(x, "x", (x.dtype,))
+    M, K = x.shape
+    if codes is None:
+        codes = torch.empty((M, K), dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    if tuple(codes.shape) != (M, K):
+        raise ValueError("codes has shape %s, the call needs %s" % (tuple(codes.shape), (M, K)))
+    with torch.cuda.device(x.device):
+        _check(lib().hikonv_quantize_rows(x.data_ptr(), _FLOAT_TYPES[x.dtype], x_row, M, K, bits, int(is_signed),
+                                          _dev_out(codes, "codes", M * K, _CODE_DTYPES, x),
+                                          _vector(scale, "scale", torch.float32, (M,), x), _stream_of(x, stream)), "hikonv_quantize_rows")
+    return codes, scale
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, p: int, q: int, x_signed: bool, w_signed: bool, w_store_bits: int = 8,
+           x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+           activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None, requant: Optional[tuple] = None,
+           out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Matrix product of codes, ``x`` [M, K] with ``w`` [N, K] (``w_store_bits`` 1, 2 or 4: dense bytes [N, K * q / 8]).
+
+    requant = (shift, lo, hi): codes, one per byte, of the sums plus an int32 ``bias``.  Scales, or a float ``out_dtype`` or ``out``:
+    ``act(sum * x_scale[m] * w_scale[n] + bias[n]) + residual[m, n]`` (bfloat16 unless ``out_dtype`` or ``out`` says
+    otherwise; scales and bias float32, residual of the output's type, which may be ``out`` itself).  Else: the exact int32 sums.
+    Rows of ``x``, ``residual`` and ``out`` may lie apart."""
+    return _linear("hikonv_linear", x, w, None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual,
+                   requant, out_dtype, out, stream)
+
+
+def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, p: int, q: int, x_signed: bool, w_signed: bool,
+                   w_store_bits: int = 8, x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None,
+                   bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
+                   requant: Optional[tuple] = None, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """``linear`` with a matrix of weights per group of rows: ``w`` [E, N, K], ``w_scale`` and ``bias`` [E, N]; rows
+    ``offsets[e]`` to ``offsets[e + 1] - 1`` (int32 [E + 1], on the device) belong to matrix e.  Rows of no group are left as they
+    were in ``out`` (undefined when the call makes it)."""
+    return _linear("hikonv_grouped_linear", x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation,
+                   residual, requant, out_dtype, out, stream)
+
+
+def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype,
+            out, stream):
+    if stream is None:
+        done = (_fast or _load_fast()).linear(x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation,
+                                              residual, requant, out_dtype, out)
+        if done is not None:
+            return done
+    grouped = name == "hikonv_grouped_linear"
+    x_row = _rows(x, "x", _CODE_DTYPES)
+    M, K = x.shape
+    if not getattr(w, "is_cuda", False) or w.dtype not in _CODE_DTYPES or not w.is_contiguous() or w.dim() != (3 if grouped else 2):
+        raise ValueError("w must be a contiguous CUDA int8/uint8 tensor of %s" % ("[E, N, K]" if grouped else "[N, K]"))
+    if w.device != x.device:
+        raise ValueError("w is on %s, x is on %s" % (w.device, x.device))
+    lead, N = tuple(w.shape[:-2]), w.shape[-2]
+    if w_store_bits not in (1, 2, 4, 8) or w.shape[-1] * 8 != K * w_store_bits:
+        raise ValueError("w has %d bytes per row, %d codes of %s bits need %s" % (w.shape[-1], K, w_store_bits, K * w_store_bits / 8))
+    if requant is not None and (x_scale is not None or w_scale is not None or out_dtype in _FLOAT_TYPES):
+        raise ValueError("requantised codes take no scales and no float type")
+    if out_dtype is None and out is not None:
+        out_dtype = out.dtype
+    if requant is not None:
+        kind, dtypes = OUT_CODES, _CODE_DTYPES
+        if out_dtype not in (None, torch.int8, torch.uint8):
+            raise ValueError("requantised codes are int8 or uint8, not %s" % out_dtype)
+    elif x_scale is not None or w_scale is not None or out_dtype in _FLOAT_TYPES:
+        out_dtype = out_dtype or torch.bfloat16
+        if out_dtype not in _FLOAT_TYPES:
+            raise ValueError("scaled sums are float32, float16 or bfloat16, not %s" % out_dtype)
+        kind, dtypes = _FLOAT_TYPES[out_dtype], (out_dtype,)
+    else:
+        kind, dtypes = OUT_SUMS, _INT32
+        if out_dtype not in (None, torch.int32):
+            raise ValueError("sums are int32, not %s" % out_dtype)
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype or (torch.int8 if kind == OUT_CODES else torch.int32), device=x.device)
+    ep = EpilogueT(out_type=kind, activation=int(activation))
+    out_row = _rows(out, "out", dtypes, x, (M, N))
+    ep.d_x_scale = _vector(x_scale, "x_scale", torch.float32, (M,), x)
+    ep.d_w_scale = _vector(w_scale, "w_scale", torch.float32, lead + (N,), x)
+    ep.d_bias = _vector(bias, "bias", torch.int32 if kind == OUT_CODES else torch.float32, lead + (N,), x)
+    if residual is not None:
+        ep.residual_row_stride = _rows(residual, "residual", dtypes, x, (M, N))
+        ep.d_residual = residual.data_ptr()
+    if requant is not None:
+        ep.shift, ep.lo, ep.hi = (int(v) for v in requant)
+    groups = ()
+    if grouped:
+        groups = (_vector(offsets, "offsets", torch.int32, (lead[0] + 1,), x), lead[0])
+    with torch.cuda.device(x.device):
+        _check(getattr(lib(), name)(x.data_ptr(), x_row, w.data_ptr(), w_store_bits, *groups, M, N, K, p, q, int(x_signed),
+                                    int(w_signed), out.data_ptr(), out_row, ctypes.byref(ep), _stream_of(x, stream)), name)
+    return out
 
 
 def pipe_rate(kind: str, iters: int = 2048, device=None, stream=None) -> dict:

@@ -23,9 +23,11 @@ EXT_PATH = os.path.join(HERE, "_fast" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-O3", "-lineinfo", "-std=c++17", "--use_fast_math",
+    "-O3", "-lineinfo", "-std=c++17",
     "-Xcompiler", "-fPIC",
 ]
+# The convolutions compute with integers only; the layers that answer in floats keep IEEE division, square roots and subnormals.
+IEEE_PREFIXES = ("hikonv_linear", "hikonv_quantize")
 
 
 def sources():
@@ -72,7 +74,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
              or os.path.getmtime(_object_of(s)) < max(os.path.getmtime(s), newest_header)]
 
     def compile_one(src: str) -> None:
-        cmd = [nvcc] + flags + ["-c", src, "-o", _object_of(src)]
+        fast = [] if os.path.basename(src).startswith(IEEE_PREFIXES) else ["--use_fast_math"]
+        cmd = [nvcc] + flags + fast + ["-c", src, "-o", _object_of(src)]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)

@@ -1,0 +1,29 @@
+// Interface between the entry points of the linear layers (hikonv_linear.cu) and their kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "hikonv_internal.h"
+
+namespace hikonv {
+
+// A linear layer as its kernels see it.  A plain layer is one group that holds all rows (offsets == nullptr, E == 1).
+struct LinearParams {
+    const uint8_t *x, *w;
+    const int32_t *offsets;
+    long long x_row, w_row;             // bytes from row to row
+    int M, N, K, E;
+    int x_u8, w_u8;                     // bytes that only unsigned arithmetic reads right (unsigned 8-bit codes)
+    int w_bits;                         // 8, or 4 / 2 / 1 dense
+    int down;                           // sums hold the products times 2^down (signed dense weights sit in a byte's upper bits)
+    int out_type, act;
+    void *out;
+    const void *residual, *bias;
+    const float *x_scale, *w_scale;
+    long long out_row, res_row;         // elements from row to row
+    int shift, lo, hi;
+};
+
+int launch_linear_mma(const LinearParams &p, cudaStream_t st);
+
+}  // namespace hikonv

@@ -11,7 +11,9 @@
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "hikonv.h"
@@ -24,6 +26,9 @@ decltype(&hikonv_conv2d) g_conv2d = nullptr;
 decltype(&hikonv_conv2d_dense) g_conv2d_dense = nullptr;
 decltype(&hikonv_conv2d_workspace_bytes) g_workspace_bytes = nullptr;
 decltype(&hikonv_pack) g_pack = nullptr;
+decltype(&hikonv_quantize_rows) g_quantize_rows = nullptr;
+decltype(&hikonv_linear) g_linear = nullptr;
+decltype(&hikonv_grouped_linear) g_grouped_linear = nullptr;
 
 // Reads arguments one after the other; `ok` stays true while all are as expected.
 struct Args {
@@ -304,6 +309,111 @@ PyObject *conv2d_dense(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// What the linear layers share: a matrix on a device whose rows may lie apart, and contiguous scales, biases and offsets.
+bool matrix(const at::Tensor *t, int64_t *row) {
+    if (!t || !t->is_cuda() || t->layout() != at::kStrided || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    *row = t->size(0) > 1 ? t->stride(0) : t->size(1);
+    return fits_int(t->size(0)) && fits_int(t->size(1));
+}
+bool out_matrix(const at::Tensor *t, int64_t M, int64_t N, at::ScalarType type, const at::Tensor &like, int64_t *row) {
+    return matrix(t, row) && t->scalar_type() == type && t->device() == like.device() && t->size(0) == M && t->size(1) == N;
+}
+bool vector_ok(const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like) {
+    return !t || (plain_cuda(t) && t->scalar_type() == type && t->device() == like.device() && t->sizes() == shape);
+}
+const void *address(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+int float_type(at::ScalarType t) {
+    return t == at::kFloat ? HIKONV_OUT_F32 : t == at::kHalf ? HIKONV_OUT_F16 : t == at::kBFloat16 ? HIKONV_OUT_BF16 : -1;
+}
+
+// quantize_rows(x, bits, is_signed, codes, scale)
+PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor();
+        const int bits = in.int32(), is_signed = in.int32() != 0;
+        const at::Tensor *codes_given = in.optional_tensor(), *scale_given = in.optional_tensor();
+        int64_t x_row;
+        if (!in.ok || !matrix(x, &x_row)) return nullptr;
+        const int type = float_type(x->scalar_type());
+        const int64_t M = x->size(0), K = x->size(1);
+        if (type < 0 || K < 1) return nullptr;
+        at::Tensor made_codes, made_scale;
+        if (!codes_given) made_codes = empty({M, K}, is_signed ? at::kChar : at::kByte, *x);
+        if (!scale_given) made_scale = empty({M}, at::kFloat, *x);
+        const at::Tensor &c = codes_given ? *codes_given : made_codes, &s = scale_given ? *scale_given : made_scale;
+        if (!output_ok(c, M * K, true, *x) || c.dim() != 2 || c.size(0) != M || !vector_ok(&s, at::kFloat, {M}, *x)) return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const void *x_ptr = x->data_ptr();
+        int8_t *c_ptr = (int8_t *)c.data_ptr();
+        float *s_ptr = (float *)s.data_ptr();
+        void *st = current_stream();
+        if (unlocked([&] { return g_quantize_rows(x_ptr, type, x_row, (int)M, (int)K, bits, is_signed, c_ptr, s_ptr, st); }) != HIKONV_OK)
+            return nullptr;
+        PyObject *pc = result(a[3], made_codes), *ps = result(a[4], made_scale);
+        PyObject *both = pc && ps ? PyTuple_Pack(2, pc, ps) : nullptr;
+        Py_XDECREF(pc);
+        Py_XDECREF(ps);
+        return both;
+    });
+}
+
+// linear(x, w, offsets or None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype, out)
+PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor(), *w = in.tensor(), *offsets = in.optional_tensor();
+        const int p = in.int32(), q = in.int32(), xs = in.int32() != 0, ws = in.int32() != 0, w_bits = in.int32();
+        const at::Tensor *x_scale = in.optional_tensor(), *w_scale = in.optional_tensor(), *bias = in.optional_tensor();
+        hikonv_epilogue_t ep{};
+        ep.activation = in.int32();
+        const at::Tensor *residual = in.optional_tensor();
+        const bool rq = in.requant(&ep.shift, &ep.lo, &ep.hi);
+        PyObject *dtype = in.next();
+        const at::Tensor *given = in.optional_tensor();
+        int64_t x_row, out_row, res_row;
+        if (!in.ok || !matrix(x, &x_row) || (x->scalar_type() != at::kChar && x->scalar_type() != at::kByte)) return nullptr;
+        if (!codes(w) || w->device() != x->device() || w->dim() != (offsets ? 3 : 2)) return nullptr;
+        const int64_t M = x->size(0), K = x->size(1), E = offsets ? w->size(0) : 1, N = w->size(w->dim() - 2);
+        if (K < 1 || N < 1 || E < 1 || !fits_int(N) || !fits_int(E) || w_bits < 1 || w_bits > 8 || w->size(w->dim() - 1) * 8 != K * w_bits) return nullptr;
+        if (dtype != Py_None && !THPDtype_Check(dtype)) return nullptr;
+        // the output's type: what `out_dtype` says, else the given output's, else what the other arguments ask for
+        const bool scaled = x_scale || w_scale;
+        const at::ScalarType type = dtype != Py_None ? ((THPDtype *)dtype)->scalar_type : given ? given->scalar_type()
+                                  : rq ? at::kChar : scaled ? at::kBFloat16 : at::kInt;
+        const int real = float_type(type);
+        if (rq ? scaled || (type != at::kChar && type != at::kByte) : real < 0 && (scaled || type != at::kInt)) return nullptr;
+        ep.out_type = rq ? HIKONV_OUT_CODES : real >= 0 ? real : HIKONV_OUT_SUMS;
+        at::Tensor made;
+        if (!given) made = empty({M, N}, type, *x);
+        const at::Tensor &y = given ? *given : made;
+        if (!out_matrix(&y, M, N, type, *x, &out_row)) return nullptr;
+        const int64_t per_column[2] = {E, N};
+        const at::IntArrayRef columns(per_column + (offsets ? 0 : 1), offsets ? 2 : 1);
+        if (!vector_ok(x_scale, at::kFloat, {M}, *x) || !vector_ok(w_scale, at::kFloat, columns, *x) ||
+            !vector_ok(bias, rq ? at::kInt : at::kFloat, columns, *x) || !vector_ok(offsets, at::kInt, {E + 1}, *x))
+            return nullptr;
+        if (residual) {
+            if (!out_matrix(residual, M, N, type, *x, &res_row)) return nullptr;
+            ep.residual_row_stride = res_row;
+        }
+        ep.d_x_scale = (const float *)address(x_scale);
+        ep.d_w_scale = (const float *)address(w_scale);
+        ep.d_bias = address(bias);
+        ep.d_residual = address(residual);
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const void *x_ptr = x->data_ptr(), *w_ptr = w->data_ptr();
+        const int32_t *off_ptr = (const int32_t *)address(offsets);
+        void *y_ptr = y.data_ptr(), *st = current_stream();
+        const int status = unlocked([&] {
+            return offsets ? g_grouped_linear(x_ptr, x_row, w_ptr, w_bits, off_ptr, (int)E, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep, st)
+                           : g_linear(x_ptr, x_row, w_ptr, w_bits, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep, st);
+        });
+        if (status != HIKONV_OK) return nullptr;
+        return result(a[15], made);
+    });
+}
+
 // bind(name, address): the entry points of the library that is loaded.
 PyObject *bind(PyObject *, PyObject *args) {
     const char *name;
@@ -317,6 +427,9 @@ PyObject *bind(PyObject *, PyObject *args) {
     else if (s == "hikonv_conv2d_dense") g_conv2d_dense = (decltype(g_conv2d_dense))ptr;
     else if (s == "hikonv_conv2d_workspace_bytes") g_workspace_bytes = (decltype(g_workspace_bytes))ptr;
     else if (s == "hikonv_pack") g_pack = (decltype(g_pack))ptr;
+    else if (s == "hikonv_quantize_rows") g_quantize_rows = (decltype(g_quantize_rows))ptr;
+    else if (s == "hikonv_linear") g_linear = (decltype(g_linear))ptr;
+    else if (s == "hikonv_grouped_linear") g_grouped_linear = (decltype(g_grouped_linear))ptr;
     else {
         PyErr_Format(PyExc_ValueError, "no entry point %s", name);
         return nullptr;
@@ -331,6 +444,8 @@ PyMethodDef methods[] = {
     {"pack", (PyCFunction)(void (*)(void))pack, METH_FASTCALL, nullptr},
     {"conv2d", (PyCFunction)(void (*)(void))conv2d, METH_FASTCALL, nullptr},
     {"conv2d_dense", (PyCFunction)(void (*)(void))conv2d_dense, METH_FASTCALL, nullptr},
+    {"quantize_rows", (PyCFunction)(void (*)(void))quantize_rows, METH_FASTCALL, nullptr},
+    {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
