@@ -519,6 +519,15 @@ int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d
                           int T, int N, int K, int p, int q, int x_signed, int w_signed, void *d_out, long long out_row_stride,
                           const hikonv_epilogue_t *epilogue, void *stream);
 
+/*
+ * hikonv_linear_wait_timeouts - warps of linear-layer kernels on the current device whose wait for their own copies or multiplies ran
+ * out (after a second) since the last call of any thread; 0 unless the device is at fault.  What such a CTA had left to write stays
+ * unwritten.  Synchronises the device, all its streams.
+ * hikonv_linear_wait_check - a debug aid for the above, as hikonv_conv2d_wait_check.
+ */
+int hikonv_linear_wait_timeouts(unsigned int *h_count);
+int hikonv_linear_wait_check(long long cycles, void *stream);
+
 const char *hikonv_status_string(int status);
 
 #ifdef __cplusplus

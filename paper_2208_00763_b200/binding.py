@@ -99,6 +99,8 @@ _SIGNATURES = {
     "hikonv_quantize_rows": (_i, [_vp, _i, _ll, _i, _i, _i, _i, _vp, _vp, _vp]),
     "hikonv_linear": (_i, [_vp, _ll, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
     "hikonv_grouped_linear": (_i, [_vp, _ll, _vp, _i, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
+    "hikonv_linear_wait_timeouts": (_i, [_vp]),
+    "hikonv_linear_wait_check": (_i, [_ll, _vp]),
     "hikonv_status_string": (ctypes.c_char_p, [_i]),
 }
 
@@ -631,6 +633,18 @@ def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale
         _check(getattr(lib(), name)(x.data_ptr(), x_row, w.data_ptr(), w_store_bits, *groups, M, N, K, p, q, int(x_signed),
                                     int(w_signed), out.data_ptr(), out_row, ctypes.byref(ep), _stream_of(x, stream)), name)
     return out
+
+
+def linear_wait_timeouts() -> int:
+    """Waits of linear-layer kernels on the current device that ran out since the last call (0 on a healthy device).  Synchronises."""
+    count = ctypes.c_uint(0)
+    _check(lib().hikonv_linear_wait_timeouts(ctypes.byref(count)), "hikonv_linear_wait_timeouts")
+    return int(count.value)
+
+
+def linear_wait_check(cycles: int, stream=None) -> None:
+    """One thread waits `cycles` for a barrier that nothing completes, gives up and is counted."""
+    _check(lib().hikonv_linear_wait_check(int(cycles), _stream(stream)), "hikonv_linear_wait_check")
 
 
 def pipe_rate(kind: str, iters: int = 2048, device=None, stream=None) -> dict:

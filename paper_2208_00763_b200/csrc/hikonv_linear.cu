@@ -1,6 +1,7 @@
 // hikonv_linear, hikonv_grouped_linear: argument checks, the choice of kernel, and the kernel for rows of any alignment and any
 // pair of code types (linear_mma_kernel).
 #include <cstring>
+#include <mutex>
 
 #include "hikonv_linear_util.cuh"
 
@@ -227,6 +228,7 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     k.x = (const uint8_t *)d_x; k.w = (const uint8_t *)d_w; k.offsets = d_offsets;
     k.x_row = x_row; k.w_row = w_row;
     k.M = M; k.N = N; k.K = K; k.E = E;
+    k.x_signed = xs; k.w_signed = ws;
     k.x_u8 = !xs && p == 8; k.w_u8 = !ws && q == 8;
     k.w_bits = w_bits;
     k.down = w_bits < 8 && ws ? 8 - w_bits : 0;
@@ -235,7 +237,7 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     k.x_scale = ep->d_x_scale; k.w_scale = ep->d_w_scale;
     k.out_row = out_row; k.res_row = res_row;
     k.shift = ep->shift; k.lo = ep->lo; k.hi = ep->hi;
-    return launch_linear_mma(k, (cudaStream_t)stream);
+    return linear_tc_takes(k) ? launch_linear_tc(k, (cudaStream_t)stream) : launch_linear_mma(k, (cudaStream_t)stream);
 }
 
 }  // namespace hikonv
@@ -254,4 +256,26 @@ extern "C" int hikonv_grouped_linear(const void *d_x, long long x_row_stride, co
                                      long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream) {
     return linear_run(d_x, x_row_stride, d_w, w_store_bits, d_offsets, 1, E, T, N, K, p, q, x_signed != 0, w_signed != 0, d_out,
                       out_row_stride, epilogue, stream);
+}
+
+extern "C" int hikonv_linear_wait_timeouts(unsigned int *h_count) {
+    if (!h_count) return HIKONV_ERR_INVALID_ARG;
+    constexpr int kDevices = 64;
+    static std::mutex mutex;
+    static unsigned int told[kDevices];                              // what earlier calls have reported
+    *h_count = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices || cudaDeviceSynchronize() != cudaSuccess) return HIKONV_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(mutex);
+    unsigned int total = 0;
+    const int rc = read_linear_timeouts(&total);
+    if (rc != HIKONV_OK) return rc;
+    *h_count = total - told[dev];
+    told[dev] = total;
+    return HIKONV_OK;
+}
+
+extern "C" int hikonv_linear_wait_check(long long cycles, void *stream) {
+    if (cycles < 0 || cycles > kWaitCycles) return HIKONV_ERR_INVALID_ARG;
+    return launch_linear_wait_check(cycles, (cudaStream_t)stream);
 }

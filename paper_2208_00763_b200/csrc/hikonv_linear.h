@@ -13,6 +13,7 @@ struct LinearParams {
     const int32_t *offsets;
     long long x_row, w_row;             // bytes from row to row
     int M, N, K, E;
+    int x_signed, w_signed;
     int x_u8, w_u8;                     // bytes that only unsigned arithmetic reads right (unsigned 8-bit codes)
     int w_bits;                         // 8, or 4 / 2 / 1 dense
     int down;                           // sums hold the products times 2^down (signed dense weights sit in a byte's upper bits)
@@ -24,6 +25,13 @@ struct LinearParams {
     int shift, lo, hi;
 };
 
+// Any alignment and any pair of types, at the rate of the older tensor path (hikonv_linear.cu).
 int launch_linear_mma(const LinearParams &p, cudaStream_t st);
+
+// hikonv_linear_tc.cu
+bool linear_tc_takes(const LinearParams &p);
+int launch_linear_tc(const LinearParams &p, cudaStream_t st);
+int read_linear_timeouts(unsigned int *h_count);             // on the current device, since it was loaded
+int launch_linear_wait_check(long long cycles, cudaStream_t st);
 
 }  // namespace hikonv

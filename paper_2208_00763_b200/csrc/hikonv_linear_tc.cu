@@ -1,0 +1,595 @@
+// Linear layers on the tensor cores: tcgen05.mma on byte codes (kind::i8, int32 sums in tensor memory), operands staged in shared
+// memory by TMA.
+//
+// The WEIGHTS are the matrix of 128 rows and the rows of x the matrix of up to 256 columns: D[n][m] = sum_k w[n][k] x[m][k].  The
+// number of columns can be any multiple of 16, so one token costs 16 columns instead of 128 rows, a group's last tile costs what it
+// has, and the columns of a tile can be chosen so that the tiles fill the SMs evenly.  A lane of tensor memory is an output column of
+// the layer: its scale and bias are one register each, and a warp writes 32 neighbours of an output row at a time.
+//
+// One CTA per SM walks over the tiles.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 take finished sums through the epilogue while the
+// next tile is multiplied (two accumulators), and, where the operands are not yet bytes of one sign, warps 12 to 19 change them in
+// shared memory between the two: dense weights are unpacked into the operand's layout, and unsigned 8-bit activations of signed weights
+// get 128 subtracted (their top bit flipped; the instruction takes either two signed or two unsigned operands here).  What that takes
+// off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.
+//
+// Small layers have fewer tiles than there are SMs: there the CTAs of a cluster share a tile's depth, and the cluster adds their sums
+// through distributed shared memory, each CTA finishing its part of the tile's output columns.
+#include <cuda.h>
+
+#include <cstring>
+
+#include "hikonv_linear_util.cuh"
+
+namespace hikonv {
+
+constexpr int kTcRows = 128;             // output columns of the layer per tile: rows of the instruction
+constexpr int kTcDepth = 128;            // codes of the depth per stage: one 128-byte swizzled row
+constexpr int kTcMostStages = 12;
+constexpr int kTcThreads = 384, kTcTransformThreads = 640, kTcTransformWarps = 8, kTcEpilogueWarps = 8;
+constexpr size_t kTcMostSmem = 226 * 1024;
+
+struct TcParams {
+    LinearParams p;
+    int nt;                              // rows of x per tile, a multiple of 16
+    int acc_cols;                        // tensor-memory columns per accumulator
+    int stages, stage_bytes, x_off, raw_off;
+    int splits, chunks;                  // CTAs that share a tile's depth; stages' worth of depth in all
+    int n_blocks, m_tiles, tokens_first;
+    uint32_t idesc;
+    int flip, ones;                      // x has its top bits flipped; so many rows (16) with ones lie behind it
+    long long wait_cycles;
+};
+
+// The front of a CTA's (dynamic) shared memory; the stages follow on the next multiple of 1024 bytes, then the tables of the groups.
+struct TcControl {
+    uint64_t full[kTcMostStages], ready[kTcMostStages], empty[kTcMostStages], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem;
+    int whole;                           // no wait of this CTA has run out
+};
+
+static __device__ unsigned int linear_timeouts;
+
+// ---- tensor cores and tensor memory
+
+__device__ __forceinline__ uint64_t smem_descriptor(uint32_t address) {
+    // rows of 128 bytes with the 128-byte swizzle, eight of them 1024 bytes after one another
+    return (uint64_t)((address & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_load16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ uint32_t tc_load1(uint32_t taddr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr));
+    return v;
+}
+__device__ __forceinline__ void tc_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                 "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void mbarrier_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ int32_t load_cluster_s32(uint32_t smem_addr, uint32_t rank) {
+    uint32_t remote;
+    int32_t v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 load_shared16(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// A ring of stages: which one is next and in which of its phases it is.
+struct Ring {
+    int stage = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++stage == stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+struct Tile {
+    int e, row0, rows, n0;
+};
+
+// Tables of the groups in shared memory: row ranges, and the number of tiles up to the end of each.
+struct GroupTables {
+    const int2 *rows;
+    const int *tile_end;
+};
+
+__device__ __forceinline__ Tile find_tc_tile(const TcParams &q, const GroupTables &g, int t) {
+    Tile r;
+    int local = t, m_tiles = q.m_tiles, first = 0, end = q.p.M;
+    r.e = 0;
+    if (q.p.offsets) {
+        int lo = 0, hi = q.p.E - 1;                    // the first group whose tiles end behind t
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (g.tile_end[mid] > t) hi = mid;
+            else lo = mid + 1;
+        }
+        r.e = lo;
+        if (lo > 0) local -= g.tile_end[lo - 1];
+        first = g.rows[lo].x;
+        end = g.rows[lo].y;
+        m_tiles = (end - first + q.nt - 1) / q.nt;
+    }
+    const int i = q.tokens_first ? local % m_tiles : local / q.n_blocks;
+    const int j = q.tokens_first ? local / m_tiles : local % q.n_blocks;
+    r.row0 = first + i * q.nt;
+    r.rows = min(q.nt, end - r.row0);
+    r.n0 = j * kTcRows;
+    return r;
+}
+
+// 16 bytes of dense weights to 16 * 8 / BITS codes in the operand's layout (row `row`, from its piece `piece` of 16 codes on).
+template <int BITS, bool UP>
+__device__ __forceinline__ void unpack_to_operand(uint4 v, uint32_t tile, int row, int piece) {
+    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+    constexpr int PIECES = 8 / BITS;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+        uint32_t o[4];
+        if constexpr (BITS == 4) {
+            uint32_t a[2], b[2];
+            unpack4<UP>(in[2 * j], a);
+            unpack4<UP>(in[2 * j + 1], b);
+            o[0] = a[0]; o[1] = a[1]; o[2] = b[0]; o[3] = b[1];
+        } else if constexpr (BITS == 2) {
+            unpack2<UP>(in[j], o);
+        } else {
+            unpack1<UP>(in[j / 2] >> (16 * (j & 1)), o);
+        }
+        store_shared16(tile + row * 128 + (((piece + j) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+    }
+}
+template <int BITS, bool UP>
+__device__ __forceinline__ void unpack_tile(uint32_t raw, uint32_t tile, int tid) {
+    constexpr int PER_ROW = BITS;                      // pieces of 16 bytes: 128 codes of BITS bits
+#pragma unroll
+    for (int i = tid; i < kTcRows * PER_ROW; i += kTcTransformWarps * 32)
+        unpack_to_operand<BITS, UP>(load_shared16(raw + i * 16), tile, i / PER_ROW, (i % PER_ROW) * (8 / BITS));
+}
+
+template <bool TRANSFORM>
+__global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 1)
+    linear_tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    TcControl &ctl = *reinterpret_cast<TcControl *>(dynamic);
+    uint64_t *bar_full = ctl.full, *bar_ready = ctl.ready, *bar_empty = ctl.empty, *bar_acc_full = ctl.acc_full, *bar_acc_empty = ctl.acc_empty;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const LinearParams &p = q.p;
+    const uint32_t stages = (smem_address(dynamic) + (uint32_t)sizeof(TcControl) + 1023u) & ~1023u;
+    uint8_t *behind = dynamic + (stages - smem_address(dynamic)) + q.stages * q.stage_bytes;
+    int2 *group_row = reinterpret_cast<int2 *>(behind);
+    int *group_tiles = reinterpret_cast<int *>(group_row + p.E);
+    const GroupTables tables{group_row, group_tiles};
+
+    grid_dependency_release();
+    if (tid == 0) {
+        for (int i = 0; i < q.stages; ++i) {
+            mbarrier_init(smem_address(&bar_full[i]), 1);
+            mbarrier_init(smem_address(&bar_ready[i]), kTcTransformWarps);
+            mbarrier_init(smem_address(&bar_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbarrier_init(smem_address(&bar_acc_full[i]), 1);
+            mbarrier_init(smem_address(&bar_acc_empty[i]), kTcEpilogueWarps);
+        }
+        mbarrier_init(smem_address(&ctl.drain), 1);
+        mbarrier_init_fence();
+        ctl.whole = 1;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(2 * q.acc_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (TRANSFORM && q.ones) {
+        // sixteen rows behind the rows of x, the first of them ones; nothing writes there again
+        for (int i = tid; i < q.stages * 128; i += blockDim.x) {
+            const uint32_t v = (i & 127) < 8 ? 0x01010101u : 0u;
+            store_shared16(stages + (i >> 7) * q.stage_bytes + q.x_off + q.nt * 128 + (i & 127) * 16, v, v, v, v);
+        }
+        proxy_fence();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl.tmem;
+    grid_dependency_wait();
+
+    int tiles = q.m_tiles * q.n_blocks;
+    if (p.offsets) {
+        for (int e = tid; e < p.E; e += blockDim.x) {
+            const int2 r = group_rows(p, e);
+            group_row[e] = r;
+            group_tiles[e] = ((r.y - r.x + q.nt - 1) / q.nt) * q.n_blocks;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int before = 0;
+            for (int e0 = 0; e0 < p.E; e0 += 32) {
+                int upto = e0 + lane < p.E ? group_tiles[e0 + lane] : 0;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+                    if (lane >= d) upto += v;
+                }
+                if (e0 + lane < p.E) group_tiles[e0 + lane] = before + upto;
+                before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+            }
+        }
+        __syncthreads();
+        tiles = group_tiles[p.E - 1];
+    }
+    const int rank = q.splits > 1 ? (int)(blockIdx.x % q.splits) : 0;
+    const int t0 = blockIdx.x / q.splits, step = gridDim.x / q.splits;
+    const int c0 = (int)((long long)q.chunks * rank / q.splits), c1 = (int)((long long)q.chunks * (rank + 1) / q.splits);
+
+    auto wait = [&](uint64_t *bar, uint32_t parity) { return mbarrier_wait(smem_address(bar), parity, q.wait_cycles); };
+    bool fine = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            Ring ring;
+            const int depth_bytes = kTcDepth * p.w_bits / 8;
+            const uint32_t bytes = (uint32_t)(q.nt * kTcDepth + kTcRows * depth_bytes);
+            int loads = 0;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tc_tile(q, tables, t);
+                const int w_row0 = tile.e * p.N + tile.n0;
+                for (int c = c0; c < c1; ++c) {
+                    fine = wait(&bar_empty[ring.stage], ring.phase ^ 1);
+                    if (!fine) break;
+                    const uint32_t at = stages + ring.stage * q.stage_bytes, bar = smem_address(&bar_full[ring.stage]);
+                    mbarrier_arrive_expect(bar, bytes);
+                    tma_load_2d(at + (p.w_bits == 8 ? 0 : q.raw_off), &map_w, c * depth_bytes, w_row0, bar);
+                    tma_load_2d(at + q.x_off, &map_x, c * kTcDepth, tile.row0, bar);
+                    ++loads;
+                    ring.next(q.stages);
+                }
+            }
+            // what is in flight has to land before the memory goes: the last load of every stage
+            for (int i = 0; i < q.stages && i < loads; ++i) {
+                ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+                if (ring.stage == q.stages - 1) ring.phase ^= 1;
+                fine &= wait(&bar_full[ring.stage], ring.phase);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            Ring ring, acc;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tc_tile(q, tables, t);
+                const uint32_t cols = q.ones ? (uint32_t)(q.nt + q.ones) : (uint32_t)((tile.rows + 15) & ~15);
+                const uint32_t idesc = q.idesc | ((cols >> 3) << 17);
+                const uint32_t d = tmem + acc.stage * q.acc_cols;
+                fine = wait(&bar_acc_empty[acc.stage], acc.phase ^ 1);
+                if (!fine) break;
+                tc_fence_after();
+                for (int c = c0; c < c1; ++c) {
+                    fine = wait(&bar_full[ring.stage], ring.phase);
+                    if (TRANSFORM) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
+                    if (!fine) break;
+                    tc_fence_after();
+                    const uint32_t at = stages + ring.stage * q.stage_bytes;
+                    const uint64_t a = smem_descriptor(at), b = smem_descriptor(at + q.x_off);
+#pragma unroll
+                    for (int k = 0; k < kTcDepth / 32; ++k) tc_mma(d, a + k * 2, b + k * 2, idesc, (c > c0 || k > 0) ? 1u : 0u);
+                    tc_commit(smem_address(&bar_empty[ring.stage]));
+                    ring.next(q.stages);
+                }
+                if (!fine) break;
+                tc_commit(smem_address(&bar_acc_full[acc.stage]));
+                acc.next(2);
+            }
+            if (!fine) {                               // multiplies in flight read shared memory and write tensor memory
+                tc_commit(smem_address(&ctl.drain));
+                wait(&ctl.drain, 0);
+            }
+        }
+    } else if (TRANSFORM && warp >= 12) {
+        Ring ring;
+        const int at_tid = tid - 12 * 32;
+        for (int t = t0; fine && t < tiles; t += step) {
+            for (int c = c0; c < c1; ++c) {
+                fine = wait(&bar_full[ring.stage], ring.phase);
+                fine = __all_sync(0xFFFFFFFFu, fine);
+                if (!fine) break;
+                const uint32_t at = stages + ring.stage * q.stage_bytes;
+                if (p.w_bits == 4) {
+                    if (p.down) unpack_tile<4, true>(at + q.raw_off, at, at_tid);
+                    else unpack_tile<4, false>(at + q.raw_off, at, at_tid);
+                } else if (p.w_bits == 2) {
+                    if (p.down) unpack_tile<2, true>(at + q.raw_off, at, at_tid);
+                    else unpack_tile<2, false>(at + q.raw_off, at, at_tid);
+                } else if (p.w_bits == 1) {
+                    if (p.down) unpack_tile<1, true>(at + q.raw_off, at, at_tid);
+                    else unpack_tile<1, false>(at + q.raw_off, at, at_tid);
+                }
+                if (q.flip)
+                    for (int i = at_tid; i < q.nt * 8; i += kTcTransformWarps * 32) {
+                        const uint32_t a = at + q.x_off + i * 16;
+                        const uint4 v = load_shared16(a);
+                        store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
+                    }
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbarrier_arrive(smem_address(&bar_ready[ring.stage]));
+                ring.next(q.stages);
+            }
+        }
+    } else if (warp >= 4 && warp < 12) {
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        Ring acc;
+        for (int t = t0; fine && t < tiles; t += step) {
+            const Tile tile = find_tc_tile(q, tables, t);
+            const int n = tile.n0 + quad * 32 + lane;
+            fine = __all_sync(0xFFFFFFFFu, wait(&bar_acc_full[acc.stage], acc.phase));
+            if (!fine) break;
+            tc_fence_after();
+            const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
+            int32_t correction = 0;
+            if (q.ones) {
+                correction = (int32_t)tc_load1(d + q.nt) * 128;
+                tc_wait_load();
+            }
+            if (q.splits > 1) {
+                // this CTA's part of the sums, [row of x][output column], over the stages: all loads have been multiplied
+                for (int col = half * 16; col < tile.rows; col += 32) {
+                    uint32_t v[16];
+                    tc_load16(d + col, v);
+                    tc_wait_load();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(stages + ((col + i) * kTcRows + quad * 32 + lane) * 4),
+                                     "r"(v[i] + (uint32_t)correction)
+                                     : "memory");
+                }
+            } else {
+                with_out_type(p.out_type, [&](auto kind) {
+                    constexpr int OUT = decltype(kind)::value;
+                    using T = typename OutElem<OUT>::type;
+                    const bool inside = n < p.N;
+                    ColumnTerms terms{1.f, 0.f, 0};
+                    if (inside) terms = column_terms<OUT>(p, tile.e, n);
+                    for (int col = half * 16; col < tile.rows; col += 32) {
+                        uint32_t v[16];
+                        T res[16];
+                        tc_load16(d + col, v);
+                        const int m = tile.row0 + col, left = tile.rows - col;
+                        float xs = 1.f;
+                        if (OUT >= HIKONV_OUT_F32 && p.x_scale && lane < left) xs = load_ordered(p.x_scale + m + (lane & 15));
+                        if (OUT >= HIKONV_OUT_F32 && p.residual) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (inside && i < left) res[i] = load_ordered((const T *)p.residual + (long long)(m + i) * p.res_row + n);
+                        }
+                        tc_wait_load();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float scale = __shfl_sync(0xFFFFFFFFu, xs, i);
+                            if (inside && i < left)
+                                ((T *)p.out)[(long long)(m + i) * p.out_row + n] =
+                                    finish<OUT>(p, ((int32_t)v[i] + correction) >> p.down, scale, terms, res[i]);
+                        }
+                    }
+                });
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbarrier_arrive(smem_address(&bar_acc_empty[acc.stage]));
+            acc.next(2);
+        }
+    }
+    if (!fine) {
+        ctl.whole = 0;
+        if (lane == 0) atomicAdd(&linear_timeouts, 1u);
+    }
+    __syncwarp();
+    if (q.splits > 1) {
+        cluster_sync_all();
+        bool all = true;
+        for (int r = 0; r < q.splits; ++r) all = all && load_cluster_s32(smem_address(&ctl.whole), r) != 0;
+        if (all && warp >= 4 && warp < 12 && t0 < tiles) {
+            const Tile tile = find_tc_tile(q, tables, t0);
+            const int columns = kTcRows / q.splits, own = (tid - 128) % columns, stride = 256 / columns;
+            const int n = tile.n0 + rank * columns + own;
+            if (n < p.N) {
+                with_out_type(p.out_type, [&](auto kind) {
+                    constexpr int OUT = decltype(kind)::value;
+                    using T = typename OutElem<OUT>::type;
+                    const ColumnTerms terms = column_terms<OUT>(p, tile.e, n);
+                    for (int i = (tid - 128) / columns; i < tile.rows; i += stride) {
+                        const int m = tile.row0 + i;
+                        float xs = 1.f;
+                        T res{};
+                        if (OUT >= HIKONV_OUT_F32 && p.x_scale) xs = load_ordered(p.x_scale + m);
+                        if (OUT >= HIKONV_OUT_F32 && p.residual) res = load_ordered((const T *)p.residual + m * p.res_row + n);
+                        int32_t sum = 0;
+                        for (int r = 0; r < q.splits; ++r) sum += load_cluster_s32(stages + (i * kTcRows + rank * columns + own) * 4, r);
+                        ((T *)p.out)[m * p.out_row + n] = finish<OUT>(p, sum >> p.down, xs, terms, res);
+                    }
+                });
+            }
+        }
+        cluster_sync_all();                            // the others may still read this CTA's part
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * q.acc_cols));
+}
+
+__global__ void linear_wait_check_kernel(long long cycles) {
+    __shared__ uint64_t bar;
+    mbarrier_init(smem_address(&bar), 1);
+    mbarrier_init_fence();
+    if (!mbarrier_wait(smem_address(&bar), 0, cycles)) atomicAdd(&linear_timeouts, 1u);
+}
+
+// ---- host
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void *ptr = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+                        found == cudaDriverEntryPointSuccess;
+        return ok ? (EncodeTiled)ptr : (EncodeTiled) nullptr;
+    }();
+    return f;
+}
+// Byte matrix [rows][row_bytes], rows `stride` bytes apart, in boxes of box_rows x box_bytes.
+static bool encode_map(CUtensorMap *map, const void *base, uint64_t row_bytes, uint64_t rows, uint64_t stride, uint32_t box_bytes, uint32_t box_rows,
+                       bool swizzled) {
+    const cuuint64_t dims[2] = {row_bytes, rows}, strides[1] = {stride};
+    const cuuint32_t box[2] = {box_bytes, box_rows}, one[2] = {1, 1};
+    const EncodeTiled f = encode_tiled();
+    return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static int sm_count_here() {
+    static thread_local int known_dev = -1, sms = 148;
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev != known_dev) {
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        known_dev = dev;
+    }
+    return sms;
+}
+
+// Whether this kernel takes the layer: rows of x and w on 16-byte boundaries, operands that are both signed or both unsigned bytes or become
+// so, and few enough tiles for 32-bit counts.
+bool linear_tc_takes(const LinearParams &p) {
+    if ((uintptr_t)p.x % 16 || (uintptr_t)p.w % 16 || (p.M > 1 && p.x_row % 16) || p.w_row % 16) return false;
+    if (p.w_u8 && p.x_signed) return false;
+    if ((long long)p.E * p.N > 0x7FFFFFFFll || p.M > (1 << 30)) return false;
+    return ((long long)p.M / 16 + (p.E < p.M ? p.E : p.M) + 1) * ceil_div(p.N, kTcRows) < 0x3FFFFFFFll;
+}
+
+// Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.
+static void choose_tile(const LinearParams &p, bool ones, int sms, int *nt_out, int *splits_out) {
+    const int n_blocks = ceil_div(p.N, kTcRows), chunks = ceil_div(p.K, kTcDepth);
+    const int most = ones ? 240 : 256;
+    double best = 1e300;
+    for (int nt = 16; nt <= most; nt += 16) {
+        // groups: on average half a tile of each is left empty
+        const int filled = p.E < p.M ? p.E : p.M;
+        const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * n_blocks;
+        for (int splits = 1; splits <= 8 && splits <= chunks; splits *= 2) {
+            // clusters of four and more do not fill every SM: their CTAs share one part of the GPU
+            if (splits > 1 && (tiles * splits > sms - 20 || nt > 128)) break;
+            const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
+            const double per_chunk = 256.0 + 2.0 * nt + (p.w_bits < 8 ? 128.0 : 0.0);
+            const double time = waves * ceil_div(chunks, splits) * per_chunk + (splits > 1 ? 1500.0 + 4.0 * nt * splits : 6.0 * nt);
+            if (time < best) {
+                best = time;
+                *nt_out = nt;
+                *splits_out = splits;
+            }
+        }
+        if (nt >= p.M) break;
+    }
+}
+
+int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
+    TcParams q;
+    memset(&q, 0, sizeof(q));
+    q.p = p;
+    const int sms = sm_count_here();
+    const bool as_unsigned = (p.x_u8 || p.w_u8) && !p.x_signed && !p.w_signed;
+    q.flip = p.x_u8 && !as_unsigned;
+    q.ones = q.flip ? 16 : 0;
+    choose_tile(p, q.flip, sms, &q.nt, &q.splits);
+    const bool transform = p.w_bits < 8 || q.flip;
+    q.chunks = ceil_div(p.K, kTcDepth);
+    q.n_blocks = ceil_div(p.N, kTcRows);
+    q.m_tiles = ceil_div(p.M, q.nt);
+    q.tokens_first = p.offsets || (long long)p.M * p.K <= (long long)p.N * p.w_row;
+    q.acc_cols = 32;
+    while (q.acc_cols < q.nt + q.ones) q.acc_cols *= 2;
+    q.x_off = kTcRows * kTcDepth;
+    q.raw_off = q.x_off + (q.nt + q.ones) * kTcDepth;
+    q.stage_bytes = (int)align_up(q.raw_off + (p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
+    q.stages = (int)((kTcMostSmem - 2048 - tables) / q.stage_bytes);
+    if (q.stages > kTcMostStages) q.stages = kTcMostStages;
+    if (q.splits > 1) {
+        const int own = ceil_div(q.chunks, q.splits);
+        const int parts = ceil_div(q.nt * kTcRows * 4, q.stage_bytes);              // the sums that are exchanged lie over the stages
+        if (q.stages > own) q.stages = own > parts ? own : parts;
+        if (q.stages < parts) return HIKONV_ERR_UNSUPPORTED;
+    }
+    // accumulators of signed operands: format 2 (int32), types 1 (signed) or 0 (unsigned) of both, 128 rows; the columns follow per tile
+    q.idesc = (2u << 4) | ((as_unsigned ? 0u : 1u) << 7) | ((as_unsigned ? 0u : 1u) << 10) | ((uint32_t)(kTcRows >> 4) << 24);
+    q.wait_cycles = kWaitCycles;
+    const size_t smem = (size_t)q.stages * q.stage_bytes + 2048 + tables;
+
+    CUtensorMap map_x, map_w;
+    if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt, true) ||
+        !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows, p.w_bits == 8))
+        return HIKONV_ERR_CUDA;
+    long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
+    const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
+    const void *kernel = transform ? (const void *)linear_tc_kernel<true> : (const void *)linear_tc_kernel<false>;
+    return with_dynamic_smem(kernel, smem > 49 * 1024 ? smem : 49 * 1024, [&] {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(grid);
+        cfg.blockDim = dim3(transform ? kTcTransformThreads : kTcThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)q.splits;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = q.splits > 1 ? 2 : 1;
+        const cudaError_t e = transform ? cudaLaunchKernelEx(&cfg, linear_tc_kernel<true>, q, map_x, map_w)
+                                        : cudaLaunchKernelEx(&cfg, linear_tc_kernel<false>, q, map_x, map_w);
+        return e == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+    });
+}
+
+int read_linear_timeouts(unsigned int *h_count) {
+    return cudaMemcpyFromSymbol(h_count, linear_timeouts, sizeof(*h_count)) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+}
+int launch_linear_wait_check(long long cycles, cudaStream_t st) { return launch_plain(linear_wait_check_kernel, dim3(1), dim3(1), 0, st, cycles); }
+
+}  // namespace hikonv

@@ -387,3 +387,15 @@ def test_refusals_of_the_binding():
     line = torch.zeros(64, dtype=torch.float32, device="cuda")
     with pytest.raises(hk.HikonvError):
         hk.linear(x, w, 8, 8, True, True, residual=line[8:40].view(4, 8), out=line[:32].view(4, 8))
+
+
+def test_no_wait_has_run_out_and_those_that_do_are_counted():
+    assert hk.linear_wait_timeouts() == 0                # over all tests of this process so far
+    side = torch.cuda.Stream()
+    for n in (1, 2):
+        for _ in range(n):
+            hk.linear_wait_check(2000000, stream=side)
+        assert hk.linear_wait_timeouts() == n
+        assert hk.linear_wait_timeouts() == 0
+    with pytest.raises(hk.HikonvError):
+        hk.linear_wait_check(1 << 40)
