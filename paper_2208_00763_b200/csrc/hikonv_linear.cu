@@ -150,9 +150,8 @@ __global__ void __launch_bounds__(256) linear_mma_kernel(const __grid_constant__
                         const int m = m0 + wm * TM * 16 + i * 16 + g + r * 8;
                         if (m >= m_end) continue;
                         const float xs = p.x_scale ? load_ordered(p.x_scale + m) : 1.f;
-                        T res{};
-                        if (OUT >= HIKONV_OUT_F32 && p.residual) res = load_ordered((const T *)p.residual + m * p.res_row + n);
-                        ((T *)p.out)[m * p.out_row + n] = finish<OUT>(p, acc[i][j][r * 2 + c] >> p.down, xs, terms, res);
+                        ((T *)p.out)[m * p.out_row + n] =
+                            finish<OUT>(p, acc[i][j][r * 2 + c] >> p.down, xs, terms, residual_at<T>(p, m, n));
                     }
             }
     });

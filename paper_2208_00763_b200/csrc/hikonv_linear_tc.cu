@@ -181,6 +181,129 @@ __device__ __forceinline__ void unpack_tile(uint32_t raw, uint32_t tile, int tid
         unpack_to_operand<BITS, UP>(load_shared16(raw + i * 16), tile, i / PER_ROW, (i % PER_ROW) * (8 / BITS));
 }
 
+__device__ __forceinline__ bool wait_all(const TcParams &q, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbarrier_wait(smem_address(bar), parity, q.wait_cycles));
+}
+
+// The epilogue of a warp: the 32 output columns of its quarter of the lanes, every other batch of 16 rows of x.  Each output costs about
+// ten instructions here, and with eight warps they have to overlap: output type and activation are constants, a batch's 16 sums and
+// residuals are in flight together, and what belongs to a column is loaded before its sums are there.
+template <int OUT, int ACT>
+__device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, uint32_t tmem,
+                                             uint64_t *acc_full, uint64_t *acc_empty) {
+    using T = typename OutElem<OUT>::type;
+    constexpr bool REAL = OUT >= HIKONV_OUT_F32;
+    const LinearParams &p = q.p;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - 4) >> 2;
+    Ring acc;
+    for (int t = t0; t < tiles; t += step) {
+        const Tile tile = find_tc_tile(q, tables, t);
+        const int n = tile.n0 + quad * 32 + lane;
+        const bool inside = n < p.N;
+        ColumnTerms terms{1.f, 0.f, 0};
+        if (inside) terms = column_terms<OUT>(p, tile.e, n);
+        if (!wait_all(q, &acc_full[acc.stage], acc.phase)) return false;
+        tc_fence_after();
+        const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
+        int32_t correction = 0;
+        if (q.ones) {
+            correction = (int32_t)tc_load1(d + q.nt) * 128;
+            tc_wait_load();
+        }
+        for (int col = half * 16; col < tile.rows; col += 32) {
+            uint32_t v[16];
+            float scale[16], res[16];
+            tc_load16(d + col, v);
+            const long long m = tile.row0 + col;
+            const int left = tile.rows - col;
+            if (REAL) {
+                float xs = 1.f;
+                if (p.x_scale && (lane & 15) < left) xs = load_ordered(p.x_scale + m + (lane & 15));
+#pragma unroll
+                for (int i = 0; i < 16; ++i) res[i] = 0.f;
+                if (p.residual && inside) {
+                    const T *r = (const T *)p.residual + m * p.res_row + n;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if constexpr (REAL)
+                            if (i < left) res[i] = to_float(load_ordered(r + i * p.res_row));
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) scale[i] = __shfl_sync(0xFFFFFFFFu, xs, i);
+            }
+            tc_wait_load();
+            if (inside) {
+                T *o = (T *)p.out + m * p.out_row + n;
+                auto one = [&](int i) {
+                    *o = finish<OUT, ACT>(p, ((int32_t)v[i] + correction) >> p.down, REAL ? scale[i] : 1.f, terms, REAL ? res[i] : 0.f);
+                    o += p.out_row;
+                };
+                if (left >= 16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) one(i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < left) one(i);
+                }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbarrier_arrive(smem_address(&acc_empty[acc.stage]));
+        acc.next(2);
+    }
+    return true;
+}
+
+// With a shared depth: this CTA's part of the sums to shared memory, [row of x][output column], over the stages (all loads have been
+// multiplied when the sums are there).
+__device__ __forceinline__ bool keep_part(const TcParams &q, const GroupTables &tables, int t, int tiles, uint32_t tmem, uint32_t part,
+                                          uint64_t *acc_full) {
+    if (t >= tiles) return true;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - 4) >> 2;
+    const Tile tile = find_tc_tile(q, tables, t);
+    if (!wait_all(q, &acc_full[0], 0)) return false;
+    tc_fence_after();
+    const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16);
+    uint32_t correction = 0;
+    if (q.ones) {
+        correction = tc_load1(d + q.nt) * 128u;
+        tc_wait_load();
+    }
+    for (int col = half * 16; col < tile.rows; col += 32) {
+        uint32_t v[16];
+        tc_load16(d + col, v);
+        tc_wait_load();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(part + ((col + i) * kTcRows + quad * 32 + lane) * 4), "r"(v[i] + correction) : "memory");
+    }
+    tc_fence_before();
+    return true;
+}
+
+// ... and the sums of all parts through the epilogue, this CTA's share of the output columns.
+template <int OUT, int ACT>
+__device__ __forceinline__ void finish_parts(const TcParams &q, const Tile &tile, int rank, uint32_t part) {
+    using T = typename OutElem<OUT>::type;
+    const LinearParams &p = q.p;
+    const int tid = threadIdx.x - 128, columns = kTcRows / q.splits, own = rank * columns + tid % columns, n = tile.n0 + own;
+    if (n >= p.N) return;
+    const ColumnTerms terms = column_terms<OUT>(p, tile.e, n);
+    for (int i = tid / columns; i < tile.rows; i += 256 / columns) {
+        const long long m = tile.row0 + i;
+        float xs = 1.f;
+        if (OUT >= HIKONV_OUT_F32 && p.x_scale) xs = load_ordered(p.x_scale + m);
+        const float res = residual_at<T>(p, m, n);
+        int32_t v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = r < q.splits ? load_cluster_s32(part + (i * kTcRows + own) * 4, r) : 0;
+        const int32_t sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        ((T *)p.out)[m * p.out_row + n] = finish<OUT, ACT>(p, sum >> p.down, xs, terms, res);
+    }
+}
+
 template <bool TRANSFORM>
 __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
@@ -351,67 +474,10 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
             }
         }
     } else if (warp >= 4 && warp < 12) {
-        const int quad = warp & 3, half = (warp - 4) >> 2;
-        Ring acc;
-        for (int t = t0; fine && t < tiles; t += step) {
-            const Tile tile = find_tc_tile(q, tables, t);
-            const int n = tile.n0 + quad * 32 + lane;
-            fine = __all_sync(0xFFFFFFFFu, wait(&bar_acc_full[acc.stage], acc.phase));
-            if (!fine) break;
-            tc_fence_after();
-            const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
-            int32_t correction = 0;
-            if (q.ones) {
-                correction = (int32_t)tc_load1(d + q.nt) * 128;
-                tc_wait_load();
-            }
-            if (q.splits > 1) {
-                // this CTA's part of the sums, [row of x][output column], over the stages: all loads have been multiplied
-                for (int col = half * 16; col < tile.rows; col += 32) {
-                    uint32_t v[16];
-                    tc_load16(d + col, v);
-                    tc_wait_load();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(stages + ((col + i) * kTcRows + quad * 32 + lane) * 4),
-                                     "r"(v[i] + (uint32_t)correction)
-                                     : "memory");
-                }
-            } else {
-                with_out_type(p.out_type, [&](auto kind) {
-                    constexpr int OUT = decltype(kind)::value;
-                    using T = typename OutElem<OUT>::type;
-                    const bool inside = n < p.N;
-                    ColumnTerms terms{1.f, 0.f, 0};
-                    if (inside) terms = column_terms<OUT>(p, tile.e, n);
-                    for (int col = half * 16; col < tile.rows; col += 32) {
-                        uint32_t v[16];
-                        T res[16];
-                        tc_load16(d + col, v);
-                        const int m = tile.row0 + col, left = tile.rows - col;
-                        float xs = 1.f;
-                        if (OUT >= HIKONV_OUT_F32 && p.x_scale && lane < left) xs = load_ordered(p.x_scale + m + (lane & 15));
-                        if (OUT >= HIKONV_OUT_F32 && p.residual) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                if (inside && i < left) res[i] = load_ordered((const T *)p.residual + (long long)(m + i) * p.res_row + n);
-                        }
-                        tc_wait_load();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float scale = __shfl_sync(0xFFFFFFFFu, xs, i);
-                            if (inside && i < left)
-                                ((T *)p.out)[(long long)(m + i) * p.out_row + n] =
-                                    finish<OUT>(p, ((int32_t)v[i] + correction) >> p.down, scale, terms, res[i]);
-                        }
-                    }
-                });
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbarrier_arrive(smem_address(&bar_acc_empty[acc.stage]));
-            acc.next(2);
-        }
+        if (q.splits > 1) fine = keep_part(q, tables, t0, tiles, tmem, stages, bar_acc_full);
+        else with_epilogue(p, [&](auto kind, auto act) {
+            fine = finish_tiles<decltype(kind)::value, decltype(act)::value>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
+        });
     }
     if (!fine) {
         ctl.whole = 0;
@@ -424,25 +490,7 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
         for (int r = 0; r < q.splits; ++r) all = all && load_cluster_s32(smem_address(&ctl.whole), r) != 0;
         if (all && warp >= 4 && warp < 12 && t0 < tiles) {
             const Tile tile = find_tc_tile(q, tables, t0);
-            const int columns = kTcRows / q.splits, own = (tid - 128) % columns, stride = 256 / columns;
-            const int n = tile.n0 + rank * columns + own;
-            if (n < p.N) {
-                with_out_type(p.out_type, [&](auto kind) {
-                    constexpr int OUT = decltype(kind)::value;
-                    using T = typename OutElem<OUT>::type;
-                    const ColumnTerms terms = column_terms<OUT>(p, tile.e, n);
-                    for (int i = (tid - 128) / columns; i < tile.rows; i += stride) {
-                        const int m = tile.row0 + i;
-                        float xs = 1.f;
-                        T res{};
-                        if (OUT >= HIKONV_OUT_F32 && p.x_scale) xs = load_ordered(p.x_scale + m);
-                        if (OUT >= HIKONV_OUT_F32 && p.residual) res = load_ordered((const T *)p.residual + m * p.res_row + n);
-                        int32_t sum = 0;
-                        for (int r = 0; r < q.splits; ++r) sum += load_cluster_s32(stages + (i * kTcRows + rank * columns + own) * 4, r);
-                        ((T *)p.out)[m * p.out_row + n] = finish<OUT>(p, sum >> p.down, xs, terms, res);
-                    }
-                });
-            }
+            with_epilogue(p, [&](auto kind, auto act) { finish_parts<decltype(kind)::value, decltype(act)::value>(q, tile, rank, stages); });
         }
         cluster_sync_all();                            // the others may still read this CTA's part
     }

@@ -137,22 +137,26 @@ __device__ __forceinline__ ColumnTerms column_terms(const LinearParams &p, int e
     return c;
 }
 
-// The value of one output from its sum (already shifted down by p.down).
-template <int OUT>
+// The value of one output from its sum (already shifted down by p.down).  ACT < 0: the activation is looked up as the kernel runs.
+template <int OUT, int ACT = -1>
 __device__ __forceinline__ typename OutElem<OUT>::type finish(const LinearParams &p, int32_t sum, float x_scale, const ColumnTerms &c,
-                                                              typename OutElem<OUT>::type residual) {
+                                                              float residual) {
     if constexpr (OUT == HIKONV_OUT_SUMS) {
         return sum;
     } else if constexpr (OUT == HIKONV_OUT_CODES) {
         const long long v = ((long long)sum + c.ibias) >> p.shift;
         return (uint8_t)(int)(v < p.lo ? p.lo : v > p.hi ? p.hi : v);
     } else {
-        float v = activate(fmaf((float)sum * x_scale, c.scale, c.bias), p.act);
-        if (p.residual) v += to_float(residual);
+        const float v = activate(fmaf((float)sum * x_scale, c.scale, c.bias), ACT < 0 ? p.act : ACT) + residual;
         typename OutElem<OUT>::type o;
         from_float(v, &o);
         return o;
     }
+}
+template <typename T>
+__device__ __forceinline__ float residual_at(const LinearParams &p, long long m, int n) {
+    if constexpr (std::is_same<T, int32_t>::value || std::is_same<T, uint8_t>::value) return 0.f;
+    else return p.residual ? to_float(load_ordered((const T *)p.residual + m * p.res_row + n)) : 0.f;
 }
 
 // Calls f with the output type as a constant.
@@ -165,6 +169,22 @@ __device__ __forceinline__ void with_out_type(int out_type, F f) {
         case HIKONV_OUT_F16: f(std::integral_constant<int, HIKONV_OUT_F16>()); break;
         default: f(std::integral_constant<int, HIKONV_OUT_BF16>()); break;
     }
+}
+// ... and the activation (none for whole numbers).
+template <typename F>
+__device__ __forceinline__ void with_epilogue(const LinearParams &p, F f) {
+    with_out_type(p.out_type, [&](auto kind) {
+        if constexpr ((int)HIKONV_OUT_F32 > (int)decltype(kind)::value) {
+            f(kind, std::integral_constant<int, HIKONV_ACT_NONE>());
+        } else {
+            switch (p.act) {
+                case HIKONV_ACT_RELU: f(kind, std::integral_constant<int, HIKONV_ACT_RELU>()); break;
+                case HIKONV_ACT_SILU: f(kind, std::integral_constant<int, HIKONV_ACT_SILU>()); break;
+                case HIKONV_ACT_GELU: f(kind, std::integral_constant<int, HIKONV_ACT_GELU>()); break;
+                default: f(kind, std::integral_constant<int, HIKONV_ACT_NONE>()); break;
+            }
+        }
+    });
 }
 
 }  // namespace hikonv
