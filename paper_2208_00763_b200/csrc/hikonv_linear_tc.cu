@@ -11,6 +11,8 @@
 // shared memory between the two: dense weights are unpacked into the operand's layout, and unsigned 8-bit activations of signed weights
 // get 128 subtracted (their top bit flipped; the instruction takes either two signed or two unsigned operands here).  What that takes
 // off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.
+// TMA wants rows on 16-byte boundaries.  Operands whose rows start anywhere are read by twelve helper warps instead, as aligned words
+// that are moved into place (and unpacked, and flipped) on their way to shared memory.
 //
 // Small layers have fewer tiles than there are SMs: there the CTAs of a cluster share a tile's depth, and the cluster adds their sums
 // through distributed shared memory, each CTA finishing its part of the tile's output columns.
@@ -25,7 +27,13 @@ namespace hikonv {
 constexpr int kTcRows = 128;             // output columns of the layer per tile: rows of the instruction
 constexpr int kTcDepth = 128;            // codes of the depth per stage: one 128-byte swizzled row
 constexpr int kTcMostStages = 12;
-constexpr int kTcThreads = 384, kTcTransformThreads = 640, kTcTransformWarps = 8, kTcEpilogueWarps = 8;
+constexpr int kFirstEpilogueWarp = 4;
+// How operands come to the multiplies: by TMA alone; by TMA and changed in place by warps of their own; read by such warps.
+enum TcMode { kTma = 0, kTransform = 1, kGather = 2 };
+template <int MODE> constexpr int kEpilogueWarps = MODE == kGather ? 4 : 8;
+template <int MODE> constexpr int kHelperWarps = MODE == kTma ? 0 : MODE == kTransform ? 8 : 12;
+template <int MODE> constexpr int kTcThreads = (kFirstEpilogueWarp + kEpilogueWarps<MODE> + kHelperWarps<MODE>) * 32;
+constexpr int kUnitRows = 32;            // operand rows that a helper warp works on at a time
 constexpr size_t kTcMostSmem = 226 * 1024;
 
 struct TcParams {
@@ -36,6 +44,7 @@ struct TcParams {
     int splits, chunks;                  // CTAs that share a tile's depth; stages' worth of depth in all
     int n_blocks, m_tiles, tokens_first;
     uint32_t idesc;
+    int units;                           // of helper work per stage
     int flip, ones;                      // x has its top bits flipped; so many rows (16) with ones lie behind it
     long long wait_cycles;
 };
@@ -152,6 +161,10 @@ __device__ __forceinline__ Tile find_tc_tile(const TcParams &q, const GroupTable
     return r;
 }
 
+__device__ __forceinline__ bool wait_all_of(const TcParams &q, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbarrier_wait(smem_address(bar), parity, q.wait_cycles));
+}
+
 // 16 bytes of dense weights to 16 * 8 / BITS codes in the operand's layout (row `row`, from its piece `piece` of 16 codes on).
 template <int BITS, bool UP>
 __device__ __forceinline__ void unpack_to_operand(uint4 v, uint32_t tile, int row, int piece) {
@@ -173,28 +186,167 @@ __device__ __forceinline__ void unpack_to_operand(uint4 v, uint32_t tile, int ro
         store_shared16(tile + row * 128 + (((piece + j) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
     }
 }
+// One unit (32 rows) of dense weights, from the bytes as TMA left them.
 template <int BITS, bool UP>
-__device__ __forceinline__ void unpack_tile(uint32_t raw, uint32_t tile, int tid) {
+__device__ __forceinline__ void unpack_unit(uint32_t raw, uint32_t tile, int row0) {
     constexpr int PER_ROW = BITS;                      // pieces of 16 bytes: 128 codes of BITS bits
+    const int lane = threadIdx.x & 31;
+    uint4 v[PER_ROW];
 #pragma unroll
-    for (int i = tid; i < kTcRows * PER_ROW; i += kTcTransformWarps * 32)
-        unpack_to_operand<BITS, UP>(load_shared16(raw + i * 16), tile, i / PER_ROW, (i % PER_ROW) * (8 / BITS));
+    for (int j = 0; j < PER_ROW; ++j) v[j] = load_shared16(raw + (row0 * PER_ROW + j * 32 + lane) * 16);
+#pragma unroll
+    for (int j = 0; j < PER_ROW; ++j) {
+        const int i = j * 32 + lane;
+        unpack_to_operand<BITS, UP>(v[j], tile, row0 + i / PER_ROW, (i % PER_ROW) * (8 / BITS));
+    }
 }
 
-__device__ __forceinline__ bool wait_all(const TcParams &q, uint64_t *bar, uint32_t parity) {
-    return __all_sync(0xFFFFFFFFu, mbarrier_wait(smem_address(bar), parity, q.wait_cycles));
+// One unit of an operand's rows that start on any byte.  BITS * 4 lanes take a row's 128 codes, a word each, as aligned words; the word
+// behind a row's last comes from one more load for all rows, and each lane moves its own and its neighbour's together.
+template <int BITS>
+struct RowUnit {
+    static constexpr int LANES = 4 * BITS, ROWS = 32 / LANES, STEPS = kUnitRows / ROWS;
+    uint32_t v[STEPS], behind;
+
+    // src: first byte of the unit's first row and of this part of the depth; left: bytes from there to the row's end; rows: how many exist.
+    __device__ __forceinline__ void load(const uint8_t *src, long long pitch, int left, int rows) {
+        const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int r = i * ROWS + sub;
+            const uint8_t *at = src + r * pitch;
+            const int off = (int)((uintptr_t)at & 3);
+            v[i] = r < rows && word * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + word) : 0u;
+        }
+        const uint8_t *at = src + lane * pitch;
+        const int off = (int)((uintptr_t)at & 3);
+        behind = lane < rows && off && LANES * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + LANES) : 0u;
+    }
+    // To the operand's layout, rows below `limit`; what lies behind the row's end becomes zero (flip: unsigned bytes less 128 everywhere).
+    template <bool UP>
+    __device__ __forceinline__ void store(uint32_t tile, int row0, int limit, const uint8_t *src, long long pitch, int left, uint32_t flip) {
+        const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
+        const int keep = left - word * 4;              // bytes of this lane's word in front of the row's end
+        const uint32_t mask = keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int r = i * ROWS + sub, row = row0 + r;
+            const uint32_t off = (uint32_t)(uintptr_t)(src + r * pitch) & 3u;
+            uint32_t next = __shfl_down_sync(0xFFFFFFFFu, v[i], 1);
+            const uint32_t last = __shfl_sync(0xFFFFFFFFu, behind, r);
+            if (word == LANES - 1) next = last;
+            const uint32_t w = __funnelshift_r(v[i], next, off * 8) & mask;
+            const uint32_t line = tile + row * 128, turn = row & 7;
+            if constexpr (BITS == 8) {
+                if (row < limit) asm volatile("st.shared.u32 [%0], %1;" ::"r"(line + ((((uint32_t)word >> 2) ^ turn) << 4) + (word & 3) * 4), "r"(w ^ flip) : "memory");
+            } else if constexpr (BITS == 4) {
+                uint32_t o[2];
+                unpack4<UP>(w, o);
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(line + ((((uint32_t)word >> 1) ^ turn) << 4) + (word & 1) * 8), "r"(o[0]), "r"(o[1])
+                             : "memory");
+            } else if constexpr (BITS == 2) {
+                uint32_t o[4];
+                unpack2<UP>(w, o);
+                store_shared16(line + (((uint32_t)word ^ turn) << 4), o[0], o[1], o[2], o[3]);
+            } else {
+                uint32_t o[4];
+                unpack1<UP>(w, o);
+                store_shared16(line + (((uint32_t)(2 * word) ^ turn) << 4), o[0], o[1], o[2], o[3]);
+                unpack1<UP>(w >> 16, o);
+                store_shared16(line + (((uint32_t)(2 * word + 1) ^ turn) << 4), o[0], o[1], o[2], o[3]);
+            }
+        }
+    }
+};
+
+// The helper warps: units of all stages of all tiles of this CTA, dealt out one after the other, so that neighbouring stages are worked on
+// side by side.
+template <int MODE>
+__device__ __forceinline__ bool help(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, int c0, int c1, uint32_t stages,
+                                     TcControl &ctl) {
+    const LinearParams &p = q.p;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
+    int unit = warp, c = c0, t = t0, stage = 0;
+    uint32_t phase = 0;
+    Tile tile;
+    if (t < tiles) tile = find_tc_tile(q, tables, t);
+    for (;; unit += kHelperWarps<MODE>) {
+        while (unit >= q.units) {                      // on to the stage that this unit belongs to
+            unit -= q.units;
+            if (++stage == q.stages) {
+                stage = 0;
+                phase ^= 1;
+            }
+            if (++c >= c1) {
+                c = c0;
+                t += step;
+                if (t < tiles) tile = find_tc_tile(q, tables, t);
+            }
+        }
+        if (t >= tiles) return true;
+        const uint32_t at = stages + stage * q.stage_bytes;
+        const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0;
+        const bool of_w = unit < w_units;
+        const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
+        if constexpr (MODE == kTransform) {
+            if (!wait_all_of(q, &ctl.full[stage], phase)) return false;
+            if (of_w) {
+                const uint32_t raw = at + q.raw_off;
+                if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, at, row0) : unpack_unit<4, false>(raw, at, row0);
+                else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, at, row0) : unpack_unit<2, false>(raw, at, row0);
+                else p.down ? unpack_unit<1, true>(raw, at, row0) : unpack_unit<1, false>(raw, at, row0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int i = row0 * 8 + j * 32 + lane;
+                    if (i < q.nt * 8) {
+                        const uint32_t a = at + q.x_off + i * 16;
+                        const uint4 v = load_shared16(a);
+                        store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
+                    }
+                }
+            }
+        } else {
+            // the loads are under way before the stage is free
+            if (of_w) {
+                const uint8_t *src = p.w + ((long long)tile.e * p.N + tile.n0 + row0) * p.w_row + (long long)c * kTcDepth * p.w_bits / 8;
+                const int left = (int)min(p.w_row - (long long)c * kTcDepth * p.w_bits / 8, 1024ll), rows = p.N - tile.n0 - row0;
+                auto run = [&](auto bits) {
+                    constexpr int BITS = decltype(bits)::value;
+                    RowUnit<BITS> u;
+                    u.load(src, p.w_row, left, rows);
+                    if (!wait_all_of(q, &ctl.empty[stage], phase ^ 1)) return false;
+                    p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, 0);
+                    return true;
+                };
+                const bool ok = p.w_bits == 8 ? run(std::integral_constant<int, 8>()) : p.w_bits == 4 ? run(std::integral_constant<int, 4>())
+                                : p.w_bits == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
+                if (!ok) return false;
+            } else {
+                const uint8_t *src = p.x + (long long)(tile.row0 + row0) * p.x_row + (long long)c * kTcDepth;
+                const int left = min(p.K - c * kTcDepth, 1024), rows = tile.rows - row0;
+                RowUnit<8> u;
+                u.load(src, p.x_row, left, rows);
+                if (!wait_all_of(q, &ctl.empty[stage], phase ^ 1)) return false;
+                u.store<false>(at + q.x_off, row0, q.nt, src, p.x_row, left, q.flip ? 0x80808080u : 0u);
+            }
+        }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[stage]));
+    }
 }
 
 // The epilogue of a warp: the 32 output columns of its quarter of the lanes, every other batch of 16 rows of x.  Each output costs about
 // ten instructions here, and with eight warps they have to overlap: output type and activation are constants, a batch's 16 sums and
 // residuals are in flight together, and what belongs to a column is loaded before its sums are there.
-template <int OUT, int ACT>
+template <int WARPS, int OUT, int ACT>
 __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, uint32_t tmem,
                                              uint64_t *acc_full, uint64_t *acc_empty) {
     using T = typename OutElem<OUT>::type;
     constexpr bool REAL = OUT >= HIKONV_OUT_F32;
     const LinearParams &p = q.p;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - 4) >> 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2;
     Ring acc;
     for (int t = t0; t < tiles; t += step) {
         const Tile tile = find_tc_tile(q, tables, t);
@@ -202,7 +354,7 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
         const bool inside = n < p.N;
         ColumnTerms terms{1.f, 0.f, 0};
         if (inside) terms = column_terms<OUT>(p, tile.e, n);
-        if (!wait_all(q, &acc_full[acc.stage], acc.phase)) return false;
+        if (!wait_all_of(q, &acc_full[acc.stage], acc.phase)) return false;
         tc_fence_after();
         const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
         int32_t correction = 0;
@@ -210,7 +362,7 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
             correction = (int32_t)tc_load1(d + q.nt) * 128;
             tc_wait_load();
         }
-        for (int col = half * 16; col < tile.rows; col += 32) {
+        for (int col = half * 16; col < tile.rows; col += WARPS * 4) {
             uint32_t v[16];
             float scale[16], res[16];
             tc_load16(d + col, v);
@@ -258,12 +410,13 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
 
 // With a shared depth: this CTA's part of the sums to shared memory, [row of x][output column], over the stages (all loads have been
 // multiplied when the sums are there).
+template <int WARPS>
 __device__ __forceinline__ bool keep_part(const TcParams &q, const GroupTables &tables, int t, int tiles, uint32_t tmem, uint32_t part,
                                           uint64_t *acc_full) {
     if (t >= tiles) return true;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - 4) >> 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2;
     const Tile tile = find_tc_tile(q, tables, t);
-    if (!wait_all(q, &acc_full[0], 0)) return false;
+    if (!wait_all_of(q, &acc_full[0], 0)) return false;
     tc_fence_after();
     const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16);
     uint32_t correction = 0;
@@ -271,7 +424,7 @@ __device__ __forceinline__ bool keep_part(const TcParams &q, const GroupTables &
         correction = tc_load1(d + q.nt) * 128u;
         tc_wait_load();
     }
-    for (int col = half * 16; col < tile.rows; col += 32) {
+    for (int col = half * 16; col < tile.rows; col += WARPS * 4) {
         uint32_t v[16];
         tc_load16(d + col, v);
         tc_wait_load();
@@ -284,14 +437,14 @@ __device__ __forceinline__ bool keep_part(const TcParams &q, const GroupTables &
 }
 
 // ... and the sums of all parts through the epilogue, this CTA's share of the output columns.
-template <int OUT, int ACT>
+template <int WARPS, int OUT, int ACT>
 __device__ __forceinline__ void finish_parts(const TcParams &q, const Tile &tile, int rank, uint32_t part) {
     using T = typename OutElem<OUT>::type;
     const LinearParams &p = q.p;
-    const int tid = threadIdx.x - 128, columns = kTcRows / q.splits, own = rank * columns + tid % columns, n = tile.n0 + own;
+    const int tid = threadIdx.x - kFirstEpilogueWarp * 32, columns = kTcRows / q.splits, own = rank * columns + tid % columns, n = tile.n0 + own;
     if (n >= p.N) return;
     const ColumnTerms terms = column_terms<OUT>(p, tile.e, n);
-    for (int i = tid / columns; i < tile.rows; i += 256 / columns) {
+    for (int i = tid / columns; i < tile.rows; i += WARPS * 32 / columns) {
         const long long m = tile.row0 + i;
         float xs = 1.f;
         if (OUT >= HIKONV_OUT_F32 && p.x_scale) xs = load_ordered(p.x_scale + m);
@@ -304,12 +457,13 @@ __device__ __forceinline__ void finish_parts(const TcParams &q, const Tile &tile
     }
 }
 
-template <bool TRANSFORM>
-__global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 1)
+template <int MODE>
+__global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     linear_tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
     extern __shared__ __align__(16) uint8_t dynamic[];
     TcControl &ctl = *reinterpret_cast<TcControl *>(dynamic);
     uint64_t *bar_full = ctl.full, *bar_ready = ctl.ready, *bar_empty = ctl.empty, *bar_acc_full = ctl.acc_full, *bar_acc_empty = ctl.acc_empty;
+    constexpr int EPI = kEpilogueWarps<MODE>, FIRST_HELPER = kFirstEpilogueWarp + EPI;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const LinearParams &p = q.p;
     const uint32_t stages = (smem_address(dynamic) + (uint32_t)sizeof(TcControl) + 1023u) & ~1023u;
@@ -322,24 +476,26 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
     if (tid == 0) {
         for (int i = 0; i < q.stages; ++i) {
             mbarrier_init(smem_address(&bar_full[i]), 1);
-            mbarrier_init(smem_address(&bar_ready[i]), kTcTransformWarps);
+            mbarrier_init(smem_address(&bar_ready[i]), q.units);
             mbarrier_init(smem_address(&bar_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbarrier_init(smem_address(&bar_acc_full[i]), 1);
-            mbarrier_init(smem_address(&bar_acc_empty[i]), kTcEpilogueWarps);
+            mbarrier_init(smem_address(&bar_acc_empty[i]), EPI);
         }
         mbarrier_init(smem_address(&ctl.drain), 1);
         mbarrier_init_fence();
         ctl.whole = 1;
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
+        if (MODE != kGather) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
+        }
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(2 * q.acc_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
-    if (TRANSFORM && q.ones) {
+    if (MODE != kTma && q.ones) {
         // sixteen rows behind the rows of x, the first of them ones; nothing writes there again
         for (int i = tid; i < q.stages * 128; i += blockDim.x) {
             const uint32_t v = (i & 127) < 8 ? 0x01010101u : 0u;
@@ -384,7 +540,7 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
     auto wait = [&](uint64_t *bar, uint32_t parity) { return mbarrier_wait(smem_address(bar), parity, q.wait_cycles); };
     bool fine = true;
     if (warp == 0) {
-        if (lane == 0) {
+        if (MODE != kGather && lane == 0) {
             Ring ring;
             const int depth_bytes = kTcDepth * p.w_bits / 8;
             const uint32_t bytes = (uint32_t)(q.nt * kTcDepth + kTcRows * depth_bytes);
@@ -422,8 +578,8 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
                 if (!fine) break;
                 tc_fence_after();
                 for (int c = c0; c < c1; ++c) {
-                    fine = wait(&bar_full[ring.stage], ring.phase);
-                    if (TRANSFORM) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
+                    if (MODE != kGather) fine = wait(&bar_full[ring.stage], ring.phase);
+                    if (MODE != kTma) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
                     if (!fine) break;
                     tc_fence_after();
                     const uint32_t at = stages + ring.stage * q.stage_bytes;
@@ -442,41 +598,12 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
                 wait(&ctl.drain, 0);
             }
         }
-    } else if (TRANSFORM && warp >= 12) {
-        Ring ring;
-        const int at_tid = tid - 12 * 32;
-        for (int t = t0; fine && t < tiles; t += step) {
-            for (int c = c0; c < c1; ++c) {
-                fine = wait(&bar_full[ring.stage], ring.phase);
-                fine = __all_sync(0xFFFFFFFFu, fine);
-                if (!fine) break;
-                const uint32_t at = stages + ring.stage * q.stage_bytes;
-                if (p.w_bits == 4) {
-                    if (p.down) unpack_tile<4, true>(at + q.raw_off, at, at_tid);
-                    else unpack_tile<4, false>(at + q.raw_off, at, at_tid);
-                } else if (p.w_bits == 2) {
-                    if (p.down) unpack_tile<2, true>(at + q.raw_off, at, at_tid);
-                    else unpack_tile<2, false>(at + q.raw_off, at, at_tid);
-                } else if (p.w_bits == 1) {
-                    if (p.down) unpack_tile<1, true>(at + q.raw_off, at, at_tid);
-                    else unpack_tile<1, false>(at + q.raw_off, at, at_tid);
-                }
-                if (q.flip)
-                    for (int i = at_tid; i < q.nt * 8; i += kTcTransformWarps * 32) {
-                        const uint32_t a = at + q.x_off + i * 16;
-                        const uint4 v = load_shared16(a);
-                        store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
-                    }
-                proxy_fence();
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive(smem_address(&bar_ready[ring.stage]));
-                ring.next(q.stages);
-            }
-        }
-    } else if (warp >= 4 && warp < 12) {
-        if (q.splits > 1) fine = keep_part(q, tables, t0, tiles, tmem, stages, bar_acc_full);
+    } else if (MODE != kTma && warp >= FIRST_HELPER) {
+        if constexpr (MODE != kTma) fine = help<MODE>(q, tables, t0, tiles, step, c0, c1, stages, ctl);
+    } else if (warp >= kFirstEpilogueWarp && warp < FIRST_HELPER) {
+        if (q.splits > 1) fine = keep_part<EPI>(q, tables, t0, tiles, tmem, stages, bar_acc_full);
         else with_epilogue(p, [&](auto kind, auto act) {
-            fine = finish_tiles<decltype(kind)::value, decltype(act)::value>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
+            fine = finish_tiles<EPI, decltype(kind)::value, decltype(act)::value>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
         });
     }
     if (!fine) {
@@ -488,9 +615,9 @@ __global__ void __launch_bounds__(TRANSFORM ? kTcTransformThreads : kTcThreads, 
         cluster_sync_all();
         bool all = true;
         for (int r = 0; r < q.splits; ++r) all = all && load_cluster_s32(smem_address(&ctl.whole), r) != 0;
-        if (all && warp >= 4 && warp < 12 && t0 < tiles) {
+        if (all && warp >= kFirstEpilogueWarp && warp < FIRST_HELPER && t0 < tiles) {
             const Tile tile = find_tc_tile(q, tables, t0);
-            with_epilogue(p, [&](auto kind, auto act) { finish_parts<decltype(kind)::value, decltype(act)::value>(q, tile, rank, stages); });
+            with_epilogue(p, [&](auto kind, auto act) { finish_parts<EPI, decltype(kind)::value, decltype(act)::value>(q, tile, rank, stages); });
         }
         cluster_sync_all();                            // the others may still read this CTA's part
     }
@@ -541,17 +668,20 @@ static int sm_count_here() {
     return sms;
 }
 
-// Whether this kernel takes the layer: rows of x and w on 16-byte boundaries, operands that are both signed or both unsigned bytes or become
-// so, and few enough tiles for 32-bit counts.
+// Whether this kernel takes the layer: operands that are both signed or both unsigned bytes or become so, and few enough tiles for
+// 32-bit counts.
 bool linear_tc_takes(const LinearParams &p) {
-    if ((uintptr_t)p.x % 16 || (uintptr_t)p.w % 16 || (p.M > 1 && p.x_row % 16) || p.w_row % 16) return false;
     if (p.w_u8 && p.x_signed) return false;
     if ((long long)p.E * p.N > 0x7FFFFFFFll || p.M > (1 << 30)) return false;
     return ((long long)p.M / 16 + (p.E < p.M ? p.E : p.M) + 1) * ceil_div(p.N, kTcRows) < 0x3FFFFFFFll;
 }
+// Whether TMA reads its rows: all on 16-byte boundaries.
+static bool rows_aligned(const LinearParams &p) {
+    return (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && (p.M == 1 || p.x_row % 16 == 0) && p.w_row % 16 == 0;
+}
 
 // Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.
-static void choose_tile(const LinearParams &p, bool ones, int sms, int *nt_out, int *splits_out) {
+static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int *nt_out, int *splits_out) {
     const int n_blocks = ceil_div(p.N, kTcRows), chunks = ceil_div(p.K, kTcDepth);
     const int most = ones ? 240 : 256;
     double best = 1e300;
@@ -563,7 +693,7 @@ static void choose_tile(const LinearParams &p, bool ones, int sms, int *nt_out, 
             // clusters of four and more do not fill every SM: their CTAs share one part of the GPU
             if (splits > 1 && (tiles * splits > sms - 20 || nt > 128)) break;
             const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
-            const double per_chunk = 256.0 + 2.0 * nt + (p.w_bits < 8 ? 128.0 : 0.0);
+            const double per_chunk = mode == kGather ? 4.0 * (kTcRows + nt) + 300.0 : 256.0 + 2.0 * nt + (p.w_bits < 8 ? 128.0 : 0.0);
             const double time = waves * ceil_div(chunks, splits) * per_chunk + (splits > 1 ? 1500.0 + 4.0 * nt * splits : 6.0 * nt);
             if (time < best) {
                 best = time;
@@ -583,8 +713,9 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     const bool as_unsigned = (p.x_u8 || p.w_u8) && !p.x_signed && !p.w_signed;
     q.flip = p.x_u8 && !as_unsigned;
     q.ones = q.flip ? 16 : 0;
-    choose_tile(p, q.flip, sms, &q.nt, &q.splits);
-    const bool transform = p.w_bits < 8 || q.flip;
+    const int mode = !rows_aligned(p) ? kGather : p.w_bits < 8 || q.flip ? kTransform : kTma;
+    choose_tile(p, mode, q.flip, sms, &q.nt, &q.splits);
+    q.units = (mode == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0) + (mode == kGather || q.flip ? ceil_div(q.nt, kUnitRows) : 0);
     q.chunks = ceil_div(p.K, kTcDepth);
     q.n_blocks = ceil_div(p.N, kTcRows);
     q.m_tiles = ceil_div(p.M, q.nt);
@@ -593,7 +724,7 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     while (q.acc_cols < q.nt + q.ones) q.acc_cols *= 2;
     q.x_off = kTcRows * kTcDepth;
     q.raw_off = q.x_off + (q.nt + q.ones) * kTcDepth;
-    q.stage_bytes = (int)align_up(q.raw_off + (p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
+    q.stage_bytes = (int)align_up(q.raw_off + (mode == kTransform && p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
     q.stages = (int)((kTcMostSmem - 2048 - tables) / q.stage_bytes);
     if (q.stages > kTcMostStages) q.stages = kTcMostStages;
@@ -609,30 +740,35 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     const size_t smem = (size_t)q.stages * q.stage_bytes + 2048 + tables;
 
     CUtensorMap map_x, map_w;
-    if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt, true) ||
+    if (mode == kGather) {
+        memset(&map_x, 0, sizeof(map_x));
+        memset(&map_w, 0, sizeof(map_w));
+    } else if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt, true) ||
         !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows, p.w_bits == 8))
         return HIKONV_ERR_CUDA;
     long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
     const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
-    const void *kernel = transform ? (const void *)linear_tc_kernel<true> : (const void *)linear_tc_kernel<false>;
-    return with_dynamic_smem(kernel, smem > 49 * 1024 ? smem : 49 * 1024, [&] {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(grid);
-        cfg.blockDim = dim3(transform ? kTcTransformThreads : kTcThreads);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)q.splits;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = q.splits > 1 ? 2 : 1;
-        const cudaError_t e = transform ? cudaLaunchKernelEx(&cfg, linear_tc_kernel<true>, q, map_x, map_w)
-                                        : cudaLaunchKernelEx(&cfg, linear_tc_kernel<false>, q, map_x, map_w);
-        return e == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
-    });
+    auto launch = [&](auto kernel, int threads) {
+        return with_dynamic_smem((const void *)kernel, smem > 49 * 1024 ? smem : 49 * 1024, [&] {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(grid);
+            cfg.blockDim = dim3((unsigned)threads);
+            cfg.dynamicSmemBytes = smem;
+            cfg.stream = st;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = (unsigned)q.splits;
+            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = q.splits > 1 ? 2 : 1;
+            return cudaLaunchKernelEx(&cfg, kernel, q, map_x, map_w) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+        });
+    };
+    if (mode == kTma) return launch(linear_tc_kernel<kTma>, kTcThreads<kTma>);
+    if (mode == kTransform) return launch(linear_tc_kernel<kTransform>, kTcThreads<kTransform>);
+    return launch(linear_tc_kernel<kGather>, kTcThreads<kGather>);
 }
 
 int read_linear_timeouts(unsigned int *h_count) {
