@@ -98,11 +98,15 @@ __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ int32_t load_cluster_s32(uint32_t smem_addr, uint32_t rank) {
+__device__ __forceinline__ uint32_t remote_address(uint32_t smem_addr, uint32_t rank) {
     uint32_t remote;
-    int32_t v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr), "r"(rank));
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    return remote;
+}
+// Without a clobber of memory, so that several are in flight; volatile, so that they stay between the two cluster barriers.
+__device__ __forceinline__ int32_t load_cluster_s32(uint32_t remote) {
+    int32_t v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote));
     return v;
 }
 __device__ __forceinline__ uint4 load_shared16(uint32_t a) {
@@ -112,6 +116,14 @@ __device__ __forceinline__ uint4 load_shared16(uint32_t a) {
 }
 __device__ __forceinline__ void store_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// One lane of a converged warp.  The warps that issue TMA copies and multiplies run their loops as a whole and issue under this: with one
+// thread in the loop, its values are not known to be uniform and a step of 128 codes took 590 cycles instead of 130.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
 }
 
 // A ring of stages: which one is next and in which of its phases it is.
@@ -211,49 +223,78 @@ struct RowUnit {
     // src: first byte of the unit's first row and of this part of the depth; left: bytes from there to the row's end; rows: how many exist.
     __device__ __forceinline__ void load(const uint8_t *src, long long pitch, int left, int rows) {
         const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
+        if (rows >= kUnitRows && left >= 4 * LANES + 4) {
+            const uint8_t *at = src + sub * pitch;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const int r = i * ROWS + sub;
-            const uint8_t *at = src + r * pitch;
-            const int off = (int)((uintptr_t)at & 3);
-            v[i] = r < rows && word * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + word) : 0u;
+            for (int i = 0; i < STEPS; ++i) {
+                v[i] = load_ordered(reinterpret_cast<const uint32_t *>((uintptr_t)at & ~(uintptr_t)3) + word);
+                at += ROWS * pitch;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int r = i * ROWS + sub;
+                const uint8_t *at = src + r * pitch;
+                const int off = (int)((uintptr_t)at & 3);
+                v[i] = r < rows && word * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + word) : 0u;
+            }
         }
         const uint8_t *at = src + lane * pitch;
         const int off = (int)((uintptr_t)at & 3);
         behind = lane < rows && off && LANES * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + LANES) : 0u;
     }
-    // To the operand's layout, rows below `limit`; what lies behind the row's end becomes zero (flip: unsigned bytes less 128 everywhere).
+
+    // To the operand's layout, rows below `limit` (a multiple of 16); what lies behind the row's end becomes zero (flip: unsigned bytes less 128 everywhere).
+    // A row's shift repeats every four rows and its swizzle every eight, so a word costs two shuffles, a select, a shift and a store.
     template <bool UP>
     __device__ __forceinline__ void store(uint32_t tile, int row0, int limit, const uint8_t *src, long long pitch, int left, uint32_t flip) {
         const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
         const int keep = left - word * 4;              // bytes of this lane's word in front of the row's end
         const uint32_t mask = keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
+        const uint32_t s0 = (uint32_t)(uintptr_t)src & 3u, sp = (uint32_t)pitch & 3u;
+        const bool words = (s0 | sp) == 0;             // rows start on words
+        const uint32_t line = tile + (row0 + sub) * 128 + word * (32 / BITS);
+        constexpr int TURNS = ROWS >= 8 ? 1 : 8 / ROWS, SHIFTS = ROWS >= 4 ? 1 : 4 / ROWS;
+        uint32_t at[TURNS], shift[SHIFTS];
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) at[i] = line ^ (((i * ROWS + sub) & 7) << 4);
+#pragma unroll
+        for (int i = 0; i < SHIFTS; ++i) shift[i] = ((s0 + (i * ROWS + sub) * sp) & 3u) * 8;
+        if (!words) {
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                uint32_t next = __shfl_down_sync(0xFFFFFFFFu, v[i], 1);
+                const uint32_t last = __shfl_sync(0xFFFFFFFFu, behind, i * ROWS + sub);
+                if (word == LANES - 1) next = last;
+                v[i] = __funnelshift_r(v[i], next, shift[i % SHIFTS]);
+            }
+        }
+        if (BITS == 8 && limit - row0 < kUnitRows) {   // the half unit behind the last whole one
+#pragma unroll
+            for (int i = 0; i < STEPS / 2; ++i)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at[i % TURNS] + i * ROWS * 128), "r"((v[i] & mask) ^ flip) : "memory");
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            const int r = i * ROWS + sub, row = row0 + r;
-            const uint32_t off = (uint32_t)(uintptr_t)(src + r * pitch) & 3u;
-            uint32_t next = __shfl_down_sync(0xFFFFFFFFu, v[i], 1);
-            const uint32_t last = __shfl_sync(0xFFFFFFFFu, behind, r);
-            if (word == LANES - 1) next = last;
-            const uint32_t w = __funnelshift_r(v[i], next, off * 8) & mask;
-            const uint32_t line = tile + row * 128, turn = row & 7;
+            const uint32_t w = v[i] & mask;
+            const uint32_t to = at[i % TURNS] + i * ROWS * 128;
             if constexpr (BITS == 8) {
-                if (row < limit) asm volatile("st.shared.u32 [%0], %1;" ::"r"(line + ((((uint32_t)word >> 2) ^ turn) << 4) + (word & 3) * 4), "r"(w ^ flip) : "memory");
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(w ^ flip) : "memory");
             } else if constexpr (BITS == 4) {
                 uint32_t o[2];
                 unpack4<UP>(w, o);
-                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(line + ((((uint32_t)word >> 1) ^ turn) << 4) + (word & 1) * 8), "r"(o[0]), "r"(o[1])
-                             : "memory");
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(to), "r"(o[0]), "r"(o[1]) : "memory");
             } else if constexpr (BITS == 2) {
                 uint32_t o[4];
                 unpack2<UP>(w, o);
-                store_shared16(line + (((uint32_t)word ^ turn) << 4), o[0], o[1], o[2], o[3]);
+                store_shared16(to, o[0], o[1], o[2], o[3]);
             } else {
                 uint32_t o[4];
                 unpack1<UP>(w, o);
-                store_shared16(line + (((uint32_t)(2 * word) ^ turn) << 4), o[0], o[1], o[2], o[3]);
+                store_shared16(to, o[0], o[1], o[2], o[3]);
                 unpack1<UP>(w >> 16, o);
-                store_shared16(line + (((uint32_t)(2 * word + 1) ^ turn) << 4), o[0], o[1], o[2], o[3]);
+                store_shared16(to ^ 16, o[0], o[1], o[2], o[3]);
             }
         }
     }
@@ -408,53 +449,86 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
     return true;
 }
 
-// With a shared depth: this CTA's part of the sums to shared memory, [row of x][output column], over the stages (all loads have been
-// multiplied when the sums are there).
-template <int WARPS>
-__device__ __forceinline__ bool keep_part(const TcParams &q, const GroupTables &tables, int t, int tiles, uint32_t tmem, uint32_t part,
-                                          uint64_t *acc_full) {
-    if (t >= tiles) return true;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = warp & 3, half = (warp - kFirstEpilogueWarp) >> 2;
-    const Tile tile = find_tc_tile(q, tables, t);
-    if (!wait_all_of(q, &acc_full[0], 0)) return false;
-    tc_fence_after();
-    const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16);
-    uint32_t correction = 0;
-    if (q.ones) {
-        correction = tc_load1(d + q.nt) * 128u;
-        tc_wait_load();
-    }
-    for (int col = half * 16; col < tile.rows; col += WARPS * 4) {
-        uint32_t v[16];
-        tc_load16(d + col, v);
-        tc_wait_load();
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(part + ((col + i) * kTcRows + quad * 32 + lane) * 4), "r"(v[i] + correction) : "memory");
-    }
-    tc_fence_before();
-    return true;
-}
-
-// ... and the sums of all parts through the epilogue, this CTA's share of the output columns.
+// With a shared depth: this CTA's part of the sums goes to shared memory, [row of x][output column], over the stages (all loads have been
+// multiplied when the sums are there); after the cluster's barrier the CTA takes the sums of all parts through the epilogue for its share
+// of the output columns.  What else that needs is loaded before the barrier.
 template <int WARPS, int OUT, int ACT>
-__device__ __forceinline__ void finish_parts(const TcParams &q, const Tile &tile, int rank, uint32_t part) {
+__device__ __forceinline__ bool finish_shared_tile(const TcParams &q, const GroupTables &tables, int t, int tiles, int rank, uint32_t tmem,
+                                                   uint32_t part, TcControl &ctl) {
     using T = typename OutElem<OUT>::type;
+    constexpr bool REAL = OUT >= HIKONV_OUT_F32;
+    constexpr int BATCH = 4;                           // rows at a time: a fetch from another SM takes several hundred cycles
     const LinearParams &p = q.p;
-    const int tid = threadIdx.x - kFirstEpilogueWarp * 32, columns = kTcRows / q.splits, own = rank * columns + tid % columns, n = tile.n0 + own;
-    if (n >= p.N) return;
-    const ColumnTerms terms = column_terms<OUT>(p, tile.e, n);
-    for (int i = tid / columns; i < tile.rows; i += WARPS * 32 / columns) {
-        const long long m = tile.row0 + i;
-        float xs = 1.f;
-        if (OUT >= HIKONV_OUT_F32 && p.x_scale) xs = load_ordered(p.x_scale + m);
-        const float res = residual_at<T>(p, m, n);
-        int32_t v[8];
+    const int tid = threadIdx.x - kFirstEpilogueWarp * 32, lane = tid & 31, quad = (tid >> 5) & 3, half = tid >> 7;
+    const int columns = kTcRows / q.splits, own = rank * columns + tid % columns, first = tid / columns, step = WARPS * 32 / columns;
+    Tile tile{0, 0, 0, 0};
+    if (t < tiles) tile = find_tc_tile(q, tables, t);
+    const int n = tile.n0 + own;
+    const bool inside = n < p.N;
+    ColumnTerms terms{1.f, 0.f, 0};
+    float xs[BATCH], res[BATCH];
+    auto fetch = [&](int i0) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = r < q.splits ? load_cluster_s32(part + (i * kTcRows + own) * 4, r) : 0;
-        const int32_t sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-        ((T *)p.out)[m * p.out_row + n] = finish<OUT, ACT>(p, sum >> p.down, xs, terms, res);
+        for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * step;
+            xs[b] = 1.f;
+            res[b] = 0.f;
+            if (REAL && inside && i < tile.rows) {
+                if (p.x_scale) xs[b] = load_ordered(p.x_scale + tile.row0 + i);
+                res[b] = residual_at<T>(p, tile.row0 + i, n);
+            }
+        }
+    };
+    if (t < tiles && inside) terms = column_terms<OUT>(p, tile.e, n);
+    fetch(first);
+    bool fine = true;
+    if (t < tiles) {
+        fine = wait_all_of(q, &ctl.acc_full[0], 0);
+        if (fine) {
+            tc_fence_after();
+            const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16);
+            uint32_t correction = 0;
+            if (q.ones) {
+                correction = tc_load1(d + q.nt) * 128u;
+                tc_wait_load();
+            }
+            for (int col = half * 16; col < tile.rows; col += WARPS * 4) {
+                uint32_t v[16];
+                tc_load16(d + col, v);
+                tc_wait_load();
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(part + ((col + i) * kTcRows + quad * 32 + lane) * 4), "r"(v[i] + correction) : "memory");
+            }
+            tc_fence_before();
+        }
     }
+    if (!fine) ctl.whole = 0;
+    uint32_t from[8], flag = 1;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) from[r] = remote_address(part + own * 4, r < q.splits ? r : 0);
+    cluster_sync_all();
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < q.splits) flag &= (uint32_t)load_cluster_s32(remote_address(smem_address(&ctl.whole), r));
+    for (int i0 = first; i0 < tile.rows; i0 += BATCH * step) {
+        if (i0 != first) fetch(i0);
+        int32_t v[8][BATCH];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) v[r][b] = r < q.splits && i0 + b * step < tile.rows ? load_cluster_s32(from[r] + (i0 + b * step) * kTcRows * 4) : 0;
+        if (flag && inside) {
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int i = i0 + b * step;
+                const int32_t sum = ((v[0][b] + v[1][b]) + (v[2][b] + v[3][b])) + ((v[4][b] + v[5][b]) + (v[6][b] + v[7][b]));
+                if (i < tile.rows) ((T *)p.out)[(tile.row0 + i) * p.out_row + n] = finish<OUT, ACT>(p, sum >> p.down, xs[b], terms, res[b]);
+            }
+        }
+    }
+    cluster_sync_all();                                // the others may still read this CTA's part
+    return fine;
 }
 
 template <int MODE>
@@ -507,10 +581,11 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl.tmem;
-    grid_dependency_wait();
 
+    // Each role waits for the kernel before where it first touches global memory; the multiplying warp never does.
     int tiles = q.m_tiles * q.n_blocks;
     if (p.offsets) {
+        grid_dependency_wait();
         for (int e = tid; e < p.E; e += blockDim.x) {
             const int2 r = group_rows(p, e);
             group_row[e] = r;
@@ -537,24 +612,29 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     const int t0 = blockIdx.x / q.splits, step = gridDim.x / q.splits;
     const int c0 = (int)((long long)q.chunks * rank / q.splits), c1 = (int)((long long)q.chunks * (rank + 1) / q.splits);
 
-    auto wait = [&](uint64_t *bar, uint32_t parity) { return mbarrier_wait(smem_address(bar), parity, q.wait_cycles); };
+    auto wait = [&](uint64_t *bar, uint32_t parity) { return wait_all_of(q, bar, parity); };
     bool fine = true;
     if (warp == 0) {
-        if (MODE != kGather && lane == 0) {
+        if (MODE != kGather) {
             Ring ring;
             const int depth_bytes = kTcDepth * p.w_bits / 8;
             const uint32_t bytes = (uint32_t)(q.nt * kTcDepth + kTcRows * depth_bytes);
+            const uint32_t w_off = p.w_bits == 8 ? 0u : (uint32_t)q.raw_off;
             int loads = 0;
             for (int t = t0; fine && t < tiles; t += step) {
                 const Tile tile = find_tc_tile(q, tables, t);
                 const int w_row0 = tile.e * p.N + tile.n0;
+                if (loads == 0) grid_dependency_wait();
                 for (int c = c0; c < c1; ++c) {
                     fine = wait(&bar_empty[ring.stage], ring.phase ^ 1);
                     if (!fine) break;
                     const uint32_t at = stages + ring.stage * q.stage_bytes, bar = smem_address(&bar_full[ring.stage]);
-                    mbarrier_arrive_expect(bar, bytes);
-                    tma_load_2d(at + (p.w_bits == 8 ? 0 : q.raw_off), &map_w, c * depth_bytes, w_row0, bar);
-                    tma_load_2d(at + q.x_off, &map_x, c * kTcDepth, tile.row0, bar);
+                    if (elect_one()) {
+                        mbarrier_arrive_expect(bar, bytes);
+                        tma_load_2d(at + w_off, &map_w, c * depth_bytes, w_row0, bar);
+                        tma_load_2d(at + q.x_off, &map_x, c * kTcDepth, tile.row0, bar);
+                    }
+                    __syncwarp();
                     ++loads;
                     ring.next(q.stages);
                 }
@@ -567,58 +647,56 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            Ring ring, acc;
-            for (int t = t0; fine && t < tiles; t += step) {
-                const Tile tile = find_tc_tile(q, tables, t);
-                const uint32_t cols = q.ones ? (uint32_t)(q.nt + q.ones) : (uint32_t)((tile.rows + 15) & ~15);
-                const uint32_t idesc = q.idesc | ((cols >> 3) << 17);
-                const uint32_t d = tmem + acc.stage * q.acc_cols;
-                fine = wait(&bar_acc_empty[acc.stage], acc.phase ^ 1);
+        Ring ring, acc;
+        for (int t = t0; fine && t < tiles; t += step) {
+            const Tile tile = find_tc_tile(q, tables, t);
+            const uint32_t cols = q.ones ? (uint32_t)(q.nt + q.ones) : (uint32_t)((tile.rows + 15) & ~15);
+            const uint32_t idesc = q.idesc | ((cols >> 3) << 17);
+            const uint32_t d = tmem + acc.stage * q.acc_cols;
+            fine = wait(&bar_acc_empty[acc.stage], acc.phase ^ 1);
+            if (!fine) break;
+            tc_fence_after();
+            for (int c = c0; c < c1; ++c) {
+                if (MODE != kGather) fine = wait(&bar_full[ring.stage], ring.phase);
+                if (MODE != kTma) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
                 if (!fine) break;
                 tc_fence_after();
-                for (int c = c0; c < c1; ++c) {
-                    if (MODE != kGather) fine = wait(&bar_full[ring.stage], ring.phase);
-                    if (MODE != kTma) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
-                    if (!fine) break;
-                    tc_fence_after();
-                    const uint32_t at = stages + ring.stage * q.stage_bytes;
-                    const uint64_t a = smem_descriptor(at), b = smem_descriptor(at + q.x_off);
+                const uint32_t at = stages + ring.stage * q.stage_bytes;
+                const uint64_t a = smem_descriptor(at), b = smem_descriptor(at + q.x_off);
+                if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kTcDepth / 32; ++k) tc_mma(d, a + k * 2, b + k * 2, idesc, (c > c0 || k > 0) ? 1u : 0u);
                     tc_commit(smem_address(&bar_empty[ring.stage]));
-                    ring.next(q.stages);
                 }
-                if (!fine) break;
-                tc_commit(smem_address(&bar_acc_full[acc.stage]));
-                acc.next(2);
+                __syncwarp();
+                ring.next(q.stages);
             }
-            if (!fine) {                               // multiplies in flight read shared memory and write tensor memory
-                tc_commit(smem_address(&ctl.drain));
-                wait(&ctl.drain, 0);
-            }
+            if (!fine) break;
+            if (elect_one()) tc_commit(smem_address(&bar_acc_full[acc.stage]));
+            __syncwarp();
+            acc.next(2);
+        }
+        if (!fine) {                                   // multiplies in flight read shared memory and write tensor memory
+            if (elect_one()) tc_commit(smem_address(&ctl.drain));
+            __syncwarp();
+            wait(&ctl.drain, 0);
         }
     } else if (MODE != kTma && warp >= FIRST_HELPER) {
+        if (MODE == kGather) grid_dependency_wait();
         if constexpr (MODE != kTma) fine = help<MODE>(q, tables, t0, tiles, step, c0, c1, stages, ctl);
     } else if (warp >= kFirstEpilogueWarp && warp < FIRST_HELPER) {
-        if (q.splits > 1) fine = keep_part<EPI>(q, tables, t0, tiles, tmem, stages, bar_acc_full);
-        else with_epilogue(p, [&](auto kind, auto act) {
-            fine = finish_tiles<EPI, decltype(kind)::value, decltype(act)::value>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
+        grid_dependency_wait();
+        with_epilogue(p, [&](auto kind, auto act) {
+            constexpr int OUT = decltype(kind)::value, ACT = decltype(act)::value;
+            if (q.splits > 1) fine = finish_shared_tile<EPI, OUT, ACT>(q, tables, t0, tiles, rank, tmem, stages, ctl);
+            else fine = finish_tiles<EPI, OUT, ACT>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
         });
     }
-    if (!fine) {
-        ctl.whole = 0;
-        if (lane == 0) atomicAdd(&linear_timeouts, 1u);
-    }
+    if (!fine && lane == 0) atomicAdd(&linear_timeouts, 1u);
     __syncwarp();
-    if (q.splits > 1) {
+    if (q.splits > 1 && (warp < kFirstEpilogueWarp || warp >= FIRST_HELPER)) {
+        if (!fine) ctl.whole = 0;
         cluster_sync_all();
-        bool all = true;
-        for (int r = 0; r < q.splits; ++r) all = all && load_cluster_s32(smem_address(&ctl.whole), r) != 0;
-        if (all && warp >= kFirstEpilogueWarp && warp < FIRST_HELPER && t0 < tiles) {
-            const Tile tile = find_tc_tile(q, tables, t0);
-            with_epilogue(p, [&](auto kind, auto act) { finish_parts<EPI, decltype(kind)::value, decltype(act)::value>(q, tile, rank, stages); });
-        }
         cluster_sync_all();                            // the others may still read this CTA's part
     }
     tc_fence_before();
