@@ -236,6 +236,8 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     k.x_scale = ep->d_x_scale; k.w_scale = ep->d_w_scale;
     k.out_row = out_row; k.res_row = res_row;
     k.shift = ep->shift; k.lo = ep->lo; k.hi = ep->hi;
+    const int rows = grouped ? ceil_div(M, E) : M;               // of a group, on average
+    if (linear_rows_takes(k, rows)) return launch_linear_rows(k, (cudaStream_t)stream);
     return linear_tc_takes(k) ? launch_linear_tc(k, (cudaStream_t)stream) : launch_linear_mma(k, (cudaStream_t)stream);
 }
 

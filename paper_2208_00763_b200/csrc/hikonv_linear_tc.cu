@@ -736,7 +736,7 @@ static bool encode_map(CUtensorMap *map, const void *base, uint64_t row_bytes, u
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static int sm_count_here() {
+int sm_count_here() {
     static thread_local int known_dev = -1, sms = 148;
     int dev = 0;
     if (cudaGetDevice(&dev) == cudaSuccess && dev != known_dev) {
