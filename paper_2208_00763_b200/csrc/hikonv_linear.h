@@ -29,7 +29,7 @@ struct LinearParams {
 int launch_linear_mma(const LinearParams &p, cudaStream_t st);
 
 // A few rows (per group) at a time (hikonv_linear_rows.cu); `rows`: how many the largest group has, or may be expected to have.
-constexpr int kLinearFewRows = 8;
+constexpr int kLinearFewRows = 16;
 bool linear_rows_takes(const LinearParams &p, int rows);
 int launch_linear_rows(const LinearParams &p, cudaStream_t st);
 
