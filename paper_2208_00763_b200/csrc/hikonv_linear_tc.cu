@@ -18,6 +18,7 @@
 // through distributed shared memory, each CTA finishing its part of the tile's output columns.
 #include <cuda.h>
 
+#include <cstddef>
 #include <cstring>
 
 #include "hikonv_linear_util.cuh"
@@ -173,8 +174,8 @@ __device__ __forceinline__ Tile find_tc_tile(const TcParams &q, const GroupTable
     return r;
 }
 
-__device__ __forceinline__ bool wait_all_of(const TcParams &q, uint64_t *bar, uint32_t parity) {
-    return __all_sync(0xFFFFFFFFu, mbarrier_wait(smem_address(bar), parity, q.wait_cycles));
+__device__ __forceinline__ bool wait_all_of(const TcParams &q, uint32_t bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
 
 // 16 bytes of dense weights to 16 * 8 / BITS codes in the operand's layout (row `row`, from its piece `piece` of 16 codes on).
@@ -330,7 +331,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
         const bool of_w = unit < w_units;
         const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
         if constexpr (MODE == kTransform) {
-            if (!wait_all_of(q, &ctl.full[stage], phase)) return false;
+            if (!wait_all_of(q, smem_address(&ctl.full[stage]), phase)) return false;
             if (of_w) {
                 const uint32_t raw = at + q.raw_off;
                 if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, at, row0) : unpack_unit<4, false>(raw, at, row0);
@@ -356,7 +357,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                     constexpr int BITS = decltype(bits)::value;
                     RowUnit<BITS> u;
                     u.load(src, p.w_row, left, rows);
-                    if (!wait_all_of(q, &ctl.empty[stage], phase ^ 1)) return false;
+                    if (!wait_all_of(q, smem_address(&ctl.empty[stage]), phase ^ 1)) return false;
                     p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, 0);
                     return true;
                 };
@@ -368,7 +369,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                 const int left = min(p.K - c * kTcDepth, 1024), rows = tile.rows - row0;
                 RowUnit<8> u;
                 u.load(src, p.x_row, left, rows);
-                if (!wait_all_of(q, &ctl.empty[stage], phase ^ 1)) return false;
+                if (!wait_all_of(q, smem_address(&ctl.empty[stage]), phase ^ 1)) return false;
                 u.store<false>(at + q.x_off, row0, q.nt, src, p.x_row, left, q.flip ? 0x80808080u : 0u);
             }
         }
@@ -383,7 +384,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
 // residuals are in flight together, and what belongs to a column is loaded before its sums are there.
 template <int WARPS, int OUT, int ACT>
 __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, uint32_t tmem,
-                                             uint64_t *acc_full, uint64_t *acc_empty) {
+                                             uint32_t acc_full, uint32_t acc_empty) {
     using T = typename OutElem<OUT>::type;
     constexpr bool REAL = OUT >= HIKONV_OUT_F32;
     const LinearParams &p = q.p;
@@ -395,7 +396,7 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
         const bool inside = n < p.N;
         ColumnTerms terms{1.f, 0.f, 0};
         if (inside) terms = column_terms<OUT>(p, tile.e, n);
-        if (!wait_all_of(q, &acc_full[acc.stage], acc.phase)) return false;
+        if (!wait_all_of(q, acc_full + 8 * acc.stage, acc.phase)) return false;
         tc_fence_after();
         const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
         int32_t correction = 0;
@@ -443,7 +444,7 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbarrier_arrive(smem_address(&acc_empty[acc.stage]));
+        if (lane == 0) mbarrier_arrive(acc_empty + 8 * acc.stage);
         acc.next(2);
     }
     return true;
@@ -483,7 +484,7 @@ __device__ __forceinline__ bool finish_shared_tile(const TcParams &q, const Grou
     fetch(first);
     bool fine = true;
     if (t < tiles) {
-        fine = wait_all_of(q, &ctl.acc_full[0], 0);
+        fine = wait_all_of(q, smem_address(&ctl.acc_full[0]), 0);
         if (fine) {
             tc_fence_after();
             const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16);
@@ -536,9 +537,12 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     linear_tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
     extern __shared__ __align__(16) uint8_t dynamic[];
     TcControl &ctl = *reinterpret_cast<TcControl *>(dynamic);
-    uint64_t *bar_full = ctl.full, *bar_ready = ctl.ready, *bar_empty = ctl.empty, *bar_acc_full = ctl.acc_full, *bar_acc_empty = ctl.acc_empty;
+    const uint32_t control = smem_address(dynamic);
+    auto barrier = [&](size_t offset, int i) { return control + (uint32_t)offset + 8u * (uint32_t)i; };
+#define HIKONV_BAR(name, i) barrier(offsetof(TcControl, name), i)
     constexpr int EPI = kEpilogueWarps<MODE>, FIRST_HELPER = kFirstEpilogueWarp + EPI;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);       // the same in all lanes, which the compiler does not see from tid
     const LinearParams &p = q.p;
     const uint32_t stages = (smem_address(dynamic) + (uint32_t)sizeof(TcControl) + 1023u) & ~1023u;
     uint8_t *behind = dynamic + (stages - smem_address(dynamic)) + q.stages * q.stage_bytes;
@@ -549,15 +553,15 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     grid_dependency_release();
     if (tid == 0) {
         for (int i = 0; i < q.stages; ++i) {
-            mbarrier_init(smem_address(&bar_full[i]), 1);
-            mbarrier_init(smem_address(&bar_ready[i]), q.units);
-            mbarrier_init(smem_address(&bar_empty[i]), 1);
+            mbarrier_init(HIKONV_BAR(full, i), 1);
+            mbarrier_init(HIKONV_BAR(ready, i), q.units);
+            mbarrier_init(HIKONV_BAR(empty, i), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbarrier_init(smem_address(&bar_acc_full[i]), 1);
-            mbarrier_init(smem_address(&bar_acc_empty[i]), EPI);
+            mbarrier_init(HIKONV_BAR(acc_full, i), 1);
+            mbarrier_init(HIKONV_BAR(acc_empty, i), EPI);
         }
-        mbarrier_init(smem_address(&ctl.drain), 1);
+        mbarrier_init(HIKONV_BAR(drain, 0), 1);
         mbarrier_init_fence();
         ctl.whole = 1;
         if (MODE != kGather) {
@@ -612,7 +616,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     const int t0 = blockIdx.x / q.splits, step = gridDim.x / q.splits;
     const int c0 = (int)((long long)q.chunks * rank / q.splits), c1 = (int)((long long)q.chunks * (rank + 1) / q.splits);
 
-    auto wait = [&](uint64_t *bar, uint32_t parity) { return wait_all_of(q, bar, parity); };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return wait_all_of(q, bar, parity); };
     bool fine = true;
     if (warp == 0) {
         if (MODE != kGather) {
@@ -626,15 +630,14 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
                 const int w_row0 = tile.e * p.N + tile.n0;
                 if (loads == 0) grid_dependency_wait();
                 for (int c = c0; c < c1; ++c) {
-                    fine = wait(&bar_empty[ring.stage], ring.phase ^ 1);
+                    fine = wait(HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
                     if (!fine) break;
-                    const uint32_t at = stages + ring.stage * q.stage_bytes, bar = smem_address(&bar_full[ring.stage]);
+                    const uint32_t at = stages + ring.stage * q.stage_bytes, bar = HIKONV_BAR(full, ring.stage);
                     if (elect_one()) {
                         mbarrier_arrive_expect(bar, bytes);
                         tma_load_2d(at + w_off, &map_w, c * depth_bytes, w_row0, bar);
                         tma_load_2d(at + q.x_off, &map_x, c * kTcDepth, tile.row0, bar);
                     }
-                    __syncwarp();
                     ++loads;
                     ring.next(q.stages);
                 }
@@ -643,43 +646,45 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             for (int i = 0; i < q.stages && i < loads; ++i) {
                 ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
                 if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                fine &= wait(&bar_full[ring.stage], ring.phase);
+                fine &= wait(HIKONV_BAR(full, ring.stage), ring.phase);
             }
         }
     } else if (warp == 1) {
         Ring ring, acc;
+        const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.x_off);
+        const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4;
         for (int t = t0; fine && t < tiles; t += step) {
             const Tile tile = find_tc_tile(q, tables, t);
             const uint32_t cols = q.ones ? (uint32_t)(q.nt + q.ones) : (uint32_t)((tile.rows + 15) & ~15);
             const uint32_t idesc = q.idesc | ((cols >> 3) << 17);
             const uint32_t d = tmem + acc.stage * q.acc_cols;
-            fine = wait(&bar_acc_empty[acc.stage], acc.phase ^ 1);
+            fine = wait(HIKONV_BAR(acc_empty, acc.stage), acc.phase ^ 1);
             if (!fine) break;
-            tc_fence_after();
+            uint32_t accumulate = 0;
             for (int c = c0; c < c1; ++c) {
-                if (MODE != kGather) fine = wait(&bar_full[ring.stage], ring.phase);
-                if (MODE != kTma) fine = fine && wait(&bar_ready[ring.stage], ring.phase);
+                // where helpers have a hand in the operands, their waits have seen the copies land
+                fine = wait(MODE == kTma ? HIKONV_BAR(full, ring.stage) : HIKONV_BAR(ready, ring.stage), ring.phase);
                 if (!fine) break;
                 tc_fence_after();
-                const uint32_t at = stages + ring.stage * q.stage_bytes;
-                const uint64_t a = smem_descriptor(at), b = smem_descriptor(at + q.x_off);
+                const uint64_t a = a0 + ring.stage * stage_units, b = b0 + ring.stage * stage_units;
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < kTcDepth / 32; ++k) tc_mma(d, a + k * 2, b + k * 2, idesc, (c > c0 || k > 0) ? 1u : 0u);
-                    tc_commit(smem_address(&bar_empty[ring.stage]));
+                    for (int k = 0; k < kTcDepth / 32; ++k) {
+                        tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
+                        accumulate = 1;
+                    }
+                    tc_commit(HIKONV_BAR(empty, ring.stage));
                 }
-                __syncwarp();
+                accumulate = 1;
                 ring.next(q.stages);
             }
             if (!fine) break;
-            if (elect_one()) tc_commit(smem_address(&bar_acc_full[acc.stage]));
-            __syncwarp();
+            if (elect_one()) tc_commit(HIKONV_BAR(acc_full, acc.stage));
             acc.next(2);
         }
         if (!fine) {                                   // multiplies in flight read shared memory and write tensor memory
-            if (elect_one()) tc_commit(smem_address(&ctl.drain));
-            __syncwarp();
-            wait(&ctl.drain, 0);
+            if (elect_one()) tc_commit(HIKONV_BAR(drain, 0));
+            wait(HIKONV_BAR(drain, 0), 0);
         }
     } else if (MODE != kTma && warp >= FIRST_HELPER) {
         if (MODE == kGather) grid_dependency_wait();
@@ -689,7 +694,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         with_epilogue(p, [&](auto kind, auto act) {
             constexpr int OUT = decltype(kind)::value, ACT = decltype(act)::value;
             if (q.splits > 1) fine = finish_shared_tile<EPI, OUT, ACT>(q, tables, t0, tiles, rank, tmem, stages, ctl);
-            else fine = finish_tiles<EPI, OUT, ACT>(q, tables, t0, tiles, step, tmem, bar_acc_full, bar_acc_empty);
+            else fine = finish_tiles<EPI, OUT, ACT>(q, tables, t0, tiles, step, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0));
         });
     }
     if (!fine && lane == 0) atomicAdd(&linear_timeouts, 1u);
@@ -703,6 +708,8 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     __syncthreads();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * q.acc_cols));
 }
+
+#undef HIKONV_BAR
 
 __global__ void linear_wait_check_kernel(long long cycles) {
     __shared__ uint64_t bar;
