@@ -26,7 +26,7 @@
 namespace hikonv {
 
 constexpr int kTcRows = 128;             // output columns of the layer per tile: rows of the instruction
-constexpr int kTcDepth = 128;            // codes of the depth per stage: one 128-byte swizzled row
+constexpr int kTcDepth = 128;            // codes of the depth per step: one 128-byte swizzled row
 constexpr int kTcMostStages = 12;
 constexpr int kFirstEpilogueWarp = 4;
 // How operands come to the multiplies: by TMA alone; by TMA and changed in place by warps of their own; read by such warps.
@@ -41,11 +41,13 @@ struct TcParams {
     LinearParams p;
     int nt;                              // rows of x per tile, a multiple of 16
     int acc_cols;                        // tensor-memory columns per accumulator
-    int stages, stage_bytes, x_off, raw_off;
-    int splits, chunks;                  // CTAs that share a tile's depth; stages' worth of depth in all
+    int stages, stage_bytes;             // a stage: `atoms` steps of kTcDepth codes, atom_bytes apart
+    int atoms, atom_bytes, x_off, raw_off;
+    int splits, chunks;                  // CTAs that share a tile's depth (log2 in split_shift); steps of the depth in all
+    int split_shift;
     int n_blocks, m_tiles, tokens_first;
     uint32_t idesc;
-    int units;                           // of helper work per stage
+    int units;                           // of helper work per step
     int flip, ones;                      // x has its top bits flipped; so many rows (16) with ones lie behind it
     long long wait_cycles;
 };
@@ -108,6 +110,11 @@ __device__ __forceinline__ uint32_t remote_address(uint32_t smem_addr, uint32_t 
 __device__ __forceinline__ int32_t load_cluster_s32(uint32_t remote) {
     int32_t v;
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote));
+    return v;
+}
+__device__ __forceinline__ int4 load_cluster_int4(uint32_t remote) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote));
     return v;
 }
 __device__ __forceinline__ uint4 load_shared16(uint32_t a) {
@@ -308,26 +315,36 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                                      TcControl &ctl) {
     const LinearParams &p = q.p;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
-    int unit = warp, c = c0, t = t0, stage = 0;
+    const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0;
+    int unit = warp, atom = 0, c = c0, t = t0, stage = 0;          // c: the step that the unit belongs to, the atom-th of its stage
     uint32_t phase = 0;
     Tile tile;
     if (t < tiles) tile = find_tc_tile(q, tables, t);
     for (;; unit += kHelperWarps<MODE>) {
-        while (unit >= q.units) {                      // on to the stage that this unit belongs to
+        while (unit >= q.units) {                      // on to the step that this unit belongs to
             unit -= q.units;
-            if (++stage == q.stages) {
-                stage = 0;
-                phase ^= 1;
-            }
-            if (++c >= c1) {
-                c = c0;
-                t += step;
-                if (t < tiles) tile = find_tc_tile(q, tables, t);
+            ++c;
+            if (++atom == q.atoms) {
+                atom = 0;
+                if (++stage == q.stages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+                if (c >= c1) {
+                    c = c0;
+                    t += step;
+                    if (t < tiles) tile = find_tc_tile(q, tables, t);
+                }
             }
         }
         if (t >= tiles) return true;
-        const uint32_t at = stages + stage * q.stage_bytes;
-        const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0;
+        const uint32_t at = stages + stage * q.stage_bytes + atom * q.atom_bytes;
+        if (c >= c1) {                                 // the last stage of a tile may have fewer steps: nothing to do, but to be counted
+            if (!wait_all_of(q, MODE == kTransform ? smem_address(&ctl.full[stage]) : smem_address(&ctl.empty[stage]), MODE == kTransform ? phase : phase ^ 1))
+                return false;
+            if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[stage]));
+            continue;
+        }
         const bool of_w = unit < w_units;
         const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
         if constexpr (MODE == kTransform) {
@@ -452,35 +469,41 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
 
 // With a shared depth: this CTA's part of the sums goes to shared memory, [row of x][output column], over the stages (all loads have been
 // multiplied when the sums are there); after the cluster's barrier the CTA takes the sums of all parts through the epilogue for its share
-// of the output columns.  What else that needs is loaded before the barrier.
+// of the output columns, four columns of two rows per thread at a time.  What else that needs is loaded before the barrier: a fetch from
+// another SM takes several hundred cycles, as one from the second-level cache does.
 template <int WARPS, int OUT, int ACT>
 __device__ __forceinline__ bool finish_shared_tile(const TcParams &q, const GroupTables &tables, int t, int tiles, int rank, uint32_t tmem,
                                                    uint32_t part, TcControl &ctl) {
     using T = typename OutElem<OUT>::type;
     constexpr bool REAL = OUT >= HIKONV_OUT_F32;
-    constexpr int BATCH = 4;                           // rows at a time: a fetch from another SM takes several hundred cycles
+    constexpr int BATCH = 2;
     const LinearParams &p = q.p;
     const int tid = threadIdx.x - kFirstEpilogueWarp * 32, lane = tid & 31, quad = (tid >> 5) & 3, half = tid >> 7;
-    const int columns = kTcRows / q.splits, own = rank * columns + tid % columns, first = tid / columns, step = WARPS * 32 / columns;
+    const int lanes = (kTcRows / 4) >> q.split_shift;      // threads that share a row
+    const int own = (rank * lanes + (tid & (lanes - 1))) * 4, step = WARPS * 32 / lanes;
+    const int first = tid / lanes;
     Tile tile{0, 0, 0, 0};
     if (t < tiles) tile = find_tc_tile(q, tables, t);
-    const int n = tile.n0 + own;
-    const bool inside = n < p.N;
-    ColumnTerms terms{1.f, 0.f, 0};
-    float xs[BATCH], res[BATCH];
+    const int n = tile.n0 + own, inside = max(0, min(4, p.N - n));       // columns that there are
+    ColumnTerms terms[4];
+    float xs[BATCH], res[BATCH][4];
     auto fetch = [&](int i0) {
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             const int i = i0 + b * step;
             xs[b] = 1.f;
-            res[b] = 0.f;
-            if (REAL && inside && i < tile.rows) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) res[b][k] = 0.f;
+            if (REAL && i < tile.rows) {
                 if (p.x_scale) xs[b] = load_ordered(p.x_scale + tile.row0 + i);
-                res[b] = residual_at<T>(p, tile.row0 + i, n);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k < inside) res[b][k] = residual_at<T>(p, tile.row0 + i, n + k);
             }
         }
     };
-    if (t < tiles && inside) terms = column_terms<OUT>(p, tile.e, n);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) terms[k] = t < tiles && k < inside ? column_terms<OUT>(p, tile.e, n + k) : ColumnTerms{1.f, 0.f, 0};
     fetch(first);
     bool fine = true;
     if (t < tiles) {
@@ -505,26 +528,49 @@ __device__ __forceinline__ bool finish_shared_tile(const TcParams &q, const Grou
         }
     }
     if (!fine) ctl.whole = 0;
-    uint32_t from[8], flag = 1;
+    uint32_t from[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) from[r] = remote_address(part + own * 4, r < q.splits ? r : 0);
+    const uint32_t flag_at = remote_address(smem_address(&ctl.whole), lane & (q.splits - 1));
     cluster_sync_all();
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-        if (r < q.splits) flag &= (uint32_t)load_cluster_s32(remote_address(smem_address(&ctl.whole), r));
-    for (int i0 = first; i0 < tile.rows; i0 += BATCH * step) {
+    const int flag = load_cluster_s32(flag_at);
+    for (int i0 = first; i0 - first < tile.rows; i0 += BATCH * step) {
         if (i0 != first) fetch(i0);
-        int32_t v[8][BATCH];
+        int32_t sum[BATCH][4] = {};
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int r0 = 0; r0 < 8; r0 += 4) {
+            if (r0 >= q.splits) break;
+            int4 v[4][BATCH];
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) v[r][b] = r < q.splits && i0 + b * step < tile.rows ? load_cluster_s32(from[r] + (i0 + b * step) * kTcRows * 4) : 0;
-        if (flag && inside) {
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const int i = i0 + b * step;
-                const int32_t sum = ((v[0][b] + v[1][b]) + (v[2][b] + v[3][b])) + ((v[4][b] + v[5][b]) + (v[6][b] + v[7][b]));
-                if (i < tile.rows) ((T *)p.out)[(tile.row0 + i) * p.out_row + n] = finish<OUT, ACT>(p, sum >> p.down, xs[b], terms, res[b]);
+                for (int b = 0; b < BATCH; ++b)
+                    v[r][b] = r0 + r < q.splits && i0 + b * step < tile.rows ? load_cluster_int4(from[r0 + r] + (i0 + b * step) * kTcRows * 4)
+                                                                             : make_int4(0, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b) sum[b][0] += v[r][b].x, sum[b][1] += v[r][b].y, sum[b][2] += v[r][b].z, sum[b][3] += v[r][b].w;
+        }
+        if (i0 == first && !__all_sync(0xFFFFFFFFu, flag)) break;
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * step;
+            if (i < tile.rows) {
+                T *o = (T *)p.out + (tile.row0 + i) * p.out_row + n;
+                T y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = finish<OUT, ACT>(p, sum[b][k] >> p.down, xs[b], terms[k], res[b][k]);
+                if (inside == 4 && (uintptr_t)o % (4 * sizeof(T)) == 0) {
+                    struct alignas(4 * sizeof(T)) Four { T v[4]; } four;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) four.v[k] = y[k];
+                    *reinterpret_cast<Four *>(o) = four;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < inside) o[k] = y[k];
+                }
             }
         }
     }
@@ -551,20 +597,22 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     const GroupTables tables{group_row, group_tiles};
 
     grid_dependency_release();
-    if (tid == 0) {
-        for (int i = 0; i < q.stages; ++i) {
-            mbarrier_init(HIKONV_BAR(full, i), 1);
-            mbarrier_init(HIKONV_BAR(ready, i), q.units);
-            mbarrier_init(HIKONV_BAR(empty, i), 1);
+    if (warp == 0) {
+        if (lane < q.stages) {
+            mbarrier_init(HIKONV_BAR(full, lane), 1);
+            mbarrier_init(HIKONV_BAR(ready, lane), q.units * q.atoms);
+            mbarrier_init(HIKONV_BAR(empty, lane), 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbarrier_init(HIKONV_BAR(acc_full, i), 1);
-            mbarrier_init(HIKONV_BAR(acc_empty, i), EPI);
+        if (lane < 2) {
+            mbarrier_init(HIKONV_BAR(acc_full, lane), 1);
+            mbarrier_init(HIKONV_BAR(acc_empty, lane), EPI);
         }
-        mbarrier_init(HIKONV_BAR(drain, 0), 1);
+        if (lane == 2) {
+            mbarrier_init(HIKONV_BAR(drain, 0), 1);
+            ctl.whole = 1;
+        }
         mbarrier_init_fence();
-        ctl.whole = 1;
-        if (MODE != kGather) {
+        if (MODE != kGather && lane == 3) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
         }
@@ -575,9 +623,9 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     }
     if (MODE != kTma && q.ones) {
         // sixteen rows behind the rows of x, the first of them ones; nothing writes there again
-        for (int i = tid; i < q.stages * 128; i += blockDim.x) {
+        for (int i = tid; i < q.stages * q.atoms * 128; i += blockDim.x) {
             const uint32_t v = (i & 127) < 8 ? 0x01010101u : 0u;
-            store_shared16(stages + (i >> 7) * q.stage_bytes + q.x_off + q.nt * 128 + (i & 127) * 16, v, v, v, v);
+            store_shared16(stages + (i >> 7) * q.atom_bytes + q.x_off + q.nt * 128 + (i & 127) * 16, v, v, v, v);
         }
         proxy_fence();
     }
@@ -612,9 +660,8 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         __syncthreads();
         tiles = group_tiles[p.E - 1];
     }
-    const int rank = q.splits > 1 ? (int)(blockIdx.x % q.splits) : 0;
-    const int t0 = blockIdx.x / q.splits, step = gridDim.x / q.splits;
-    const int c0 = (int)((long long)q.chunks * rank / q.splits), c1 = (int)((long long)q.chunks * (rank + 1) / q.splits);
+    const int rank = blockIdx.x & (q.splits - 1), t0 = blockIdx.x >> q.split_shift, step = gridDim.x >> q.split_shift;
+    const int c0 = (q.chunks * rank) >> q.split_shift, c1 = (q.chunks * (rank + 1)) >> q.split_shift;
 
     auto wait = [&](uint32_t bar, uint32_t parity) { return wait_all_of(q, bar, parity); };
     bool fine = true;
@@ -629,14 +676,18 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
                 const Tile tile = find_tc_tile(q, tables, t);
                 const int w_row0 = tile.e * p.N + tile.n0;
                 if (loads == 0) grid_dependency_wait();
-                for (int c = c0; c < c1; ++c) {
+                for (int c = c0; c < c1; c += q.atoms) {
                     fine = wait(HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
                     if (!fine) break;
-                    const uint32_t at = stages + ring.stage * q.stage_bytes, bar = HIKONV_BAR(full, ring.stage);
+                    const uint32_t bar = HIKONV_BAR(full, ring.stage);
+                    const int some = min(q.atoms, c1 - c);
                     if (elect_one()) {
-                        mbarrier_arrive_expect(bar, bytes);
-                        tma_load_2d(at + w_off, &map_w, c * depth_bytes, w_row0, bar);
-                        tma_load_2d(at + q.x_off, &map_x, c * kTcDepth, tile.row0, bar);
+                        uint32_t at = stages + ring.stage * q.stage_bytes;
+                        mbarrier_arrive_expect(bar, bytes * some);
+                        for (int i = 0; i < some; ++i, at += q.atom_bytes) {
+                            tma_load_2d(at + w_off, &map_w, (c + i) * depth_bytes, w_row0, bar);
+                            tma_load_2d(at + q.x_off, &map_x, (c + i) * kTcDepth, tile.row0, bar);
+                        }
                     }
                     ++loads;
                     ring.next(q.stages);
@@ -652,7 +703,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     } else if (warp == 1) {
         Ring ring, acc;
         const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.x_off);
-        const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4;
+        const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4, atom_units = (uint32_t)q.atom_bytes >> 4;
         for (int t = t0; fine && t < tiles; t += step) {
             const Tile tile = find_tc_tile(q, tables, t);
             const uint32_t cols = q.ones ? (uint32_t)(q.nt + q.ones) : (uint32_t)((tile.rows + 15) & ~15);
@@ -661,17 +712,20 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             fine = wait(HIKONV_BAR(acc_empty, acc.stage), acc.phase ^ 1);
             if (!fine) break;
             uint32_t accumulate = 0;
-            for (int c = c0; c < c1; ++c) {
+            for (int c = c0; c < c1; c += q.atoms) {
                 // where helpers have a hand in the operands, their waits have seen the copies land
                 fine = wait(MODE == kTma ? HIKONV_BAR(full, ring.stage) : HIKONV_BAR(ready, ring.stage), ring.phase);
                 if (!fine) break;
                 tc_fence_after();
-                const uint64_t a = a0 + ring.stage * stage_units, b = b0 + ring.stage * stage_units;
+                const int some = min(q.atoms, c1 - c);
                 if (elect_one()) {
+                    uint64_t a = a0 + ring.stage * stage_units, b = b0 + ring.stage * stage_units;
+                    for (int i = 0; i < some; ++i, a += atom_units, b += atom_units) {
 #pragma unroll
-                    for (int k = 0; k < kTcDepth / 32; ++k) {
-                        tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
-                        accumulate = 1;
+                        for (int k = 0; k < kTcDepth / 32; ++k) {
+                            tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
+                            accumulate = 1;
+                        }
                     }
                     tc_commit(HIKONV_BAR(empty, ring.stage));
                 }
@@ -809,16 +863,20 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     while (q.acc_cols < q.nt + q.ones) q.acc_cols *= 2;
     q.x_off = kTcRows * kTcDepth;
     q.raw_off = q.x_off + (q.nt + q.ones) * kTcDepth;
-    q.stage_bytes = (int)align_up(q.raw_off + (mode == kTransform && p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
-    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
-    q.stages = (int)((kTcMostSmem - 2048 - tables) / q.stage_bytes);
+    q.atom_bytes = (int)align_up(q.raw_off + (mode == kTransform && p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
+    while ((1 << q.split_shift) < q.splits) ++q.split_shift;
+    // a step of a narrow tile is shorter than the loop around it: several to a stage
+    q.atoms = q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, room = kTcMostSmem - 2048 - tables;
+    while (q.atoms > 1 && room / (q.atoms * q.atom_bytes) < 4) q.atoms /= 2;
+    q.stage_bytes = q.atoms * q.atom_bytes;
+    q.stages = (int)(room / q.stage_bytes);
     if (q.stages > kTcMostStages) q.stages = kTcMostStages;
-    if (q.splits > 1) {
-        const int own = ceil_div(q.chunks, q.splits);
-        const int parts = ceil_div(q.nt * kTcRows * 4, q.stage_bytes);              // the sums that are exchanged lie over the stages
-        if (q.stages > own) q.stages = own > parts ? own : parts;
-        if (q.stages < parts) return HIKONV_ERR_UNSUPPORTED;
-    }
+    const int own = ceil_div(ceil_div(q.chunks, q.splits), q.atoms);                  // stages that a CTA fills for a tile
+    const int parts = q.splits > 1 ? ceil_div(q.nt * kTcRows * 4, q.stage_bytes) : 1; // the sums that are exchanged lie over the stages
+    if (q.stages < parts) return HIKONV_ERR_UNSUPPORTED;
+    const long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
+    if (tiles * q.splits <= sms && q.stages > own) q.stages = own > parts ? own : parts;
     // accumulators of signed operands: format 2 (int32), types 1 (signed) or 0 (unsigned) of both, 128 rows; the columns follow per tile
     q.idesc = (2u << 4) | ((as_unsigned ? 0u : 1u) << 7) | ((as_unsigned ? 0u : 1u) << 10) | ((uint32_t)(kTcRows >> 4) << 24);
     q.wait_cycles = kWaitCycles;
@@ -831,7 +889,6 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     } else if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt, true) ||
         !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows, p.w_bits == 8))
         return HIKONV_ERR_CUDA;
-    long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
     const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
     auto launch = [&](auto kernel, int threads) {
         return with_dynamic_smem((const void *)kernel, smem > 49 * 1024 ? smem : 49 * 1024, [&] {
