@@ -308,92 +308,89 @@ struct RowUnit {
     }
 };
 
-// The helper warps: units of all stages of all tiles of this CTA, dealt out one after the other, so that neighbouring stages are worked on
-// side by side.
+// The helper warps: the units of each stage dealt out over the warps, on from where the stage before left off, so that neighbouring stages
+// are worked on side by side.  Every warp waits once per stage and reports once, whether or not a unit fell to it.
 template <int MODE>
 __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, int c0, int c1, uint32_t stages,
                                      TcControl &ctl) {
+    constexpr int WARPS = kHelperWarps<MODE>;
     const LinearParams &p = q.p;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
-    const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0;
-    int unit = warp, atom = 0, c = c0, t = t0, stage = 0;          // c: the step that the unit belongs to, the atom-th of its stage
-    uint32_t phase = 0;
-    Tile tile;
-    if (t < tiles) tile = find_tc_tile(q, tables, t);
-    for (;; unit += kHelperWarps<MODE>) {
-        while (unit >= q.units) {                      // on to the step that this unit belongs to
-            unit -= q.units;
-            ++c;
-            if (++atom == q.atoms) {
-                atom = 0;
-                if (++stage == q.stages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
-                if (c >= c1) {
-                    c = c0;
-                    t += step;
-                    if (t < tiles) tile = find_tc_tile(q, tables, t);
-                }
+    const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0, depth_bytes = kTcDepth * p.w_bits / 8;
+    const uint32_t flip = q.flip ? 0x80808080u : 0u;
+    Ring ring;
+    int turn = warp;                                   // the unit of this stage that falls to this warp first
+    for (int t = t0; t < tiles; t += step) {
+        const Tile tile = find_tc_tile(q, tables, t);
+        for (int c = c0; c < c1; c += q.atoms) {
+            const int some = min(q.atoms, c1 - c), total = some * q.units;
+            const uint32_t stage = stages + ring.stage * q.stage_bytes;
+            const uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
+            const uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
+            bool waited = false;
+            if (MODE == kTransform || turn >= total) {
+                if (!wait_all_of(q, wait_for, parity)) return false;
+                waited = true;
             }
-        }
-        if (t >= tiles) return true;
-        const uint32_t at = stages + stage * q.stage_bytes + atom * q.atom_bytes;
-        if (c >= c1) {                                 // the last stage of a tile may have fewer steps: nothing to do, but to be counted
-            if (!wait_all_of(q, MODE == kTransform ? smem_address(&ctl.full[stage]) : smem_address(&ctl.empty[stage]), MODE == kTransform ? phase : phase ^ 1))
-                return false;
-            if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[stage]));
-            continue;
-        }
-        const bool of_w = unit < w_units;
-        const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
-        if constexpr (MODE == kTransform) {
-            if (!wait_all_of(q, smem_address(&ctl.full[stage]), phase)) return false;
-            if (of_w) {
-                const uint32_t raw = at + q.raw_off;
-                if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, at, row0) : unpack_unit<4, false>(raw, at, row0);
-                else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, at, row0) : unpack_unit<2, false>(raw, at, row0);
-                else p.down ? unpack_unit<1, true>(raw, at, row0) : unpack_unit<1, false>(raw, at, row0);
-            } else {
+            int i = turn, atom = 0, unit = turn;
+            for (; i < total; i += WARPS, unit += WARPS) {
+                while (unit >= q.units) unit -= q.units, ++atom;
+                const uint32_t at = stage + atom * q.atom_bytes;
+                const bool of_w = unit < w_units;
+                const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
+                if constexpr (MODE == kTransform) {
+                    if (of_w) {
+                        const uint32_t raw = at + q.raw_off;
+                        if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, at, row0) : unpack_unit<4, false>(raw, at, row0);
+                        else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, at, row0) : unpack_unit<2, false>(raw, at, row0);
+                        else p.down ? unpack_unit<1, true>(raw, at, row0) : unpack_unit<1, false>(raw, at, row0);
+                    } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int i = row0 * 8 + j * 32 + lane;
-                    if (i < q.nt * 8) {
-                        const uint32_t a = at + q.x_off + i * 16;
-                        const uint4 v = load_shared16(a);
-                        store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
+                        for (int j = 0; j < 8; ++j) {
+                            const int k = row0 * 8 + j * 32 + lane;
+                            if (k < q.nt * 8) {
+                                const uint32_t a = at + q.x_off + k * 16;
+                                const uint4 v = load_shared16(a);
+                                store_shared16(a, v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
+                            }
+                        }
                     }
+                } else {
+                    // the loads are under way before the stage is free
+                    if (of_w) {
+                        const long long begin = (long long)(c + atom) * depth_bytes;
+                        const uint8_t *src = p.w + ((long long)tile.e * p.N + tile.n0 + row0) * p.w_row + begin;
+                        const int left = (int)min(p.w_row - begin, 1024ll), rows = p.N - tile.n0 - row0;
+                        auto run = [&](auto bits) {
+                            RowUnit<decltype(bits)::value> u;
+                            u.load(src, p.w_row, left, rows);
+                            if (!waited && !wait_all_of(q, wait_for, parity)) return false;
+                            p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, 0);
+                            return true;
+                        };
+                        const bool ok = p.w_bits == 8 ? run(std::integral_constant<int, 8>()) : p.w_bits == 4 ? run(std::integral_constant<int, 4>())
+                                        : p.w_bits == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
+                        if (!ok) return false;
+                    } else {
+                        const int begin = (c + atom) * kTcDepth;
+                        const uint8_t *src = p.x + (long long)(tile.row0 + row0) * p.x_row + begin;
+                        const int left = min(p.K - begin, 1024), rows = tile.rows - row0;
+                        RowUnit<8> u;
+                        u.load(src, p.x_row, left, rows);
+                        if (!waited && !wait_all_of(q, wait_for, parity)) return false;
+                        u.store<false>(at + q.x_off, row0, q.nt, src, p.x_row, left, flip);
+                    }
+                    waited = true;
                 }
             }
-        } else {
-            // the loads are under way before the stage is free
-            if (of_w) {
-                const uint8_t *src = p.w + ((long long)tile.e * p.N + tile.n0 + row0) * p.w_row + (long long)c * kTcDepth * p.w_bits / 8;
-                const int left = (int)min(p.w_row - (long long)c * kTcDepth * p.w_bits / 8, 1024ll), rows = p.N - tile.n0 - row0;
-                auto run = [&](auto bits) {
-                    constexpr int BITS = decltype(bits)::value;
-                    RowUnit<BITS> u;
-                    u.load(src, p.w_row, left, rows);
-                    if (!wait_all_of(q, smem_address(&ctl.empty[stage]), phase ^ 1)) return false;
-                    p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, 0);
-                    return true;
-                };
-                const bool ok = p.w_bits == 8 ? run(std::integral_constant<int, 8>()) : p.w_bits == 4 ? run(std::integral_constant<int, 4>())
-                                : p.w_bits == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
-                if (!ok) return false;
-            } else {
-                const uint8_t *src = p.x + (long long)(tile.row0 + row0) * p.x_row + (long long)c * kTcDepth;
-                const int left = min(p.K - c * kTcDepth, 1024), rows = tile.rows - row0;
-                RowUnit<8> u;
-                u.load(src, p.x_row, left, rows);
-                if (!wait_all_of(q, smem_address(&ctl.empty[stage]), phase ^ 1)) return false;
-                u.store<false>(at + q.x_off, row0, q.nt, src, p.x_row, left, q.flip ? 0x80808080u : 0u);
-            }
+            turn = i - total;
+            proxy_fence();
+            __syncwarp();
+            if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[ring.stage]));
+            ring.next(q.stages);
         }
-        proxy_fence();
-        __syncwarp();
-        if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[stage]));
     }
+    return true;
 }
 
 // The epilogue of a warp: the 32 output columns of its quarter of the lanes, every other batch of 16 rows of x.  Each output costs about
@@ -600,7 +597,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     if (warp == 0) {
         if (lane < q.stages) {
             mbarrier_init(HIKONV_BAR(full, lane), 1);
-            mbarrier_init(HIKONV_BAR(ready, lane), q.units * q.atoms);
+            mbarrier_init(HIKONV_BAR(ready, lane), MODE == kTma ? 1 : kHelperWarps<MODE>);
             mbarrier_init(HIKONV_BAR(empty, lane), 1);
         }
         if (lane < 2) {
