@@ -32,7 +32,7 @@ constexpr int kFirstEpilogueWarp = 4;
 // How operands come to the multiplies: by TMA alone; by TMA and changed in place by warps of their own; read by such warps.
 enum TcMode { kTma = 0, kTransform = 1, kGather = 2 };
 template <int MODE> constexpr int kEpilogueWarps = MODE == kGather ? 4 : 8;
-template <int MODE> constexpr int kHelperWarps = MODE == kTma ? 0 : MODE == kTransform ? 8 : 12;
+template <int MODE> constexpr int kHelperWarps = MODE == kTma ? 0 : 12;
 template <int MODE> constexpr int kTcThreads = (kFirstEpilogueWarp + kEpilogueWarps<MODE> + kHelperWarps<MODE>) * 32;
 constexpr int kUnitRows = 32;            // operand rows that a helper warp works on at a time
 constexpr size_t kTcMostSmem = 226 * 1024;
@@ -43,18 +43,22 @@ struct TcParams {
     int acc_cols;                        // tensor-memory columns per accumulator
     int stages, stage_bytes;             // a stage: `atoms` steps of kTcDepth codes, atom_bytes apart
     int atoms, atom_bytes, x_off, raw_off;
+    int teams;                           // of helper warps: each takes every so manieth stage
+    int a_slots, a_column;               // unpacked weights: slots of `atoms` steps, 32 columns each, of tensor memory from this column on (0: none)
+    int tmem_cols;
     int splits, chunks;                  // CTAs that share a tile's depth (log2 in split_shift); steps of the depth in all
     int split_shift;
     int n_blocks, m_tiles, tokens_first;
     uint32_t idesc;
     int units;                           // of helper work per step
     int flip, ones;                      // x has its top bits flipped; so many rows (16) with ones lie behind it
+    int held;                            // bytes of all stages and slots: the tables of the groups lie behind them
     long long wait_cycles;
 };
 
 // The front of a CTA's (dynamic) shared memory; the stages follow on the next multiple of 1024 bytes, then the tables of the groups.
 struct TcControl {
-    uint64_t full[kTcMostStages], ready[kTcMostStages], empty[kTcMostStages], acc_full[2], acc_empty[2], drain;
+    uint64_t full[kTcMostStages], ready[kTcMostStages], empty[kTcMostStages], unpacked_empty[kTcMostStages], acc_full[2], acc_empty[2], drain;
     uint32_t tmem;
     int whole;                           // no wait of this CTA has run out
 };
@@ -72,6 +76,21 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint3
                  "l"(b), "r"(idesc), "r"(accumulate)
                  : "memory");
 }
+// ... with the first operand in tensor memory: a lane per row, four codes per column.
+__device__ __forceinline__ void tc_mma_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_store32(uint32_t taddr, const uint32_t (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+                 "%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+                 "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]),
+                 "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -185,40 +204,33 @@ __device__ __forceinline__ bool wait_all_of(const TcParams &q, uint32_t bar, uin
     return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
 
-// 16 bytes of dense weights to 16 * 8 / BITS codes in the operand's layout (row `row`, from its piece `piece` of 16 codes on).
+// One unit (32 rows, a quarter of the lanes) of dense weights, from the bytes as TMA left them (swizzled, so that a lane can read its row
+// without bank conflicts) to tensor memory: 128 codes of a lane's row are 32 columns.  Through shared memory instead, a step of 128
+// codes moved 60 KB there with 48 rows of x, which bound it: 550 cycles against TODO.
 template <int BITS, bool UP>
-__device__ __forceinline__ void unpack_to_operand(uint4 v, uint32_t tile, int row, int piece) {
-    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-    constexpr int PIECES = 8 / BITS;
+__device__ __forceinline__ void unpack_unit(uint32_t raw, uint32_t to, int row0) {
+    constexpr int PIECES = BITS;                       // of 16 bytes
+    const int row = row0 + (threadIdx.x & 31);
+    const uint32_t turn = BITS == 4 ? (row >> 1) & 3 : BITS == 2 ? (row >> 2) & 1 : 0;
+    uint32_t o[32];
 #pragma unroll
-    for (int j = 0; j < PIECES; ++j) {
-        uint32_t o[4];
-        if constexpr (BITS == 4) {
-            uint32_t a[2], b[2];
-            unpack4<UP>(in[2 * j], a);
-            unpack4<UP>(in[2 * j + 1], b);
-            o[0] = a[0]; o[1] = a[1]; o[2] = b[0]; o[3] = b[1];
-        } else if constexpr (BITS == 2) {
-            unpack2<UP>(in[j], o);
-        } else {
-            unpack1<UP>(in[j / 2] >> (16 * (j & 1)), o);
+    for (int i = 0; i < PIECES; ++i) {
+        const uint4 v = load_shared16(raw + row * PIECES * 16 + ((i ^ turn) << 4));
+        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t *at = &o[(i * 4 + j) * (8 / BITS)];
+            if constexpr (BITS == 4) {
+                unpack4<UP>(in[j], *reinterpret_cast<uint32_t(*)[2]>(at));
+            } else if constexpr (BITS == 2) {
+                unpack2<UP>(in[j], *reinterpret_cast<uint32_t(*)[4]>(at));
+            } else {
+                unpack1<UP>(in[j], *reinterpret_cast<uint32_t(*)[4]>(at));
+                unpack1<UP>(in[j] >> 16, *reinterpret_cast<uint32_t(*)[4]>(at + 4));
+            }
         }
-        store_shared16(tile + row * 128 + (((piece + j) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
     }
-}
-// One unit (32 rows) of dense weights, from the bytes as TMA left them.
-template <int BITS, bool UP>
-__device__ __forceinline__ void unpack_unit(uint32_t raw, uint32_t tile, int row0) {
-    constexpr int PER_ROW = BITS;                      // pieces of 16 bytes: 128 codes of BITS bits
-    const int lane = threadIdx.x & 31;
-    uint4 v[PER_ROW];
-#pragma unroll
-    for (int j = 0; j < PER_ROW; ++j) v[j] = load_shared16(raw + (row0 * PER_ROW + j * 32 + lane) * 16);
-#pragma unroll
-    for (int j = 0; j < PER_ROW; ++j) {
-        const int i = j * 32 + lane;
-        unpack_to_operand<BITS, UP>(v[j], tile, row0 + i / PER_ROW, (i % PER_ROW) * (8 / BITS));
-    }
+    tc_store32(to + ((uint32_t)row0 << 16), o);
 }
 
 // One unit of an operand's rows that start on any byte.  BITS * 4 lanes take a row's 128 codes, a word each, as aligned words; the word
@@ -308,43 +320,55 @@ struct RowUnit {
     }
 };
 
-// The helper warps: the units of each stage dealt out over the warps, on from where the stage before left off, so that neighbouring stages
-// are worked on side by side.  Every warp waits once per stage and reports once, whether or not a unit fell to it.
+// The helper warps: the units of a stage dealt out over a team of them, on from where its stage before left off.  A stage costs a warp
+// some 400 cycles beside its units (waits, fences, the report), so there are several teams where a stage has few units.
 template <int MODE>
 __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, int c0, int c1, uint32_t stages,
-                                     TcControl &ctl) {
-    constexpr int WARPS = kHelperWarps<MODE>;
+                                     uint32_t tmem, TcControl &ctl) {
     const LinearParams &p = q.p;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
     const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0, depth_bytes = kTcDepth * p.w_bits / 8;
     const uint32_t flip = q.flip ? 0x80808080u : 0u;
-    Ring ring;
-    int turn = warp;                                   // the unit of this stage that falls to this warp first
+    Ring ring, unpacked;                               // stages, and slots of unpacked weights
+    const int team_warps = kHelperWarps<MODE> / q.teams, team = warp / team_warps;
+    int turn = warp % team_warps, due = team;          // the unit that falls to this warp first, and the stages until this team's next
     for (int t = t0; t < tiles; t += step) {
         const Tile tile = find_tc_tile(q, tables, t);
         for (int c = c0; c < c1; c += q.atoms) {
+            if (due-- > 0) {
+                ring.next(q.stages);
+                unpacked.next(q.a_slots);
+                continue;
+            }
+            due = q.teams - 1;
             const int some = min(q.atoms, c1 - c), total = some * q.units;
-            const uint32_t stage = stages + ring.stage * q.stage_bytes;
-            const uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
-            const uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
+            const uint32_t stage = stages + ring.stage * q.stage_bytes, slot = tmem + q.a_column + unpacked.stage * q.atoms * 32;
+            // what to wait for: copies that have landed, and, if weights are unpacked, room for them (half of the lanes ask for each)
+            uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
+            uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
+            if (MODE == kTransform && q.a_column && (lane & 1)) {
+                wait_for = smem_address(&ctl.unpacked_empty[unpacked.stage]);
+                parity = unpacked.phase ^ 1;
+            }
             bool waited = false;
             if (MODE == kTransform || turn >= total) {
                 if (!wait_all_of(q, wait_for, parity)) return false;
+                if (MODE == kTransform) tc_fence_after();
                 waited = true;
             }
             int i = turn, atom = 0, unit = turn;
-            for (; i < total; i += WARPS, unit += WARPS) {
+            for (; i < total; i += team_warps, unit += team_warps) {
                 while (unit >= q.units) unit -= q.units, ++atom;
-                const uint32_t at = stage + atom * q.atom_bytes;
+                const uint32_t at = stage + atom * q.atom_bytes, to = slot + atom * 32;
                 const bool of_w = unit < w_units;
                 const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
                 if constexpr (MODE == kTransform) {
                     if (of_w) {
                         const uint32_t raw = at + q.raw_off;
-                        if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, at, row0) : unpack_unit<4, false>(raw, at, row0);
-                        else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, at, row0) : unpack_unit<2, false>(raw, at, row0);
-                        else p.down ? unpack_unit<1, true>(raw, at, row0) : unpack_unit<1, false>(raw, at, row0);
-                    } else {
+                        if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, to, row0) : unpack_unit<4, false>(raw, to, row0);
+                        else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, to, row0) : unpack_unit<2, false>(raw, to, row0);
+                        else p.down ? unpack_unit<1, true>(raw, to, row0) : unpack_unit<1, false>(raw, to, row0);
+                    } else if (q.flip) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int k = row0 * 8 + j * 32 + lane;
@@ -384,10 +408,15 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                 }
             }
             turn = i - total;
-            proxy_fence();
+            if (MODE == kTransform && q.a_column) {
+                tc_wait_store();
+                tc_fence_before();
+            }
+            if (MODE == kGather || q.flip) proxy_fence();
             __syncwarp();
-            if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[ring.stage]));
+            if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[unpacked.stage]));
             ring.next(q.stages);
+            unpacked.next(q.a_slots);
         }
     }
     return true;
@@ -588,7 +617,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);       // the same in all lanes, which the compiler does not see from tid
     const LinearParams &p = q.p;
     const uint32_t stages = (smem_address(dynamic) + (uint32_t)sizeof(TcControl) + 1023u) & ~1023u;
-    uint8_t *behind = dynamic + (stages - smem_address(dynamic)) + q.stages * q.stage_bytes;
+    uint8_t *behind = dynamic + (stages - smem_address(dynamic)) + q.held;
     int2 *group_row = reinterpret_cast<int2 *>(behind);
     int *group_tiles = reinterpret_cast<int *>(group_row + p.E);
     const GroupTables tables{group_row, group_tiles};
@@ -597,8 +626,9 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     if (warp == 0) {
         if (lane < q.stages) {
             mbarrier_init(HIKONV_BAR(full, lane), 1);
-            mbarrier_init(HIKONV_BAR(ready, lane), MODE == kTma ? 1 : kHelperWarps<MODE>);
+            mbarrier_init(HIKONV_BAR(ready, lane), MODE == kTma ? 1 : kHelperWarps<MODE> / q.teams);
             mbarrier_init(HIKONV_BAR(empty, lane), 1);
+            mbarrier_init(HIKONV_BAR(unpacked_empty, lane), 1);
         }
         if (lane < 2) {
             mbarrier_init(HIKONV_BAR(acc_full, lane), 1);
@@ -615,7 +645,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         }
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(2 * q.acc_cols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(q.tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (MODE != kTma && q.ones) {
@@ -698,7 +728,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             }
         }
     } else if (warp == 1) {
-        Ring ring, acc;
+        Ring ring, unpacked, acc;
         const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.x_off);
         const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4, atom_units = (uint32_t)q.atom_bytes >> 4;
         for (int t = t0; fine && t < tiles; t += step) {
@@ -711,23 +741,37 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             uint32_t accumulate = 0;
             for (int c = c0; c < c1; c += q.atoms) {
                 // where helpers have a hand in the operands, their waits have seen the copies land
-                fine = wait(MODE == kTma ? HIKONV_BAR(full, ring.stage) : HIKONV_BAR(ready, ring.stage), ring.phase);
+                fine = MODE == kTma ? wait(HIKONV_BAR(full, ring.stage), ring.phase) : wait(HIKONV_BAR(ready, unpacked.stage), unpacked.phase);
                 if (!fine) break;
                 tc_fence_after();
                 const int some = min(q.atoms, c1 - c);
                 if (elect_one()) {
-                    uint64_t a = a0 + ring.stage * stage_units, b = b0 + ring.stage * stage_units;
-                    for (int i = 0; i < some; ++i, a += atom_units, b += atom_units) {
+                    uint64_t b = b0 + ring.stage * stage_units;
+                    if (MODE == kTransform && q.a_column) {
+                        uint32_t a = tmem + q.a_column + unpacked.stage * q.atoms * 32;
+                        for (int i = 0; i < some; ++i, a += 32, b += atom_units) {
 #pragma unroll
-                        for (int k = 0; k < kTcDepth / 32; ++k) {
-                            tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
-                            accumulate = 1;
+                            for (int k = 0; k < kTcDepth / 32; ++k) {
+                                tc_mma_from_tmem(d, a + k * 8, b + k * 2, idesc, accumulate);
+                                accumulate = 1;
+                            }
+                        }
+                    } else {
+                        uint64_t a = a0 + ring.stage * stage_units;
+                        for (int i = 0; i < some; ++i, a += atom_units, b += atom_units) {
+#pragma unroll
+                            for (int k = 0; k < kTcDepth / 32; ++k) {
+                                tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
+                                accumulate = 1;
+                            }
                         }
                     }
                     tc_commit(HIKONV_BAR(empty, ring.stage));
+                    if (MODE == kTransform && q.a_column) tc_commit(HIKONV_BAR(unpacked_empty, unpacked.stage));
                 }
                 accumulate = 1;
                 ring.next(q.stages);
+                unpacked.next(q.a_slots);
             }
             if (!fine) break;
             if (elect_one()) tc_commit(HIKONV_BAR(acc_full, acc.stage));
@@ -739,7 +783,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         }
     } else if (MODE != kTma && warp >= FIRST_HELPER) {
         if (MODE == kGather) grid_dependency_wait();
-        if constexpr (MODE != kTma) fine = help<MODE>(q, tables, t0, tiles, step, c0, c1, stages, ctl);
+        if constexpr (MODE != kTma) fine = help<MODE>(q, tables, t0, tiles, step, c0, c1, stages, tmem, ctl);
     } else if (warp >= kFirstEpilogueWarp && warp < FIRST_HELPER) {
         grid_dependency_wait();
         with_epilogue(p, [&](auto kind, auto act) {
@@ -757,7 +801,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * q.acc_cols));
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(q.tmem_cols));
 }
 
 #undef HIKONV_BAR
@@ -783,14 +827,14 @@ static EncodeTiled encode_tiled() {
     }();
     return f;
 }
-// Byte matrix [rows][row_bytes], rows `stride` bytes apart, in boxes of box_rows x box_bytes.
-static bool encode_map(CUtensorMap *map, const void *base, uint64_t row_bytes, uint64_t rows, uint64_t stride, uint32_t box_bytes, uint32_t box_rows,
-                       bool swizzled) {
+// Byte matrix [rows][row_bytes], rows `stride` bytes apart, in boxes of box_rows x box_bytes, swizzled over a box row.
+static bool encode_map(CUtensorMap *map, const void *base, uint64_t row_bytes, uint64_t rows, uint64_t stride, uint32_t box_bytes, uint32_t box_rows) {
     const cuuint64_t dims[2] = {row_bytes, rows}, strides[1] = {stride};
     const cuuint32_t box[2] = {box_bytes, box_rows}, one[2] = {1, 1};
     const EncodeTiled f = encode_tiled();
     return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                  : box_bytes == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -819,7 +863,8 @@ static bool rows_aligned(const LinearParams &p) {
 // Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.
 static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int *nt_out, int *splits_out) {
     const int n_blocks = ceil_div(p.N, kTcRows), chunks = ceil_div(p.K, kTcDepth);
-    const int most = ones ? 240 : 256;
+    // unpacked weights take tensor memory from the accumulators
+    const int most = mode == kTransform && p.w_bits < 8 ? 208 : ones ? 240 : 256;
     double best = 1e300;
     for (int nt = 16; nt <= most; nt += 16) {
         // groups: on average half a tile of each is left empty
@@ -851,40 +896,56 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     q.ones = q.flip ? 16 : 0;
     const int mode = !rows_aligned(p) ? kGather : p.w_bits < 8 || q.flip ? kTransform : kTma;
     choose_tile(p, mode, q.flip, sms, &q.nt, &q.splits);
+    // units that unpack weights fall to the warps of their lanes: their number per step is a multiple of four
     q.units = (mode == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0) + (mode == kGather || q.flip ? ceil_div(q.nt, kUnitRows) : 0);
+    if (mode == kTransform && p.w_bits < 8) q.units = (int)align_up(q.units, 4);
     q.chunks = ceil_div(p.K, kTcDepth);
     q.n_blocks = ceil_div(p.N, kTcRows);
     q.m_tiles = ceil_div(p.M, q.nt);
     q.tokens_first = p.offsets || (long long)p.M * p.K <= (long long)p.N * p.w_row;
-    q.acc_cols = 32;
-    while (q.acc_cols < q.nt + q.ones) q.acc_cols *= 2;
-    q.x_off = kTcRows * kTcDepth;
+    q.acc_cols = (int)align_up(q.nt + q.ones, 32);
+    // Dense weights arrive as they are stored and are unpacked into tensor memory.
+    const bool apart = mode == kTransform && p.w_bits < 8;
+    const int operand_bytes = kTcRows * kTcDepth;
+    q.x_off = apart ? 0 : operand_bytes;
     q.raw_off = q.x_off + (q.nt + q.ones) * kTcDepth;
-    q.atom_bytes = (int)align_up(q.raw_off + (mode == kTransform && p.w_bits < 8 ? kTcRows * kTcDepth * p.w_bits / 8 : 0), 1024);
+    q.atom_bytes = (int)align_up(q.raw_off + (apart ? operand_bytes * p.w_bits / 8 : 0), 1024);
     while ((1 << q.split_shift) < q.splits) ++q.split_shift;
     // a step of a narrow tile is shorter than the loop around it: several to a stage
-    q.atoms = q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
-    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, room = kTcMostSmem - 2048 - tables;
-    while (q.atoms > 1 && room / (q.atoms * q.atom_bytes) < 4) q.atoms /= 2;
+    q.atoms = apart ? 1 : q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, all = kTcMostSmem - 2048 - tables;
+    while (q.atoms > 1 && all / (q.atoms * q.atom_bytes) < 4) q.atoms /= 2;
     q.stage_bytes = q.atoms * q.atom_bytes;
-    q.stages = (int)(room / q.stage_bytes);
+    q.stages = (int)(all / q.stage_bytes);
     if (q.stages > kTcMostStages) q.stages = kTcMostStages;
     const int own = ceil_div(ceil_div(q.chunks, q.splits), q.atoms);                  // stages that a CTA fills for a tile
     const int parts = q.splits > 1 ? ceil_div(q.nt * kTcRows * 4, q.stage_bytes) : 1; // the sums that are exchanged lie over the stages
     if (q.stages < parts) return HIKONV_ERR_UNSUPPORTED;
     const long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
     if (tiles * q.splits <= sms && q.stages > own) q.stages = own > parts ? own : parts;
+    q.a_slots = q.stages;
+    if (apart) {
+        q.a_column = 2 * q.acc_cols;
+        q.a_slots = (512 - q.a_column) / (32 * q.atoms);
+        if (q.a_slots > 6) q.a_slots = 6;
+        if (q.a_slots < 1) return HIKONV_ERR_UNSUPPORTED;
+    }
+    q.tmem_cols = 32;
+    while (q.tmem_cols < 2 * q.acc_cols + (apart ? q.a_slots * 32 * q.atoms : 0)) q.tmem_cols *= 2;
+    q.held = q.stages * q.stage_bytes;
+    // teams of at least four warps, since a warp reaches a quarter of the lanes of tensor memory only
+    q.teams = q.units * q.atoms <= 4 ? 3 : 1;
     // accumulators of signed operands: format 2 (int32), types 1 (signed) or 0 (unsigned) of both, 128 rows; the columns follow per tile
     q.idesc = (2u << 4) | ((as_unsigned ? 0u : 1u) << 7) | ((as_unsigned ? 0u : 1u) << 10) | ((uint32_t)(kTcRows >> 4) << 24);
     q.wait_cycles = kWaitCycles;
-    const size_t smem = (size_t)q.stages * q.stage_bytes + 2048 + tables;
+    const size_t smem = (size_t)q.held + 2048 + tables;
 
     CUtensorMap map_x, map_w;
     if (mode == kGather) {
         memset(&map_x, 0, sizeof(map_x));
         memset(&map_w, 0, sizeof(map_w));
-    } else if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt, true) ||
-        !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows, p.w_bits == 8))
+    } else if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt) ||
+        !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows))
         return HIKONV_ERR_CUDA;
     const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
     auto launch = [&](auto kernel, int threads) {
