@@ -154,30 +154,30 @@ __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const __gr
         const int rows = min(TOK, range.y - m0);
         if (STAGED) {
             if (m0 > range.x) __syncthreads();
-            for (int r = 0; r < rows; ++r) {
+            const int units = (pieces * XW + GROUP - 1) / GROUP;
+            for (int at = tid; at < rows * units; at += kRowsThreads) {
+                const int r = at / units, u = at - r * units;
                 const uint8_t *x = p.x + (m0 + r) * p.x_row;
-                for (int u = tid; u * GROUP < pieces * XW; u += kRowsThreads) {
-                    uint32_t v[GROUP];
-                    const int k0 = u * GROUP * 4 - off * PER_BYTE;
-                    if (k0 >= 0 && k0 + GROUP * 4 <= p.K) {
-                        load_bytes<GROUP>(x + k0, GROUP * 4, v);
-                    } else {
+                uint32_t v[GROUP];
+                const int k0 = u * GROUP * 4 - off * PER_BYTE;
+                if (k0 >= 0 && k0 + GROUP * 4 <= p.K) {
+                    load_bytes<GROUP>(x + k0, GROUP * 4, v);
+                } else {
 #pragma unroll
-                        for (int i = 0; i < GROUP; ++i) {
-                            v[i] = 0;
+                    for (int i = 0; i < GROUP; ++i) {
+                        v[i] = 0;
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) {
-                                const int k = k0 + i * 4 + b;
-                                if (k >= 0 && k < p.K) v[i] |= (uint32_t)load_ordered(x + k) << (8 * b);
-                            }
+                        for (int b = 0; b < 4; ++b) {
+                            const int k = k0 + i * 4 + b;
+                            if (k >= 0 && k < p.K) v[i] |= (uint32_t)load_ordered(x + k) << (8 * b);
                         }
                     }
-                    reorder<PER_BYTE>(v);
+                }
+                reorder<PER_BYTE>(v);
 #pragma unroll
-                    for (int i = 0; i < GROUP; i += 4) {
-                        const int h = (u * GROUP + i) / 4 % PER_BYTE, j = (u * GROUP + i) / XW;
-                        *reinterpret_cast<uint4 *>(sx + r * q.x_pitch + (h * q.x_pieces + j) * 4) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                    }
+                for (int i = 0; i < GROUP; i += 4) {
+                    const int h = (u * GROUP + i) / 4 % PER_BYTE, j = (u * GROUP + i) / XW;
+                    *reinterpret_cast<uint4 *>(sx + r * q.x_pitch + (h * q.x_pieces + j) * 4) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                 }
             }
             __syncthreads();
@@ -270,9 +270,20 @@ static long long staged_pitch(const LinearParams &p) { return (staged_pieces(p) 
 // Rows of x at a time.
 static int rows_at_a_time(const LinearParams &p) { return p.offsets || p.M <= 8 ? 8 : 16; }
 
+// Where this kernel is the faster one.  Both are a set-up and a time per weight, in us, measured on weights from memory, for x = N K E /
+// 2^24 weights and up to 8 or 16 rows: 8-bit 2.0 + 3.1 x or 2.0 + 3.7 x here against 4.3 + 2.4 x on tcgen05 tiles; 4-bit 2.0 + 2.0 x or
+// 2.0 + 2.7 x against 5.6 + 2.3 x; 2-bit 2.0 + 2.7 x or 2.0 + 3.9 x against 5.6 + 2.1 x; 1-bit 2.0 + 5.8 x or 2.0 + 9 x.  Rows that x is
+// staged for cost 0.9 us per 4096 codes of x more, and tiles that read such rows 7 + 5.5 x, so there M K decides.
 bool linear_rows_takes(const LinearParams &p, int rows) {
     if (rows > (p.offsets ? 8 : kLinearFewRows) || p.E > 65535) return false;
-    return rows_as_they_are(p) || staged_pitch(p) * 4 * (p.offsets ? 8 : p.M) <= kRowsMostSmem;
+    if (!rows_as_they_are(p))
+        return staged_pitch(p) * 4 * (p.offsets ? 8 : p.M) <= kRowsMostSmem && (long long)rows * p.K <= 28 * 1024;
+    const double x = (double)p.N * p.K * p.E / (1 << 24);
+    const bool eight = rows_at_a_time(p) == 8;
+    const double tiles = p.w_bits == 8 ? 4.3 + 2.4 * x : 5.6 + (p.w_bits == 4 ? 2.3 : 2.1) * x;
+    const double here = 2.0 + x * (p.w_bits == 8 ? (eight ? 3.1 : 3.7) : p.w_bits == 4 ? (eight ? 2.0 : 2.7) : p.w_bits == 2 ? (eight ? 2.7 : 3.9)
+                                                                                                                 : (eight ? 5.8 : 9.0));
+    return here <= tiles;
 }
 
 template <int BITS, int TOK, bool STAGED>
@@ -307,9 +318,12 @@ int launch_linear_rows(const LinearParams &p, cudaStream_t st) {
         q.x_pitch = (int)staged_pitch(p);
     }
     const int parts = (int)((p.w_row + 63) / 64);
-    // as many warps per tile as leave each four 64-byte parts of a row, fewer where the tiles alone fill the GPU
+    // As many warps per tile as leave each four 64-byte parts of a row, but no more CTAs than the GPU holds at once: each that comes
+    // later waits for its first weights anew (eight groups of 2048 x 2048 4-bit weights, 8 rows: 13.3 us in 1024 CTAs, 8.5 in 512,
+    // 6.4 in 256; 1 x 4096 x 16384 8-bit: 16.7, 15.3, 13.9).
     q.ksplit = 1;
-    while (q.ksplit < kRowsWarps && parts >= 2 * q.ksplit * 2 && (long long)q.class_tiles * q.classes * p.E * q.ksplit < (long long)sms * 64) q.ksplit *= 2;
+    while (q.ksplit < kRowsWarps && parts >= 4 * q.ksplit) q.ksplit *= 2;
+    while (q.ksplit > 1 && (long long)q.class_tiles * q.classes * p.E * q.ksplit > (long long)sms * 2 * kRowsWarps) q.ksplit /= 2;
     const int ways = ceil_div(q.class_tiles, kRowsWarps / q.ksplit);
     const dim3 grid((unsigned)(ways * q.classes), (unsigned)p.E);
     const size_t smem = (size_t)q.x_pitch * 4 * (p.offsets ? 8 : p.M);

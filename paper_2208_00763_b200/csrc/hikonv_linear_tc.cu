@@ -343,17 +343,15 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
             due = q.teams - 1;
             const int some = min(q.atoms, c1 - c), total = some * q.units;
             const uint32_t stage = stages + ring.stage * q.stage_bytes, slot = tmem + q.a_column + unpacked.stage * q.atoms * 32;
-            // what to wait for: copies that have landed, and, if weights are unpacked, room for them (half of the lanes ask for each)
-            uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
-            uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
-            if (MODE == kTransform && q.a_column && (lane & 1)) {
-                wait_for = smem_address(&ctl.unpacked_empty[unpacked.stage]);
-                parity = unpacked.phase ^ 1;
-            }
+            const uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
+            const uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
             bool waited = false;
+            if (MODE == kTransform && q.a_column) {
+                if (!wait_all_of(q, smem_address(&ctl.unpacked_empty[unpacked.stage]), unpacked.phase ^ 1)) return false;
+                tc_fence_after();
+            }
             if (MODE == kTransform || turn >= total) {
                 if (!wait_all_of(q, wait_for, parity)) return false;
-                if (MODE == kTransform) tc_fence_after();
                 waited = true;
             }
             int i = turn, atom = 0, unit = turn;
@@ -860,22 +858,31 @@ static bool rows_aligned(const LinearParams &p) {
     return (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && (p.M == 1 || p.x_row % 16 == 0) && p.w_row % 16 == 0;
 }
 
-// Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.
+// Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.  A step of 128 codes costs the longest of its
+// multiplies (2 per row), its way from the second-level cache (70 bytes per cycle and SM) and the helpers' work on it; a tile alone on its
+// SM costs 3000 for the set-up and the end of its epilogue; one with a shared depth two barriers of the cluster, which are dearer the
+// larger it is, and the fetches of all parts.
+// Against measured times of 4096 x 4096 with 64 and 256 rows, 8192 x 8192 with 48: 16.3, 16.3 and 18.7 thousand cycles for 15.2, 16.7
+// and 18.9, and the order of the shapes tried is the measured one.
 static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int *nt_out, int *splits_out) {
     const int n_blocks = ceil_div(p.N, kTcRows), chunks = ceil_div(p.K, kTcDepth);
     // unpacked weights take tensor memory from the accumulators
-    const int most = mode == kTransform && p.w_bits < 8 ? 208 : ones ? 240 : 256;
+    const int most = mode == kTransform && p.w_bits < 8 ? 192 : ones ? 240 : 256;
     double best = 1e300;
     for (int nt = 16; nt <= most; nt += 16) {
         // groups: on average half a tile of each is left empty
         const int filled = p.E < p.M ? p.E : p.M;
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * n_blocks;
+        const double bytes = kTcRows * kTcDepth * p.w_bits / 8.0 + nt * (double)kTcDepth;
+        double step = 2.0 * nt > bytes / 70.0 ? 2.0 * nt : bytes / 70.0;
+        const double help = mode == kGather ? 240.0 * (4 + ceil_div(nt, kUnitRows)) : mode == kTransform ? 370.0 : 200.0;
+        if (step < help) step = help;
         for (int splits = 1; splits <= 8 && splits <= chunks; splits *= 2) {
             // clusters of four and more do not fill every SM: their CTAs share one part of the GPU
             if (splits > 1 && (tiles * splits > sms - 20 || nt > 128)) break;
             const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
-            const double per_chunk = mode == kGather ? 4.0 * (kTcRows + nt) + 300.0 : 256.0 + 2.0 * nt + (p.w_bits < 8 ? 128.0 : 0.0);
-            const double time = waves * ceil_div(chunks, splits) * per_chunk + (splits > 1 ? 1500.0 + 4.0 * nt * splits : 6.0 * nt);
+            const double time = waves * ceil_div(chunks, splits) * step + (mode == kGather ? 6000.0 : 3000.0) +
+                                (splits > 1 ? 2500.0 + 500.0 * splits + 62.0 * nt / splits + 8.0 * nt : 800.0 + 20.0 * nt);
             if (time < best) {
                 best = time;
                 *nt_out = nt;
@@ -933,8 +940,16 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     q.tmem_cols = 32;
     while (q.tmem_cols < 2 * q.acc_cols + (apart ? q.a_slots * 32 * q.atoms : 0)) q.tmem_cols *= 2;
     q.held = q.stages * q.stage_bytes;
-    // teams of at least four warps, since a warp reaches a quarter of the lanes of tensor memory only
-    q.teams = q.units * q.atoms <= 4 ? 3 : 1;
+    // Teams of at least four warps, since a warp reaches a quarter of the lanes of tensor memory only.  A team that waits for the parity of
+    // a barrier must know that the use before the last is over, or it takes an older use for its own.  Of slot s for stage n: the team saw
+    // the multiplies of stage n - 3 - a_slots end, which are not before those of n - 2 a_slots if there are three slots.  Of stage n's
+    // copies, after that: all multiplies up to stage n - a_slots are over, so the copies of n - stages have landed if there are no
+    // fewer stages than slots.
+    q.teams = 1;
+    if (apart && q.units * q.atoms == 4 && q.stages >= 3 && q.a_slots >= 3) {
+        q.teams = 3;
+        if (q.a_slots > q.stages) q.a_slots = q.stages;
+    }
     // accumulators of signed operands: format 2 (int32), types 1 (signed) or 0 (unsigned) of both, 128 rows; the columns follow per tile
     q.idesc = (2u << 4) | ((as_unsigned ? 0u : 1u) << 7) | ((as_unsigned ? 0u : 1u) << 10) | ((uint32_t)(kTcRows >> 4) << 24);
     q.wait_cycles = kWaitCycles;
