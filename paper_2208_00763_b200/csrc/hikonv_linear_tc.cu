@@ -34,6 +34,7 @@ enum TcMode { kTma = 0, kTransform = 1, kGather = 2 };
 template <int MODE> constexpr int kEpilogueWarps = MODE == kGather ? 4 : 8;
 template <int MODE> constexpr int kHelperWarps = MODE == kTma ? 0 : 12;
 template <int MODE> constexpr int kTcThreads = (kFirstEpilogueWarp + kEpilogueWarps<MODE> + kHelperWarps<MODE>) * 32;
+template <int MODE> constexpr int kEpilogueBatch = MODE == kTma ? 16 : 8;       // rows of x at a time: what the registers hold
 constexpr int kUnitRows = 32;            // operand rows that a helper warp works on at a time
 constexpr size_t kTcMostSmem = 226 * 1024;
 
@@ -100,6 +101,12 @@ __device__ __forceinline__ void tc_load16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
                    "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tc_load_columns(uint32_t taddr, uint32_t (&v)[16]) { tc_load16(taddr, v); }
+__device__ __forceinline__ void tc_load_columns(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr));
 }
 __device__ __forceinline__ uint32_t tc_load1(uint32_t taddr) {
@@ -420,10 +427,10 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
     return true;
 }
 
-// The epilogue of a warp: the 32 output columns of its quarter of the lanes, every other batch of 16 rows of x.  Each output costs about
-// ten instructions here, and with eight warps they have to overlap: output type and activation are constants, a batch's 16 sums and
+// The epilogue of a warp: the 32 output columns of its quarter of the lanes, every so manieth batch of B rows of x.  Each output costs about
+// ten instructions here, and with eight warps they have to overlap: output type and activation are constants, a batch's sums and
 // residuals are in flight together, and what belongs to a column is loaded before its sums are there.
-template <int WARPS, int OUT, int ACT>
+template <int WARPS, int B, int OUT, int ACT>
 __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, uint32_t tmem,
                                              uint32_t acc_full, uint32_t acc_empty) {
     using T = typename OutElem<OUT>::type;
@@ -437,6 +444,27 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
         const bool inside = n < p.N;
         ColumnTerms terms{1.f, 0.f, 0};
         if (inside) terms = column_terms<OUT>(p, tile.e, n);
+        // scales of the rows of a batch, a lane each, asked for a batch ahead: a load here and now would take as long as all of a batch
+        auto row_scales = [&](int col) {
+            const int i = col + (lane & (B - 1));
+            return REAL && p.x_scale && i < tile.rows ? load_ordered(p.x_scale + tile.row0 + i) : 1.f;
+        };
+        float xs_next = row_scales(half * B);
+        // ... and the residuals of a batch: loads that depend on nothing, converted when they are used
+        T res_next[B];
+        auto row_residuals = [&](int col) {
+            if (!REAL || !p.residual || !inside || col >= tile.rows) return;
+            const T *r = (const T *)p.residual + (long long)(tile.row0 + col) * p.res_row + n;
+            if (tile.rows - col >= B) {
+#pragma unroll
+                for (int i = 0; i < B; ++i) res_next[i] = load_ordered(r + i * p.res_row);
+            } else {
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+                    if (col + i < tile.rows) res_next[i] = load_ordered(r + i * p.res_row);
+            }
+        };
+        row_residuals(half * B);
         if (!wait_all_of(q, acc_full + 8 * acc.stage, acc.phase)) return false;
         tc_fence_after();
         const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16);
@@ -445,40 +473,40 @@ __device__ __forceinline__ bool finish_tiles(const TcParams &q, const GroupTable
             correction = (int32_t)tc_load1(d + q.nt) * 128;
             tc_wait_load();
         }
-        for (int col = half * 16; col < tile.rows; col += WARPS * 4) {
-            uint32_t v[16];
-            float scale[16], res[16];
-            tc_load16(d + col, v);
+        for (int col = half * B; col < tile.rows; col += WARPS / 4 * B) {
+            uint32_t v[B];
+            float scale[B];
+            T res[B];
+            tc_load_columns(d + col, v);
             const long long m = tile.row0 + col;
             const int left = tile.rows - col;
             if (REAL) {
-                float xs = 1.f;
-                if (p.x_scale && (lane & 15) < left) xs = load_ordered(p.x_scale + m + (lane & 15));
+                const float xs = xs_next;
+                xs_next = row_scales(col + WARPS / 4 * B);
+                if (p.residual) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) res[i] = 0.f;
-                if (p.residual && inside) {
-                    const T *r = (const T *)p.residual + m * p.res_row + n;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if constexpr (REAL)
-                            if (i < left) res[i] = to_float(load_ordered(r + i * p.res_row));
+                    for (int i = 0; i < B; ++i) res[i] = res_next[i];
+                    row_residuals(col + WARPS / 4 * B);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) scale[i] = __shfl_sync(0xFFFFFFFFu, xs, i);
+                for (int i = 0; i < B; ++i) scale[i] = __shfl_sync(0xFFFFFFFFu, xs, i);
             }
             tc_wait_load();
             if (inside) {
                 T *o = (T *)p.out + m * p.out_row + n;
                 auto one = [&](int i) {
-                    *o = finish<OUT, ACT>(p, ((int32_t)v[i] + correction) >> p.down, REAL ? scale[i] : 1.f, terms, REAL ? res[i] : 0.f);
+                    float r = 0.f;
+                    if constexpr (REAL)
+                        if (p.residual) r = to_float(res[i]);
+                    *o = finish<OUT, ACT>(p, ((int32_t)v[i] + correction) >> p.down, REAL ? scale[i] : 1.f, terms, r);
                     o += p.out_row;
                 };
-                if (left >= 16) {
+                if (left >= B) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) one(i);
+                    for (int i = 0; i < B; ++i) one(i);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
+                    for (int i = 0; i < B; ++i)
                         if (i < left) one(i);
                 }
             }
@@ -787,7 +815,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         with_epilogue(p, [&](auto kind, auto act) {
             constexpr int OUT = decltype(kind)::value, ACT = decltype(act)::value;
             if (q.splits > 1) fine = finish_shared_tile<EPI, OUT, ACT>(q, tables, t0, tiles, rank, tmem, stages, ctl);
-            else fine = finish_tiles<EPI, OUT, ACT>(q, tables, t0, tiles, step, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0));
+            else fine = finish_tiles<EPI, kEpilogueBatch<MODE>, OUT, ACT>(q, tables, t0, tiles, step, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0));
         });
     }
     if (!fine && lane == 0) atomicAdd(&linear_timeouts, 1u);
