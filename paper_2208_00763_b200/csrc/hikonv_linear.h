@@ -25,9 +25,6 @@ struct LinearParams {
     int shift, lo, hi;
 };
 
-// Any alignment and any pair of types, at the rate of the older tensor path (hikonv_linear.cu).
-int launch_linear_mma(const LinearParams &p, cudaStream_t st);
-
 // A few rows (per group) at a time (hikonv_linear_rows.cu); `rows`: how many the largest group has, or may be expected to have.
 constexpr int kLinearFewRows = 16;
 bool linear_rows_takes(const LinearParams &p, int rows);
@@ -35,8 +32,7 @@ int launch_linear_rows(const LinearParams &p, cudaStream_t st);
 
 int sm_count_here();                                         // of the current device
 
-// hikonv_linear_tc.cu
-bool linear_tc_takes(const LinearParams &p);
+// All others (hikonv_linear_tc.cu).
 int launch_linear_tc(const LinearParams &p, cudaStream_t st);
 int read_linear_timeouts(unsigned int *h_count);             // on the current device, since it was loaded
 int launch_linear_wait_check(long long cycles, cudaStream_t st);

@@ -10,7 +10,8 @@
 // next tile is multiplied (two accumulators), and, where the operands are not yet bytes of one sign, warps 12 to 19 change them in
 // shared memory between the two: dense weights are unpacked into the operand's layout, and unsigned 8-bit activations of signed weights
 // get 128 subtracted (their top bit flipped; the instruction takes either two signed or two unsigned operands here).  What that takes
-// off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.
+// off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.  Unsigned 8-bit
+// weights of signed activations, the rare case, are flipped too, and 128 sum_k x[m][k] is added by multiplying x twice by a tile of 64s.
 // TMA wants rows on 16-byte boundaries.  Operands whose rows start anywhere are read by twelve helper warps instead, as aligned words
 // that are moved into place (and unpacked, and flipped) on their way to shared memory.
 //
@@ -53,6 +54,7 @@ struct TcParams {
     uint32_t idesc;
     int units;                           // of helper work per step
     int flip, ones;                      // x has its top bits flipped; so many rows (16) with ones lie behind it
+    int flip_w, halves_off;              // w has; a tile of 64s lies there, behind the first stage
     int held;                            // bytes of all stages and slots: the tables of the groups lie behind them
     long long wait_cycles;
 };
@@ -334,7 +336,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                                      uint32_t tmem, TcControl &ctl) {
     const LinearParams &p = q.p;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
-    const int w_units = MODE == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0, depth_bytes = kTcDepth * p.w_bits / 8;
+    const int w_units = MODE == kGather || p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0, depth_bytes = kTcDepth * p.w_bits / 8;
     const uint32_t flip = q.flip ? 0x80808080u : 0u;
     Ring ring, unpacked;                               // stages, and slots of unpacked weights
     const int team_warps = kHelperWarps<MODE> / q.teams, team = warp / team_warps;
@@ -368,19 +370,20 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                 const bool of_w = unit < w_units;
                 const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
                 if constexpr (MODE == kTransform) {
-                    if (of_w) {
+                    if (of_w && p.w_bits < 8) {
                         const uint32_t raw = at + q.raw_off;
                         if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, to, row0) : unpack_unit<4, false>(raw, to, row0);
                         else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, to, row0) : unpack_unit<2, false>(raw, to, row0);
                         else p.down ? unpack_unit<1, true>(raw, to, row0) : unpack_unit<1, false>(raw, to, row0);
-                    } else if (q.flip) {
+                    } else if (of_w || q.flip) {
+                        const int pieces = (of_w ? kTcRows : q.nt) * 8;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int k = row0 * 8 + j * 32 + lane;
-                            if (k < q.nt * 8) {
-                                const uint32_t a = at + q.x_off + k * 16;
+                            if (k < pieces) {
+                                const uint32_t a = at + (of_w ? 0 : q.x_off) + k * 16;
                                 const uint4 v = load_shared16(a);
-                                store_shared16(a, v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
+                                store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
                             }
                         }
                     }
@@ -394,7 +397,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                             RowUnit<decltype(bits)::value> u;
                             u.load(src, p.w_row, left, rows);
                             if (!waited && !wait_all_of(q, wait_for, parity)) return false;
-                            p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, 0);
+                            p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0u) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, q.flip_w ? 0x80808080u : 0u);
                             return true;
                         };
                         const bool ok = p.w_bits == 8 ? run(std::integral_constant<int, 8>()) : p.w_bits == 4 ? run(std::integral_constant<int, 4>())
@@ -417,7 +420,7 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                 tc_wait_store();
                 tc_fence_before();
             }
-            if (MODE == kGather || q.flip) proxy_fence();
+            if (MODE == kGather || q.flip || q.flip_w) proxy_fence();
             __syncwarp();
             if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[unpacked.stage]));
             ring.next(q.stages);
@@ -682,6 +685,11 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         }
         proxy_fence();
     }
+    if (MODE != kTma && q.flip_w) {
+        for (int i = tid; i < kTcRows * kTcDepth / 16; i += blockDim.x)
+            store_shared16(stages + q.halves_off + i * 16, 0x40404040u, 0x40404040u, 0x40404040u, 0x40404040u);
+        proxy_fence();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -755,6 +763,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         }
     } else if (warp == 1) {
         Ring ring, unpacked, acc;
+        const uint64_t halves = smem_descriptor(stages + q.halves_off);
         const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.x_off);
         const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4, atom_units = (uint32_t)q.atom_bytes >> 4;
         for (int t = t0; fine && t < tiles; t += step) {
@@ -789,6 +798,10 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
                             for (int k = 0; k < kTcDepth / 32; ++k) {
                                 tc_mma(d, a + k * 2, b + k * 2, idesc, accumulate);
                                 accumulate = 1;
+                                if (MODE != kTma && q.flip_w) {
+                                    tc_mma(d, halves, b + k * 2, idesc, 1);
+                                    tc_mma(d, halves, b + k * 2, idesc, 1);
+                                }
                             }
                         }
                     }
@@ -874,10 +887,8 @@ int sm_count_here() {
     return sms;
 }
 
-// Whether this kernel takes the layer: operands that are both signed or both unsigned bytes or become so, and few enough tiles for
-// 32-bit counts.
-bool linear_tc_takes(const LinearParams &p) {
-    if (p.w_u8 && p.x_signed) return false;
+// Whether the layer has few enough tiles and rows of weights for 32-bit counts.
+static bool fits(const LinearParams &p) {
     if ((long long)p.E * p.N > 0x7FFFFFFFll || p.M > (1 << 30)) return false;
     return ((long long)p.M / 16 + (p.E < p.M ? p.E : p.M) + 1) * ceil_div(p.N, kTcRows) < 0x3FFFFFFFll;
 }
@@ -922,6 +933,7 @@ static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int
 }
 
 int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
+    if (!fits(p)) return HIKONV_ERR_UNSUPPORTED;
     TcParams q;
     memset(&q, 0, sizeof(q));
     q.p = p;
@@ -929,10 +941,11 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     const bool as_unsigned = (p.x_u8 || p.w_u8) && !p.x_signed && !p.w_signed;
     q.flip = p.x_u8 && !as_unsigned;
     q.ones = q.flip ? 16 : 0;
-    const int mode = !rows_aligned(p) ? kGather : p.w_bits < 8 || q.flip ? kTransform : kTma;
+    q.flip_w = p.w_u8 && !as_unsigned;
+    const int mode = !rows_aligned(p) ? kGather : p.w_bits < 8 || q.flip || q.flip_w ? kTransform : kTma;
     choose_tile(p, mode, q.flip, sms, &q.nt, &q.splits);
     // units that unpack weights fall to the warps of their lanes: their number per step is a multiple of four
-    q.units = (mode == kGather || p.w_bits < 8 ? kTcRows / kUnitRows : 0) + (mode == kGather || q.flip ? ceil_div(q.nt, kUnitRows) : 0);
+    q.units = (mode == kGather || p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0) + (mode == kGather || q.flip ? ceil_div(q.nt, kUnitRows) : 0);
     if (mode == kTransform && p.w_bits < 8) q.units = (int)align_up(q.units, 4);
     q.chunks = ceil_div(p.K, kTcDepth);
     q.n_blocks = ceil_div(p.N, kTcRows);
@@ -948,7 +961,7 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     while ((1 << q.split_shift) < q.splits) ++q.split_shift;
     // a step of a narrow tile is shorter than the loop around it: several to a stage
     q.atoms = apart ? 1 : q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
-    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, all = kTcMostSmem - 2048 - tables;
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, all = kTcMostSmem - 2048 - tables - (q.flip_w ? operand_bytes : 0);
     while (q.atoms > 1 && all / (q.atoms * q.atom_bytes) < 4) q.atoms /= 2;
     q.stage_bytes = q.atoms * q.atom_bytes;
     q.stages = (int)(all / q.stage_bytes);
@@ -967,7 +980,8 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     }
     q.tmem_cols = 32;
     while (q.tmem_cols < 2 * q.acc_cols + (apart ? q.a_slots * 32 * q.atoms : 0)) q.tmem_cols *= 2;
-    q.held = q.stages * q.stage_bytes;
+    q.halves_off = q.stages * q.stage_bytes;
+    q.held = q.halves_off + (q.flip_w ? operand_bytes : 0);
     // Teams of at least four warps, since a warp reaches a quarter of the lanes of tensor memory only.  A team that waits for the parity of
     // a barrier must know that the use before the last is over, or it takes an older use for its own.  Of slot s for stage n: the team saw
     // the multiplies of stage n - 3 - a_slots end, which are not before those of n - 2 a_slots if there are three slots.  Of stage n's

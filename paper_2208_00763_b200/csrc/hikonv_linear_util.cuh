@@ -32,15 +32,6 @@ __device__ __forceinline__ void load_bytes(const uint8_t *src, int bytes, uint32
     for (int i = 0; i < W; ++i) out[i] = __funnelshift_r(v[i], v[i + 1], off * 8);
 }
 
-// Clears all but the first `bytes` bytes of 16.
-__device__ __forceinline__ void keep_bytes(uint32_t (&v)[4], int bytes) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int left = bytes - 4 * i;
-        v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
-    }
-}
-
 // Dense codes to one per byte.  Unsigned codes take their value; signed ones go to the upper bits of their byte, where the sign
 // is the byte's (their value times 2^(8 - b): the sums are shifted back once at the end, exactly), which saves the sign extension.
 // UP: 0xF0F0F0F0-like masks and left shifts; the codes of a word come in order.
@@ -71,29 +62,6 @@ __device__ __forceinline__ void unpack1(uint32_t w, uint32_t (&out)[4]) {
         const uint32_t n = (w >> (4 * i)) & 0xFu;
         const uint32_t spread = (n * 0x00204081u) & 0x01010101u;
         out[i] = UP ? spread << 7 : spread;
-    }
-}
-
-// Sixteen weights from byte `src` on (dense: 2 b bytes), `valid` of them inside the row; what lies behind is anything.
-__device__ __forceinline__ void load_weights16(const uint8_t *src, int valid, int bits, bool up, uint32_t (&out)[4]) {
-    if (bits == 8) {
-        load_bytes<4>(src, valid, out);
-    } else if (bits == 4) {
-        uint32_t v[2], lo[2], hi[2];
-        load_bytes<2>(src, (valid * 4 + 7) >> 3, v);
-        if (up) { unpack4<true>(v[0], lo); unpack4<true>(v[1], hi); }
-        else { unpack4<false>(v[0], lo); unpack4<false>(v[1], hi); }
-        out[0] = lo[0]; out[1] = lo[1]; out[2] = hi[0]; out[3] = hi[1];
-    } else if (bits == 2) {
-        uint32_t v[1];
-        load_bytes<1>(src, (valid * 2 + 7) >> 3, v);
-        if (up) unpack2<true>(v[0], out);
-        else unpack2<false>(v[0], out);
-    } else {
-        uint32_t v[1];
-        load_bytes<1>(src, (valid + 7) >> 3, v);
-        if (up) unpack1<true>(v[0], out);
-        else unpack1<false>(v[0], out);
     }
 }
 
