@@ -473,7 +473,7 @@ int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, in
 /*
  * hikonv_linear - matrix product of codes with everything that follows it in the same launch.
  * (The paper's layers are convolutions; a fully connected layer is the 1x1 convolution of one pixel per row.  Its depth is
- * long and nothing overlaps, so the products run on byte dot products and tensor cores instead of packed words.)
+ * long and nothing overlaps, so the products run on tensor cores instead of packed words.)
  *   sum[m][n] = sum_k x[m][k] w[n][k], exact
  *   SUMS:            out = sum                                                       (int32)
  *   CODES:           out = clamp((sum + bias[n]) >> shift, lo, hi), arithmetic shift, bias int32 or NULL; the addition does
@@ -488,8 +488,10 @@ int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, in
  * Depth: K max|x| W <= 2^31 - 1 with W = 128 for signed weights (dense ones are multiplied as the upper bits of a byte) and
  * 2^q - 1 for unsigned ones, else HIKONV_ERR_NO_FIT.
  * out must not overlap any input, except that it may be the residual itself (same address and stride), else
- * HIKONV_ERR_INVALID_ARG.  M == 0 launches nothing; N, K >= 1.  Any alignment of codes is accepted; rows of x and w that
- * start on 16-byte boundaries are read fastest.  No workspace is needed.
+ * HIKONV_ERR_INVALID_ARG.  M == 0 launches nothing; N, K >= 1.
+ * Any alignment of codes is accepted.  Rows of x and w that start on 16-byte boundaries are read as they are; others may be copied to
+ * such rows first, in d_workspace (16-byte aligned, hikonv_linear_workspace_bytes of it; NULL where that is 0).  The bytes around a
+ * row that lie in the same 16 aligned bytes as part of it may be read, nothing else outside the operands.
  */
 typedef struct {
     int out_type;                   /* hikonv_out_type                                             */
@@ -503,7 +505,13 @@ typedef struct {
 } hikonv_epilogue_t;
 
 int hikonv_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, int M, int N, int K, int p, int q,
-                  int x_signed, int w_signed, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream);
+                  int x_signed, int w_signed, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue,
+                  void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace of a call on these operands (host only; nothing is read through the pointers): 0 where no rows have to be copied.
+ * E: groups of hikonv_grouped_linear (M is its T), or 0 for hikonv_linear. */
+size_t hikonv_linear_workspace_bytes(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, int E, int M, int N,
+                                     int K);
 
 /*
  * hikonv_grouped_linear - hikonv_linear with one matrix of weights per group of rows (the experts of a mixture).
@@ -517,7 +525,7 @@ int hikonv_linear(const void *d_x, long long x_row_stride, const void *d_w, int 
 #define HIKONV_MAX_GROUPS 1024
 int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, const int32_t *d_offsets, int E,
                           int T, int N, int K, int p, int q, int x_signed, int w_signed, void *d_out, long long out_row_stride,
-                          const hikonv_epilogue_t *epilogue, void *stream);
+                          const hikonv_epilogue_t *epilogue, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /*
  * hikonv_linear_wait_timeouts - warps of linear-layer kernels on the current device whose wait for their own copies or multiplies ran

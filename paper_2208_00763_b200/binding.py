@@ -97,8 +97,9 @@ _SIGNATURES = {
     "hikonv_conv2d_layout": (_i, [_i] * 11 + [ctypes.POINTER(TuningT), ctypes.POINTER(LayoutT), ctypes.POINTER(_i)]),
     "hikonv_pipe_rate": (_i, [_i, _i, _vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "hikonv_quantize_rows": (_i, [_vp, _i, _ll, _i, _i, _i, _i, _vp, _vp, _vp]),
-    "hikonv_linear": (_i, [_vp, _ll, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
-    "hikonv_grouped_linear": (_i, [_vp, _ll, _vp, _i, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
+    "hikonv_linear": (_i, [_vp, _ll, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp, _sz, _vp]),
+    "hikonv_grouped_linear": (_i, [_vp, _ll, _vp, _i, _vp] + [_i] * 8 + [_vp, _ll, ctypes.POINTER(EpilogueT), _vp, _sz, _vp]),
+    "hikonv_linear_workspace_bytes": (_sz, [_vp, _ll, _vp] + [_i] * 5),
     "hikonv_linear_wait_timeouts": (_i, [_vp]),
     "hikonv_linear_wait_check": (_i, [_ll, _vp]),
     "hikonv_status_string": (ctypes.c_char_p, [_i]),
@@ -106,7 +107,8 @@ _SIGNATURES = {
 
 
 _FAST_ENTRY_POINTS = ("hikonv_conv1d", "hikonv_conv1d_dense", "hikonv_pack", "hikonv_conv2d", "hikonv_conv2d_dense",
-                      "hikonv_conv2d_workspace_bytes", "hikonv_quantize_rows", "hikonv_linear", "hikonv_grouped_linear")
+                      "hikonv_conv2d_workspace_bytes", "hikonv_quantize_rows", "hikonv_linear", "hikonv_grouped_linear",
+                      "hikonv_linear_workspace_bytes")
 
 
 def exported_names():
@@ -528,6 +530,14 @@ def _stream_of(t: torch.Tensor, stream) -> int:
     return _raw_stream(t.device.index) if stream is None else int(stream.cuda_stream)
 
 
+def _empty(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
+    """Memory that a call on `stream` may write at once: the allocator's for that stream, which nothing on another one still uses."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def quantize_rows(x: torch.Tensor, bits: int, is_signed: bool = True, codes: Optional[torch.Tensor] = None,
                   scale: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """Codes of ``bits`` bits, one per byte, and one float scale per row of the matrix ``x`` (float32, float16 or bfloat16; its rows
@@ -542,9 +552,9 @@ def quantize_rows(x: torch.Tensor, bits: int, is_signed: bool = True, codes: Opt
     x_row = _rows(x, "x", (x.dtype,))
     M, K = x.shape
     if codes is None:
-        codes = torch.empty((M, K), dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
+        codes = _empty((M, K), torch.int8 if is_signed else torch.uint8, x, stream)
     if scale is None:
-        scale = torch.empty(M, dtype=torch.float32, device=x.device)
+        scale = _empty(M, torch.float32, x, stream)
     if tuple(codes.shape) != (M, K):
         raise ValueError("codes has shape %s, the call needs %s" % (tuple(codes.shape), (M, K)))
     with torch.cuda.device(x.device):
@@ -557,34 +567,43 @@ def quantize_rows(x: torch.Tensor, bits: int, is_signed: bool = True, codes: Opt
 def linear(x: torch.Tensor, w: torch.Tensor, p: int, q: int, x_signed: bool, w_signed: bool, w_store_bits: int = 8,
            x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
            activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None, requant: Optional[tuple] = None,
-           out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+           out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+           stream=None) -> torch.Tensor:
     """Matrix product of codes, ``x`` [M, K] with ``w`` [N, K] (``w_store_bits`` 1, 2 or 4: dense bytes [N, K * q / 8]).
 
     requant = (shift, lo, hi): codes, one per byte, of the sums plus an int32 ``bias``.  Scales, or a float ``out_dtype`` or ``out``:
     ``act(sum * x_scale[m] * w_scale[n] + bias[n]) + residual[m, n]`` (bfloat16 unless ``out_dtype`` or ``out`` says
     otherwise; scales and bias float32, residual of the output's type, which may be ``out`` itself).  Else: the exact int32 sums.
-    Rows of ``x``, ``residual`` and ``out`` may lie apart."""
+    Rows of ``x``, ``residual`` and ``out`` may lie apart.  Rows of ``x`` and ``w`` that do not start on 16-byte boundaries may be copied
+    to such first, into ``workspace`` (``linear_workspace_bytes``; made by the call when it is not given)."""
     return _linear("hikonv_linear", x, w, None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual,
-                   requant, out_dtype, out, stream)
+                   requant, out_dtype, out, workspace, stream)
+
+
+def linear_workspace_bytes(x: torch.Tensor, w: torch.Tensor, w_store_bits: int = 8) -> int:
+    """Bytes that ``linear`` (``w`` [N, K]) or ``grouped_linear`` (``w`` [E, N, K]) needs to copy rows of these operands: 0 for most."""
+    M, K = x.shape
+    groups = w.shape[0] if w.dim() == 3 else 0
+    return int(lib().hikonv_linear_workspace_bytes(x.data_ptr(), x.stride(0), w.data_ptr(), w_store_bits, groups, M, w.shape[-2], K))
 
 
 def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, p: int, q: int, x_signed: bool, w_signed: bool,
                    w_store_bits: int = 8, x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None,
                    bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
                    requant: Optional[tuple] = None, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
-                   stream=None) -> torch.Tensor:
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """``linear`` with a matrix of weights per group of rows: ``w`` [E, N, K], ``w_scale`` and ``bias`` [E, N]; rows
     ``offsets[e]`` to ``offsets[e + 1] - 1`` (int32 [E + 1], on the device) belong to matrix e.  Rows of no group are left as they
     were in ``out`` (undefined when the call makes it)."""
     return _linear("hikonv_grouped_linear", x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation,
-                   residual, requant, out_dtype, out, stream)
+                   residual, requant, out_dtype, out, workspace, stream)
 
 
 def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype,
-            out, stream):
+            out, workspace, stream):
     if stream is None:
         done = (_fast or _load_fast()).linear(x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation,
-                                              residual, requant, out_dtype, out)
+                                              residual, requant, out_dtype, out, workspace)
         if done is not None:
             return done
     grouped = name == "hikonv_grouped_linear"
@@ -615,7 +634,7 @@ def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale
         if out_dtype not in (None, torch.int32):
             raise ValueError("sums are int32, not %s" % out_dtype)
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype or (torch.int8 if kind == OUT_CODES else torch.int32), device=x.device)
+        out = _empty((M, N), out_dtype or (torch.int8 if kind == OUT_CODES else torch.int32), x, stream)
     ep = EpilogueT(out_type=kind, activation=int(activation))
     out_row = _rows(out, "out", dtypes, x, (M, N))
     ep.d_x_scale = _vector(x_scale, "x_scale", torch.float32, (M,), x)
@@ -630,8 +649,14 @@ def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale
     if grouped:
         groups = (_vector(offsets, "offsets", torch.int32, (lead[0] + 1,), x), lead[0])
     with torch.cuda.device(x.device):
+        need = int(lib().hikonv_linear_workspace_bytes(x.data_ptr(), x_row, w.data_ptr(), w_store_bits, lead[0] if grouped else 0, M, N, K))
+        if need and workspace is None:
+            workspace = _empty(need, torch.uint8, x, stream)
+        if workspace is not None and (not workspace.is_cuda or workspace.device != x.device or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous CUDA tensor on x's device")
+        space = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
         _check(getattr(lib(), name)(x.data_ptr(), x_row, w.data_ptr(), w_store_bits, *groups, M, N, K, p, q, int(x_signed),
-                                    int(w_signed), out.data_ptr(), out_row, ctypes.byref(ep), _stream_of(x, stream)), name)
+                                    int(w_signed), out.data_ptr(), out_row, ctypes.byref(ep), *space, _stream_of(x, stream)), name)
     return out
 
 

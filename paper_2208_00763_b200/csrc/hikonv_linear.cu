@@ -16,7 +16,8 @@ static bool overlap(const void *a, size_t an, const void *b, size_t bn) {
 }
 
 static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_bits, const int32_t *d_offsets, int grouped, int E, int M,
-                      int N, int K, int p, int q, int xs, int ws, void *d_out, long long out_row, const hikonv_epilogue_t *ep, void *stream) {
+                      int N, int K, int p, int q, int xs, int ws, void *d_out, long long out_row, const hikonv_epilogue_t *ep, void *workspace, size_t workspace_bytes,
+                      void *stream) {
     const int rc = validate_codes(p, q);
     if (rc != HIKONV_OK) return rc;
     if (!ep || M < 0 || N < 1 || K < 1 || E < 1) return HIKONV_ERR_INVALID_ARG;
@@ -55,6 +56,10 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
         overlap(d_out, out_bytes, ep->d_residual, ((size_t)(M - 1) * res_row + N) * elem))
         return HIKONV_ERR_INVALID_ARG;
 
+    if (overlap(workspace, workspace_bytes, d_out, out_bytes) || overlap(workspace, workspace_bytes, d_x, (size_t)(M - 1) * x_row + K) ||
+        overlap(workspace, workspace_bytes, d_w, (size_t)E * N * w_row))
+        return HIKONV_ERR_INVALID_ARG;
+
     LinearParams k;
     memset(&k, 0, sizeof(k));
     k.x = (const uint8_t *)d_x; k.w = (const uint8_t *)d_w; k.offsets = d_offsets;
@@ -70,7 +75,8 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     k.out_row = out_row; k.res_row = res_row;
     k.shift = ep->shift; k.lo = ep->lo; k.hi = ep->hi;
     const int rows = grouped ? ceil_div(M, E) : M;               // of a group, on average
-    return linear_rows_takes(k, rows) ? launch_linear_rows(k, (cudaStream_t)stream) : launch_linear_tc(k, (cudaStream_t)stream);
+    return linear_rows_takes(k, rows) ? launch_linear_rows(k, (cudaStream_t)stream)
+                                      : launch_linear_tc(k, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 }  // namespace hikonv
@@ -79,16 +85,30 @@ using namespace hikonv;
 
 extern "C" int hikonv_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, int M, int N, int K, int p, int q,
                              int x_signed, int w_signed, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue,
-                             void *stream) {
+                             void *d_workspace, size_t workspace_bytes, void *stream) {
     return linear_run(d_x, x_row_stride, d_w, w_store_bits, nullptr, 0, 1, M, N, K, p, q, x_signed != 0, w_signed != 0, d_out, out_row_stride,
-                      epilogue, stream);
+                      epilogue, d_workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t hikonv_linear_workspace_bytes(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, int E, int M, int N,
+                                                int K) {
+    if (E < 0 || M < 1 || N < 1 || K < 1 || (w_store_bits != 1 && w_store_bits != 2 && w_store_bits != 4 && w_store_bits != 8)) return 0;
+    static const int32_t some = 0;                               // a layer of groups; the kernels' choice asks for no more than that
+    LinearParams k;
+    memset(&k, 0, sizeof(k));
+    k.x = (const uint8_t *)d_x; k.w = (const uint8_t *)d_w; k.offsets = E > 0 ? &some : nullptr;
+    k.x_row = M == 1 ? K : x_row_stride; k.w_row = (long long)K * w_store_bits / 8;
+    k.M = M; k.N = N; k.K = K; k.E = E > 0 ? E : 1;
+    k.w_bits = w_store_bits;
+    return linear_rows_takes(k, E > 0 ? ceil_div(M, E) : M) ? 0 : linear_tc_workspace(k);
 }
 
 extern "C" int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, const int32_t *d_offsets,
                                      int E, int T, int N, int K, int p, int q, int x_signed, int w_signed, void *d_out,
-                                     long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream) {
+                                     long long out_row_stride, const hikonv_epilogue_t *epilogue, void *d_workspace, size_t workspace_bytes,
+                                     void *stream) {
     return linear_run(d_x, x_row_stride, d_w, w_store_bits, d_offsets, 1, E, T, N, K, p, q, x_signed != 0, w_signed != 0, d_out,
-                      out_row_stride, epilogue, stream);
+                      out_row_stride, epilogue, d_workspace, workspace_bytes, stream);
 }
 
 extern "C" int hikonv_linear_wait_timeouts(unsigned int *h_count) {

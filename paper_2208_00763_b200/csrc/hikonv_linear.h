@@ -33,7 +33,8 @@ int launch_linear_rows(const LinearParams &p, cudaStream_t st);
 int sm_count_here();                                         // of the current device
 
 // All others (hikonv_linear_tc.cu).
-int launch_linear_tc(const LinearParams &p, cudaStream_t st);
+size_t linear_tc_workspace(const LinearParams &p);           // bytes, 16-byte aligned, for rows that do not start on such boundaries
+int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cudaStream_t st);
 int read_linear_timeouts(unsigned int *h_count);             // on the current device, since it was loaded
 int launch_linear_wait_check(long long cycles, cudaStream_t st);
 

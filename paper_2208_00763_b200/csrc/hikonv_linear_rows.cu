@@ -272,18 +272,18 @@ static int rows_at_a_time(const LinearParams &p) { return p.offsets || p.M <= 8 
 
 // Where this kernel is the faster one.  Both are a set-up and a time per weight, in us, measured on weights from memory, for x = N K E /
 // 2^24 weights and up to 8 or 16 rows: 8-bit 2.0 + 3.1 x or 2.0 + 3.7 x here against 4.3 + 2.4 x on tcgen05 tiles; 4-bit 2.0 + 2.0 x or
-// 2.0 + 2.7 x against 5.6 + 2.3 x; 2-bit 2.0 + 2.7 x or 2.0 + 3.9 x against 5.6 + 2.1 x; 1-bit 2.0 + 5.8 x or 2.0 + 9 x.  Rows that x is
-// staged for cost 0.9 us per 4096 codes of x more, and tiles that read such rows 7 + 5.5 x, so there M K decides.
+// 2.0 + 2.7 x against 5.6 + 2.3 x; 2-bit 2.0 + 2.7 x or 2.0 + 3.9 x against 5.6 + 2.1 x; 1-bit 2.0 + 5.8 x or 2.0 + 9 x.  Rows that do not
+// start on 16-byte boundaries: 1 us and 0.9 us per 4096 staged codes of x more here, a launch and a copy of the weights more there.
 bool linear_rows_takes(const LinearParams &p, int rows) {
     if (rows > (p.offsets ? 8 : kLinearFewRows) || p.E > 65535) return false;
-    if (!rows_as_they_are(p))
-        return staged_pitch(p) * 4 * (p.offsets ? 8 : p.M) <= kRowsMostSmem && (long long)rows * p.K <= 28 * 1024;
+    const bool stays = rows_as_they_are(p);
+    if (!stays && staged_pitch(p) * 4 * (p.offsets ? 8 : p.M) > kRowsMostSmem) return false;
     const double x = (double)p.N * p.K * p.E / (1 << 24);
     const bool eight = rows_at_a_time(p) == 8;
-    const double tiles = p.w_bits == 8 ? 4.3 + 2.4 * x : 5.6 + (p.w_bits == 4 ? 2.3 : 2.1) * x;
+    const double tiles = (p.w_bits == 8 ? 4.3 + 2.4 * x : 5.6 + (p.w_bits == 4 ? 2.3 : 2.1) * x) + (stays ? 0.0 : 0.9 + 4.8 * x * p.w_bits / 8);
     const double here = 2.0 + x * (p.w_bits == 8 ? (eight ? 3.1 : 3.7) : p.w_bits == 4 ? (eight ? 2.0 : 2.7) : p.w_bits == 2 ? (eight ? 2.7 : 3.9)
                                                                                                                  : (eight ? 5.8 : 9.0));
-    return here <= tiles;
+    return here + (stays ? 0.0 : 1.0 + 0.9 / 4096 * rows * p.K) <= tiles;
 }
 
 template <int BITS, int TOK, bool STAGED>

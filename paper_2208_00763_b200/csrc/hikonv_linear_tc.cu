@@ -12,8 +12,8 @@
 // get 128 subtracted (their top bit flipped; the instruction takes either two signed or two unsigned operands here).  What that takes
 // off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.  Unsigned 8-bit
 // weights of signed activations, the rare case, are flipped too, and 128 sum_k x[m][k] is added by multiplying x twice by a tile of 64s.
-// TMA wants rows on 16-byte boundaries.  Operands whose rows start anywhere are read by twelve helper warps instead, as aligned words
-// that are moved into place (and unpacked, and flipped) on their way to shared memory.
+// TMA wants rows on 16-byte boundaries.  Operands whose rows start anywhere are copied to rows that do in a launch of their own
+// (align_rows_kernel): read by helper warps word by word instead, 433 x 9100 x 4352 took 103 us and 333 x 1001 x 1501 13.3.
 //
 // Small layers have fewer tiles than there are SMs: there the CTAs of a cluster share a tile's depth, and the cluster adds their sums
 // through distributed shared memory, each CTA finishing its part of the tile's output columns.
@@ -30,11 +30,11 @@ constexpr int kTcRows = 128;             // output columns of the layer per tile
 constexpr int kTcDepth = 128;            // codes of the depth per step: one 128-byte swizzled row
 constexpr int kTcMostStages = 12;
 constexpr int kFirstEpilogueWarp = 4;
-// How operands come to the multiplies: by TMA alone; by TMA and changed in place by warps of their own; read by such warps.
-enum TcMode { kTma = 0, kTransform = 1, kGather = 2 };
-template <int MODE> constexpr int kEpilogueWarps = MODE == kGather ? 4 : 8;
+// How operands come to the multiplies: by TMA alone, or by TMA and changed by warps of their own.
+enum TcMode { kTma = 0, kTransform = 1 };
+constexpr int kEpilogueWarps = 8;
 template <int MODE> constexpr int kHelperWarps = MODE == kTma ? 0 : 12;
-template <int MODE> constexpr int kTcThreads = (kFirstEpilogueWarp + kEpilogueWarps<MODE> + kHelperWarps<MODE>) * 32;
+template <int MODE> constexpr int kTcThreads = (kFirstEpilogueWarp + kEpilogueWarps + kHelperWarps<MODE>) * 32;
 template <int MODE> constexpr int kEpilogueBatch = MODE == kTma ? 16 : 8;       // rows of x at a time: what the registers hold
 constexpr int kUnitRows = 32;            // operand rows that a helper warp works on at a time
 constexpr size_t kTcMostSmem = 226 * 1024;
@@ -127,7 +127,8 @@ __device__ __forceinline__ void mbarrier_arrive(uint32_t bar) {
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 __device__ __forceinline__ uint32_t remote_address(uint32_t smem_addr, uint32_t rank) {
     uint32_t remote;
@@ -242,107 +243,17 @@ __device__ __forceinline__ void unpack_unit(uint32_t raw, uint32_t to, int row0)
     tc_store32(to + ((uint32_t)row0 << 16), o);
 }
 
-// One unit of an operand's rows that start on any byte.  BITS * 4 lanes take a row's 128 codes, a word each, as aligned words; the word
-// behind a row's last comes from one more load for all rows, and each lane moves its own and its neighbour's together.
-template <int BITS>
-struct RowUnit {
-    static constexpr int LANES = 4 * BITS, ROWS = 32 / LANES, STEPS = kUnitRows / ROWS;
-    uint32_t v[STEPS], behind;
-
-    // src: first byte of the unit's first row and of this part of the depth; left: bytes from there to the row's end; rows: how many exist.
-    __device__ __forceinline__ void load(const uint8_t *src, long long pitch, int left, int rows) {
-        const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
-        if (rows >= kUnitRows && left >= 4 * LANES + 4) {
-            const uint8_t *at = src + sub * pitch;
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                v[i] = load_ordered(reinterpret_cast<const uint32_t *>((uintptr_t)at & ~(uintptr_t)3) + word);
-                at += ROWS * pitch;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int r = i * ROWS + sub;
-                const uint8_t *at = src + r * pitch;
-                const int off = (int)((uintptr_t)at & 3);
-                v[i] = r < rows && word * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + word) : 0u;
-            }
-        }
-        const uint8_t *at = src + lane * pitch;
-        const int off = (int)((uintptr_t)at & 3);
-        behind = lane < rows && off && LANES * 4 - off < left ? load_ordered(reinterpret_cast<const uint32_t *>(at - off) + LANES) : 0u;
-    }
-
-    // To the operand's layout, rows below `limit` (a multiple of 16); what lies behind the row's end becomes zero (flip: unsigned bytes less 128 everywhere).
-    // A row's shift repeats every four rows and its swizzle every eight, so a word costs two shuffles, a select, a shift and a store.
-    template <bool UP>
-    __device__ __forceinline__ void store(uint32_t tile, int row0, int limit, const uint8_t *src, long long pitch, int left, uint32_t flip) {
-        const int lane = threadIdx.x & 31, sub = lane / LANES, word = lane % LANES;
-        const int keep = left - word * 4;              // bytes of this lane's word in front of the row's end
-        const uint32_t mask = keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
-        const uint32_t s0 = (uint32_t)(uintptr_t)src & 3u, sp = (uint32_t)pitch & 3u;
-        const bool words = (s0 | sp) == 0;             // rows start on words
-        const uint32_t line = tile + (row0 + sub) * 128 + word * (32 / BITS);
-        constexpr int TURNS = ROWS >= 8 ? 1 : 8 / ROWS, SHIFTS = ROWS >= 4 ? 1 : 4 / ROWS;
-        uint32_t at[TURNS], shift[SHIFTS];
-#pragma unroll
-        for (int i = 0; i < TURNS; ++i) at[i] = line ^ (((i * ROWS + sub) & 7) << 4);
-#pragma unroll
-        for (int i = 0; i < SHIFTS; ++i) shift[i] = ((s0 + (i * ROWS + sub) * sp) & 3u) * 8;
-        if (!words) {
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                uint32_t next = __shfl_down_sync(0xFFFFFFFFu, v[i], 1);
-                const uint32_t last = __shfl_sync(0xFFFFFFFFu, behind, i * ROWS + sub);
-                if (word == LANES - 1) next = last;
-                v[i] = __funnelshift_r(v[i], next, shift[i % SHIFTS]);
-            }
-        }
-        if (BITS == 8 && limit - row0 < kUnitRows) {   // the half unit behind the last whole one
-#pragma unroll
-            for (int i = 0; i < STEPS / 2; ++i)
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at[i % TURNS] + i * ROWS * 128), "r"((v[i] & mask) ^ flip) : "memory");
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const uint32_t w = v[i] & mask;
-            const uint32_t to = at[i % TURNS] + i * ROWS * 128;
-            if constexpr (BITS == 8) {
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(w ^ flip) : "memory");
-            } else if constexpr (BITS == 4) {
-                uint32_t o[2];
-                unpack4<UP>(w, o);
-                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(to), "r"(o[0]), "r"(o[1]) : "memory");
-            } else if constexpr (BITS == 2) {
-                uint32_t o[4];
-                unpack2<UP>(w, o);
-                store_shared16(to, o[0], o[1], o[2], o[3]);
-            } else {
-                uint32_t o[4];
-                unpack1<UP>(w, o);
-                store_shared16(to, o[0], o[1], o[2], o[3]);
-                unpack1<UP>(w >> 16, o);
-                store_shared16(to ^ 16, o[0], o[1], o[2], o[3]);
-            }
-        }
-    }
-};
-
 // The helper warps: the units of a stage dealt out over a team of them, on from where its stage before left off.  A stage costs a warp
 // some 400 cycles beside its units (waits, fences, the report), so there are several teams where a stage has few units.
-template <int MODE>
 __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &tables, int t0, int tiles, int step, int c0, int c1, uint32_t stages,
                                      uint32_t tmem, TcControl &ctl) {
     const LinearParams &p = q.p;
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps<MODE>;
-    const int w_units = MODE == kGather || p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0, depth_bytes = kTcDepth * p.w_bits / 8;
-    const uint32_t flip = q.flip ? 0x80808080u : 0u;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kFirstEpilogueWarp - kEpilogueWarps;
+    const int w_units = p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0;
     Ring ring, unpacked;                               // stages, and slots of unpacked weights
-    const int team_warps = kHelperWarps<MODE> / q.teams, team = warp / team_warps;
+    const int team_warps = kHelperWarps<kTransform> / q.teams, team = warp / team_warps;
     int turn = warp % team_warps, due = team;          // the unit that falls to this warp first, and the stages until this team's next
     for (int t = t0; t < tiles; t += step) {
-        const Tile tile = find_tc_tile(q, tables, t);
         for (int c = c0; c < c1; c += q.atoms) {
             if (due-- > 0) {
                 ring.next(q.stages);
@@ -350,77 +261,43 @@ __device__ __forceinline__ bool help(const TcParams &q, const GroupTables &table
                 continue;
             }
             due = q.teams - 1;
-            const int some = min(q.atoms, c1 - c), total = some * q.units;
+            const int total = min(q.atoms, c1 - c) * q.units;
             const uint32_t stage = stages + ring.stage * q.stage_bytes, slot = tmem + q.a_column + unpacked.stage * q.atoms * 32;
-            const uint32_t wait_for = MODE == kTransform ? smem_address(&ctl.full[ring.stage]) : smem_address(&ctl.empty[ring.stage]);
-            const uint32_t parity = MODE == kTransform ? ring.phase : ring.phase ^ 1;
-            bool waited = false;
-            if (MODE == kTransform && q.a_column) {
+            if (q.a_column) {
                 if (!wait_all_of(q, smem_address(&ctl.unpacked_empty[unpacked.stage]), unpacked.phase ^ 1)) return false;
                 tc_fence_after();
             }
-            if (MODE == kTransform || turn >= total) {
-                if (!wait_all_of(q, wait_for, parity)) return false;
-                waited = true;
-            }
+            if (!wait_all_of(q, smem_address(&ctl.full[ring.stage]), ring.phase)) return false;
             int i = turn, atom = 0, unit = turn;
             for (; i < total; i += team_warps, unit += team_warps) {
                 while (unit >= q.units) unit -= q.units, ++atom;
                 const uint32_t at = stage + atom * q.atom_bytes, to = slot + atom * 32;
                 const bool of_w = unit < w_units;
                 const int row0 = (of_w ? unit : unit - w_units) * kUnitRows;
-                if constexpr (MODE == kTransform) {
-                    if (of_w && p.w_bits < 8) {
-                        const uint32_t raw = at + q.raw_off;
-                        if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, to, row0) : unpack_unit<4, false>(raw, to, row0);
-                        else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, to, row0) : unpack_unit<2, false>(raw, to, row0);
-                        else p.down ? unpack_unit<1, true>(raw, to, row0) : unpack_unit<1, false>(raw, to, row0);
-                    } else if (of_w || q.flip) {
-                        const int pieces = (of_w ? kTcRows : q.nt) * 8;
+                if (of_w && p.w_bits < 8) {
+                    const uint32_t raw = at + q.raw_off;
+                    if (p.w_bits == 4) p.down ? unpack_unit<4, true>(raw, to, row0) : unpack_unit<4, false>(raw, to, row0);
+                    else if (p.w_bits == 2) p.down ? unpack_unit<2, true>(raw, to, row0) : unpack_unit<2, false>(raw, to, row0);
+                    else p.down ? unpack_unit<1, true>(raw, to, row0) : unpack_unit<1, false>(raw, to, row0);
+                } else if (of_w || q.flip) {
+                    const int pieces = (of_w ? kTcRows : q.nt) * 8;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int k = row0 * 8 + j * 32 + lane;
-                            if (k < pieces) {
-                                const uint32_t a = at + (of_w ? 0 : q.x_off) + k * 16;
-                                const uint4 v = load_shared16(a);
-                                store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
-                            }
+                    for (int j = 0; j < 8; ++j) {
+                        const int k = row0 * 8 + j * 32 + lane;
+                        if (k < pieces) {
+                            const uint32_t a = at + (of_w ? 0 : q.x_off) + k * 16;
+                            const uint4 v = load_shared16(a);
+                            store_shared16(a, v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u);
                         }
                     }
-                } else {
-                    // the loads are under way before the stage is free
-                    if (of_w) {
-                        const long long begin = (long long)(c + atom) * depth_bytes;
-                        const uint8_t *src = p.w + ((long long)tile.e * p.N + tile.n0 + row0) * p.w_row + begin;
-                        const int left = (int)min(p.w_row - begin, 1024ll), rows = p.N - tile.n0 - row0;
-                        auto run = [&](auto bits) {
-                            RowUnit<decltype(bits)::value> u;
-                            u.load(src, p.w_row, left, rows);
-                            if (!waited && !wait_all_of(q, wait_for, parity)) return false;
-                            p.down ? u.template store<true>(at, row0, kTcRows, src, p.w_row, left, 0u) : u.template store<false>(at, row0, kTcRows, src, p.w_row, left, q.flip_w ? 0x80808080u : 0u);
-                            return true;
-                        };
-                        const bool ok = p.w_bits == 8 ? run(std::integral_constant<int, 8>()) : p.w_bits == 4 ? run(std::integral_constant<int, 4>())
-                                        : p.w_bits == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
-                        if (!ok) return false;
-                    } else {
-                        const int begin = (c + atom) * kTcDepth;
-                        const uint8_t *src = p.x + (long long)(tile.row0 + row0) * p.x_row + begin;
-                        const int left = min(p.K - begin, 1024), rows = tile.rows - row0;
-                        RowUnit<8> u;
-                        u.load(src, p.x_row, left, rows);
-                        if (!waited && !wait_all_of(q, wait_for, parity)) return false;
-                        u.store<false>(at + q.x_off, row0, q.nt, src, p.x_row, left, flip);
-                    }
-                    waited = true;
                 }
             }
             turn = i - total;
-            if (MODE == kTransform && q.a_column) {
+            if (q.a_column) {
                 tc_wait_store();
                 tc_fence_before();
             }
-            if (MODE == kGather || q.flip || q.flip_w) proxy_fence();
+            if (q.flip || q.flip_w) proxy_fence();
             __syncwarp();
             if (lane == 0) mbarrier_arrive(smem_address(&ctl.ready[unpacked.stage]));
             ring.next(q.stages);
@@ -641,7 +518,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     const uint32_t control = smem_address(dynamic);
     auto barrier = [&](size_t offset, int i) { return control + (uint32_t)offset + 8u * (uint32_t)i; };
 #define HIKONV_BAR(name, i) barrier(offsetof(TcControl, name), i)
-    constexpr int EPI = kEpilogueWarps<MODE>, FIRST_HELPER = kFirstEpilogueWarp + EPI;
+    constexpr int EPI = kEpilogueWarps, FIRST_HELPER = kFirstEpilogueWarp + EPI;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);       // the same in all lanes, which the compiler does not see from tid
     const LinearParams &p = q.p;
@@ -668,7 +545,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             ctl.whole = 1;
         }
         mbarrier_init_fence();
-        if (MODE != kGather && lane == 3) {
+        if (lane == 3) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
         }
@@ -727,39 +604,37 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     auto wait = [&](uint32_t bar, uint32_t parity) { return wait_all_of(q, bar, parity); };
     bool fine = true;
     if (warp == 0) {
-        if (MODE != kGather) {
-            Ring ring;
-            const int depth_bytes = kTcDepth * p.w_bits / 8;
-            const uint32_t bytes = (uint32_t)(q.nt * kTcDepth + kTcRows * depth_bytes);
-            const uint32_t w_off = p.w_bits == 8 ? 0u : (uint32_t)q.raw_off;
-            int loads = 0;
-            for (int t = t0; fine && t < tiles; t += step) {
-                const Tile tile = find_tc_tile(q, tables, t);
-                const int w_row0 = tile.e * p.N + tile.n0;
-                if (loads == 0) grid_dependency_wait();
-                for (int c = c0; c < c1; c += q.atoms) {
-                    fine = wait(HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
-                    if (!fine) break;
-                    const uint32_t bar = HIKONV_BAR(full, ring.stage);
-                    const int some = min(q.atoms, c1 - c);
-                    if (elect_one()) {
-                        uint32_t at = stages + ring.stage * q.stage_bytes;
-                        mbarrier_arrive_expect(bar, bytes * some);
-                        for (int i = 0; i < some; ++i, at += q.atom_bytes) {
-                            tma_load_2d(at + w_off, &map_w, (c + i) * depth_bytes, w_row0, bar);
-                            tma_load_2d(at + q.x_off, &map_x, (c + i) * kTcDepth, tile.row0, bar);
-                        }
+        Ring ring;
+        const int depth_bytes = kTcDepth * p.w_bits / 8;
+        const uint32_t bytes = (uint32_t)(q.nt * kTcDepth + kTcRows * depth_bytes);
+        const uint32_t w_off = p.w_bits == 8 ? 0u : (uint32_t)q.raw_off;
+        int loads = 0;
+        for (int t = t0; fine && t < tiles; t += step) {
+            const Tile tile = find_tc_tile(q, tables, t);
+            const int w_row0 = tile.e * p.N + tile.n0;
+            if (loads == 0) grid_dependency_wait();
+            for (int c = c0; c < c1; c += q.atoms) {
+                fine = wait(HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
+                if (!fine) break;
+                const uint32_t bar = HIKONV_BAR(full, ring.stage);
+                const int some = min(q.atoms, c1 - c);
+                if (elect_one()) {
+                    uint32_t at = stages + ring.stage * q.stage_bytes;
+                    mbarrier_arrive_expect(bar, bytes * some);
+                    for (int i = 0; i < some; ++i, at += q.atom_bytes) {
+                        tma_load_2d(at + w_off, &map_w, (c + i) * depth_bytes, w_row0, bar);
+                        tma_load_2d(at + q.x_off, &map_x, (c + i) * kTcDepth, tile.row0, bar);
                     }
-                    ++loads;
-                    ring.next(q.stages);
                 }
+                ++loads;
+                ring.next(q.stages);
             }
-            // what is in flight has to land before the memory goes: the last load of every stage
-            for (int i = 0; i < q.stages && i < loads; ++i) {
-                ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
-                if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                fine &= wait(HIKONV_BAR(full, ring.stage), ring.phase);
-            }
+        }
+        // what is in flight has to land before the memory goes: the last load of every stage
+        for (int i = 0; i < q.stages && i < loads; ++i) {
+            ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+            if (ring.stage == q.stages - 1) ring.phase ^= 1;
+            fine &= wait(HIKONV_BAR(full, ring.stage), ring.phase);
         }
     } else if (warp == 1) {
         Ring ring, unpacked, acc;
@@ -821,8 +696,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             wait(HIKONV_BAR(drain, 0), 0);
         }
     } else if (MODE != kTma && warp >= FIRST_HELPER) {
-        if (MODE == kGather) grid_dependency_wait();
-        if constexpr (MODE != kTma) fine = help<MODE>(q, tables, t0, tiles, step, c0, c1, stages, tmem, ctl);
+        if constexpr (MODE != kTma) fine = help(q, tables, t0, tiles, step, c0, c1, stages, tmem, ctl);
     } else if (warp >= kFirstEpilogueWarp && warp < FIRST_HELPER) {
         grid_dependency_wait();
         with_epilogue(p, [&](auto kind, auto act) {
@@ -844,6 +718,28 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
 }
 
 #undef HIKONV_BAR
+
+// Rows of bytes from any address and pitch to rows on 16-byte boundaries, two matrices in one launch; a thread per 16 bytes.  What lies
+// behind a row in its last piece is anything.
+struct AlignRows {
+    const uint8_t *src;
+    uint8_t *dst;
+    long long src_row;
+    int bytes, pieces;                   // of a row
+    long long total;                     // pieces of the matrix
+};
+__global__ void __launch_bounds__(256) align_rows_kernel(const AlignRows a, const AlignRows b, int a_blocks) {
+    grid_dependency_release();
+    grid_dependency_wait();
+    const AlignRows &m = (int)blockIdx.x < a_blocks ? a : b;
+    const long long i = ((long long)blockIdx.x - ((int)blockIdx.x < a_blocks ? 0 : a_blocks)) * 256 + threadIdx.x;
+    if (i >= m.total) return;
+    const long long row = m.total <= 0xFFFFFFFFll ? (long long)((uint32_t)i / (uint32_t)m.pieces) : i / m.pieces;
+    const int at = (int)(i - row * m.pieces) * 16;
+    uint32_t v[4];
+    load_bytes<4>(m.src + row * m.src_row + at, min(16, m.bytes - at), v);
+    *reinterpret_cast<uint4 *>(m.dst + i * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+}
 
 __global__ void linear_wait_check_kernel(long long cycles) {
     __shared__ uint64_t bar;
@@ -892,9 +788,33 @@ static bool fits(const LinearParams &p) {
     if ((long long)p.E * p.N > 0x7FFFFFFFll || p.M > (1 << 30)) return false;
     return ((long long)p.M / 16 + (p.E < p.M ? p.E : p.M) + 1) * ceil_div(p.N, kTcRows) < 0x3FFFFFFFll;
 }
-// Whether TMA reads its rows: all on 16-byte boundaries.
-static bool rows_aligned(const LinearParams &p) {
-    return (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && (p.M == 1 || p.x_row % 16 == 0) && p.w_row % 16 == 0;
+// Whether TMA reads the rows of x, and of w, as they are: all on 16-byte boundaries.
+static bool x_aligned(const LinearParams &p) { return (uintptr_t)p.x % 16 == 0 && (p.M == 1 || p.x_row % 16 == 0); }
+static bool w_aligned(const LinearParams &p) { return (uintptr_t)p.w % 16 == 0 && p.w_row % 16 == 0; }
+
+size_t linear_tc_workspace(const LinearParams &p) {
+    return (x_aligned(p) ? 0 : (size_t)p.M * align_up(p.K, 16)) + (w_aligned(p) ? 0 : (size_t)p.E * p.N * align_up(p.w_row, 16));
+}
+
+// Copies what is not aligned into the workspace and points the layer there.
+static int align_operands(LinearParams *p, void *workspace, cudaStream_t st) {
+    uint8_t *to = (uint8_t *)workspace;
+    AlignRows m[2] = {};
+    int n = 0;
+    auto add = [&](const uint8_t **base, long long *row, long long rows, long long bytes) {
+        AlignRows &a = m[n++];
+        a.src = *base; a.src_row = *row; a.dst = to;
+        a.bytes = (int)bytes; a.pieces = (int)((bytes + 15) / 16); a.total = rows * a.pieces;
+        *base = to;
+        *row = (long long)a.pieces * 16;
+        to += a.total * 16;
+    };
+    const bool x_stays = x_aligned(*p), w_stays = w_aligned(*p);
+    if (!x_stays) add(&p->x, &p->x_row, p->M, p->K);
+    if (!w_stays) add(&p->w, &p->w_row, (long long)p->E * p->N, p->w_row);
+    const long long a_blocks = (m[0].total + 255) / 256, b_blocks = (m[1].total + 255) / 256;
+    if (a_blocks + b_blocks > 0x7FFFFFFFll) return HIKONV_ERR_UNSUPPORTED;
+    return launch_dependent(align_rows_kernel, dim3((unsigned)(a_blocks + b_blocks)), dim3(256), 0, st, m[0], m[1], (int)a_blocks);
 }
 
 // Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.  A step of 128 codes costs the longest of its
@@ -914,13 +834,13 @@ static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * n_blocks;
         const double bytes = kTcRows * kTcDepth * p.w_bits / 8.0 + nt * (double)kTcDepth;
         double step = 2.0 * nt > bytes / 70.0 ? 2.0 * nt : bytes / 70.0;
-        const double help = mode == kGather ? 240.0 * (4 + ceil_div(nt, kUnitRows)) : mode == kTransform ? 370.0 : 200.0;
+        const double help = mode == kTransform ? 370.0 : 200.0;
         if (step < help) step = help;
         for (int splits = 1; splits <= 8 && splits <= chunks; splits *= 2) {
             // clusters of four and more do not fill every SM: their CTAs share one part of the GPU
             if (splits > 1 && (tiles * splits > sms - 20 || nt > 128)) break;
             const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
-            const double time = waves * ceil_div(chunks, splits) * step + (mode == kGather ? 6000.0 : 3000.0) +
+            const double time = waves * ceil_div(chunks, splits) * step + 3000.0 +
                                 (splits > 1 ? 2500.0 + 500.0 * splits + 62.0 * nt / splits + 8.0 * nt : 800.0 + 20.0 * nt);
             if (time < best) {
                 best = time;
@@ -932,8 +852,13 @@ static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int
     }
 }
 
-int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
+int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cudaStream_t st) {
     if (!fits(p)) return HIKONV_ERR_UNSUPPORTED;
+    if (const size_t need = linear_tc_workspace(p)) {
+        if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need) return HIKONV_ERR_WORKSPACE;
+        const int rc = align_operands(&p, workspace, st);
+        if (rc != HIKONV_OK) return rc;
+    }
     TcParams q;
     memset(&q, 0, sizeof(q));
     q.p = p;
@@ -942,10 +867,10 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     q.flip = p.x_u8 && !as_unsigned;
     q.ones = q.flip ? 16 : 0;
     q.flip_w = p.w_u8 && !as_unsigned;
-    const int mode = !rows_aligned(p) ? kGather : p.w_bits < 8 || q.flip || q.flip_w ? kTransform : kTma;
+    const int mode = p.w_bits < 8 || q.flip || q.flip_w ? kTransform : kTma;
     choose_tile(p, mode, q.flip, sms, &q.nt, &q.splits);
     // units that unpack weights fall to the warps of their lanes: their number per step is a multiple of four
-    q.units = (mode == kGather || p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0) + (mode == kGather || q.flip ? ceil_div(q.nt, kUnitRows) : 0);
+    q.units = (p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0) + (q.flip ? ceil_div(q.nt, kUnitRows) : 0);
     if (mode == kTransform && p.w_bits < 8) q.units = (int)align_up(q.units, 4);
     q.chunks = ceil_div(p.K, kTcDepth);
     q.n_blocks = ceil_div(p.N, kTcRows);
@@ -998,11 +923,8 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
     const size_t smem = (size_t)q.held + 2048 + tables;
 
     CUtensorMap map_x, map_w;
-    if (mode == kGather) {
-        memset(&map_x, 0, sizeof(map_x));
-        memset(&map_w, 0, sizeof(map_w));
-    } else if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt) ||
-        !encode_map(&map_w, p.w, (uint64_t)p.w_row, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows))
+    if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, p.M > 1 ? (uint64_t)p.x_row : (uint64_t)align_up(p.K, 16), kTcDepth, (uint32_t)q.nt) ||
+        !encode_map(&map_w, p.w, (uint64_t)p.K * p.w_bits / 8, (uint64_t)p.E * p.N, (uint64_t)p.w_row, (uint32_t)(kTcDepth * p.w_bits / 8), kTcRows))
         return HIKONV_ERR_CUDA;
     const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
     auto launch = [&](auto kernel, int threads) {
@@ -1023,9 +945,7 @@ int launch_linear_tc(const LinearParams &p, cudaStream_t st) {
             return cudaLaunchKernelEx(&cfg, kernel, q, map_x, map_w) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
         });
     };
-    if (mode == kTma) return launch(linear_tc_kernel<kTma>, kTcThreads<kTma>);
-    if (mode == kTransform) return launch(linear_tc_kernel<kTransform>, kTcThreads<kTransform>);
-    return launch(linear_tc_kernel<kGather>, kTcThreads<kGather>);
+    return mode == kTma ? launch(linear_tc_kernel<kTma>, kTcThreads<kTma>) : launch(linear_tc_kernel<kTransform>, kTcThreads<kTransform>);
 }
 
 int read_linear_timeouts(unsigned int *h_count) {

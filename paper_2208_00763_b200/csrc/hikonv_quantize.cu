@@ -99,27 +99,40 @@ __device__ __forceinline__ uint32_t word_max(uint32_t w, uint32_t top, __nv_bflo
     return *reinterpret_cast<const uint32_t *>(&m);
 }
 
-// Rows on 16-byte boundaries (codes on 8-byte ones): VECS pieces of eight values per thread, in registers.
-template <typename T, int VECS, bool SIGNED>
-__global__ void __launch_bounds__(512, VECS >= 4 && sizeof(T) == 4 ? 1 : 2) quantize_vectors_kernel(const QuantizeParams p) {
+// VECS pieces of eight values per thread, in registers.  Pieces are taken from 16-byte boundaries.  Unless ALIGNED (every row starts on one,
+// codes on an 8-byte one), a row begins `lead` values into its first piece, and what lies in front of it or behind its end is left out;
+// its codes are moved into aligned words with the help of the lane before, which has the bytes that a word begins with.
+template <typename T, int VECS, bool SIGNED, bool ALIGNED>
+__global__ void __launch_bounds__(512, VECS >= 4 && sizeof(T) == 4 ? 1 : 2) quantize_pieces_kernel(const QuantizeParams p) {
     constexpr int WORDS = sizeof(T) * 2;                // of eight values
     __shared__ float part[32];
     grid_dependency_release();
     grid_dependency_wait();
-    const int at = p.threads == 32 ? threadIdx.x & 31 : threadIdx.x;
+    const int lane = threadIdx.x & 31, at = p.threads == 32 ? lane : threadIdx.x;
     const int row = p.threads == 32 ? blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
     if (row >= p.M) return;                             // whole warps; rows of a whole CTA are all there
     const T *x = (const T *)p.x + row * p.x_row;
-    const int pieces = p.K / 8;
+    const int lead = ALIGNED ? 0 : (int)((uintptr_t)x & 15) / (int)sizeof(T);
+    auto whole = [&](int j) { return j * 8 - lead >= 0 && j * 8 - lead + 8 <= p.K; };
     uint32_t v[VECS][WORDS];
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
-        const int j = at + i * p.threads;
+        const int j = at + i * p.threads, k0 = j * 8 - lead;
 #pragma unroll
-        for (int h = 0; h < WORDS / 4; ++h) {
-            uint4 o = make_uint4(0, 0, 0, 0);
-            if (j < pieces) o = load_ordered(reinterpret_cast<const uint4 *>(x + j * 8) + h);
-            v[i][4 * h] = o.x; v[i][4 * h + 1] = o.y; v[i][4 * h + 2] = o.z; v[i][4 * h + 3] = o.w;
+        for (int h = 0; h < WORDS; ++h) v[i][h] = 0;
+        if (whole(j)) {
+#pragma unroll
+            for (int h = 0; h < WORDS / 4; ++h) {
+                const uint4 o = load_ordered(reinterpret_cast<const uint4 *>(x + k0) + h);
+                v[i][4 * h] = o.x; v[i][4 * h + 1] = o.y; v[i][4 * h + 2] = o.z; v[i][4 * h + 3] = o.w;
+            }
+        } else if (!ALIGNED) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k0 + k >= 0 && k0 + k < p.K) {
+                    if constexpr (sizeof(T) == 4) v[i][k] = __float_as_uint(load_ordered((const float *)x + k0 + k));
+                    else v[i][k / 2] |= (uint32_t)load_ordered((const unsigned short *)x + k0 + k) << (16 * (k & 1));
+                }
         }
     }
     auto value = [&](int i, int k) {
@@ -146,8 +159,7 @@ __global__ void __launch_bounds__(512, VECS >= 4 && sizeof(T) == 4 ? 1 : 2) quan
     if (at == 0) p.scale[row] = by.scale;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
-        const int j = at + i * p.threads;
-        if (j >= pieces) break;
+        const int j = at + i * p.threads, k0 = j * 8 - lead;
         uint32_t o[8];
         float open = by.quick ? 0.f : 1.f;
 #pragma unroll
@@ -162,97 +174,85 @@ __global__ void __launch_bounds__(512, VECS >= 4 && sizeof(T) == 4 ? 1 : 2) quan
             for (int k = 0; k < 8; ++k) o[k] = quantize_exactly(value(i, k), by.scale, by.lo, by.hi);
         }
         auto four = [&](int k) { return byte_permute(byte_permute(o[k], o[k + 1], 0x0040), byte_permute(o[k + 2], o[k + 3], 0x0040), 0x5410); };
-        *reinterpret_cast<uint2 *>(p.codes + (size_t)row * p.K + j * 8) = make_uint2(four(0), four(4));
+        const uint32_t low = four(0), high = four(4);
+        int8_t *to = p.codes + (size_t)row * p.K + k0;
+        if constexpr (ALIGNED) {
+            if (whole(j)) *reinterpret_cast<uint2 *>(to) = make_uint2(low, high);
+        } else {
+            const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, high, 1);
+            const int off = (int)((uintptr_t)to & 3);
+            if (whole(j)) {
+                uint32_t *word = reinterpret_cast<uint32_t *>(to - off);
+                const bool joined = off == 0 || (lane > 0 && whole(j - 1)), joins = off == 0 || (lane < 31 && whole(j + 1));
+                if (joined) word[0] = __funnelshift_l(before, low, 8 * off);
+                else
+                    for (int b = 0; b < 4 - off; ++b) to[b] = (int8_t)(low >> (8 * b));
+                word[1] = __funnelshift_l(low, high, 8 * off);
+                if (!joins)
+                    for (int b = 4 - off; b < 4; ++b) to[4 + b] = (int8_t)(high >> (8 * b));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k0 + k >= 0 && k0 + k < p.K) to[k] = (int8_t)o[k];
+            }
+        }
     }
 }
 
-// Any alignment: VALUES single values per thread in registers, neighbours on neighbouring threads; longer rows (VALUES == 0) are
-// read twice, the second time from the caches.
-template <typename T, int VALUES, bool SIGNED>
-__global__ void __launch_bounds__(1024, 1) quantize_values_kernel(const QuantizeParams p) {
+// Longer rows, of any alignment: a CTA reads its row twice, the second time from the caches.
+template <typename T, bool SIGNED>
+__global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeParams p) {
     __shared__ float part[32];
     grid_dependency_release();
     grid_dependency_wait();
     const int row = blockIdx.x;
     const T *x = (const T *)p.x + row * p.x_row;
     int8_t *codes = p.codes + (size_t)row * p.K;
-    float v[VALUES > 0 ? VALUES : 1], top = 0.f;
-    if (VALUES > 0) {
-#pragma unroll
-        for (int i = 0; i < VALUES; ++i) {
-            const int k = threadIdx.x + i * p.threads;
-            v[i] = k < p.K ? quantize_float(load_ordered(x + k)) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < VALUES; ++i) top = max_nan(top, SIGNED ? fabsf(v[i]) : v[i]);
-    } else {
-        for (int k = threadIdx.x; k < p.K; k += p.threads) {
-            const float a = quantize_float(load_ordered(x + k));
-            top = max_nan(top, SIGNED ? fabsf(a) : a);
-        }
+    float top = 0.f;
+    for (int k = threadIdx.x; k < p.K; k += p.threads) {
+        const float a = quantize_float(load_ordered(x + k));
+        top = max_nan(top, SIGNED ? fabsf(a) : a);
     }
     top = row_max(top, p.threads, part);
     const RowScale by(top, p);
     if (threadIdx.x == 0) p.scale[row] = by.scale;
-    auto one = [&](float a) {
+    for (int k = threadIdx.x; k < p.K; k += p.threads) {
+        const float a = quantize_float(load_ordered(x + k));
         float distance;
         uint32_t c = quantize_quickly<SIGNED>(a, by.inverse, &distance);
         if (!by.quick || distance >= kOpen) c = quantize_exactly(a, by.scale, by.lo, by.hi);
-        return (int8_t)c;
-    };
-    if constexpr (VALUES > 0) {
-        uint32_t c[VALUES];
-        float open = by.quick ? 0.f : 1.f;
-#pragma unroll
-        for (int i = 0; i < VALUES; i += 2) {
-            float d0, d1;
-            c[i] = quantize_quickly<SIGNED>(v[i], by.inverse, &d0);
-            c[i + 1] = quantize_quickly<SIGNED>(v[i + 1], by.inverse, &d1);
-            open = fmaxf(fmaxf(d0, d1), open);
-        }
-        if (open >= kOpen) {                            // rare
-#pragma unroll
-            for (int i = 0; i < VALUES; ++i) c[i] = quantize_exactly(v[i], by.scale, by.lo, by.hi);
-        }
-#pragma unroll
-        for (int i = 0; i < VALUES; ++i) {
-            const int k = threadIdx.x + i * p.threads;
-            if (k < p.K) codes[k] = (int8_t)c[i];
-        }
-    } else {
-        for (int k = threadIdx.x; k < p.K; k += p.threads) codes[k] = one(quantize_float(load_ordered(x + k)));
+        codes[k] = (int8_t)c;
     }
+}
+
+template <typename T, bool SIGNED, bool ALIGNED>
+static int launch_pieces(QuantizeParams p, cudaStream_t st) {
+    // A warp per row up to 64 pieces; then a CTA with two pieces per thread, four or eight where that makes more than 256 threads (so that
+    // several CTAs share an SM, and one row's loads overlap another's arithmetic).
+    const int pieces = ALIGNED ? p.K / 8 : (p.K + 14) / 8;                  // a row may begin seven values into its first
+    if (pieces <= 64) {
+        p.threads = 32;
+        const int warps = p.M >= sm_count_here() * 8 ? 8 : 1;
+        const dim3 grid((unsigned)ceil_div(p.M, warps)), block((unsigned)(warps * 32));
+        return pieces <= 32 ? launch_dependent(quantize_pieces_kernel<T, 1, SIGNED, ALIGNED>, grid, block, 0, st, p)
+                            : launch_dependent(quantize_pieces_kernel<T, 2, SIGNED, ALIGNED>, grid, block, 0, st, p);
+    }
+    const int per = pieces <= 512 ? 2 : pieces <= 1024 ? 4 : 8;
+    p.threads = ceil_div(ceil_div(pieces, per), 32) * 32;
+    const dim3 grid((unsigned)p.M), block((unsigned)p.threads);
+    return per == 2   ? launch_dependent(quantize_pieces_kernel<T, 2, SIGNED, ALIGNED>, grid, block, 0, st, p)
+           : per == 4 ? launch_dependent(quantize_pieces_kernel<T, 4, SIGNED, ALIGNED>, grid, block, 0, st, p)
+                      : launch_dependent(quantize_pieces_kernel<T, 8, SIGNED, ALIGNED>, grid, block, 0, st, p);
 }
 
 template <typename T, bool SIGNED>
 static int launch_quantize(QuantizeParams p, cudaStream_t st) {
-    const bool vectors = (uintptr_t)p.x % 16 == 0 && (p.M == 1 || p.x_row * sizeof(T) % 16 == 0) && (uintptr_t)p.codes % 8 == 0 && p.K % 8 == 0;
-    if (vectors && p.K <= 8 * 8 * 512) {
-        // a warp per row up to 512 values; then a CTA with two pieces per thread, four or eight where that makes more than 256 threads (so
-        // that several CTAs share an SM, and one row's loads overlap another's arithmetic)
-        const int pieces = p.K / 8;
-        if (pieces <= 64) {
-            p.threads = 32;
-            const int warps = p.M >= sm_count_here() * 8 ? 8 : 1;
-            const dim3 grid((unsigned)ceil_div(p.M, warps)), block((unsigned)(warps * 32));
-            return pieces <= 32 ? launch_dependent(quantize_vectors_kernel<T, 1, SIGNED>, grid, block, 0, st, p)
-                                : launch_dependent(quantize_vectors_kernel<T, 2, SIGNED>, grid, block, 0, st, p);
-        }
-        const int per = pieces <= 512 ? 2 : pieces <= 1024 ? 4 : 8;
-        p.threads = ceil_div(ceil_div(pieces, per), 32) * 32;
-        const dim3 grid((unsigned)p.M), block((unsigned)p.threads);
-        return per == 2   ? launch_dependent(quantize_vectors_kernel<T, 2, SIGNED>, grid, block, 0, st, p)
-               : per == 4 ? launch_dependent(quantize_vectors_kernel<T, 4, SIGNED>, grid, block, 0, st, p)
-                          : launch_dependent(quantize_vectors_kernel<T, 8, SIGNED>, grid, block, 0, st, p);
-    }
-    // eight values per thread up to 256 threads, then 16, then 32
-    const int per = p.K <= 8 * 256 ? 8 : p.K <= 16 * 1024 ? 16 : 32;
-    p.threads = ceil_div(p.K, per) >= 1024 ? 1024 : ceil_div(ceil_div(p.K, per), 32) * 32;
-    const dim3 grid((unsigned)p.M), block((unsigned)p.threads);
-    if (per == 8) return launch_dependent(quantize_values_kernel<T, 8, SIGNED>, grid, block, 0, st, p);
-    if (per == 16) return launch_dependent(quantize_values_kernel<T, 16, SIGNED>, grid, block, 0, st, p);
-    if (p.K <= 32 * 1024) return launch_dependent(quantize_values_kernel<T, 32, SIGNED>, grid, block, 0, st, p);
-    return launch_dependent(quantize_values_kernel<T, 0, SIGNED>, grid, block, 0, st, p);
+    constexpr int most = 8 * 8 * 512;                   // values that 512 threads hold
+    const bool aligned = (uintptr_t)p.x % 16 == 0 && (p.M == 1 || p.x_row * sizeof(T) % 16 == 0) && (uintptr_t)p.codes % 8 == 0 && p.K % 8 == 0;
+    if (aligned && p.K <= most) return launch_pieces<T, SIGNED, true>(p, st);
+    if (p.K <= most - 16) return launch_pieces<T, SIGNED, false>(p, st);
+    p.threads = 1024;
+    return launch_dependent(quantize_long_kernel<T, SIGNED>, dim3((unsigned)p.M), dim3(1024), 0, st, p);
 }
 
 }  // namespace hikonv

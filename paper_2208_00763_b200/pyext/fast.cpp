@@ -29,6 +29,7 @@ decltype(&hikonv_pack) g_pack = nullptr;
 decltype(&hikonv_quantize_rows) g_quantize_rows = nullptr;
 decltype(&hikonv_linear) g_linear = nullptr;
 decltype(&hikonv_grouped_linear) g_grouped_linear = nullptr;
+decltype(&hikonv_linear_workspace_bytes) g_linear_workspace_bytes = nullptr;
 
 // Reads arguments one after the other; `ok` stays true while all are as expected.
 struct Args {
@@ -358,7 +359,8 @@ PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// linear(x, w, offsets or None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype, out)
+// linear(x, w, offsets or None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype, out,
+//        workspace)
 PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&]() -> PyObject * {
         Args in{a, n};
@@ -370,7 +372,7 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor *residual = in.optional_tensor();
         const bool rq = in.requant(&ep.shift, &ep.lo, &ep.hi);
         PyObject *dtype = in.next();
-        const at::Tensor *given = in.optional_tensor();
+        const at::Tensor *given = in.optional_tensor(), *space = in.optional_tensor();
         int64_t x_row, out_row, res_row;
         if (!in.ok || !matrix(x, &x_row) || (x->scalar_type() != at::kChar && x->scalar_type() != at::kByte)) return nullptr;
         if (!codes(w) || w->device() != x->device() || w->dim() != (offsets ? 3 : 2)) return nullptr;
@@ -404,10 +406,19 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const c10::cuda::OptionalCUDAGuard guard(x->device());
         const void *x_ptr = x->data_ptr(), *w_ptr = w->data_ptr();
         const int32_t *off_ptr = (const int32_t *)address(offsets);
-        void *y_ptr = y.data_ptr(), *st = current_stream();
+        const size_t need = g_linear_workspace_bytes(x_ptr, x_row, w_ptr, w_bits, offsets ? (int)E : 0, (int)M, (int)N, (int)K);
+        at::Tensor made_space;
+        if (need && !space) {
+            made_space = empty({(int64_t)need}, at::kByte, *x);
+            space = &made_space;
+        }
+        if (space && (!plain_cuda(space) || space->device() != x->device())) return nullptr;
+        void *y_ptr = y.data_ptr(), *st = current_stream(), *space_ptr = space ? space->data_ptr() : nullptr;
+        const size_t space_bytes = space ? (size_t)space->numel() * space->element_size() : 0;
         const int status = unlocked([&] {
-            return offsets ? g_grouped_linear(x_ptr, x_row, w_ptr, w_bits, off_ptr, (int)E, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep, st)
-                           : g_linear(x_ptr, x_row, w_ptr, w_bits, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep, st);
+            return offsets ? g_grouped_linear(x_ptr, x_row, w_ptr, w_bits, off_ptr, (int)E, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep,
+                                              space_ptr, space_bytes, st)
+                           : g_linear(x_ptr, x_row, w_ptr, w_bits, (int)M, (int)N, (int)K, p, q, xs, ws, y_ptr, out_row, &ep, space_ptr, space_bytes, st);
         });
         if (status != HIKONV_OK) return nullptr;
         return result(a[15], made);
@@ -430,6 +441,7 @@ PyObject *bind(PyObject *, PyObject *args) {
     else if (s == "hikonv_quantize_rows") g_quantize_rows = (decltype(g_quantize_rows))ptr;
     else if (s == "hikonv_linear") g_linear = (decltype(g_linear))ptr;
     else if (s == "hikonv_grouped_linear") g_grouped_linear = (decltype(g_grouped_linear))ptr;
+    else if (s == "hikonv_linear_workspace_bytes") g_linear_workspace_bytes = (decltype(g_linear_workspace_bytes))ptr;
     else {
         PyErr_Format(PyExc_ValueError, "no entry point %s", name);
         return nullptr;

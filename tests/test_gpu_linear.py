@@ -83,6 +83,23 @@ def test_sums_of_dense_weights(q, ws):
             assert_exact(got, ol.sums(x, w), "%s" % ((M, K, N, p, q, xs, ws),))
 
 
+def test_dense_weights_over_many_stages_and_tiles():
+    # long walks through the rings of the unpacking warps: several tiles per CTA, depths that end inside a step, flipped activations
+    for M, K, N in ((400, 4128, 256), (2100, 1056, 1300), (200, 6144, 512)):
+        for q, xs, ws in ((4, True, True), (4, False, True), (2, True, False), (1, True, True)):
+            x, w = draw((M, K), (N, K), 8, q, xs, ws, seed=K)
+            got = hk.linear(rows_on_device(x), weights_on_device(w, q), 8, q, xs, ws, w_store_bits=q)
+            assert_exact(got, ol.sums(x, w), "%s" % ((M, K, N, q, xs, ws),))
+
+
+def test_bytes_over_many_tiles():
+    # more tiles than SMs, operands of every pair of types, rows that start on 16-byte boundaries and rows that do not
+    for M, K, N in ((2100, 272, 1300), (1500, 333, 1700)):
+        for xs, ws in ((True, True), (False, True), (True, False), (False, False)):
+            x, w = draw((M, K), (N, K), 8, 8, xs, ws, seed=K)
+            assert_exact(hk.linear(rows_on_device(x), weights_on_device(w, 8), 8, 8, xs, ws), ol.sums(x, w), "%s" % ((M, K, N, xs, ws),))
+
+
 @pytest.mark.parametrize("kind", ["min", "max", "mixed"])
 def test_extreme_codes_at_the_largest_depth(kind):
     for p, q, xs, ws, store in ((8, 8, True, True, 8), (8, 8, False, True, 8), (8, 8, False, False, 8), (8, 4, True, True, 4), (8, 1, True, True, 1),
@@ -168,6 +185,28 @@ def test_weights_that_start_anywhere():
             view.copy_(dw)
             for rows in (M, 2):
                 assert_exact(hk.linear(rows_on_device(x[:rows]), view, 8, q, True, True, w_store_bits=store), ol.sums(x[:rows], w), "lead %d" % lead)
+
+
+def test_given_workspaces():
+    x, w = draw((70, 333), (90, 333), 8, 8, True, True, seed=9)
+    dx, dw = rows_on_device(x), weights_on_device(w, 8)
+    need = hk.linear_workspace_bytes(dx, dw)
+    assert need == (70 + 90) * 336
+    buf = torch.full((need + 64,), 3, dtype=torch.uint8, device="cuda")
+    got = hk.linear(dx, dw, 8, 8, True, True, workspace=buf[32:need + 32])
+    assert_exact(got, ol.sums(x, w))
+    assert (buf[:32] == 3).all() and (buf[need + 32:] == 3).all()
+    with pytest.raises(hk.HikonvError):
+        hk.linear(dx, dw, 8, 8, True, True, workspace=buf[:16])
+    with pytest.raises(ValueError):
+        hk.linear(dx, dw, 8, 8, True, True, workspace=torch.empty(need, dtype=torch.uint8))
+    # made by the call, on a stream of the caller's
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [hk.linear(dx, dw, 8, 8, True, True, stream=side) for _ in range(20)]
+    torch.cuda.synchronize()
+    for y in got:
+        assert_exact(y, ol.sums(x, w))
 
 
 def test_no_rows_and_one_value():

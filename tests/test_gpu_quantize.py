@@ -82,6 +82,16 @@ def test_given_outputs_and_what_lies_around_them():
     assert c.shape == (0, 16) and s.shape == (0,)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_codes_that_start_on_any_byte(dtype):
+    for K in (1, 3, 9, 77, 520, 1001, 8190):
+        x = torch.randn(6, K, generator=torch.Generator().manual_seed(K)).to(dtype).cuda()
+        for lead in range(5):
+            buf = torch.full((6 * K + 16,), 55, dtype=torch.int8, device="cuda")
+            check(x, 8, True, codes=buf[lead:lead + 6 * K].view(6, K))
+            assert (buf[:lead] == 55).all() and (buf[lead + 6 * K:] == 55).all()
+
+
 def test_captured_and_other_streams():
     x = torch.randn(40, 256, device="cuda").bfloat16()
     codes = torch.zeros((40, 256), dtype=torch.int8, device="cuda")

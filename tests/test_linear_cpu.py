@@ -18,13 +18,15 @@ def built_library():
 
 # addresses that no call here may follow, far enough apart that nothing overlaps
 X, W, OUT, SCALE, SCALE2, BIAS, RES, OFF = (0x100000000000 + (i << 40) for i in range(8))
-GOOD = dict(x=X, x_row=64, w=W, store=8, M=4, N=32, K=64, p=8, q=8, xs=1, ws=1, out=OUT, out_row=32, ep=dict(out_type=hk.OUT_BF16))
+WS = 0x900000000000
+GOOD = dict(ws_ptr=None, ws_bytes=0, x=X, x_row=64, w=W, store=8, M=4, N=32, K=64, p=8, q=8, xs=1, ws=1, out=OUT, out_row=32, ep=dict(out_type=hk.OUT_BF16))
 
 
 def call(grouped=False, offsets=OFF, E=3, **change):
     a = {**GOOD, **change}
     ep = None if a["ep"] is None else ctypes.byref(hk.EpilogueT(**a["ep"]))
-    sizes = (a["M"], a["N"], a["K"], a["p"], a["q"], a["xs"], a["ws"], a["out"], a["out_row"], ep, None)
+    sizes = (a["M"], a["N"], a["K"], a["p"], a["q"], a["xs"], a["ws"], a["out"], a["out_row"], ep, a["ws_ptr"], a["ws_bytes"],
+             None)
     if grouped:
         return hk.lib().hikonv_grouped_linear(a["x"], a["x_row"], a["w"], a["store"], offsets, E, *sizes)
     return hk.lib().hikonv_linear(a["x"], a["x_row"], a["w"], a["store"], *sizes)
@@ -75,6 +77,26 @@ def test_refusals_of_groups():
     assert call(grouped=True, E=hk.MAX_GROUPS + 1) == hk.ERR_UNSUPPORTED
     assert call(grouped=True, offsets=OUT + 8) == hk.ERR_INVALID_ARG
     assert call(grouped=True, E=3, out=W + 3 * 32 * 64 - 2) == hk.ERR_INVALID_ARG
+
+
+def space(**change):
+    a = {**GOOD, **change}
+    return hk.lib().hikonv_linear_workspace_bytes(a["x"], a["x_row"], a["w"], a["store"], a.get("E", 0), a["M"], a["N"], a["K"])
+
+
+def test_workspace():
+    # what is aligned needs none, nor do a few rows; else both operands or either, their rows rounded up to 16 bytes
+    assert space() == 0 and space(M=100, K=60, x_row=64, E=3) == 3 * 32 * 64
+    big = dict(M=100, K=60, x_row=60)
+    assert space(**big) == 100 * 64 + 32 * 64
+    assert space(M=100, x_row=65) == 100 * 64 and space(M=100, x=X + 1) == 100 * 64 and space(M=100, w=W + 4) == 32 * 64
+    assert space(M=100, K=60, x_row=64, store=4) == 32 * 32
+    assert space(M=1, K=60) == 0 and space(M=0) == 0 and space(store=3) == 0
+    need = space(**big)
+    for ptr, size in ((None, 0), (WS, need - 1), (WS + 8, need)):
+        assert call(**big, ws_ptr=ptr, ws_bytes=size) == hk.ERR_WORKSPACE
+    for ptr in (X + 16, W, OUT):
+        assert call(**big, ws_ptr=ptr, ws_bytes=need) == hk.ERR_INVALID_ARG
 
 
 def test_no_rows_is_fine_without_memory():
