@@ -817,6 +817,14 @@ static int align_operands(LinearParams *p, void *workspace, cudaStream_t st) {
     return launch_dependent(align_rows_kernel, dim3((unsigned)(a_blocks + b_blocks)), dim3(256), 0, st, m[0], m[1], (int)a_blocks);
 }
 
+// Steps per stage where weights are unpacked: as many as leave three slots of tensor memory and three stages.  The loops around a stage
+// cost the issuing warps and the helpers as much as a step of it.
+static int unpacked_atoms(int nt, int ones, int w_bits) {
+    const int acc = (int)align_up(nt + ones, 32), bytes = (nt + ones) * kTcDepth + kTcRows * kTcDepth * w_bits / 8;
+    for (int atoms = 4; atoms > 1; atoms /= 2)
+        if ((512 - 2 * acc) / (32 * atoms) >= 3 && 3 * atoms * (int)align_up(bytes, 1024) <= (int)kTcMostSmem - 16 * 1024) return atoms;
+    return 1;
+}
 // Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.  A step of 128 codes costs the longest of its
 // multiplies (2 per row), its way from the second-level cache (70 bytes per cycle and SM) and the helpers' work on it; a tile alone on its
 // SM costs 3000 for the set-up and the end of its epilogue; one with a shared depth two barriers of the cluster, which are dearer the
@@ -834,7 +842,8 @@ static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * n_blocks;
         const double bytes = kTcRows * kTcDepth * p.w_bits / 8.0 + nt * (double)kTcDepth;
         double step = 2.0 * nt > bytes / 70.0 ? 2.0 * nt : bytes / 70.0;
-        const double help = mode == kTransform ? 370.0 : 200.0;
+        const int atoms = mode == kTransform && p.w_bits < 8 ? unpacked_atoms(nt, ones ? 16 : 0, p.w_bits) : 0;
+        const double help = mode != kTransform ? 200.0 : atoms == 4 ? 300.0 : atoms == 2 ? 400.0 : atoms == 1 ? 460.0 : 370.0;
         if (step < help) step = help;
         for (int splits = 1; splits <= 8 && splits <= chunks; splits *= 2) {
             // clusters of four and more do not fill every SM: their CTAs share one part of the GPU
@@ -885,9 +894,9 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
     q.atom_bytes = (int)align_up(q.raw_off + (apart ? operand_bytes * p.w_bits / 8 : 0), 1024);
     while ((1 << q.split_shift) < q.splits) ++q.split_shift;
     // a step of a narrow tile is shorter than the loop around it: several to a stage
-    q.atoms = apart ? 1 : q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
+    q.atoms = apart ? unpacked_atoms(q.nt, q.ones, p.w_bits) : q.nt <= 32 ? 4 : q.nt <= 96 ? 2 : 1;
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0, all = kTcMostSmem - 2048 - tables - (q.flip_w ? operand_bytes : 0);
-    while (q.atoms > 1 && all / (q.atoms * q.atom_bytes) < 4) q.atoms /= 2;
+    while (q.atoms > 1 && all / (q.atoms * q.atom_bytes) < (apart ? 3u : 4u)) q.atoms /= 2;
     q.stage_bytes = q.atoms * q.atom_bytes;
     q.stages = (int)(all / q.stage_bytes);
     if (q.stages > kTcMostStages) q.stages = kTcMostStages;
@@ -913,7 +922,7 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
     // copies, after that: all multiplies up to stage n - a_slots are over, so the copies of n - stages have landed if there are no
     // fewer stages than slots.
     q.teams = 1;
-    if (apart && q.units * q.atoms == 4 && q.stages >= 3 && q.a_slots >= 3) {
+    if (apart && q.units == 4 && q.stages >= 3 && q.a_slots >= 3) {
         q.teams = 3;
         if (q.a_slots > q.stages) q.a_slots = q.stages;
     }
