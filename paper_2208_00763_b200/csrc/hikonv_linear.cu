@@ -21,7 +21,7 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     const int rc = validate_codes(p, q);
     if (rc != HIKONV_OK) return rc;
     if (!ep || M < 0 || N < 1 || K < 1 || E < 1) return HIKONV_ERR_INVALID_ARG;
-    if (E > HIKONV_MAX_GROUPS) return HIKONV_ERR_UNSUPPORTED;
+    if (E > HIKONV_MAX_GROUPS || M > (1 << 30) || N > (1 << 30)) return HIKONV_ERR_UNSUPPORTED;
     const int type = ep->out_type, real = type >= HIKONV_OUT_F32;
     if (type < HIKONV_OUT_SUMS || type > HIKONV_OUT_BF16) return HIKONV_ERR_INVALID_ARG;
     if (ep->activation < HIKONV_ACT_NONE || ep->activation > HIKONV_ACT_GELU) return HIKONV_ERR_INVALID_ARG;
@@ -41,7 +41,7 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     const long long res_row = M == 1 ? N : ep->residual_row_stride;
     if (!d_x || !d_w || !d_out || (grouped && !d_offsets)) return HIKONV_ERR_INVALID_ARG;
     if (x_row < K || out_row < N || (ep->d_residual && res_row < N)) return HIKONV_ERR_INVALID_ARG;
-    if (x_row > (1ll << 40) || out_row > (1ll << 40) || res_row > (1ll << 40)) return HIKONV_ERR_INVALID_ARG;   // byte offsets stay in 64 bits
+    if (x_row >= (1ll << 40) || out_row >= (1ll << 40) || res_row >= (1ll << 40)) return HIKONV_ERR_INVALID_ARG;   // byte offsets stay in 64 bits
     const size_t elem = element_bytes(type);
     if ((uintptr_t)d_out % elem || (uintptr_t)ep->d_residual % elem || (uintptr_t)ep->d_bias % 4 || (uintptr_t)ep->d_x_scale % 4 ||
         (uintptr_t)ep->d_w_scale % 4 || (uintptr_t)d_offsets % 4)

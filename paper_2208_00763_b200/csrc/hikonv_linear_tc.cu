@@ -532,7 +532,6 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     int *group_tiles = reinterpret_cast<int *>(group_row + p.E);
     const GroupTables tables{group_row, group_tiles};
 
-    grid_dependency_release();
     if (warp == 0) {
         if (lane < q.stages) {
             mbarrier_init(HIKONV_BAR(full, lane), 1);
@@ -575,8 +574,11 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl.tmem;
+    // Not before this CTA has its tensor memory: a CTA of the kernel behind that came to this SM first could take it, and wait for this
+    // one to end while this one waits for the memory.
+    grid_dependency_release();
 
-    // Each role waits for the kernel before where it first touches global memory; the multiplying warp never does.
+    // Each role waits for the kernel before where it first touches global memory, or waits, with a bound, for what others bring from there.
     int tiles = q.m_tiles * q.n_blocks;
     if (p.offsets) {
         grid_dependency_wait();
@@ -587,15 +589,16 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
         }
         __syncthreads();
         if (warp == 0) {
-            int before = 0;
+            // in 64 bits, and no more than an index holds: groups that overlap, which only wrong offsets make, may have any number
+            long long before = 0;
             for (int e0 = 0; e0 < p.E; e0 += 32) {
-                int upto = e0 + lane < p.E ? group_tiles[e0 + lane] : 0;
+                long long upto = e0 + lane < p.E ? group_tiles[e0 + lane] : 0;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
-                    const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+                    const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
                     if (lane >= d) upto += v;
                 }
-                if (e0 + lane < p.E) group_tiles[e0 + lane] = before + upto;
+                if (e0 + lane < p.E) group_tiles[e0 + lane] = (int)min(before + upto, 0x3FFFFFFFll);
                 before += __shfl_sync(0xFFFFFFFFu, upto, 31);
             }
         }
@@ -641,6 +644,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             fine &= wait(HIKONV_BAR(full, ring.stage), ring.phase);
         }
     } else if (warp == 1) {
+        grid_dependency_wait();
         Ring ring, unpacked, acc;
         const uint64_t halves = smem_descriptor(stages + q.halves_off);
         const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.x_off);
@@ -700,6 +704,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
             wait(HIKONV_BAR(drain, 0), 0);
         }
     } else if (MODE != kTma && warp >= FIRST_HELPER) {
+        grid_dependency_wait();
         if constexpr (MODE != kTma) fine = help(q, tables, t0, tiles, step, c0, c1, stages, tmem, ctl);
     } else if (warp >= kFirstEpilogueWarp && warp < FIRST_HELPER) {
         grid_dependency_wait();

@@ -102,7 +102,7 @@ def test_bytes_over_many_tiles():
 
 @pytest.mark.parametrize("kind", ["min", "max", "mixed"])
 def test_extreme_codes_at_the_largest_depth(kind):
-    for p, q, xs, ws, store in ((8, 8, True, True, 8), (8, 8, False, True, 8), (8, 8, False, False, 8), (8, 4, True, True, 4), (8, 1, True, True, 1),
+    for p, q, xs, ws, store in ((8, 8, True, True, 8), (8, 8, False, True, 8), (8, 8, False, False, 8), (8, 8, True, False, 8), (8, 4, True, True, 4), (8, 1, True, True, 1),
                                 (8, 2, False, True, 2), (4, 4, False, False, 4)):
         per = (128 if xs else (1 << p) - 1) * (128 if ws else (1 << q) - 1)
         K = min((2 ** 31 - 1) // per, 140000) // 16 * 16

@@ -39,7 +39,8 @@ REFUSED = [
     (hk.ERR_INVALID_ARG, dict(p=0)), (hk.ERR_INVALID_ARG, dict(p=9)), (hk.ERR_INVALID_ARG, dict(q=0)), (hk.ERR_INVALID_ARG, dict(q=9)),
     (hk.ERR_INVALID_ARG, dict(x=None)), (hk.ERR_INVALID_ARG, dict(w=None)), (hk.ERR_INVALID_ARG, dict(out=None)),
     (hk.ERR_INVALID_ARG, dict(x_row=63)), (hk.ERR_INVALID_ARG, dict(out_row=31)), (hk.ERR_INVALID_ARG, dict(x_row=-64)),
-    (hk.ERR_INVALID_ARG, dict(x_row=1 << 50)), (hk.ERR_INVALID_ARG, dict(out_row=1 << 50)),
+    (hk.ERR_UNSUPPORTED, dict(M=(1 << 30) + 1)), (hk.ERR_UNSUPPORTED, dict(N=(1 << 30) + 1, out_row=1 << 31)),
+    (hk.ERR_INVALID_ARG, dict(x_row=1 << 40)), (hk.ERR_INVALID_ARG, dict(x_row=1 << 50)), (hk.ERR_INVALID_ARG, dict(out_row=1 << 50)),
     (hk.ERR_INVALID_ARG, dict(store=4)), (hk.ERR_INVALID_ARG, dict(store=3, q=3)), (hk.ERR_INVALID_ARG, dict(store=0)),
     (hk.ERR_UNSUPPORTED, dict(store=4, q=4, K=63)), (hk.ERR_UNSUPPORTED, dict(store=1, q=1, K=60)),
     (hk.ERR_NO_FIT, dict(K=131072, x_row=131072)), (hk.ERR_NO_FIT, dict(K=33026, x_row=33026, xs=0, ws=0)),
