@@ -275,19 +275,33 @@ static long long staged_pitch(const LinearParams &p) { return (staged_pieces(p) 
 static int rows_at_a_time(const LinearParams &p) { return p.offsets || p.M <= 8 ? 8 : 16; }
 
 // Where this kernel is the faster one.  Both are a set-up and a time per weight, in us, measured on weights from memory, for x = N K E /
-// 2^24 weights and up to 8 or 16 rows: 8-bit 2.0 + 3.1 x or 2.0 + 3.7 x here against 4.3 + 2.4 x on tcgen05 tiles; 4-bit 2.0 + 2.0 x or
-// 2.0 + 2.7 x against 5.6 + 2.3 x; 2-bit 2.0 + 2.7 x or 2.0 + 3.9 x against 5.6 + 2.1 x; 1-bit 2.0 + 5.8 x or 2.0 + 9 x.  Rows that do not
-// start on 16-byte boundaries: 1 us and 0.9 us per 4096 staged codes of x more here, a launch and a copy of the weights more there.
+// 2^24 weights and R rows, at x from 1/64 to 32.  Here: 8-bit 2.0 + 3.1 x, or 2.0 + 3.6 x beyond 8 rows; 4-bit 2.0 + 2.0 x or
+// 2.0 + 2.65 x; 2-bit 2.2 + (1.65 + R / 15) x; 1-bit 2.5 + (1.5 + R / 5) x; and 4.2 us per 2^20 outputs.  On tcgen05 tiles, whose set-up
+// has more CTAs to join where there is depth to share: 8-bit 3.0 + 1.3 d + 2.4 x for d = min(1, K / 2048); fewer bits
+// 3.2 + 2.8 d + 1.35 x, in groups 5.6 + 1.85 x (4-bit) or 5.6 + 1.6 x.  Rows that do not start on 16-byte boundaries: 1 us and 0.9 us per
+// 4096 staged codes of x more here, a launch and a copy of the weights more there.
 bool linear_rows_takes(const LinearParams &p, int rows) {
     if (rows > (p.offsets ? 8 : kLinearFewRows) || p.E > 65535) return false;
     const bool stays = rows_as_they_are(p);
     if (!stays && staged_pitch(p) * 4 * (p.offsets ? 8 : p.M) > kRowsMostSmem) return false;
-    const double x = (double)p.N * p.K * p.E / (1 << 24);
+    const double x = (double)p.N * p.K * p.E / (1 << 24), depth = p.K < 2048 ? p.K / 2048.0 : 1.0;
     const bool eight = rows_at_a_time(p) == 8;
-    const double tiles = (p.w_bits == 8 ? 4.3 + 2.4 * x : 5.6 + (p.w_bits == 4 ? 2.3 : 2.1) * x) + (stays ? 0.0 : 0.9 + 4.8 * x * p.w_bits / 8);
-    const double here = 2.0 + x * (p.w_bits == 8 ? (eight ? 3.1 : 3.7) : p.w_bits == 4 ? (eight ? 2.0 : 2.7) : p.w_bits == 2 ? (eight ? 2.7 : 3.9)
-                                                                                                                 : (eight ? 5.8 : 9.0));
-    return here + (stays ? 0.0 : 1.0 + 0.9 / 4096 * rows * p.K) <= tiles;
+    double here, tiles;
+    switch (p.w_bits) {
+        case 8: here = 2.0 + (eight ? 3.1 : 3.6) * x; break;
+        case 4: here = 2.0 + (eight ? 2.0 : 2.65) * x; break;
+        case 2: here = 2.2 + (1.65 + rows / 15.0) * x; break;
+        default: here = 2.5 + (1.5 + rows / 5.0) * x;
+    }
+    here += 4.2 * p.M * p.N / (1 << 20);
+    if (p.w_bits == 8) tiles = 3.0 + 1.3 * depth + 2.4 * x;
+    else if (!p.offsets) tiles = 3.2 + 2.8 * depth + 1.35 * x;
+    else tiles = 5.6 + (p.w_bits == 4 ? 1.85 : 1.6) * x;
+    if (!stays) {
+        here += 1.0 + 0.9 / 4096 * rows * p.K;
+        tiles += 0.9 + 4.8 * x * p.w_bits / 8;
+    }
+    return here <= tiles;
 }
 
 template <int BITS, int TOK, bool STAGED>
@@ -321,12 +335,11 @@ int launch_linear_rows(const LinearParams &p, cudaStream_t st) {
         q.x_pieces = (int)staged_pieces(p);
         q.x_pitch = (int)staged_pitch(p);
     }
-    const int parts = (int)((p.w_row + 63) / 64);
-    // As many warps per tile as leave each four 64-byte parts of a row, but no more CTAs than the GPU holds at once: each that comes
-    // later waits for its first weights anew (eight groups of 2048 x 2048 4-bit weights, 8 rows: 13.3 us in 1024 CTAs, 8.5 in 512,
-    // 6.4 in 256; 1 x 4096 x 16384 8-bit: 16.7, 15.3, 13.9).
-    q.ksplit = 1;
-    while (q.ksplit < kRowsWarps && parts >= 4 * q.ksplit) q.ksplit *= 2;
+    // All warps of a CTA on one tile, however short its rows: they share the tile's outputs, too (16 x 1024 x 1024 1-bit: 9.5 us by one
+    // warp per tile, 3.4 by eight).  But no more CTAs than the GPU holds at once: each that comes later waits for its first weights anew
+    // (eight groups of 2048 x 2048 4-bit weights, 8 rows: 13.3 us in 1024 CTAs, 8.5 in 512, 6.4 in 256; 1 x 4096 x 16384 8-bit: 16.7,
+    // 15.3, 13.9).
+    q.ksplit = kRowsWarps;
     while (q.ksplit > 1 && (long long)q.class_tiles * q.classes * p.E * q.ksplit > (long long)sms * 2 * kRowsWarps) q.ksplit /= 2;
     const int ways = ceil_div(q.class_tiles, kRowsWarps / q.ksplit);
     const dim3 grid((unsigned)(ways * q.classes), (unsigned)p.E);
