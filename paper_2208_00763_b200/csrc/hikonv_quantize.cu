@@ -3,10 +3,11 @@
 // A row is read once: its values stay in registers between the maximum and the divisions.  The call is a stream (2 or 4 bytes in
 // and one out per value), bound by HBM for many rows and by latency for one.
 //
-// The division is that of the definition, rounded to nearest in 32 bits, and a code is its rounded quotient; a multiply by the
-// reciprocal differs next to the halves between two codes.  So a thread multiplies first and divides only where that leaves the code
-// open, in one value of some ten thousand.  4096 x 16384 bf16 values: 85 us with a division each and the row read twice, 60 with the
-// row in registers, 44 to 47 now (4.5 TB/s), about 16 instructions per value, which bound it; as fp32 53 us (6.3 TB/s, as fast as a copy).
+// The division is that of the definition, rounded to nearest in 32 bits, and a code is its rounded quotient.  It is done by the scale's
+// reciprocal and two corrections, by instructions that take two values, without a branch: between bf16 values exact halves are so frequent
+// that a test for open codes found one in every second warp.  4096 x 16384 bf16 values: 85 us with a library division each and the row
+// read twice, 60 with the row in registers, 44 by a rounded product and a division where that left a code open, 38 to 39 now (5.2 TB/s), about
+// 11 instructions per value at 62 % of the issue rate; as fp32 53 us (6.3 TB/s, as fast as a copy).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -43,18 +44,34 @@ __device__ __forceinline__ uint32_t quantize_exactly(float v, float scale, float
     const float q = __fdiv_rn(v, scale);
     return q != q ? 0u : (uint32_t)__float2int_rn(fminf(fmaxf(q, lo), hi)) & 255u;
 }
-// The same by the rounded reciprocal of the scale, for a finite row and a normal scale; `distance`: of the product from the whole number
-// next to it.  The reciprocal and the product are off by half a step each, so the product is within 2^-22.9 of
-// the quotient, relative, and the quotient's own rounding adds 2^-24: below 256 the two differ by less than 2^-14.4.  Where
-// the distance is below 1/2 - 2^-14, both round to the same code.  Adding 1.5 * 2^23 rounds to nearest, ties to even, and leaves the
-// code in the low byte.  Bounds are needed below zero for unsigned codes alone: no product is above hi (1 + 2^-22) in magnitude.
-template <bool SIGNED>
-__device__ __forceinline__ uint32_t quantize_quickly(float v, float inverse, float *distance) {
-    const float p = __fmul_rn(v, inverse), q = SIGNED ? p : fmaxf(p, 0.f), lifted = q + 12582912.f;
-    *distance = fabsf(q - (lifted - 12582912.f));
-    return __float_as_uint(lifted);
+// The same by the rounded reciprocal, two values at a time, for a finite row and a scale in the range that RowScale names.  Two steps
+// after Markstein (Computation of elementary functions on the IBM RISC System/6000 processor, 1990): q' = q + (v - q s) / s, with the
+// remainder by a fused multiply-add and 1 / s by its rounded value y.  The product v y is within 1.5 steps of v / s; after the first step
+// q is off by at most 1/2 + 2^-22 steps u, its remainder is exact, and the second rounds v / s + e with |e| <= (1/2 + 2^-22) u s |1/s - y|.
+// For s in [1, 2) that is below (1/2 + 2^-22) u s 2^-25, while v / s, a quotient of 24-bit numbers, lies at least u 2^-24 / s from any
+// point between two floats: the same rounding for s^2 (1/2 + 2^-22) < 2, that is for all but the last few mantissas.
+// Adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves the code in the low byte.  Bounds are needed below zero
+// for unsigned codes alone: the largest value's quotient rounds to hi or to a float next to it.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
 }
-constexpr float kOpen = 0.5f - 0x1p-14f;
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+template <bool SIGNED>
+__device__ __forceinline__ void quantize_two(float v0, float v1, uint64_t minus_scale, uint64_t inverse, uint32_t &o0, uint32_t &o1) {
+    const uint64_t v = SIGNED ? pair(v0, v1) : pair(fmaxf(v0, 0.f), fmaxf(v1, 0.f));
+    uint64_t q, lifted;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(v), "l"(inverse));
+    q = fma_pair(fma_pair(q, minus_scale, v), inverse, q);
+    q = fma_pair(fma_pair(q, minus_scale, v), inverse, q);
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(lifted) : "l"(q), "l"(pair(12582912.f, 12582912.f)));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(o0), "=r"(o1) : "l"(lifted));
+}
 
 // A row's scale, and how its codes are found.
 struct RowScale {
@@ -65,7 +82,8 @@ struct RowScale {
         inverse = __frcp_rn(scale);
         lo = (float)p.lo;
         hi = (float)p.hi;
-        quick = scale >= 0x1p-120f && scale <= 0x1p120f;
+        // remainders far from underflow, and a mantissa at least sixteen steps below 2
+        quick = scale >= 0x1p-64f && scale <= 0x1p64f && (__float_as_uint(scale) & 0x7FFFF0u) != 0x7FFFF0u;
     }
 };
 
@@ -159,19 +177,15 @@ __global__ void __launch_bounds__(512, VECS >= 4 && sizeof(T) == 4 ? 1 : 2) quan
     top = row_max(top, p.threads, part);
     const RowScale by(top, p);
     if (at == 0) p.scale[row] = by.scale;
+    const uint64_t minus_scale = pair(-by.scale, -by.scale), inverse = pair(by.inverse, by.inverse);
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
         const int j = at + i * p.threads, k0 = j * 8 - lead;
         uint32_t o[8];
-        float open = by.quick ? 0.f : 1.f;
+        if (by.quick) {
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            float d0, d1;
-            o[k] = quantize_quickly<SIGNED>(value(i, k), by.inverse, &d0);
-            o[k + 1] = quantize_quickly<SIGNED>(value(i, k + 1), by.inverse, &d1);
-            open = fmaxf(fmaxf(d0, d1), open);
-        }
-        if (open >= kOpen) {                            // rare, about one time in thirty for a warp
+            for (int k = 0; k < 8; k += 2) quantize_two<SIGNED>(value(i, k), value(i, k + 1), minus_scale, inverse, o[k], o[k + 1]);
+        } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) o[k] = quantize_exactly(value(i, k), by.scale, by.lo, by.hi);
         }
@@ -218,11 +232,12 @@ __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeParam
     top = row_max(top, p.threads, part);
     const RowScale by(top, p);
     if (threadIdx.x == 0) p.scale[row] = by.scale;
+    const uint64_t minus_scale = pair(-by.scale, -by.scale), inverse = pair(by.inverse, by.inverse);
     for (int k = threadIdx.x; k < p.K; k += p.threads) {
         const float a = quantize_float(load_ordered(x + k));
-        float distance;
-        uint32_t c = quantize_quickly<SIGNED>(a, by.inverse, &distance);
-        if (!by.quick || distance >= kOpen) c = quantize_exactly(a, by.scale, by.lo, by.hi);
+        uint32_t c, none;
+        if (by.quick) quantize_two<SIGNED>(a, 0.f, minus_scale, inverse, c, none);
+        else c = quantize_exactly(a, by.scale, by.lo, by.hi);
         codes[k] = (int8_t)c;
     }
 }

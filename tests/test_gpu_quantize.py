@@ -61,6 +61,26 @@ def test_ties_to_even(dtype):
     check(x.abs() + x.abs(), 8, False)
 
 
+@pytest.mark.parametrize("repeat", [1, 34])             # 34: rows longer than the registers hold
+@pytest.mark.parametrize("bits,signed", WIDTHS)
+def test_quotients_next_to_halves(bits, signed, repeat):
+    """Values a few floats to either side of (n + 1/2) scale, for scales of many mantissas (those next to 1 and 2 among them) and sizes."""
+    rng = np.random.default_rng(bits)
+    hi = (1 << (bits - 1)) - 1 if signed else (1 << bits) - 1
+    mantissas = np.concatenate([np.arange(24), (1 << 23) - 1 - np.arange(24), rng.integers(0, 1 << 23, 200)])
+    exponents = np.concatenate([[0, -64, 63, -63, 64, -100, 110], rng.integers(-60, 60, len(mantissas) - 7)])
+    scale = (np.ldexp(1.0 + mantissas / 2.0**23, rng.permutation(exponents))).astype(np.float32)
+    top = (scale.astype(np.float64) * hi).astype(np.float32)
+    scale = (top / np.float32(hi)).astype(np.float32)               # the definition's, which need not be the one wished for
+    n = rng.integers(0, hi, (len(scale), 997)) + 0.5
+    x = (n * scale[:, None].astype(np.float64)).astype(np.float32)
+    x = (x.view(np.int32) + rng.integers(-3, 4, x.shape, dtype=np.int32)).view(np.float32)
+    x *= rng.choice(np.float32([-1, 1]), x.shape) if signed else np.float32(1)
+    x = np.minimum(np.maximum(x, -top[:, None]), top[:, None])
+    x[:, 0] = top
+    check(torch.from_numpy(np.tile(x, (1, repeat))).cuda(), bits, signed)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_rows_apart_and_rows_that_are_one(dtype):
     g = torch.Generator().manual_seed(5)
