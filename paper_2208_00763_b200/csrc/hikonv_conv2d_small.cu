@@ -13,6 +13,7 @@
 // (The layers of the compact CNN run in two launches for one image, too.)
 #include <type_traits>
 
+#include "hikonv_cluster.cuh"
 #include "hikonv_cuda.cuh"
 #include "hikonv_conv2d_small.h"
 #include "hikonv_conv2d_util.cuh"

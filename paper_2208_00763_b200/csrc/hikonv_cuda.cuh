@@ -196,9 +196,4 @@ __device__ __forceinline__ bool mbarrier_wait(uint32_t bar, uint32_t parity, lon
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
-// Cluster barriers.  Not the .aligned forms: those want all threads of a warp at the instruction together, and the code in front of them
-// has branches that the threads of a warp take apart.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-
 }  // namespace hikonv

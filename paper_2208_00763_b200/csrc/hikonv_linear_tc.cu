@@ -25,6 +25,7 @@
 #include <cstddef>
 #include <cstring>
 
+#include "hikonv_cluster.cuh"
 #include "hikonv_linear_util.cuh"
 
 namespace hikonv {
