@@ -214,6 +214,45 @@ __device__ __forceinline__ Tile find_tc_tile(const TcParams &q, const GroupTable
     return r;
 }
 
+// Row ranges that overlap, which only offsets that decrease somewhere make, to ranges that do not, by one warp.  The grid, the stages
+// and the shared depth (one tile per cluster) count on no more tiles than disjoint ranges of M rows have.  From the front, the rows go
+// to the group that holds the next one and reaches furthest, up to its end: each group has one stretch at most, a row that any group
+// claims has one group, and a row that just one claims has that one.
+__device__ __forceinline__ void separate_groups(int2 *rows, int E) {
+    const int lane = threadIdx.x & 31;
+    for (int at = 0;;) {
+        int reach = at, best = 0x7FFFFFFF, next = 0x7FFFFFFF;
+        for (int e = lane; e < E; e += 32) {
+            const int2 r = rows[e];
+            if (r.x == r.y || r.y <= at) continue;
+            if (r.x > at) {
+                next = min(next, r.x);
+            } else if (r.y > reach) {
+                reach = r.y;
+                best = e;
+            }
+        }
+        __syncwarp();
+        const int to = __reduce_max_sync(0xFFFFFFFFu, reach);
+        if (to > at) {
+            best = __reduce_min_sync(0xFFFFFFFFu, reach == to ? best : 0x7FFFFFFF);
+            if (lane == 0) rows[best].x = ~at;         // taken: below zero until all are
+            __syncwarp();
+            at = to;
+        } else {
+            at = __reduce_min_sync(0xFFFFFFFFu, next);
+            if (at == 0x7FFFFFFF) break;
+        }
+    }
+    for (int e = lane; e < E; e += 32) {
+        int2 r = rows[e];
+        if (r.x < 0) r.x = ~r.x;
+        else r.y = r.x;
+        rows[e] = r;
+    }
+    __syncwarp();
+}
+
 __device__ __forceinline__ bool wait_all_of(const TcParams &q, uint32_t bar, uint32_t parity) {
     return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
@@ -583,14 +622,21 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
     int tiles = q.m_tiles * q.n_blocks;
     if (p.offsets) {
         grid_dependency_wait();
+        int decreasing = 0;
         for (int e = tid; e < p.E; e += blockDim.x) {
             const int2 r = group_rows(p, e);
             group_row[e] = r;
+            decreasing |= load_ordered(p.offsets + e + 1) < load_ordered(p.offsets + e);
             group_tiles[e] = ((r.y - r.x + q.nt - 1) / q.nt) * q.n_blocks;
         }
-        __syncthreads();
+        if (__syncthreads_or(decreasing)) {
+            if (warp == 0) separate_groups(group_row, p.E);
+            __syncthreads();
+            for (int e = tid; e < p.E; e += blockDim.x) group_tiles[e] = ((group_row[e].y - group_row[e].x + q.nt - 1) / q.nt) * q.n_blocks;
+            __syncthreads();
+        }
         if (warp == 0) {
-            // in 64 bits, and no more than an index holds: groups that overlap, which only wrong offsets make, may have any number
+            // no more in all than the host counted; as 32-bit sums they cost the kernel a spilled register
             long long before = 0;
             for (int e0 = 0; e0 < p.E; e0 += 32) {
                 long long upto = e0 + lane < p.E ? group_tiles[e0 + lane] : 0;
@@ -599,7 +645,7 @@ __global__ void __launch_bounds__(kTcThreads<MODE>, 1)
                     const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
                     if (lane >= d) upto += v;
                 }
-                if (e0 + lane < p.E) group_tiles[e0 + lane] = (int)min(before + upto, 0x3FFFFFFFll);
+                if (e0 + lane < p.E) group_tiles[e0 + lane] = (int)(before + upto);
                 before += __shfl_sync(0xFFFFFFFFu, upto, 31);
             }
         }
@@ -920,6 +966,7 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
         q.a_column = 2 * q.acc_cols;
         q.a_slots = (512 - q.a_column) / (32 * q.atoms);
         if (q.a_slots > 6) q.a_slots = 6;
+        if (q.a_slots > q.stages) q.a_slots = q.stages;      // as many of their barriers are there as of the stages'
         if (q.a_slots < 1) return HIKONV_ERR_UNSUPPORTED;
     }
     q.tmem_cols = 32;
@@ -929,13 +976,10 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
     // Teams of at least four warps, since a warp reaches a quarter of the lanes of tensor memory only.  A team that waits for the parity of
     // a barrier must know that the use before the last is over, or it takes an older use for its own.  Of slot s for stage n: the team saw
     // the multiplies of stage n - 3 - a_slots end, which are not before those of n - 2 a_slots if there are three slots.  Of stage n's
-    // copies, after that: all multiplies up to stage n - a_slots are over, so the copies of n - stages have landed if there are no
+    // copies, after that: all multiplies up to stage n - a_slots are over, so the copies of n - stages have landed, since there are no
     // fewer stages than slots.
     q.teams = 1;
-    if (apart && q.units == 4 && q.stages >= 3 && q.a_slots >= 3) {
-        q.teams = 3;
-        if (q.a_slots > q.stages) q.a_slots = q.stages;
-    }
+    if (apart && q.units == 4 && q.stages >= 3 && q.a_slots >= 3) q.teams = 3;
     // accumulators of signed operands: format 2 (int32), types 1 (signed) or 0 (unsigned) of both, 128 rows; the columns follow per tile
     q.idesc = (2u << 4) | ((as_unsigned ? 0u : 1u) << 7) | ((as_unsigned ? 0u : 1u) << 10) | ((uint32_t)(kTcRows >> 4) << 24);
     q.wait_cycles = kWaitCycles;

@@ -1,0 +1,51 @@
+"""GPU parity of the linear layers at the ends of what their documentation allows."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import linear as ol
+from paper_2208_00763_b200 import binding as hk
+from test_gpu_linear import draw, rows_on_device, weights_on_device
+
+pytestmark = pytest.mark.gpu
+
+
+def _claims(offsets, T):
+    """The groups that claim each row: bounds outside 0 .. T are the nearest one, groups that end before they begin are empty."""
+    b = np.clip(np.asarray(offsets, dtype=np.int64), 0, T)
+    return [[e for e in range(len(b) - 1) if b[e] <= m < b[e + 1]] for m in range(T)]
+
+
+WRONG = {
+    "two alternate": [0, 64, 300, 64, 300, 64, 300, 64, 300],
+    "one holds all": [0, 300, 10, 20, 40, 50, 290, 299, 300],
+    "the last holds all": [250, 260, 100, 130, 20, 60, 50, 0, 300],
+    "out of bounds": [-5, 200, 2 ** 31 - 1, 100, 150, -2 ** 31, 250, 90, 400],
+    "random": np.random.default_rng(3).integers(-40, 340, 41).tolist(),
+}
+
+
+# an 8-bit layer deep enough that clusters share its tiles, dense ones of one and of many steps, flipped activations, and a few rows
+@pytest.mark.parametrize("name", list(WRONG))
+@pytest.mark.parametrize("T,K,N,q,xs,store", [(300, 4096, 128, 8, True, 8), (300, 128, 128, 4, True, 4), (300, 1024, 200, 4, False, 4),
+                                              (300, 640, 130, 8, False, 8), (30, 256, 70, 4, True, 4)])
+def test_offsets_that_decrease_spoil_no_row_of_one_group(name, T, K, N, q, xs, store):
+    offsets = WRONG[name]
+    E = len(offsets) - 1
+    x, w = draw((T, K), (E, N, K), 8, q, xs, True, seed=T + K)
+    buf = torch.full((T + 2, N), 123456789, dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        hk.grouped_linear(rows_on_device(x), weights_on_device(w, store), torch.tensor(offsets, dtype=torch.int32, device="cuda"), 8, q, xs, True,
+                          w_store_bits=store, out=buf[1:T + 1])
+    torch.cuda.synchronize()
+    assert hk.linear_wait_timeouts() == 0
+    got = buf.cpu().numpy().astype(np.int64)
+    assert (got[[0, T + 1]] == 123456789).all()
+    every = [ol.sums(x, w[e]) for e in range(E)]
+    for m, groups in enumerate(_claims(offsets, T)):
+        if not groups:
+            assert (got[m + 1] == 123456789).all(), m
+        elif len(groups) == 1:
+            assert np.array_equal(got[m + 1], every[groups[0]][m]), m
+        else:                                            # one of the groups that claim it, value by value
+            assert (np.stack([every[e][m] for e in groups]) == got[m + 1]).any(axis=0).all(), m
