@@ -881,6 +881,8 @@ static int unpacked_atoms(int nt, int ones, int w_bits) {
         if ((512 - 2 * acc) / (32 * atoms) >= 3 && 3 * atoms * (int)align_up(bytes, 1024) <= (int)kTcMostSmem - 16 * 1024) return atoms;
     return 1;
 }
+// Steps of a depth, which may be anything up to 2^31 - 1.
+static int depth_steps(int K) { return (K - 1) / kTcDepth + 1; }
 // Rows of x per tile and CTAs per tile that a model of the time, in cycles, likes best.  A step of 128 codes costs the longest of its
 // multiplies (2 per row), its way from the second-level cache (70 bytes per cycle and SM) and the helpers' work on it; a tile alone on its
 // SM costs 3000 for the set-up and the end of its epilogue; one with a shared depth two barriers of the cluster, which are dearer the
@@ -888,7 +890,7 @@ static int unpacked_atoms(int nt, int ones, int w_bits) {
 // Against measured times of 4096 x 4096 with 64 and 256 rows, 8192 x 8192 with 48: 16.3, 16.3 and 18.7 thousand cycles for 15.2, 16.7
 // and 18.9, and the order of the shapes tried is the measured one.
 static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int *nt_out, int *splits_out) {
-    const int n_blocks = ceil_div(p.N, kTcRows), chunks = ceil_div(p.K, kTcDepth);
+    const int n_blocks = ceil_div(p.N, kTcRows), chunks = depth_steps(p.K);
     // unpacked weights take tensor memory from the accumulators
     const int most = mode == kTransform && p.w_bits < 8 ? 192 : ones ? 240 : 256;
     double best = 1e300;
@@ -937,7 +939,7 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
     // units that unpack weights fall to the warps of their lanes: their number per step is a multiple of four
     q.units = (p.w_bits < 8 || q.flip_w ? kTcRows / kUnitRows : 0) + (q.flip ? ceil_div(q.nt, kUnitRows) : 0);
     if (mode == kTransform && p.w_bits < 8) q.units = (int)align_up(q.units, 4);
-    q.chunks = ceil_div(p.K, kTcDepth);
+    q.chunks = depth_steps(p.K);
     q.n_blocks = ceil_div(p.N, kTcRows);
     q.m_tiles = ceil_div(p.M, q.nt);
     q.tokens_first = p.offsets || (long long)p.M * p.K <= (long long)p.N * p.w_row;

@@ -49,3 +49,23 @@ def test_offsets_that_decrease_spoil_no_row_of_one_group(name, T, K, N, q, xs, s
             assert np.array_equal(got[m + 1], every[groups[0]][m]), m
         else:                                            # one of the groups that claim it, value by value
             assert (np.stack([every[e][m] for e in groups]) == got[m + 1]).any(axis=0).all(), m
+
+
+@pytest.mark.parametrize("store", [8, 1])
+def test_the_largest_depths(store):
+    # one-bit codes: the last multiple of 16 below 2^31, whose steps do not fit a rounded-up count
+    M, N, K = 2, 2, 2 ** 31 - 16
+    x = torch.randint(0, 2, (M, K), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(store))
+    w = torch.randint(0, 2, (N, K), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(9))
+    x[1], w[1] = 1, 1                                    # the largest sum
+    stored = w
+    if store == 1:
+        stored = torch.zeros((N, K // 8), dtype=torch.uint8, device="cuda")
+        for i in range(8):
+            stored |= w[:, i::8] << i
+    got = hk.linear(x, stored, 1, 1, False, False, w_store_bits=store)
+    part = 1 << 26
+    want = torch.stack([torch.stack([sum((x[m, k:k + part] & w[n, k:k + part]).sum(dtype=torch.int64) for k in range(0, K, part))
+                                     for n in range(N)]) for m in range(M)])
+    assert torch.equal(got.to(torch.int64), want) and want[1, 1] == K
+    assert hk.linear_wait_timeouts() == 0
