@@ -222,10 +222,11 @@ __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeParam
     grid_dependency_release();
     grid_dependency_wait();
     const int row = blockIdx.x;
+    const uint32_t K = p.K;                             // unsigned: up to a CTA's threads beyond 2^31 - 1
     const T *x = (const T *)p.x + row * p.x_row;
     int8_t *codes = p.codes + (size_t)row * p.K;
     float top = 0.f;
-    for (int k = threadIdx.x; k < p.K; k += p.threads) {
+    for (uint32_t k = threadIdx.x; k < K; k += p.threads) {
         const float a = quantize_float(load_ordered(x + k));
         top = max_nan(top, SIGNED ? fabsf(a) : a);
     }
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeParam
     const RowScale by(top, p);
     if (threadIdx.x == 0) p.scale[row] = by.scale;
     const uint64_t minus_scale = pair(-by.scale, -by.scale), inverse = pair(by.inverse, by.inverse);
-    for (int k = threadIdx.x; k < p.K; k += p.threads) {
+    for (uint32_t k = threadIdx.x; k < K; k += p.threads) {
         const float a = quantize_float(load_ordered(x + k));
         uint32_t c, none;
         if (by.quick) quantize_two<SIGNED>(a, 0.f, minus_scale, inverse, c, none);
@@ -250,7 +251,7 @@ static int launch_pieces(QuantizeParams p, cudaStream_t st) {
     if (pieces <= 64) {
         p.threads = 32;
         const int warps = p.M >= sm_count_here() * 8 ? 8 : 1;
-        const dim3 grid((unsigned)ceil_div(p.M, warps)), block((unsigned)(warps * 32));
+        const dim3 grid((unsigned)((p.M - 1) / warps + 1)), block((unsigned)(warps * 32));
         return pieces <= 32 ? launch_dependent(quantize_pieces_kernel<T, 1, SIGNED, ALIGNED>, grid, block, 0, st, p)
                             : launch_dependent(quantize_pieces_kernel<T, 2, SIGNED, ALIGNED>, grid, block, 0, st, p);
     }

@@ -69,3 +69,30 @@ def test_the_largest_depths(store):
                                      for n in range(N)]) for m in range(M)])
     assert torch.equal(got.to(torch.int64), want) and want[1, 1] == K
     assert hk.linear_wait_timeouts() == 0
+
+
+def _quantized_as_defined(x, codes, scale, part=1 << 26):
+    """Signed 8-bit codes and scales of the rows of x against the definition, by parts; divisions by tensors on the device are IEEE's."""
+    M, K = x.shape
+    hi = torch.tensor(127.0, device="cuda")
+    if K == 1:
+        for m in range(0, M, part):
+            v = x[m:m + part, 0].float()
+            assert torch.equal(scale[m:m + part], v.abs() / hi)
+            want = torch.where(v == 0, torch.zeros_like(v), v / scale[m:m + part]).round()
+            assert torch.equal(codes[m:m + part, 0].float(), want)
+    else:
+        for m in range(M):
+            top = max(x[m, k:k + part].abs().max().item() for k in range(0, K, part))
+            assert scale[m] == torch.tensor(top, device="cuda") / hi
+            for k in range(0, K, part):
+                assert torch.equal(codes[m, k:k + part].float(), (x[m, k:k + part].float() / scale[m]).round())
+
+
+@pytest.mark.parametrize("M,K", [(1, 2 ** 31 - 1), (2 ** 31 - 1, 1), (2 ** 31 - 7, 1)])
+def test_the_longest_and_the_most_rows_to_quantise(M, K):
+    x = torch.empty((M, K), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    x[-1, -1] = 9.5                                      # the last value counts
+    codes, scale = hk.quantize_rows(x, 8)
+    _quantized_as_defined(x, codes, scale)
+    assert codes[-1, -1] == 127
