@@ -43,7 +43,7 @@ def floats(s, x_scale=None, w_scale=None, bias=None, act=NONE, residual=None):
 
     The sum becomes a float (half a step), is multiplied by x_scale (half a step) and goes with w_scale and bias into one fused
     multiply-add (half a step of its result): 2 U |product| + U |v|.  The activations' slopes stay below 1.13.  SILU adds an
-    exponential of 2 ulp, a sum and a quotient of 2 ulp: (4 + 1 + 4) U relative.  GELU: its argument is off by two half steps, where
+    exponential of 2 ulp, a product, a sum and a quotient rounded to nearest: (4 + 1 + 1 + 1) U relative.  GELU: its argument is off by two half steps, where
     the slope of erf times the argument is below 0.5, erf by 2 ulp of at most 1, the sum by U of at most 2, then two products:
     (1 + 4 + 2) U |v| / 2 + 2 U |value|.  The residual's sum adds U |result|."""
     prod = np.asarray(s, dtype=np.float64)
@@ -55,7 +55,7 @@ def floats(s, x_scale=None, w_scale=None, bias=None, act=NONE, residual=None):
     y = _activate(v, act)
     bound = 1.13 * (2 * U32 * np.abs(prod) + U32 * np.abs(v))
     if act == SILU:
-        bound = bound + 9 * U32 * np.abs(y)
+        bound = bound + 7 * U32 * np.abs(y)
     elif act == GELU:
         bound = bound + 3.5 * U32 * np.abs(v) + 2 * U32 * np.abs(y)
     if residual is not None:

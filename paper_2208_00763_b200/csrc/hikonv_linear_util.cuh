@@ -80,9 +80,20 @@ __device__ __forceinline__ void from_float(float v, float *o) { *o = v; }
 __device__ __forceinline__ void from_float(float v, __half *o) { *o = __float2half_rn(v); }
 __device__ __forceinline__ void from_float(float v, __nv_bfloat16 *o) { *o = __float2bfloat16_rn(v); }
 
+// v / (1 + exp(-v)), for v < 0 as v exp(v) / (1 + exp(v)): no exponential overflows, so results down to the smallest normal numbers (v near
+// -91.8) keep their bits.  The divisor d lies in [1, 2], so the quotient q of the approximate reciprocal (within 2^-23) needs one step after
+// Markstein, q + (a - q d) / d, to be within 2^-20 of a step of the rounded one; a library division, whose code for other divisors would
+// be called, spilled registers of the tiled kernel.  Where exp(-|v|) is 0, the step is left out: it would make infinity a NaN.
+__device__ __forceinline__ float silu(float v) {
+    const float t = expf(-fabsf(v)), d = 1.f + t, a = v < 0.f ? v * t : v;
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    const float q = a * r;
+    return t == 0.f ? a : fmaf(fmaf(-q, d, a), r, q);
+}
 __device__ __forceinline__ float activate(float v, int act) {
     if (act == HIKONV_ACT_RELU) return v < 0.f ? 0.f : v;                      // a NaN stays
-    if (act == HIKONV_ACT_SILU) return __fdividef(v, 1.f + expf(-v));
+    if (act == HIKONV_ACT_SILU) return silu(v);
     if (act == HIKONV_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
     return v;
 }

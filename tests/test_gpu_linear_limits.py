@@ -96,3 +96,31 @@ def test_the_longest_and_the_most_rows_to_quantise(M, K):
     codes, scale = hk.quantize_rows(x, 8)
     _quantized_as_defined(x, codes, scale)
     assert codes[-1, -1] == 127
+
+
+@pytest.mark.parametrize("M", [3, 12, 40, 700])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_silu_over_its_whole_range(M, dtype):
+    """Sums of zero, so that the activation's argument is the bias, exactly.  exp(-|v|) is off by 2 steps, 4 U (U = 2^-24) of its value, which
+    v < 0 passes on to the result once at most; a product, a sum and a quotient (half a step and 2^-20 of one) add U each: 7 U.  Where the exponential is
+    subnormal (v below -87.3) its steps are 2^-149, times |v|; the product's and the quotient's are half of one such step each."""
+    K = 64
+    v = torch.cat([torch.linspace(-112, -84, 2001), torch.linspace(-84, 112, 1500), torch.tensor([0.0, -0.0, 1e-40, -1e-40, 3e38, -3e38, float("inf")])])
+    N = len(v)
+    w = torch.ones((N, K), dtype=torch.int8, device="cuda")
+    got = hk.linear(torch.zeros((M, K), dtype=torch.int8, device="cuda"), w, 8, 8, True, True, bias=v.cuda(), activation=hk.ACT_SILU, out_dtype=dtype)
+    y = got.cpu().double()
+    assert torch.equal(y, y[:1].expand_as(y))            # all rows alike, bit for bit but for signs of zero
+    exact = v.double()
+    exact = torch.where(exact < -700, torch.zeros_like(exact), exact / (1 + torch.exp(-exact.clamp(min=-700))))
+    u = 2.0 ** -24
+    tol = 1.01 * 7 * u * exact.abs() + (2 * v.double().abs().clamp(max=112) + 1) * 2.0 ** -149
+    info = torch.finfo(dtype)
+    if dtype != torch.float32:
+        tol = tol + info.eps / 2 * (exact.abs() + tol) + info.smallest_normal * info.eps / 2
+    over = exact.abs() >= info.max                       # the infinite one, and for float16 what exceeds it
+    assert torch.equal(y[0][over], torch.full_like(y[0][over], float("inf")))
+    err = (y[0] - exact).abs()
+    assert (err[~over] <= tol[~over]).all(), [(v[i].item(), y[0][i].item(), exact[i].item()) for i in torch.nonzero(~over & (err > tol))[:3, 0]]
+    normal = ~over & (exact.abs() >= info.smallest_normal)
+    assert (y[0][normal] != 0).all()                     # no normal result is lost
