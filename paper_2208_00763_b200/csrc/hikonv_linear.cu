@@ -56,10 +56,6 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
         overlap(d_out, out_bytes, ep->d_residual, ((size_t)(M - 1) * res_row + N) * elem))
         return HIKONV_ERR_INVALID_ARG;
 
-    if (overlap(workspace, workspace_bytes, d_out, out_bytes) || overlap(workspace, workspace_bytes, d_x, (size_t)(M - 1) * x_row + K) ||
-        overlap(workspace, workspace_bytes, d_w, (size_t)E * N * w_row))
-        return HIKONV_ERR_INVALID_ARG;
-
     LinearParams k;
     memset(&k, 0, sizeof(k));
     k.x = (const uint8_t *)d_x; k.w = (const uint8_t *)d_w; k.offsets = d_offsets;
@@ -75,8 +71,15 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
     k.out_row = out_row; k.res_row = res_row;
     k.shift = ep->shift; k.lo = ep->lo; k.hi = ep->hi;
     const int rows = grouped ? ceil_div(M, E) : M;               // of a group, on average
-    return linear_rows_takes(k, rows) ? launch_linear_rows(k, (cudaStream_t)stream)
-                                      : launch_linear_tc(k, workspace, workspace_bytes, (cudaStream_t)stream);
+    if (linear_rows_takes(k, rows)) return launch_linear_rows(k, (cudaStream_t)stream);
+    // the copied rows lie over nothing that is read or written
+    const size_t need = linear_tc_workspace(k);
+    const struct { const void *at; size_t bytes; } operands[] = {
+        {d_x, (size_t)(M - 1) * x_row + K}, {d_w, (size_t)E * N * w_row}, {d_out, out_bytes}, {d_offsets, ((size_t)E + 1) * 4},
+        {ep->d_x_scale, (size_t)M * 4}, {ep->d_w_scale, columns}, {ep->d_bias, columns}, {ep->d_residual, ((size_t)(M - 1) * res_row + N) * elem}};
+    for (const auto &o : operands)
+        if (overlap(workspace, need, o.at, o.bytes)) return HIKONV_ERR_INVALID_ARG;
+    return launch_linear_tc(k, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 }  // namespace hikonv

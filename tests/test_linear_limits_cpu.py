@@ -7,6 +7,7 @@ import pytest
 
 from paper_2208_00763_b200 import binding as hk
 from paper_2208_00763_b200 import build as lib_build
+from test_linear_cpu import BIAS, F, OFF, OUT, RES, SCALE, SCALE2, W, X, call, space
 
 TESTS = os.path.dirname(os.path.abspath(__file__))
 
@@ -36,3 +37,33 @@ for K in %s:
         print(call(**a), call(grouped=True, E=1, offsets=1 << 41, **a), call(**{**a, 'M': 1, 'N': 1}), flush=True)
 """ % depths)
     assert made == [str(hk.ERR_CUDA)] * 3 * (len(depths) + sum(K % 8 == 0 for K in depths))
+
+
+def test_the_workspace_overlaps_no_operand():
+    # a layer whose rows are copied; every operand that the kernels still read or write after the copy, its first and its last byte
+    M, N, K, E = 100, 32, 60, 3
+    ep = dict(F, d_x_scale=SCALE, d_w_scale=SCALE2, d_bias=BIAS, d_residual=RES, residual_row_stride=40)
+    for grouped in (False, True):
+        columns = N * (E if grouped else 1)
+        big = dict(M=M, N=N, K=K, x_row=60, ep=ep)
+        need = M * 64 + columns * 64
+        assert space(**big, E=E if grouped else 0) == need
+        ends = [(SCALE, M * 4), (SCALE2, columns * 4), (BIAS, columns * 4), (RES, (M - 1) * 80 + N * 2), (X, (M - 1) * 60 + K), (W, columns * K),
+                (OUT, (M - 1) * 64 + N * 2)] + ([(OFF, (E + 1) * 4)] if grouped else [])
+        for at, size in ends:
+            first_behind = -(-(at + size) // 16) * 16
+            for ptr in (at - need + 16, at, first_behind - 16):
+                assert call(grouped=grouped, E=E, **big, ws_ptr=ptr, ws_bytes=need) == hk.ERR_INVALID_ARG, (grouped, hex(at), hex(ptr))
+
+
+def test_a_workspace_behind_or_beside_what_is_used_is_fine():
+    M, N, K = 100, 32, 60
+    ep = dict(F, d_x_scale=SCALE, d_bias=BIAS)
+    need = M * 64 + N * 64
+    # next to an operand; with an operand behind the bytes that the call needs; and none of it needed
+    made = without_devices("""
+ep = dict(F, d_x_scale=SCALE, d_bias=BIAS)
+big = dict(M=%d, N=%d, K=%d, x_row=60, ep=ep)
+print(call(**big, ws_ptr=SCALE - %d, ws_bytes=%d), call(**big, ws_ptr=SCALE - %d, ws_bytes=1 << 30), call(ep=ep, ws_ptr=SCALE, ws_bytes=1 << 20))
+""" % (M, N, K, need, need, need))
+    assert made == [str(hk.ERR_CUDA)] * 3
