@@ -601,12 +601,12 @@ def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, p: i
 
 def _linear(name, x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual, requant, out_dtype,
             out, workspace, stream):
-    if stream is None:
+    grouped = name == "hikonv_grouped_linear"
+    if stream is None and grouped == (offsets is not None):
         done = (_fast or _load_fast()).linear(x, w, offsets, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation,
                                               residual, requant, out_dtype, out, workspace)
         if done is not None:
             return done
-    grouped = name == "hikonv_grouped_linear"
     x_row = _rows(x, "x", _CODE_DTYPES)
     M, K = x.shape
     if not getattr(w, "is_cuda", False) or w.dtype not in _CODE_DTYPES or not w.is_contiguous() or w.dim() != (3 if grouped else 2):

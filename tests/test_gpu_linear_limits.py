@@ -124,3 +124,13 @@ def test_silu_over_its_whole_range(M, dtype):
     assert (err[~over] <= tol[~over]).all(), [(v[i].item(), y[0][i].item(), exact[i].item()) for i in torch.nonzero(~over & (err > tol))[:3, 0]]
     normal = ~over & (exact.abs() >= info.smallest_normal)
     assert (y[0][normal] != 0).all()                     # no normal result is lost
+
+
+def test_groups_without_offsets_are_refused():
+    # whatever the weights' shape: a call by groups is never taken for a plain one
+    x = torch.zeros((4, 16), dtype=torch.int8, device="cuda")
+    for stream in (None, torch.cuda.current_stream()):
+        with pytest.raises(ValueError):
+            hk.grouped_linear(x, torch.zeros((8, 16), dtype=torch.int8, device="cuda"), None, 8, 8, True, True, stream=stream)
+        with pytest.raises(hk.HikonvError):
+            hk.grouped_linear(x, torch.zeros((1, 8, 16), dtype=torch.int8, device="cuda"), None, 8, 8, True, True, stream=stream)
