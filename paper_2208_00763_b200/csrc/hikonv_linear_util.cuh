@@ -80,16 +80,17 @@ __device__ __forceinline__ void from_float(float v, float *o) { *o = v; }
 __device__ __forceinline__ void from_float(float v, __half *o) { *o = __float2half_rn(v); }
 __device__ __forceinline__ void from_float(float v, __nv_bfloat16 *o) { *o = __float2bfloat16_rn(v); }
 
-// v / (1 + exp(-v)), for v < 0 as v exp(v) / (1 + exp(v)): no exponential overflows, so results down to the smallest normal numbers (v near
-// -91.8) keep their bits.  The divisor d lies in [1, 2], so the quotient q of the approximate reciprocal (within 2^-23) needs one step after
-// Markstein, q + (a - q d) / d, to be within 2^-20 of a step of the rounded one; a library division, whose code for other divisors would
-// be called, spilled registers of the tiled kernel.  Where exp(-|v|) is 0, the step is left out: it would make infinity a NaN.
+// v / (1 + exp(-v)), for v < 0 as v exp(v) / (1 + exp(v)): no exponential overflows, so results down to the smallest normal numbers (v
+// near -91.8) keep their bits.  The divisor d lies in [1, 2], so the quotient q of the approximate reciprocal (within 2^-23) needs one step after
+// Markstein, q + (a - q d) / d, to be within 2^-20 of a step of the rounded one.  The remainder of infinity is a NaN, which fminf drops.
+// 512 x 2048 x 4096 to fp32: 9.5 us, against 8.9 by an approximate division that loses results below v = -87.3 and 9.1 by the uncorrected
+// product with the reciprocal; a library division, whose code for other divisors is called, spilled 27 registers of the tiled kernel.
 __device__ __forceinline__ float silu(float v) {
     const float t = expf(-fabsf(v)), d = 1.f + t, a = v < 0.f ? v * t : v;
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
     const float q = a * r;
-    return t == 0.f ? a : fmaf(fmaf(-q, d, a), r, q);
+    return fmaf(fminf(fmaf(-q, d, a), 3e38f), r, q);
 }
 __device__ __forceinline__ float activate(float v, int act) {
     if (act == HIKONV_ACT_RELU) return v < 0.f ? 0.f : v;                      // a NaN stays
