@@ -488,7 +488,8 @@ int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, in
  * Depth: K max|x| W <= 2^31 - 1 with W = 128 for signed weights (dense ones are multiplied as the upper bits of a byte) and
  * 2^q - 1 for unsigned ones, else HIKONV_ERR_NO_FIT.
  * out must not overlap any input, except that it may be the residual itself (same address and stride), else
- * HIKONV_ERR_INVALID_ARG.  M == 0 launches nothing; N, K >= 1; M, N <= 2^30.
+ * HIKONV_ERR_INVALID_ARG.  x, residual and out may be columns of one buffer, their rows equally many bytes apart; with other strides the
+ * ranges from their first byte to their last must be apart.  M == 0 launches nothing; N, K >= 1; M, N <= 2^30.
  * Any alignment of codes is accepted.  Rows of x and w that start on 16-byte boundaries are read as they are; others may be copied to
  * such rows first, in d_workspace (16-byte aligned, hikonv_linear_workspace_bytes of it, which overlap no operand, else
  * HIKONV_ERR_INVALID_ARG; NULL where that is 0).  The bytes around a row that lie in the same 16 aligned bytes as part of it may be read,

@@ -134,3 +134,26 @@ def test_groups_without_offsets_are_refused():
             hk.grouped_linear(x, torch.zeros((8, 16), dtype=torch.int8, device="cuda"), None, 8, 8, True, True, stream=stream)
         with pytest.raises(hk.HikonvError):
             hk.grouped_linear(x, torch.zeros((1, 8, 16), dtype=torch.int8, device="cuda"), None, 8, 8, True, True, stream=stream)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 64, 40), (5, 64, 40), (14, 33, 70), (70, 512, 130), (300, 100, 257)])
+def test_columns_of_one_buffer(M, K, N):
+    x, w = draw((M, K), (N, K), 8, 8, True, True, seed=M)
+    s, dw = ol.sums(x, w), weights_on_device(w, 8)
+    # the output beside the residual, on either side, with room in front, between and behind
+    res = np.random.default_rng(M).integers(-1000, 1000, (M, N)).astype(np.float32)
+    for at_res, at_out in ((0, N), (N, 0), (3, N + 5), (N + 4, 1)):
+        buf = torch.full((M, 2 * N + 8), 7.0, device="cuda")
+        buf[:, at_res:at_res + N] = torch.from_numpy(res).cuda()
+        want = buf.clone()
+        want[:, at_out:at_out + N] = torch.from_numpy((s + res).astype(np.float32)).cuda()      # whole numbers below 2^24: exact
+        hk.linear(rows_on_device(x), dw, 8, 8, True, True, residual=buf[:, at_res:at_res + N], out=buf[:, at_out:at_out + N])
+        assert torch.equal(buf, want)
+    # codes beside the codes that they come from
+    for at_x, at_out in ((0, K), (N, 0), (5, K + 6), (N + 16, 3), (16, K + 16)):
+        buf = torch.full((M, K + N + 32), 5, dtype=torch.uint8, device="cuda")
+        buf[:, at_x:at_x + K] = torch.from_numpy(x.astype(np.uint8)).cuda()
+        want = buf.clone()
+        want[:, at_out:at_out + N] = torch.from_numpy(ol.codes(s, None, 9, 0, 255).astype(np.uint8)).cuda()
+        hk.linear(buf[:, at_x:at_x + K], dw, 8, 8, True, True, requant=(9, 0, 255), out=buf[:, at_out:at_out + N])
+        assert torch.equal(buf, want)

@@ -7,7 +7,7 @@ import pytest
 
 from paper_2208_00763_b200 import binding as hk
 from paper_2208_00763_b200 import build as lib_build
-from test_linear_cpu import BIAS, F, OFF, OUT, RES, SCALE, SCALE2, W, X, call, space
+from test_linear_cpu import BIAS, C, F, OFF, OUT, RES, SCALE, SCALE2, W, X, call, space
 
 TESTS = os.path.dirname(os.path.abspath(__file__))
 
@@ -66,4 +66,27 @@ ep = dict(F, d_x_scale=SCALE, d_bias=BIAS)
 big = dict(M=%d, N=%d, K=%d, x_row=60, ep=ep)
 print(call(**big, ws_ptr=SCALE - %d, ws_bytes=%d), call(**big, ws_ptr=SCALE - %d, ws_bytes=1 << 30), call(ep=ep, ws_ptr=SCALE, ws_bytes=1 << 20))
 """ % (M, N, K, need, need, need))
+    assert made == [str(hk.ERR_CUDA)] * 3
+
+
+def test_columns_of_one_buffer():
+    # bf16 rows of 64 bytes, 128 apart, four of them: the residual's lie between the output's, or in front or behind, or share a value
+    apart = [64, -64, 64 - 3 * 128, 64 + 2 * 128, 66 + 3 * 128, -66 - 3 * 128]
+    shared = [62, 66, -62, -66, 128, 66 - 3 * 128, 62 + 3 * 128]
+    for off in shared:
+        for grouped in (False, True):
+            assert call(grouped=grouped, out_row=64, ep=dict(F, d_residual=OUT + off, residual_row_stride=64)) == hk.ERR_INVALID_ARG, off
+    made = without_devices("for off in %s:\n"
+                           "    print(*(call(grouped=g, out_row=64, ep=dict(F, d_residual=OUT + off, residual_row_stride=64)) for g in (False, True)))" % apart)
+    assert made == [str(hk.ERR_CUDA)] * 2 * len(apart)
+
+
+def test_columns_of_one_buffer_with_other_strides():
+    # rows 128 and 130 bytes apart meet somewhere, or may
+    for off in (0, 64, -64):
+        assert call(out_row=64, ep=dict(F, d_residual=OUT + off, residual_row_stride=65)) == hk.ERR_INVALID_ARG
+    # codes next to the codes they come from: 64 bytes of x, 32 of out, 96 apart
+    for off in (63, -31, 65, 96, 0):
+        assert call(x_row=96, out=X + off, out_row=96, ep=dict(C, hi=1)) == hk.ERR_INVALID_ARG
+    made = without_devices("print(*(call(x_row=96, out=X + off, out_row=96, ep=dict(C, hi=1)) for off in (64, -32, 64 + 96)))")
     assert made == [str(hk.ERR_CUDA)] * 3
