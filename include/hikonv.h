@@ -446,7 +446,8 @@ int hikonv_pipe_rate(int kind, int iters, uint32_t *d_scratch_word, double *h_op
  *      are one); columns are contiguous, elements naturally aligned.
  *   signed:   scale[r] = max_k |x[r][k]| / (2^(bits-1) - 1), bits in 2..8
  *   unsigned: scale[r] = max(0, max_k x[r][k]) / (2^bits - 1), bits in 1..8
- *   codes[r][k] = clamp(round(x[r][k] / scale[r]), lo, hi), divisions in 32 bits, rounded to nearest, ties to even.
+ *   codes[r][k] = clamp(round(x[r][k] / scale[r]), lo, hi), divisions in 32 bits, rounded to nearest, ties to even; lo and hi are
+ *      the ends of the codes' range (signed codes meet the lower one, -2^(bits-1), only where the scale is subnormal and was rounded down)
  * Codes are stored one per byte, rows without gaps; scales are float.  A row of zeros (unsigned: without a positive value)
  * has scale 0 and codes 0.  A row with a NaN has scale NaN; a row whose largest magnitude is infinite has scale infinity; a
  * quotient that is NaN has code 0 (so what is computed from such a row is NaN, as 0 times its scale is).  Subnormal
@@ -463,8 +464,8 @@ typedef enum {
 typedef enum {
     HIKONV_ACT_NONE = 0,
     HIKONV_ACT_RELU = 1, /* max(v, 0)                         */
-    HIKONV_ACT_SILU = 2, /* v / (1 + exp(-v))                 */
-    HIKONV_ACT_GELU = 3  /* v (1 + erf(v / sqrt(2))) / 2      */
+    HIKONV_ACT_SILU = 2, /* v / (1 + exp(-v)); every normal result keeps its bits; NaN for -infinity */
+    HIKONV_ACT_GELU = 3  /* v (1 + erf(v / sqrt(2))) / 2 in just these steps: within 2^-22 |v|, also where the result is far smaller */
 } hikonv_activation;
 
 int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, int M, int K, int bits, int is_signed,
@@ -492,7 +493,8 @@ int hikonv_quantize_rows(const void *d_x, int x_type, long long x_row_stride, in
  * ranges from their first byte to their last must be apart.  M == 0 launches nothing; N, K >= 1; M, N <= 2^30.
  * Any alignment of codes is accepted.  Rows of x and w that start on 16-byte boundaries are read as they are; others may be copied to
  * such rows first, in d_workspace (16-byte aligned, hikonv_linear_workspace_bytes of it, which overlap no operand, else
- * HIKONV_ERR_INVALID_ARG; NULL where that is 0).  The bytes around a row that lie in the same 16 aligned bytes as part of it may be read,
+ * HIKONV_ERR_INVALID_ARG; NULL where that is 0), which serves one call at a time: calls that may run at once need their own, as do
+ * captured graphs that are replayed at once.  The bytes around a row that lie in the same 16 aligned bytes as part of it may be read,
  * nothing else outside the operands.
  */
 typedef struct {
@@ -522,7 +524,7 @@ size_t hikonv_linear_workspace_bytes(const void *d_x, long long x_row_stride, co
  *   into a graph and replayed with other groups.  Rows in front of offsets[0] and behind offsets[E] - 1 are left as they
  *   were.  Offsets outside 0 .. T are taken as the nearest bound, and a group that ends before it begins as empty: no
  *   memory outside the tensors is touched, but rows that two groups claim are undefined.
- *   1 <= E <= HIKONV_MAX_GROUPS, T == 0 launches nothing.  Everything else as for hikonv_linear with M = T.
+ *   1 <= E <= HIKONV_MAX_GROUPS, E N < 2^31, T == 0 launches nothing.  Everything else as for hikonv_linear with M = T.
  */
 #define HIKONV_MAX_GROUPS 1024
 int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d_w, int w_store_bits, const int32_t *d_offsets, int E,

@@ -569,13 +569,15 @@ def linear(x: torch.Tensor, w: torch.Tensor, p: int, q: int, x_signed: bool, w_s
            activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None, requant: Optional[tuple] = None,
            out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
            stream=None) -> torch.Tensor:
-    """Matrix product of codes, ``x`` [M, K] with ``w`` [N, K] (``w_store_bits`` 1, 2 or 4: dense bytes [N, K * q / 8]).
+    """Matrix product of codes, ``x`` [M, K] with ``w`` [N, K] (``w_store_bits`` 1, 2 or 4: dense bytes [N, K * q / 8], which
+    ``inputs.to_dense`` packs on the host, once).
 
     requant = (shift, lo, hi): codes, one per byte, of the sums plus an int32 ``bias``.  Scales, or a float ``out_dtype`` or ``out``:
     ``act(sum * x_scale[m] * w_scale[n] + bias[n]) + residual[m, n]`` (bfloat16 unless ``out_dtype`` or ``out`` says
     otherwise; scales and bias float32, residual of the output's type, which may be ``out`` itself).  Else: the exact int32 sums.
-    Rows of ``x``, ``residual`` and ``out`` may lie apart.  Rows of ``x`` and ``w`` that do not start on 16-byte boundaries may be copied
-    to such first, into ``workspace`` (``linear_workspace_bytes``; made by the call when it is not given)."""
+    Rows of ``x``, ``residual`` and ``out`` may lie apart, and be columns of one buffer if they are equally many bytes apart.  Rows of
+    ``x`` and ``w`` that do not start on 16-byte boundaries may be copied to such first, into ``workspace`` (``linear_workspace_bytes``;
+    made by the call when it is not given)."""
     return _linear("hikonv_linear", x, w, None, p, q, x_signed, w_signed, w_store_bits, x_scale, w_scale, bias, activation, residual,
                    requant, out_dtype, out, workspace, stream)
 

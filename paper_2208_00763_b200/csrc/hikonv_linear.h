@@ -25,7 +25,9 @@ struct LinearParams {
     int shift, lo, hi;
 };
 
-// A few rows (per group) at a time (hikonv_linear_rows.cu); `rows`: how many the largest group has, or may be expected to have.
+// A few rows (per group) at a time (hikonv_linear_rows.cu); `rows`: how many a group has on average, since the host does not see the bounds of
+// the groups.  A group that has most of the rows is walked over eight rows at a time by its own CTAs alone: 64 rows over eight groups of
+// 2048 x 2048 8-bit weights take 8.3 us where every group has eight, 37 us where one has all.
 constexpr int kLinearFewRows = 16;
 bool linear_rows_takes(const LinearParams &p, int rows);
 int launch_linear_rows(const LinearParams &p, cudaStream_t st);

@@ -10,7 +10,8 @@
 // next tile is multiplied (two accumulators), and, where the operands are not yet bytes of one sign, warps 12 to 23 change them between
 // the two: dense weights are unpacked into tensor memory, and unsigned 8-bit activations of signed weights get 128 subtracted (their top bit flipped; the instruction takes either two signed or two unsigned operands here).  What that takes
 // off, 128 sum_k w[n][k], comes from the multiply itself: a row of ones behind the rows of x makes a column of those sums.  Unsigned 8-bit
-// weights of signed activations, the rare case, are flipped too, and 128 sum_k x[m][k] is added by multiplying x twice by a tile of 64s.
+// weights of signed activations, the rare case, are flipped too, and 128 sum_k x[m][k] is added by multiplying x twice by a tile of 64s:
+// 4096^3 in 143 us, where signed codes take 66 and unsigned activations of signed weights 102.
 // TMA wants rows on 16-byte boundaries.  Operands whose rows start anywhere are copied to rows that do in a launch of their own
 // (align_rows_kernel): read by helper warps word by word instead, 433 x 9100 x 4352 took 103 us and 333 x 1001 x 1501 13.3.
 //
@@ -887,8 +888,9 @@ static int depth_steps(int K) { return (K - 1) / kTcDepth + 1; }
 // multiplies (2 per row), its way from the second-level cache (70 bytes per cycle and SM) and the helpers' work on it; a tile alone on its
 // SM costs 3000 for the set-up and the end of its epilogue; one with a shared depth two barriers of the cluster, which are dearer the
 // larger it is, and the fetches of all parts.
-// Against measured times of 4096 x 4096 with 64 and 256 rows, 8192 x 8192 with 48: 16.3, 16.3 and 18.7 thousand cycles for 15.2, 16.7
-// and 18.9, and the order of the shapes tried is the measured one.
+// It ranks shapes of one layer and leaves out the launch and the way from memory: 8-bit 4096 x 4096 with 64 and 256 rows and 8192 x 8192 with
+// 48 are 11.8, 16.3 and 18.7 thousand cycles of it and take 7.0, 8.6 and 15.5 us with weights from memory.  2048^3 is 19.4 thousand with 240
+// rows per tile (144 tiles, one wave), 20.2 with 256, and takes 10.2 us.
 static void choose_tile(const LinearParams &p, int mode, bool ones, int sms, int *nt_out, int *splits_out) {
     const int n_blocks = ceil_div(p.N, kTcRows), chunks = depth_steps(p.K);
     // unpacked weights take tensor memory from the accumulators

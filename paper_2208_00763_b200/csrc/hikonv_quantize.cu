@@ -7,7 +7,7 @@
 // reciprocal and two corrections, by instructions that take two values, without a branch: between bf16 values exact halves are so frequent
 // that a test for open codes found one in every second warp.  4096 x 16384 bf16 values: 85 us with a library division each and the row
 // read twice, 60 with the row in registers, 44 by a rounded product and a division where that left a code open, 38 to 39 now (5.2 TB/s), about
-// 11 instructions per value at 62 % of the issue rate; as fp32 53 us (6.3 TB/s, as fast as a copy).
+// 11 instructions per value at 57 % of the issue rate; as fp32 53 us (6.3 TB/s, as fast as a copy).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

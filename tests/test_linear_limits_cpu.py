@@ -1,5 +1,6 @@
 """CPU checks of the linear layers' entry points at the ends of what their documentation allows."""
 import os
+import re
 import subprocess
 import sys
 
@@ -90,3 +91,11 @@ def test_columns_of_one_buffer_with_other_strides():
         assert call(x_row=96, out=X + off, out_row=96, ep=dict(C, hi=1)) == hk.ERR_INVALID_ARG
     made = without_devices("print(*(call(x_row=96, out=X + off, out_row=96, ep=dict(C, hi=1)) for off in (64, -32, 64 + 96)))")
     assert made == [str(hk.ERR_CUDA)] * 3
+
+
+def test_what_the_linear_kernels_read_they_read_with_ordinary_loads():
+    # they are launched while the kernel before may still write; the read-only path promises data that stays constant meanwhile
+    csrc = os.path.join(os.path.dirname(TESTS), "paper_2208_00763_b200", "csrc")
+    for name in ("hikonv_linear_util.cuh", "hikonv_linear_rows.cu", "hikonv_linear_tc.cu", "hikonv_quantize.cu"):
+        text = re.sub(r"//.*", "", open(os.path.join(csrc, name)).read())
+        assert not re.search(r"__ldg\(|ld\.global\.nc|__ldc[sagv]\(|const\s+\w+\s*\*\s*__restrict__", text), name
