@@ -540,6 +540,103 @@ int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d
 int hikonv_linear_wait_timeouts(unsigned int *h_count);
 int hikonv_linear_wait_check(long long cycles, void *stream);
 
+/*
+ * A mixture of experts: hikonv_sort_by_expert, hikonv_rows_to_experts (or hikonv_quantize_blocks), products of groups of rows,
+ * hikonv_rows_from_experts.  All of it stays on the device: no count comes back to the host, so calls can be captured into a graph.
+ *
+ * hikonv_sort_by_expert - places of pairs (token, choice) in the order of their experts, equal ones in their own order.
+ *   experts: [T][k] int32 or int64 (index_bytes 4 or 8), row t starting at element t * experts_row_stride.
+ *   offsets: [E + 1]; pairs of expert e have the places offsets[e] .. offsets[e + 1] - 1, as hikonv_grouped_linear's groups have rows.
+ *   slots:   [T][k], the place of each pair.  Pairs whose expert is outside 0 .. E - 1 have none: their slots are -2 - place, with places
+ *            behind offsets[E], so that every place below T k belongs to one pair.
+ * T k <= 2^30, 1 <= E <= HIKONV_MAX_GROUPS; T == 0 makes all offsets 0.  The outputs must not overlap the input or each other.
+ * d_workspace: hikonv_sort_by_expert_workspace_bytes of it (0 for up to 4096 pairs), 4-byte aligned, for one call at a time.
+ */
+int hikonv_sort_by_expert(const void *d_experts, int index_bytes, long long experts_row_stride, int T, int k, int E, int32_t *d_offsets,
+                          int32_t *d_slots, void *d_workspace, size_t workspace_bytes, void *stream);
+size_t hikonv_sort_by_expert_workspace_bytes(int T, int k, int E);
+
+/*
+ * hikonv_rows_to_experts - rows of tokens to the places of their pairs: out[slots[t][j]] = x[t] for every slot in 0 .. R - 1.
+ *   x: [T][H] elements of 1, 2 or 4 bytes, rows x_row_stride elements apart (0 when all rows are one); out: [R][H], out_row_stride >= H.
+ * Rows of out that no slot names are left as they were; a row that two slots name is undefined.  Its gradient is
+ * hikonv_rows_from_experts without weights.  T k <= 2^30, H <= 2^23.  out must not overlap x or slots.
+ */
+int hikonv_rows_to_experts(const void *d_x, int element_bytes, long long x_row_stride, const int32_t *d_slots, int T, int k, int H, void *d_out,
+                           long long out_row_stride, int R, void *stream);
+
+/*
+ * hikonv_rows_from_experts - rows back to their tokens: out[t] = residual[t] + sum_j weights[t][j] y[slots[t][j]], over the slots in
+ * 0 .. R - 1, added in the order of j in 32-bit arithmetic and rounded once.
+ *   y: [R][H], out, residual (or NULL): [T][H], all of type (hikonv_out_type: F32, F16 or BF16), strides in elements (y's may be 0)
+ *   weights: [T][k] float, or NULL for ones.  What lies at other slots (a weight that is NaN, say) does not count.
+ * A token without any such slot gets its residual, or zeros.  out may be the residual itself (same address and stride) and overlaps nothing else.
+ */
+int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, int R, const int32_t *d_slots, const float *d_weights, int T, int k,
+                             int H, const void *d_residual, long long residual_row_stride, void *d_out, long long out_row_stride, void *stream);
+
+/*
+ * hikonv_rows_from_experts_grad - its gradient for y and the weights from the one for out (which the residual's is, too).
+ *   grad_y[slots[t][j]] = weights[t][j] grad[t]; zeros in row -2 - slots[t][j] for slots below -1, so that every row is written when
+ *      slots come from hikonv_sort_by_expert and R = T k.  Rows outside 0 .. R - 1 are left out.
+ *   grad_weights[t][j] = sum_h grad[t][h] y[slots[t][j]][h], 32-bit sums in an order that depends on the sizes alone; 0 without a row
+ *   weights and grad_weights: [T][k] float, or both NULL (then y is not read).
+ * Outputs must overlap neither inputs nor each other.
+ */
+int hikonv_rows_from_experts_grad(const void *d_grad, int type, long long grad_row_stride, const void *d_y, long long y_row_stride, int R,
+                                  const int32_t *d_slots, const float *d_weights, int T, int k, int H, void *d_grad_y,
+                                  long long grad_y_row_stride, float *d_grad_weights, void *stream);
+
+/*
+ * Matrix products of 8-bit floating point numbers with a scale for each block of 128 along the depth.
+ *
+ * hikonv_quantize_blocks - rows of floats to such blocks, in their order or to the places of experts.
+ *   x: [M][K] of x_type (hikonv_out_type: F32, F16 or BF16), rows x_row_stride elements apart (0 when all rows are one)
+ *   scale[b][m] = max |x[m][128 b .. 128 b + 127]| / max(type); values[m][k] = x[m][k] / scale[k / 128][m], divided in 32 bits and rounded to
+ *      nearest, ties to even.  max(type): 448 for E4M3, 57344 for E5M2.
+ *   values: one byte each, rows values_row_stride bytes apart, on 16-byte boundaries; bytes behind a row's K values are left as they were.
+ *   scale: [ceil(K / 128)][rows], scale_row_stride elements from block to block.
+ *   slots: NULL (k and R are 0), or [M][k]: row m goes to the rows slots[m][j] in 0 .. R - 1 of values and of scale; others are left as they were.
+ * A block of zeros has scale 0 and values 0.  A block with a NaN has scale NaN and values NaN; one whose largest magnitude is infinite has
+ * scale infinity, values 0 and, for the infinite ones, NaN (so what is computed from such a block is NaN).  Subnormals are kept.
+ * M k <= 2^30.  Outputs must overlap neither x, slots nor each other.
+ */
+typedef enum {
+    HIKONV_F8_E4M3 = 0, /* 4 bits of exponent, 3 of mantissa, no infinity */
+    HIKONV_F8_E5M2 = 1
+} hikonv_f8_type;
+int hikonv_quantize_blocks(const void *d_x, int x_type, long long x_row_stride, int M, int K, int f8_type, const int32_t *d_slots, int k, int R,
+                           uint8_t *d_values, long long values_row_stride, float *d_scale, long long scale_row_stride, void *stream);
+
+/*
+ * hikonv_quantize_tiles - weights to tiles of 128 x 128 with a scale each: scale[n / 128][b] as above over the tile's rows and columns.
+ *   w: [E][N][K], rows w_row_stride elements apart throughout; values: [E][N][K], rows values_row_stride bytes apart, on 16-byte
+ *   boundaries; scale: [E][ceil(N / 128)][ceil(K / 128)].  Done once, when weights are loaded.
+ */
+int hikonv_quantize_tiles(const void *d_w, int w_type, long long w_row_stride, int E, int N, int K, int f8_type, uint8_t *d_values,
+                          long long values_row_stride, float *d_scale, void *stream);
+
+/*
+ * hikonv_linear_f8 - out = act(sum + bias[n]) + residual[m][n] with
+ *   sum[m][n] = sum_b x_scale[b][m] w_scale[n / 128][b] sum_{k in block b} x[m][k] w[n][k]
+ *   x: [M][K] of x_f8 (hikonv_f8_type), w: [N][K] of w_f8, rows so many bytes apart, on 16-byte boundaries (else HIKONV_ERR_UNSUPPORTED)
+ *   x_scale: [ceil(K / 128)][M], x_scale_row_stride (>= M) elements from block to block; w_scale: [ceil(N / 128)][ceil(K / 128)]
+ *   epilogue: out_type F32, F16 or BF16, activation, d_bias (float) and d_residual as for hikonv_linear; d_x_scale and d_w_scale, shift, lo
+ *      and hi NULL or 0
+ * Products of a block are summed by the tensor cores in 32-bit arithmetic; blocks are added in 32 bits in an order that depends on
+ * sizes and alignment alone.  out must overlap no input but the residual (same address and stride).
+ *
+ * hikonv_grouped_linear_f8 - with a matrix per group of rows: w: [E][N][K] (rows equally far apart throughout), w_scale: [E][..][..],
+ *   d_bias: [E][N]; rows offsets[e] .. offsets[e + 1] - 1 belong to matrix e.  Offsets as for hikonv_grouped_linear; rows of no group are
+ *   left as they were.  M, N <= 2^30, E N < 2^31.
+ */
+int hikonv_linear_f8(const void *d_x, int x_f8, long long x_row_stride, const void *d_w, int w_f8, long long w_row_stride, int M, int N, int K,
+                     const float *d_x_scale, long long x_scale_row_stride, const float *d_w_scale, void *d_out, long long out_row_stride,
+                     const hikonv_epilogue_t *epilogue, void *stream);
+int hikonv_grouped_linear_f8(const void *d_x, int x_f8, long long x_row_stride, const void *d_w, int w_f8, long long w_row_stride,
+                             const int32_t *d_offsets, int E, int T, int N, int K, const float *d_x_scale, long long x_scale_row_stride,
+                             const float *d_w_scale, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream);
+
 const char *hikonv_status_string(int status);
 
 #ifdef __cplusplus

@@ -4,7 +4,7 @@ PyTorch is used for device memory and streams; every arithmetic step runs in the
 library.  Loading fails loudly when the library has not been built: there is no fallback.
 
 The calls of every step (``conv1d``, ``conv1d_dense``, ``pack``, ``conv2d``, ``conv2d_dense`` without tuning record and
-explicit stream, ``quantize_rows``, ``linear`` and ``grouped_linear`` without explicit stream) go through the extension module ``_fast`` first, which makes the same checks on the tensors natively and
+explicit stream, ``quantize_rows``, ``linear``, ``grouped_linear`` and the calls of a mixture of experts without explicit stream) go through the extension module ``_fast`` first, which makes the same checks on the tensors natively and
 returns None where anything is amiss; the Python code below then raises the error.
 """
 from __future__ import annotations
@@ -26,6 +26,7 @@ GB_SINGLE, GB_1D, GB_DNN = 0, 1, 2
 OUT_SUMS, OUT_CODES, OUT_F32, OUT_F16, OUT_BF16 = range(5)
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
 MAX_GROUPS = 1024
+F8_E4M3, F8_E5M2 = range(2)
 PIPE_KINDS = {"mad_wide_u32": 0, "mad_wide_s32": 1, "mad_lo_s32": 2, "logic": 3, "shift": 4, "prmt": 5,
               "mad_wide_with_logic": 6, "fma_f64": 7}
 
@@ -102,13 +103,24 @@ _SIGNATURES = {
     "hikonv_linear_workspace_bytes": (_sz, [_vp, _ll, _vp] + [_i] * 5),
     "hikonv_linear_wait_timeouts": (_i, [_vp]),
     "hikonv_linear_wait_check": (_i, [_ll, _vp]),
+    "hikonv_sort_by_expert": (_i, [_vp, _i, _ll, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "hikonv_sort_by_expert_workspace_bytes": (_sz, [_i, _i, _i]),
+    "hikonv_rows_to_experts": (_i, [_vp, _i, _ll, _vp, _i, _i, _i, _vp, _ll, _i, _vp]),
+    "hikonv_rows_from_experts": (_i, [_vp, _i, _ll, _i, _vp, _vp, _i, _i, _i, _vp, _ll, _vp, _ll, _vp]),
+    "hikonv_rows_from_experts_grad": (_i, [_vp, _i, _ll, _vp, _ll, _i, _vp, _vp, _i, _i, _i, _vp, _ll, _vp, _vp]),
+    "hikonv_quantize_blocks": (_i, [_vp, _i, _ll, _i, _i, _i, _vp, _i, _i, _vp, _ll, _vp, _ll, _vp]),
+    "hikonv_quantize_tiles": (_i, [_vp, _i, _ll, _i, _i, _i, _i, _vp, _ll, _vp, _vp]),
+    "hikonv_linear_f8": (_i, [_vp, _i, _ll, _vp, _i, _ll, _i, _i, _i, _vp, _ll, _vp, _vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
+    "hikonv_grouped_linear_f8": (_i, [_vp, _i, _ll, _vp, _i, _ll, _vp, _i, _i, _i, _i, _vp, _ll, _vp, _vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
     "hikonv_status_string": (ctypes.c_char_p, [_i]),
 }
 
 
 _FAST_ENTRY_POINTS = ("hikonv_conv1d", "hikonv_conv1d_dense", "hikonv_pack", "hikonv_conv2d", "hikonv_conv2d_dense",
                       "hikonv_conv2d_workspace_bytes", "hikonv_quantize_rows", "hikonv_linear", "hikonv_grouped_linear",
-                      "hikonv_linear_workspace_bytes")
+                      "hikonv_linear_workspace_bytes", "hikonv_sort_by_expert", "hikonv_sort_by_expert_workspace_bytes",
+                      "hikonv_rows_to_experts", "hikonv_rows_from_experts", "hikonv_rows_from_experts_grad", "hikonv_quantize_blocks",
+                      "hikonv_linear_f8", "hikonv_grouped_linear_f8")
 
 
 def exported_names():
@@ -672,6 +684,279 @@ def linear_wait_timeouts() -> int:
 def linear_wait_check(cycles: int, stream=None) -> None:
     """One thread waits `cycles` for a barrier that nothing completes, gives up and is counted."""
     _check(lib().hikonv_linear_wait_check(int(cycles), _stream(stream)), "hikonv_linear_wait_check")
+
+
+# ------------------------------------------------------------------ a mixture of experts
+
+_F8_TYPES = {torch.float8_e4m3fn: F8_E4M3, torch.float8_e5m2: F8_E5M2}
+_INDEX_TYPES = {torch.int32: 4, torch.int64: 8}
+
+
+def _slots(slots: torch.Tensor, like: torch.Tensor, rows: Optional[int] = None) -> tuple:
+    """Checks the places of pairs; returns (address, T, k)."""
+    if getattr(slots, "dim", lambda: 0)() != 2:
+        raise ValueError("slots must be a matrix, a row per token")
+    T, k = slots.shape
+    if rows is not None and T != rows:
+        raise ValueError("slots has %d rows, there are %d tokens" % (T, rows))
+    return _vector(slots, "slots", torch.int32, (T, k), like), T, k
+
+
+def sort_by_expert(experts: torch.Tensor, n_experts: int, offsets: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """Places of (token, choice) pairs in the order of their experts: ``experts`` [T, k] int32 or int64, as ``torch.topk`` gives them (its
+    rows may lie apart).  Returns (offsets, slots), int32: the pairs of expert e have the places ``offsets[e]`` to ``offsets[e + 1] - 1``
+    (what ``grouped_linear`` and ``grouped_linear_f8`` take), ``slots`` [T, k] the place of each pair, equal experts in the pairs' order.
+    Experts outside 0 .. n_experts - 1 mean none: such a pair's slot is -2 - place, with places behind ``offsets[-1]``."""
+    if stream is None:
+        done = (_fast or _load_fast()).sort_by_expert(experts, n_experts, offsets, slots, workspace)
+        if done is not None:
+            return done
+    if getattr(experts, "dtype", None) not in _INDEX_TYPES:
+        raise ValueError("experts must be an int32 or int64 matrix")
+    row = _rows(experts, "experts", (experts.dtype,))
+    T, k = experts.shape
+    if offsets is None:
+        offsets = _empty(n_experts + 1, torch.int32, experts, stream)
+    if slots is None:
+        slots = _empty((T, k), torch.int32, experts, stream)
+    with torch.cuda.device(experts.device):
+        need = int(lib().hikonv_sort_by_expert_workspace_bytes(T, k, n_experts))
+        if need and workspace is None:
+            workspace = _empty(need, torch.uint8, experts, stream)
+        if workspace is not None and (not workspace.is_cuda or workspace.device != experts.device or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous CUDA tensor on experts' device")
+        space = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        _check(lib().hikonv_sort_by_expert(experts.data_ptr(), _INDEX_TYPES[experts.dtype], row, T, k, n_experts,
+                                           _vector(offsets, "offsets", torch.int32, (n_experts + 1,), experts),
+                                           _vector(slots, "slots", torch.int32, (T, k), experts), *space, _stream_of(experts, stream)),
+               "hikonv_sort_by_expert")
+    return offsets, slots
+
+
+def sort_by_expert_workspace_bytes(tokens: int, choices: int, n_experts: int) -> int:
+    """Bytes that ``sort_by_expert`` needs between its launches: 0 for up to 4096 pairs."""
+    return int(lib().hikonv_sort_by_expert_workspace_bytes(tokens, choices, n_experts))
+
+
+def rows_to_experts(x: torch.Tensor, slots: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows of tokens to the places of their pairs: ``out[slots[t, j]] = x[t]``, for any type of 1, 2 or 4 bytes.  ``out`` [T k, H] unless it
+    is given (with as many rows as wanted); rows that no slot names are left as they were (undefined when the call makes it).  Its gradient
+    is ``rows_from_experts`` without weights."""
+    if stream is None:
+        done = (_fast or _load_fast()).rows_to_experts(x, slots, out)
+        if done is not None:
+            return done
+    if getattr(x, "dtype", None) is None or x.dtype.itemsize not in (1, 2, 4) or x.dtype.is_complex:
+        raise ValueError("x must be a matrix of 1-, 2- or 4-byte elements")
+    x_row = _rows(x, "x", (x.dtype,))
+    H = x.shape[1]
+    places, T, k = _slots(slots, x, x.shape[0])
+    if out is None:
+        out = _empty((T * k, H), x.dtype, x, stream)
+    out_row = _rows(out, "out", (x.dtype,), x, (out.shape[0], H) if out.dim() == 2 else (T * k, H))
+    with torch.cuda.device(x.device):
+        _check(lib().hikonv_rows_to_experts(x.data_ptr(), x.dtype.itemsize, x_row, places, T, k, H, out.data_ptr(), out_row, out.shape[0],
+                                            _stream_of(x, stream)), "hikonv_rows_to_experts")
+    return out
+
+
+def rows_from_experts(y: torch.Tensor, slots: torch.Tensor, weights: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows of experts back to their tokens: ``out[t] = residual[t] + sum_j weights[t, j] * y[slots[t, j]]`` in 32-bit arithmetic, rounded
+    once.  ``y`` [rows, H] float32, float16 or bfloat16, ``weights`` [T, k] float32 (None: ones), ``residual`` of y's type, which may be
+    ``out`` itself.  Pairs without a place add nothing, whatever their weight."""
+    if stream is None:
+        done = (_fast or _load_fast()).rows_from_experts(y, slots, weights, residual, out)
+        if done is not None:
+            return done
+    if getattr(y, "dtype", None) not in _FLOAT_TYPES:
+        raise ValueError("y must be a float32, float16 or bfloat16 matrix")
+    y_row = _rows(y, "y", (y.dtype,))
+    R, H = y.shape
+    places, T, k = _slots(slots, y)
+    if out is None:
+        out = _empty((T, H), y.dtype, y, stream)
+    out_row = _rows(out, "out", (y.dtype,), y, (T, H))
+    res_row = H if residual is None else _rows(residual, "residual", (y.dtype,), y, (T, H))
+    with torch.cuda.device(y.device):
+        _check(lib().hikonv_rows_from_experts(y.data_ptr(), _FLOAT_TYPES[y.dtype], y_row, R, places,
+                                              _vector(weights, "weights", torch.float32, (T, k), y), T, k, H,
+                                              None if residual is None else residual.data_ptr(), res_row, out.data_ptr(), out_row,
+                                              _stream_of(y, stream)), "hikonv_rows_from_experts")
+    return out
+
+
+def rows_from_experts_grad(grad: torch.Tensor, y: Optional[torch.Tensor], slots: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                           grad_y: Optional[torch.Tensor] = None, grad_weights: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """The gradient of ``rows_from_experts``, from the one for its output: (grad_y, grad_weights).  ``grad_y[slots[t, j]]`` is
+    ``weights[t, j] * grad[t]``, zeros in the places of pairs without expert; ``grad_weights[t, j]`` the product of ``grad[t]`` with the
+    pair's row of ``y``, 0 without one.  Without weights ``y`` is not read (it may be None) and there is no grad_weights.  ``grad_y`` has a row for
+    each pair unless it is given; then rows that no slot names are left as they were.  The residual's gradient is ``grad`` itself."""
+    if stream is None:
+        done = (_fast or _load_fast()).rows_from_experts_grad(grad, y, slots, weights, grad_y, grad_weights)
+        if done is not None:
+            return done
+    if getattr(grad, "dtype", None) not in _FLOAT_TYPES:
+        raise ValueError("grad must be a float32, float16 or bfloat16 matrix")
+    grad_row = _rows(grad, "grad", (grad.dtype,))
+    H = grad.shape[1]
+    places, T, k = _slots(slots, grad, grad.shape[0])
+    if weights is None and grad_weights is not None:
+        raise ValueError("grad_weights without weights")
+    if weights is not None and y is None:
+        raise ValueError("the gradient of weights needs y")
+    if grad_y is None:
+        grad_y = _empty((T * k if y is None else y.shape[0], H), grad.dtype, grad, stream)
+    grad_y_row = _rows(grad_y, "grad_y", (grad.dtype,), grad, (grad_y.shape[0] if grad_y.dim() == 2 else T * k, H))
+    R = grad_y.shape[0]
+    y_row = H if weights is None else _rows(y, "y", (grad.dtype,), grad, (R, H))
+    if weights is not None and grad_weights is None:
+        grad_weights = _empty((T, k), torch.float32, grad, stream)
+    with torch.cuda.device(grad.device):
+        _check(lib().hikonv_rows_from_experts_grad(grad.data_ptr(), _FLOAT_TYPES[grad.dtype], grad_row, None if weights is None else y.data_ptr(),
+                                                   y_row, R, places, _vector(weights, "weights", torch.float32, (T, k), grad), T, k, H,
+                                                   grad_y.data_ptr(), grad_y_row,
+                                                   _vector(grad_weights, "grad_weights", torch.float32, (T, k), grad), _stream_of(grad, stream)),
+               "hikonv_rows_from_experts_grad")
+    return grad_y, grad_weights
+
+
+# ------------------------------------------------------------------ blocks of 8-bit floating point numbers
+
+def _f8_rows(rows: tuple, K: int, dtype: torch.dtype, like: torch.Tensor, stream) -> torch.Tensor:
+    """A tensor [*rows, K] whose rows begin on 16-byte boundaries."""
+    return _empty((*rows, (K + 15) // 16 * 16), dtype, like, stream)[..., :K]
+
+
+def quantize_blocks(x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, slots: Optional[torch.Tensor] = None,
+                    values: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """Rows of floats to 8-bit floating point numbers with a scale for each block of 128: (values [M, K], scale [ceil(K / 128), M]), with
+    ``x[m, k]`` about ``values[m, k] * scale[k // 128, m]``.  With ``slots`` [M, k] (of ``sort_by_expert``) row m goes to the rows
+    ``slots[m, j]`` instead: values [M k, K] unless given; rows that no slot names are left as they were.  Rows of values begin on 16-byte
+    boundaries (the call's own are so far apart)."""
+    if stream is None:
+        done = (_fast or _load_fast()).quantize_blocks(x, dtype, slots, values, scale)
+        if done is not None:
+            return done
+    if getattr(x, "dtype", None) not in _FLOAT_TYPES:
+        raise ValueError("x must be a float32, float16 or bfloat16 matrix")
+    if dtype not in _F8_TYPES:
+        raise ValueError("values are float8_e4m3fn or float8_e5m2, not %s" % dtype)
+    x_row = _rows(x, "x", (x.dtype,))
+    M, K = x.shape
+    places, k = None, 0
+    if slots is not None:
+        places, _, k = _slots(slots, x, M)
+    rows = values.shape[0] if values is not None and values.dim() == 2 else M * k if slots is not None else M
+    if values is None:
+        values = _f8_rows((rows,), K, dtype, x, stream)
+    values_row = _rows(values, "values", (dtype,), x, (rows if slots is not None else M, K))
+    blocks = (K + 127) // 128
+    if scale is None:
+        scale = _empty((blocks, rows), torch.float32, x, stream)
+    scale_row = _rows(scale, "scale", (torch.float32,), x, (blocks, rows))
+    with torch.cuda.device(x.device):
+        _check(lib().hikonv_quantize_blocks(x.data_ptr(), _FLOAT_TYPES[x.dtype], x_row, M, K, _F8_TYPES[dtype], places, k,
+                                            rows if slots is not None else 0, values.data_ptr(), values_row, scale.data_ptr(), scale_row,
+                                            _stream_of(x, stream)), "hikonv_quantize_blocks")
+    return values, scale
+
+
+def quantize_tiles(w: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, values: Optional[torch.Tensor] = None,
+                   scale: Optional[torch.Tensor] = None, stream=None) -> tuple:
+    """Weights [N, K] or [E, N, K] to 8-bit floating point numbers with a scale for each tile of 128 x 128: (values, scale
+    [.., ceil(N / 128), ceil(K / 128)]).  Done once, when weights are loaded."""
+    if getattr(w, "dtype", None) not in _FLOAT_TYPES:
+        raise ValueError("w must be float32, float16 or bfloat16")
+    if dtype not in _F8_TYPES:
+        raise ValueError("values are float8_e4m3fn or float8_e5m2, not %s" % dtype)
+    w_row = _weight_rows(w, "w", (w.dtype,))
+    lead, N, K = tuple(w.shape[:-2]), w.shape[-2], w.shape[-1]
+    if values is None:
+        values = _f8_rows((*lead, N), K, dtype, w, stream)
+    values_row = _weight_rows(values, "values", (dtype,), w, w.shape)
+    tiles = lead + ((N + 127) // 128, (K + 127) // 128)
+    if scale is None:
+        scale = _empty(tiles, torch.float32, w, stream)
+    with torch.cuda.device(w.device):
+        _check(lib().hikonv_quantize_tiles(w.data_ptr(), _FLOAT_TYPES[w.dtype], w_row, lead[0] if lead else 1, N, K, _F8_TYPES[dtype],
+                                           values.data_ptr(), values_row, _vector(scale, "scale", torch.float32, tiles, w),
+                                           _stream_of(w, stream)), "hikonv_quantize_tiles")
+    return values, scale
+
+
+def _weight_rows(w: torch.Tensor, name: str, dtypes, like: Optional[torch.Tensor] = None, shape=None) -> int:
+    """Checks a matrix of weights, or one per expert, whose rows are equally far apart throughout; returns that distance in elements."""
+    if not getattr(w, "is_cuda", False) or w.layout != torch.strided or w.dim() not in (2, 3):
+        raise ValueError("%s must be a CUDA tensor of [N, K] or [E, N, K]" % name)
+    if w.dtype not in dtypes:
+        raise ValueError("%s must have dtype %s, not %s" % (name, " or ".join(str(d) for d in dtypes), w.dtype))
+    if like is not None and w.device != like.device:
+        raise ValueError("%s is on %s, not on %s" % (name, w.device, like.device))
+    if shape is not None and tuple(w.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, the call needs %s" % (name, tuple(w.shape), tuple(shape)))
+    N, K = w.shape[-2:]
+    if K > 1 and w.stride(-1) != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    row = w.stride(-2) if N > 1 else w.stride(0) if w.dim() == 3 and w.shape[0] > 1 else K
+    if w.dim() == 3 and w.shape[0] > 1 and w.stride(0) != N * row:
+        raise ValueError("%s must have its matrices one behind the other" % name)
+    return row
+
+
+def linear_f8(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Matrix product of 8-bit floating point numbers with a scale for each block of 128: ``x`` [M, K] and ``x_scale`` [ceil(K / 128), M] as
+    ``quantize_blocks`` gives them, ``w`` [N, K] and ``w_scale`` [ceil(N / 128), ceil(K / 128)] as ``quantize_tiles`` does:
+    ``act(sum + bias[n]) + residual[m, n]`` in bfloat16 unless ``out_dtype`` or ``out`` says otherwise (float32, float16).  Either operand
+    is float8_e4m3fn or float8_e5m2, with rows on 16-byte boundaries; bias float32; residual of the output's type, which may be ``out``."""
+    return _linear_f8("hikonv_linear_f8", x, w, None, x_scale, w_scale, bias, activation, residual, out_dtype, out, stream)
+
+
+def grouped_linear_f8(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, x_scale: torch.Tensor, w_scale: torch.Tensor,
+                      bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
+                      out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``linear_f8`` with a matrix of weights per group of rows: ``w`` [E, N, K], ``w_scale`` [E, ..], ``bias`` [E, N]; rows
+    ``offsets[e]`` to ``offsets[e + 1] - 1`` (int32 [E + 1], on the device) belong to matrix e.  Rows of no group are left as they
+    were in ``out`` (undefined when the call makes it)."""
+    return _linear_f8("hikonv_grouped_linear_f8", x, w, offsets, x_scale, w_scale, bias, activation, residual, out_dtype, out, stream)
+
+
+def _linear_f8(name, x, w, offsets, x_scale, w_scale, bias, activation, residual, out_dtype, out, stream):
+    grouped = name == "hikonv_grouped_linear_f8"
+    if stream is None and grouped == (offsets is not None):
+        done = (_fast or _load_fast()).linear_f8(x, w, offsets, x_scale, w_scale, bias, activation, residual, out_dtype, out)
+        if done is not None:
+            return done
+    x_row = _rows(x, "x", tuple(_F8_TYPES))
+    M, K = x.shape
+    w_row = _weight_rows(w, "w", tuple(_F8_TYPES), x)
+    if w.dim() != (3 if grouped else 2) or w.shape[-1] != K:
+        raise ValueError("w has shape %s, the call needs %s of depth %d" % (tuple(w.shape), "[E, N, K]" if grouped else "[N, K]", K))
+    lead, N = tuple(w.shape[:-2]), w.shape[-2]
+    blocks = (K + 127) // 128
+    scale_row = _rows(x_scale, "x_scale", (torch.float32,), x, (blocks, M))
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if out is None else out.dtype
+    if out_dtype not in _FLOAT_TYPES:
+        raise ValueError("the output is float32, float16 or bfloat16, not %s" % out_dtype)
+    if out is None:
+        out = _empty((M, N), out_dtype, x, stream)
+    ep = EpilogueT(out_type=_FLOAT_TYPES[out_dtype], activation=int(activation))
+    out_row = _rows(out, "out", (out_dtype,), x, (M, N))
+    ep.d_bias = _vector(bias, "bias", torch.float32, lead + (N,), x)
+    if residual is not None:
+        ep.residual_row_stride = _rows(residual, "residual", (out_dtype,), x, (M, N))
+        ep.d_residual = residual.data_ptr()
+    w_scales = _vector(w_scale, "w_scale", torch.float32, lead + ((N + 127) // 128, blocks), x)
+    groups = (_vector(offsets, "offsets", torch.int32, (lead[0] + 1,), x), lead[0]) if grouped else ()
+    with torch.cuda.device(x.device):
+        _check(getattr(lib(), name)(x.data_ptr(), _F8_TYPES[x.dtype], x_row, w.data_ptr(), _F8_TYPES[w.dtype], w_row, *groups, M, N, K,
+                                    x_scale.data_ptr(), scale_row, w_scales, out.data_ptr(), out_row, ctypes.byref(ep), _stream_of(x, stream)),
+               name)
+    return out
 
 
 def pipe_rate(kind: str, iters: int = 2048, device=None, stream=None) -> dict:

@@ -27,7 +27,7 @@ NVCC_FLAGS = [
     "-Xcompiler", "-fPIC",
 ]
 # The convolutions compute with integers only; the layers that answer in floats keep IEEE division, square roots and subnormals.
-IEEE_PREFIXES = ("hikonv_linear", "hikonv_quantize")
+IEEE_PREFIXES = ("hikonv_linear", "hikonv_quantize", "hikonv_experts")
 
 
 def sources():

@@ -1,0 +1,517 @@
+// hikonv_sort_by_expert, hikonv_rows_to_experts, hikonv_rows_from_experts and its gradient: a mixture of experts around the products of
+// hikonv_grouped_linear and hikonv_grouped_linear_f8.
+//
+// Sorting is a stable counting sort: pairs of token and choice keep their order within an expert, so results do not depend on the order
+// in which warps run.  Rows are moved by token: a token's row is read once however many experts it goes to, and what an expert's rows
+// give back to a token is summed in registers, in the order of its choices.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "hikonv_cuda.cuh"
+#include "hikonv_linear.h"
+
+namespace hikonv {
+
+// ---- sorting
+
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortSteps = 8;
+constexpr int kSortBlock = kSortThreads * kSortSteps;       // pairs whose experts the registers of a CTA hold
+constexpr int kSortMostCtas = 128;
+
+struct SortParams {
+    const void *experts;
+    int wide;                            // 8-byte indices
+    long long row;                       // elements from token to token
+    long long pairs;
+    int k, E, ctas;
+    long long per_cta;                   // pairs, a multiple of kSortBlock
+    int32_t *offsets, *slots;
+    uint32_t *counts;                    // [ctas][E + 1], null for one CTA
+};
+
+// The expert of a pair, E for none.
+__device__ __forceinline__ int expert_of(const SortParams &p, long long pair) {
+    long long at = pair;
+    if (p.row != p.k) {
+        const long long t = pair <= 0x7FFFFFFF ? (long long)((uint32_t)pair / (uint32_t)p.k) : pair / p.k;
+        at = t * p.row + (pair - t * p.k);
+    }
+    const long long e = p.wide ? load_ordered((const long long *)p.experts + at) : (long long)load_ordered((const int32_t *)p.experts + at);
+    return e >= 0 && e < p.E ? (int)e : p.E;
+}
+
+// How many pairs of each expert a CTA's stretch has.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortParams p) {
+    extern __shared__ uint32_t hist[];
+    grid_dependency_release();
+    grid_dependency_wait();
+    for (int e = threadIdx.x; e <= p.E; e += kSortThreads) hist[e] = 0;
+    __syncthreads();
+    const long long a = blockIdx.x * p.per_cta, b = min(a + p.per_cta, p.pairs);
+    for (long long i = a + threadIdx.x; i < b; i += kSortThreads) atomicAdd(hist + expert_of(p, i), 1u);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= p.E; e += kSortThreads) p.counts[(long long)blockIdx.x * (p.E + 1) + e] = hist[e];
+}
+
+// Places of a CTA's stretch.  Every warp takes neighbouring pairs, 32 at a time: the lanes of one expert find each other, and the place is
+// the expert's next one in this warp plus the lanes before.
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortParams p) {
+    extern __shared__ uint32_t shared[];
+    const int E1 = p.E + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t *hist = shared, *next = shared + kSortWarps * E1, *total = next + E1, *sums = total + E1;     // [warp][E1]: of each expert in each warp; next place; all pairs
+    grid_dependency_release();
+    for (int i = tid; i < (kSortWarps + 2) * E1; i += kSortThreads) shared[i] = 0;
+    grid_dependency_wait();
+    __syncthreads();
+    const long long begin = blockIdx.x * p.per_cta, end = min(begin + p.per_cta, p.pairs);
+    int key[kSortSteps];
+    uint32_t same[kSortSteps];
+    auto read = [&](long long from) {                   // the block's experts, and how many each warp has
+#pragma unroll
+        for (int s = 0; s < kSortSteps; ++s) {
+            const long long i = from + (warp * kSortSteps + s) * 32 + lane;
+            key[s] = i < end ? expert_of(p, i) : -1;
+        }
+#pragma unroll
+        for (int s = 0; s < kSortSteps; ++s) {
+            if (from + (warp * kSortSteps + s) * 32 >= end) break;
+            same[s] = __match_any_sync(0xFFFFFFFFu, key[s]);
+            if (key[s] >= 0 && lane == __ffs(same[s]) - 1) hist[warp * E1 + key[s]] += __popc(same[s]);
+            __syncwarp();
+        }
+    };
+    read(begin);
+    if (p.counts) {
+        // columns of the counts, by several threads each: what lies in front of this CTA, and all
+        int parts = 1;
+        while (parts * 2 * E1 <= kSortThreads && parts < p.ctas) parts *= 2;
+        for (int i = tid; i < parts * E1; i += kSortThreads) {
+            const int e = i % E1;
+            uint32_t before = 0, all = 0;
+            for (int c = i / E1; c < p.ctas; c += parts) {
+                const uint32_t v = load_ordered(p.counts + (long long)c * E1 + e);
+                all += v;
+                if (c < (int)blockIdx.x) before += v;
+            }
+            atomicAdd(next + e, before);
+            atomicAdd(total + e, all);
+        }
+        __syncthreads();
+    } else {
+        __syncthreads();
+        for (int e = tid; e < E1; e += kSortThreads) {
+            uint32_t all = 0;
+            for (int w = 0; w < kSortWarps; ++w) all += hist[w * E1 + e];
+            total[e] = all;
+        }
+        __syncthreads();
+    }
+    // where each expert begins
+    const int items = (E1 + kSortThreads - 1) / kSortThreads;
+    uint32_t mine = 0;
+    for (int i = 0; i < items; ++i) mine += tid * items + i < E1 ? total[tid * items + i] : 0;
+    uint32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += v;
+    }
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    uint32_t start = upto - mine;
+    for (int w = 0; w < warp; ++w) start += sums[w];
+    for (int i = 0; i < items; ++i) {
+        const int e = tid * items + i;
+        if (e >= E1) break;
+        if (blockIdx.x == 0) p.offsets[e] = (int32_t)start;
+        next[e] += start;
+        start += total[e];
+    }
+    __syncthreads();
+    for (long long from = begin; from < end;) {
+        for (int e = tid; e < E1; e += kSortThreads) {
+            uint32_t at = next[e];
+            for (int w = 0; w < kSortWarps; ++w) {
+                const uint32_t v = hist[w * E1 + e];
+                hist[w * E1 + e] = at;
+                at += v;
+            }
+            next[e] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kSortSteps; ++s) {
+            const long long i = from + (warp * kSortSteps + s) * 32 + lane;
+            if (i - lane >= end) break;
+            if (key[s] >= 0) {
+                const int place = (int)(hist[warp * E1 + key[s]] + __popc(same[s] & ((1u << lane) - 1)));
+                p.slots[i] = key[s] < p.E ? place : -2 - place;
+            }
+            __syncwarp();
+            if (key[s] >= 0 && lane == __ffs(same[s]) - 1) hist[warp * E1 + key[s]] += __popc(same[s]);
+            __syncwarp();
+        }
+        from += kSortBlock;
+        if (from >= end) break;
+        __syncthreads();
+        for (int i = tid; i < kSortWarps * E1; i += kSortThreads) hist[i] = 0;
+        __syncthreads();
+        read(from);
+        __syncthreads();
+    }
+}
+
+static int sort_ctas(long long pairs, long long *per_cta) {
+    const long long blocks = (pairs + kSortBlock - 1) / kSortBlock, per = (blocks + kSortMostCtas - 1) / kSortMostCtas;
+    *per_cta = (per > 0 ? per : 1) * kSortBlock;
+    return blocks > 0 ? (int)((blocks + per - 1) / per) : 1;
+}
+
+// ---- rows
+
+struct RowsParams {
+    const void *x, *y, *residual;        // rows of tokens; rows of experts; added to a token's sum
+    void *out, *out_y;
+    float *out_weights;
+    const int32_t *slots;
+    const float *weights;
+    long long x_row, y_row, res_row, out_row, out_y_row;    // elements
+    int T, k, H, R;
+};
+
+template <typename T> __device__ __forceinline__ float rows_float(T v);
+template <> __device__ __forceinline__ float rows_float(float v) { return v; }
+template <> __device__ __forceinline__ float rows_float(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float rows_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T rows_round(float v);
+template <> __device__ __forceinline__ float rows_round(float v) { return v; }
+template <> __device__ __forceinline__ __half rows_round(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 rows_round(float v) { return __float2bfloat16_rn(v); }
+
+// V neighbouring values of a row, loaded and stored as one.
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Pack {
+    T v[V];
+};
+
+// A thread takes one column of packs of one token.  Block: (columns, tokens).
+struct Place {
+    int t;
+    long long c;
+};
+template <int V>
+__device__ __forceinline__ Place row_place() {
+    return {(int)(blockIdx.x * blockDim.y + threadIdx.y), ((long long)blockIdx.y * blockDim.x + threadIdx.x) * V};
+}
+
+// Copies: T stands for so many bytes.
+template <typename T>
+__global__ void __launch_bounds__(256) rows_to_kernel(const RowsParams p) {
+    grid_dependency_release();
+    grid_dependency_wait();
+    const Place at = row_place<1>();
+    if (at.t >= p.T || at.c >= p.H) return;
+    const T v = load_ordered((const T *)p.x + at.t * p.x_row + at.c);
+    const int32_t *slots = p.slots + (long long)at.t * p.k;
+#pragma unroll 4
+    for (int j = 0; j < p.k; ++j) {
+        const int s = load_ordered(slots + j);
+        if (s >= 0 && s < p.R) ((T *)p.out)[s * p.out_row + at.c] = v;
+    }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
+    constexpr int BATCH = 4;
+    grid_dependency_release();
+    grid_dependency_wait();
+    const Place at = row_place<V>();
+    if (at.t >= p.T || at.c >= p.H) return;
+    const int32_t *slots = p.slots + (long long)at.t * p.k;
+    const float *weights = p.weights ? p.weights + (long long)at.t * p.k : nullptr;
+    float sum[V] = {};
+    if (p.residual) {
+        const Pack<T, V> r = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.residual + at.t * p.res_row + at.c));
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = rows_float(r.v[i]);
+    }
+    for (int j0 = 0; j0 < p.k; j0 += BATCH) {
+        int s[BATCH];
+        float w[BATCH];
+        Pack<T, V> y[BATCH];
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            s[b] = j0 + b < p.k ? load_ordered(slots + j0 + b) : -1;
+            if (s[b] >= p.R) s[b] = -1;
+            w[b] = weights && s[b] >= 0 ? load_ordered(weights + j0 + b) : 1.f;
+        }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+            if (s[b] >= 0) y[b] = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.y + s[b] * p.y_row + at.c));
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+            if (s[b] >= 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] = fmaf(w[b], rows_float(y[b].v[i]), sum[i]);
+            }
+    }
+    Pack<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = rows_round<T>(sum[i]);
+    *reinterpret_cast<Pack<T, V> *>((T *)p.out + at.t * p.out_row + at.c) = o;
+}
+
+// The gradient: a token by blockDim.x threads, which walk along its row; dot products of a batch of choices in registers.
+constexpr int kGradBatch = 8;
+template <typename T, int V>
+__global__ void __launch_bounds__(256) rows_from_grad_kernel(const RowsParams p) {
+    __shared__ float part[8][kGradBatch];
+    grid_dependency_release();
+    grid_dependency_wait();
+    const int t = blockIdx.x * blockDim.y + threadIdx.y;
+    const bool inside = t < p.T;
+    const int lane = threadIdx.x & 31, warp = threadIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5), warps = blockDim.x / 32;
+    const T *g = (const T *)p.x + (inside ? t : 0) * p.x_row;
+    for (int j0 = 0; j0 < p.k; j0 += kGradBatch) {
+        const int some = min(kGradBatch, p.k - j0);
+        const long long pair = (long long)(inside ? t : 0) * p.k + j0;
+        int s[kGradBatch];
+        float w[kGradBatch], dot[kGradBatch];
+#pragma unroll
+        for (int j = 0; j < kGradBatch; ++j) {
+            s[j] = inside && j < some ? load_ordered(p.slots + pair + j) : -1;
+            w[j] = s[j] < 0 ? 0.f : p.weights ? load_ordered(p.weights + pair + j) : 1.f;
+            dot[j] = 0.f;
+        }
+        for (int c = threadIdx.x * V; c < p.H && inside; c += blockDim.x * V) {
+            const Pack<T, V> gv = load_ordered(reinterpret_cast<const Pack<T, V> *>(g + c));
+            Pack<T, V> y[kGradBatch];
+            if (p.weights) {
+#pragma unroll
+                for (int j = 0; j < kGradBatch; ++j)
+                    if (s[j] >= 0 && s[j] < p.R) y[j] = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.y + s[j] * p.y_row + c));
+            }
+#pragma unroll
+            for (int j = 0; j < kGradBatch; ++j) {
+                const int row = s[j] >= 0 ? s[j] : -2 - s[j];          // -1: nowhere
+                if (row < 0 || row >= p.R) continue;
+                Pack<T, V> o;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float v = rows_float(gv.v[i]);
+                    o.v[i] = rows_round<T>(s[j] >= 0 ? w[j] * v : 0.f);
+                    if (p.weights && s[j] >= 0) dot[j] = fmaf(v, rows_float(y[j].v[i]), dot[j]);
+                }
+                *reinterpret_cast<Pack<T, V> *>((T *)p.out_y + row * p.out_y_row + c) = o;
+            }
+        }
+        if (!p.weights) continue;
+#pragma unroll
+        for (int j = 0; j < kGradBatch; ++j) {
+#pragma unroll
+            for (int d = 16; d; d /= 2) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], d);
+            if (lane == 0) part[warp][j] = dot[j];
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < some && inside) {
+            float sum = 0.f;
+            for (int i = 0; i < warps; ++i) sum += part[threadIdx.y * warps + i][threadIdx.x];
+            p.out_weights[pair + threadIdx.x] = sum;
+        }
+        __syncthreads();
+    }
+}
+
+// Threads along a row and tokens per block, of 256 in all; at least `least` along the row.
+static dim3 row_block(long long columns, int least) {
+    int x = least;
+    while (x < 256 && x < columns) x *= 2;
+    return dim3((unsigned)x, (unsigned)(256 / x));
+}
+static dim3 row_grid(const dim3 &block, int T, long long columns) {
+    return dim3((unsigned)((T - 1) / block.y + 1), (unsigned)((columns + block.x - 1) / block.x));
+}
+// The largest of 16, 8, .. `least` bytes that divides them all.
+static int common_bytes(int least, std::initializer_list<long long> all) {
+    int b = 16;
+    for (const auto v : all)
+        while (b > least && v % b) b /= 2;
+    return b;
+}
+
+// A matrix in memory, as the checks of overlap see it.
+struct Region {
+    const void *at;
+    long long row, bytes, rows;          // bytes from row to row, of a row; rows
+};
+static Region vector_region(const void *at, long long bytes) { return {at, bytes, bytes, 1}; }
+// Whether the first overlaps any of the others.
+static bool meets(const Region &a, std::initializer_list<Region> others) {
+    for (const Region &b : others)
+        if (rows_overlap(a.at, a.row, a.bytes, a.rows, b.at, b.row, b.bytes, b.rows)) return true;
+    return false;
+}
+// Strides up to what keeps byte offsets in 64 bits.
+static bool row_ok(long long row, long long H) { return row >= H && row <= (1ll << 40); }
+
+template <typename T>
+static int launch_rows_to(RowsParams p, cudaStream_t st) {
+    const dim3 block = row_block(p.H, 1);
+    return launch_dependent(rows_to_kernel<T>, row_grid(block, p.T, p.H), block, 0, st, p);
+}
+template <typename T, int V>
+static int launch_rows_from(const RowsParams &p, cudaStream_t st) {
+    const long long columns = p.H / V;
+    const dim3 block = row_block(columns, 1);
+    return launch_dependent(rows_from_kernel<T, V>, row_grid(block, p.T, columns), block, 0, st, p);
+}
+template <typename T, int V>
+static int launch_rows_from_grad(const RowsParams &p, cudaStream_t st) {
+    const dim3 block = row_block(p.H / V, 32);
+    return launch_dependent(rows_from_grad_kernel<T, V>, dim3((unsigned)((p.T - 1) / block.y + 1)), block, 0, st, p);
+}
+// Calls f with the type and whether packs of 16 bytes fit.
+template <typename F>
+static int with_rows_type(int type, int bytes, F f) {
+    if (type == HIKONV_OUT_F32) return bytes == 16 ? f(Pack<float, 4>()) : f(Pack<float, 1>());
+    if (type == HIKONV_OUT_F16) return bytes == 16 ? f(Pack<__half, 8>()) : f(Pack<__half, 1>());
+    return bytes == 16 ? f(Pack<__nv_bfloat16, 8>()) : f(Pack<__nv_bfloat16, 1>());
+}
+static bool is_float_type(int type) { return type == HIKONV_OUT_F32 || type == HIKONV_OUT_F16 || type == HIKONV_OUT_BF16; }
+static bool pairs_ok(int T, int k) { return T >= 0 && k >= 1 && (long long)T * k <= (1 << 30); }
+
+}  // namespace hikonv
+
+using namespace hikonv;
+
+extern "C" size_t hikonv_sort_by_expert_workspace_bytes(int T, int k, int E) {
+    if (!pairs_ok(T, k) || E < 1 || E > HIKONV_MAX_GROUPS) return 0;
+    long long per;
+    const int ctas = sort_ctas((long long)T * k, &per);
+    return ctas > 1 ? (size_t)ctas * (E + 1) * 4 : 0;
+}
+
+extern "C" int hikonv_sort_by_expert(const void *d_experts, int index_bytes, long long experts_row_stride, int T, int k, int E, int32_t *d_offsets,
+                                     int32_t *d_slots, void *d_workspace, size_t workspace_bytes, void *stream) {
+    if ((index_bytes != 4 && index_bytes != 8) || T < 0 || k < 1 || E < 1) return HIKONV_ERR_INVALID_ARG;
+    if (!pairs_ok(T, k) || E > HIKONV_MAX_GROUPS) return HIKONV_ERR_UNSUPPORTED;
+    if (T <= 1) experts_row_stride = k;
+    if (!d_offsets || (T > 0 && (!d_experts || !d_slots)) || experts_row_stride < 0 || experts_row_stride > (1ll << 40)) return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_experts % index_bytes || (uintptr_t)d_offsets % 4 || (uintptr_t)d_slots % 4) return HIKONV_ERR_INVALID_ARG;
+    const long long pairs = (long long)T * k;
+    SortParams p{d_experts, index_bytes == 8, experts_row_stride, pairs, k, E, 1, 0, d_offsets, d_slots, nullptr};
+    p.ctas = sort_ctas(pairs, &p.per_cta);
+    const long long counts = p.ctas > 1 ? (long long)p.ctas * (E + 1) * 4 : 0;
+    const Region experts{d_experts, experts_row_stride * index_bytes, (long long)k * index_bytes, T}, offsets = vector_region(d_offsets, (E + 1) * 4ll),
+        slots = vector_region(d_slots, pairs * 4), space = vector_region(d_workspace, counts);
+    if (T > 0 && (meets(experts, {offsets, slots}) || meets(offsets, {slots}))) return HIKONV_ERR_INVALID_ARG;
+    if (counts) {
+        if (!d_workspace || (uintptr_t)d_workspace % 4 || workspace_bytes < (size_t)counts) return HIKONV_ERR_WORKSPACE;
+        if (meets(space, {experts, offsets, slots})) return HIKONV_ERR_INVALID_ARG;
+        p.counts = (uint32_t *)d_workspace;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    if (p.counts) {
+        const int rc = launch_dependent(sort_count_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), (size_t)(E + 1) * 4, st, p);
+        if (rc != HIKONV_OK) return rc;
+    }
+    const size_t smem = ((size_t)(kSortWarps + 2) * (E + 1) + kSortWarps) * 4;
+    return with_dynamic_smem((const void *)sort_place_kernel, smem,
+                             [&] { return launch_dependent(sort_place_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), smem, st, p); });
+}
+
+extern "C" int hikonv_rows_to_experts(const void *d_x, int element_bytes, long long x_row_stride, const int32_t *d_slots, int T, int k, int H, void *d_out,
+                                      long long out_row_stride, int R, void *stream) {
+    if ((element_bytes != 1 && element_bytes != 2 && element_bytes != 4) || T < 0 || k < 1 || H < 1 || R < 0) return HIKONV_ERR_INVALID_ARG;
+    if (!pairs_ok(T, k) || H > (1 << 23)) return HIKONV_ERR_UNSUPPORTED;
+    if (T == 0 || R == 0) return HIKONV_OK;
+    if (T == 1) x_row_stride = H;
+    if (R == 1) out_row_stride = H;
+    // a stride of 0: all tokens' rows are one
+    if (!d_x || !d_slots || !d_out || x_row_stride < 0 || x_row_stride > (1ll << 40) || !row_ok(out_row_stride, H)) return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_x % element_bytes || (uintptr_t)d_out % element_bytes || (uintptr_t)d_slots % 4) return HIKONV_ERR_INVALID_ARG;
+    const long long size = element_bytes;
+    if (meets({d_out, out_row_stride * size, H * size, R}, {{d_x, x_row_stride * size, H * size, T}, vector_region(d_slots, (long long)T * k * 4)}))
+        return HIKONV_ERR_INVALID_ARG;
+    const int bytes = common_bytes(element_bytes, {(long long)(uintptr_t)d_x, (long long)(uintptr_t)d_out, x_row_stride * size, out_row_stride * size, H * size});
+    const int per = bytes / element_bytes;
+    RowsParams p{};
+    p.x = d_x; p.out = d_out; p.slots = d_slots;
+    p.x_row = x_row_stride / per; p.out_row = out_row_stride / per;
+    p.T = T; p.k = k; p.H = H / per; p.R = R;
+    cudaStream_t st = (cudaStream_t)stream;
+    switch (bytes) {
+        case 16: return launch_rows_to<uint4>(p, st);
+        case 8: return launch_rows_to<uint2>(p, st);
+        case 4: return launch_rows_to<uint32_t>(p, st);
+        case 2: return launch_rows_to<uint16_t>(p, st);
+        default: return launch_rows_to<uint8_t>(p, st);
+    }
+}
+
+extern "C" int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, int R, const int32_t *d_slots, const float *d_weights, int T, int k,
+                                        int H, const void *d_residual, long long residual_row_stride, void *d_out, long long out_row_stride, void *stream) {
+    if (!is_float_type(type) || T < 0 || k < 1 || H < 1 || R < 0) return HIKONV_ERR_INVALID_ARG;
+    if (!pairs_ok(T, k) || H > (1 << 23)) return HIKONV_ERR_UNSUPPORTED;
+    if (T == 0) return HIKONV_OK;
+    const int size = type == HIKONV_OUT_F32 ? 4 : 2;
+    if (T == 1) residual_row_stride = out_row_stride = H;
+    if (R <= 1) y_row_stride = H;
+    if (!d_residual) residual_row_stride = H;
+    if ((!d_y && R > 0) || !d_slots || !d_out || y_row_stride < 0 || y_row_stride > (1ll << 40) || !row_ok(residual_row_stride, H) || !row_ok(out_row_stride, H))
+        return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_y % size || (uintptr_t)d_out % size || (uintptr_t)d_residual % size || (uintptr_t)d_slots % 4 || (uintptr_t)d_weights % 4)
+        return HIKONV_ERR_INVALID_ARG;
+    const Region y{d_y, y_row_stride * size, H * size, R}, out{d_out, out_row_stride * size, H * size, T}, residual{d_residual, residual_row_stride * size, H * size, T},
+        slots = vector_region(d_slots, (long long)T * k * 4), weights = vector_region(d_weights, (long long)T * k * 4);
+    if (meets(out, {y, slots, weights}) || (!(d_residual == d_out && residual_row_stride == out_row_stride) && meets(out, {residual})))
+        return HIKONV_ERR_INVALID_ARG;
+    RowsParams p{};
+    p.y = d_y; p.residual = d_residual; p.out = d_out; p.slots = d_slots; p.weights = d_weights;
+    p.y_row = y_row_stride; p.res_row = residual_row_stride; p.out_row = out_row_stride;
+    p.T = T; p.k = k; p.H = H; p.R = R;
+    const int bytes = common_bytes(size, {(long long)(uintptr_t)d_y, (long long)(uintptr_t)d_out, (long long)(uintptr_t)d_residual, y.row, residual.row, out.row, y.bytes});
+    cudaStream_t st = (cudaStream_t)stream;
+    return with_rows_type(type, bytes, [&](auto pack) {
+        return launch_rows_from<std::remove_reference_t<decltype(pack.v[0])>, sizeof(pack) / sizeof(pack.v[0])>(p, st);
+    });
+}
+
+extern "C" int hikonv_rows_from_experts_grad(const void *d_grad, int type, long long grad_row_stride, const void *d_y, long long y_row_stride, int R,
+                                             const int32_t *d_slots, const float *d_weights, int T, int k, int H, void *d_grad_y,
+                                             long long grad_y_row_stride, float *d_grad_weights, void *stream) {
+    if (!is_float_type(type) || T < 0 || k < 1 || H < 1 || R < 0) return HIKONV_ERR_INVALID_ARG;
+    if (!pairs_ok(T, k) || H > (1 << 23)) return HIKONV_ERR_UNSUPPORTED;
+    if ((d_weights != nullptr) != (d_grad_weights != nullptr)) return HIKONV_ERR_INVALID_ARG;
+    if (T == 0) return HIKONV_OK;
+    const int size = type == HIKONV_OUT_F32 ? 4 : 2;
+    const long long pairs = (long long)T * k;
+    if (T == 1) grad_row_stride = H;
+    if (R <= 1) y_row_stride = grad_y_row_stride = H;
+    if (!d_weights) y_row_stride = H;
+    // strides of 0: one row for all
+    if (!d_grad || !d_slots || (R > 0 && (!d_grad_y || (d_weights && !d_y)))) return HIKONV_ERR_INVALID_ARG;
+    if (grad_row_stride < 0 || grad_row_stride > (1ll << 40) || y_row_stride < 0 || y_row_stride > (1ll << 40) || !row_ok(grad_y_row_stride, H))
+        return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_grad % size || (d_weights && (uintptr_t)d_y % size) || (uintptr_t)d_grad_y % size || (uintptr_t)d_slots % 4 ||
+        (uintptr_t)d_weights % 4 || (uintptr_t)d_grad_weights % 4)
+        return HIKONV_ERR_INVALID_ARG;
+    const long long bytes_of_row = (long long)H * size;
+    const Region grad{d_grad, grad_row_stride * size, bytes_of_row, T}, y{d_weights ? d_y : nullptr, y_row_stride * size, bytes_of_row, R},
+        grad_y{d_grad_y, grad_y_row_stride * size, bytes_of_row, R}, slots = vector_region(d_slots, pairs * 4), weights = vector_region(d_weights, pairs * 4),
+        grad_weights = vector_region(d_grad_weights, pairs * 4);
+    if (meets(grad_y, {grad, y, slots, weights, grad_weights}) || meets(grad_weights, {grad, y, slots, weights})) return HIKONV_ERR_INVALID_ARG;
+    RowsParams p{};
+    p.x = d_grad; p.y = d_y; p.out_y = d_grad_y; p.out_weights = d_grad_weights; p.slots = d_slots; p.weights = d_weights;
+    p.x_row = grad_row_stride; p.y_row = y_row_stride; p.out_y_row = grad_y_row_stride;
+    p.T = T; p.k = k; p.H = H; p.R = R;
+    const int bytes = common_bytes(size, {(long long)(uintptr_t)grad.at, (long long)(uintptr_t)y.at, (long long)(uintptr_t)grad_y.at, grad.row, y.row, grad_y.row,
+                                          bytes_of_row});
+    cudaStream_t st = (cudaStream_t)stream;
+    return with_rows_type(type, bytes, [&](auto pack) {
+        return launch_rows_from_grad<std::remove_reference_t<decltype(pack.v[0])>, sizeof(pack) / sizeof(pack.v[0])>(p, st);
+    });
+}

@@ -63,6 +63,22 @@ int move_period(const hikonv_layout_t &L, const SplitConsts &sc, int p, int q, i
 // after a group's last channel included) with cf channels between two, or 0 when the groups' sums may not be added while packed.
 int most_split_moves(const hikonv_layout_t &L, const SplitConsts &sc, int p, int q, int f_signed, int g_signed, int K, int cf, int groups, bool packed_add);
 
+// Whether two memory ranges have a byte in common.
+inline bool overlap(const void *a, size_t an, const void *b, size_t bn) {
+    return a && b && an && bn && (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
+// Bytes from the first of so many rows to the last one's end.
+inline size_t rows_extent(size_t rows, size_t row, size_t bytes) { return rows ? (rows - 1) * row + bytes : 0; }
+// Whether two matrices of a_rows and b_rows rows, so many bytes apart and long, have a byte in common.  Rows equally far apart (and no longer)
+// may lie between one another, as columns of one buffer do; where the distances differ, the ranges from the first byte to the last must be apart.
+inline bool rows_overlap(const void *a, size_t a_row, size_t a_bytes, size_t a_rows, const void *b, size_t b_row, size_t b_bytes, size_t b_rows) {
+    if (!overlap(a, rows_extent(a_rows, a_row, a_bytes), b, rows_extent(b_rows, b_row, b_bytes))) return false;
+    if (a_rows == 1 || b_rows == 1 || a_row != b_row || a_row < a_bytes || b_row < b_bytes) return true;
+    const size_t ahead = (uintptr_t)b >= (uintptr_t)a ? ((uintptr_t)b - (uintptr_t)a) % a_row
+                                                      : (a_row - ((uintptr_t)a - (uintptr_t)b) % a_row) % a_row;    // of b's rows to a's before
+    return ahead < a_bytes || ahead + b_bytes > a_row;
+}
+
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Words per packed kernel row in the 2-D kernels' shared memory, and the cap on channels per stage that

@@ -10,19 +10,6 @@ namespace hikonv {
 static size_t element_bytes(int out_type) {
     return out_type == HIKONV_OUT_CODES ? 1 : out_type == HIKONV_OUT_SUMS || out_type == HIKONV_OUT_F32 ? 4 : 2;
 }
-// Whether two memory ranges have a byte in common.
-static bool overlap(const void *a, size_t an, const void *b, size_t bn) {
-    return a && b && an && bn && (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
-}
-// Whether two matrices of M rows, so many bytes apart and long (no longer than apart), have a byte in common.  Rows equally far apart may lie
-// between one another, as columns of one buffer do; where the distances differ, the ranges from the first byte to the last must be apart.
-static bool rows_overlap(const void *a, size_t a_row, size_t a_bytes, const void *b, size_t b_row, size_t b_bytes, size_t M) {
-    if (!overlap(a, (M - 1) * a_row + a_bytes, b, (M - 1) * b_row + b_bytes)) return false;
-    if (M == 1 || a_row != b_row) return true;
-    const size_t ahead = (uintptr_t)b >= (uintptr_t)a ? ((uintptr_t)b - (uintptr_t)a) % a_row
-                                                      : (a_row - ((uintptr_t)a - (uintptr_t)b) % a_row) % a_row;    // of b's rows to a's before
-    return ahead < a_bytes || ahead + b_bytes > a_row;
-}
 
 static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_bits, const int32_t *d_offsets, int grouped, int E, int M,
                       int N, int K, int p, int q, int xs, int ws, void *d_out, long long out_row, const hikonv_epilogue_t *ep, void *workspace, size_t workspace_bytes,
@@ -57,12 +44,12 @@ static int linear_run(const void *d_x, long long x_row, const void *d_w, int w_b
         return HIKONV_ERR_INVALID_ARG;
     const long long w_row = (long long)K * w_bits / 8;
     const size_t out_bytes = ((size_t)(M - 1) * out_row + N) * elem, columns = (size_t)E * N * 4;
-    if (rows_overlap(d_out, out_row * elem, N * elem, d_x, x_row, K, M) || overlap(d_out, out_bytes, d_w, (size_t)E * N * w_row) ||
+    if (rows_overlap(d_out, out_row * elem, N * elem, M, d_x, x_row, K, M) || overlap(d_out, out_bytes, d_w, (size_t)E * N * w_row) ||
         overlap(d_out, out_bytes, d_offsets, ((size_t)E + 1) * 4) || overlap(d_out, out_bytes, ep->d_x_scale, (size_t)M * 4) ||
         overlap(d_out, out_bytes, ep->d_w_scale, columns) || overlap(d_out, out_bytes, ep->d_bias, columns))
         return HIKONV_ERR_INVALID_ARG;
     if (ep->d_residual && !(ep->d_residual == d_out && res_row == out_row) &&
-        rows_overlap(d_out, out_row * elem, N * elem, ep->d_residual, res_row * elem, N * elem, M))
+        rows_overlap(d_out, out_row * elem, N * elem, M, ep->d_residual, res_row * elem, N * elem, M))
         return HIKONV_ERR_INVALID_ARG;
 
     LinearParams k;
@@ -132,9 +119,11 @@ extern "C" int hikonv_linear_wait_timeouts(unsigned int *h_count) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices || cudaDeviceSynchronize() != cudaSuccess) return HIKONV_ERR_CUDA;
     std::lock_guard<std::mutex> lock(mutex);
-    unsigned int total = 0;
-    const int rc = read_linear_timeouts(&total);
+    unsigned int total = 0, of_f8 = 0;
+    int rc = read_linear_timeouts(&total);
+    if (rc == HIKONV_OK) rc = read_linear_f8_timeouts(&of_f8);
     if (rc != HIKONV_OK) return rc;
+    total += of_f8;
     *h_count = total - told[dev];
     told[dev] = total;
     return HIKONV_OK;

@@ -38,6 +38,7 @@ int sm_count_here();                                         // of the current d
 size_t linear_tc_workspace(const LinearParams &p);           // bytes, 16-byte aligned, for rows that do not start on such boundaries
 int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cudaStream_t st);
 int read_linear_timeouts(unsigned int *h_count);             // on the current device, since it was loaded
+int read_linear_f8_timeouts(unsigned int *h_count);          // likewise, of hikonv_linear_f8.cu
 int launch_linear_wait_check(long long cycles, cudaStream_t st);
 
 }  // namespace hikonv

@@ -1,0 +1,715 @@
+// hikonv_linear_f8, hikonv_grouped_linear_f8: matrix products of 8-bit floating point numbers with a scale for each block of 128 along the
+// depth, on the tensor cores (tcgen05.mma kind::f8f6f4, 32-bit sums in tensor memory), operands staged in shared memory by TMA.
+//
+// A step is a block of 128: its products are summed by the tensor cores from zero, and warps of their own take the sums from tensor memory
+// and add them, times x_scale[b][m] w_scale[n / 128][b], to 32-bit sums in registers while the next blocks are multiplied.
+//
+// The 128 lanes of tensor memory are rows of x on long inputs (TOKENS: a lane has one scale per step, and a thread's sums are
+// neighbours in a row of the output) and output columns where rows are few (the number of rows is then that of the instruction's
+// columns, any multiple of 16, and the CTAs of a cluster may share the depth of a tile).
+//
+// One CTA per SM walks over the tiles.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 add up and finish.
+#include <cstddef>
+#include <cstring>
+
+#include "hikonv_linear_tiles.cuh"
+
+namespace hikonv {
+
+constexpr int kF8Rows = 128, kF8Depth = 128;
+constexpr int kF8MostStages = 12, kF8MostAccs = 8;
+constexpr int kF8FirstAdder = 4, kF8Adders = 8, kF8Threads = (kF8FirstAdder + kF8Adders) * 32;
+constexpr int kF8Ahead = 8;                             // steps whose scales of x are on their way
+constexpr size_t kF8MostSmem = 226 * 1024;
+
+struct F8Params {
+    LinearParams p;
+    long long xs_row;                    // elements from block to block of x_scale
+    int nt, width;                       // rows of x and output columns per tile
+    int m_tiles, n_blocks, tokens_first;
+    int chunks, w_blocks;                // blocks of the depth; of the output columns, 128 each
+    int splits, split_shift;
+    int stages, stage_bytes, b_off;
+    int acc_cols, accs, tmem_cols;
+    uint32_t idesc;
+    int feed_off, turn_off, held;        // behind the stages: the adders' scales; their buffers for turning outputs; the tables of the groups
+    int whole_stores;                    // rows of out and residual on 32-byte boundaries
+    long long wait_cycles;
+};
+
+struct F8Control {
+    uint64_t full[kF8MostStages], empty[kF8MostStages], acc_full[kF8MostAccs], acc_empty[kF8MostAccs], drain;
+    uint32_t tmem;
+    int whole;                           // no wait of this CTA has run out
+};
+
+static __device__ unsigned int linear_f8_timeouts;
+
+__device__ __forceinline__ void f8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[8]) { tc_load_columns(taddr, v); }
+__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[16]) { tc_load16(taddr, v); }
+__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+                 "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]),
+                   "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]),
+                   "=r"(v[30]), "=r"(v[31])
+                 : "r"(taddr));
+}
+// The wait for tcgen05.ld, which what it loaded goes through: no arithmetic on it can be moved in front.
+template <int N>
+__device__ __forceinline__ void f8_loaded(uint32_t (&v)[N]) {
+    tc_wait_load();
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
+}
+__device__ __forceinline__ uint64_t f8_two(uint32_t a, uint32_t b) { return (uint64_t)b << 32 | a; }
+__device__ __forceinline__ uint64_t f8_two(float a, float b) { return f8_two(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ uint64_t f8_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t f8_mul(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float f8_low(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float f8_high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ float4 load_cluster_float4(uint32_t remote) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote));
+    return v;
+}
+__device__ __forceinline__ void load_global32(const void *a, uint32_t (&v)[8]) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(a)
+                 : "memory");
+}
+__device__ __forceinline__ void store_global32(void *a, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+                 "r"(v[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ bool f8_wait(const F8Params &q, uint32_t bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
+}
+
+// A warp that adds up: the 32 lanes of its quarter, CPW of the columns.  Sums are pairs of floats.
+template <bool TOKENS, int CPW>
+struct Adder {
+    const F8Params &q;
+    const uint32_t tmem, acc_full, acc_empty;
+    const int c0, c1;
+    uint8_t *const feed;                 // this warp's: kF8Ahead slots of scales
+    int lane, quad, half;
+    Ring acc;
+    uint64_t sum[CPW / 2];
+    float ws, ws_next;                   // w_scale of 32 steps, a lane each
+
+    static constexpr int kSlot = (TOKENS ? 32 : CPW < 32 ? 32 : CPW) * 4;
+
+    __device__ __forceinline__ Adder(const F8Params &q_, uint32_t tmem_, uint32_t full, uint32_t empty, int c0_, int c1_, uint8_t *feeds)
+        : q(q_), tmem(tmem_), acc_full(full), acc_empty(empty), c0(c0_), c1(c1_),
+          feed(feeds + ((threadIdx.x >> 5) - kF8FirstAdder) * (kF8Ahead * kSlot)) {
+        lane = threadIdx.x & 31;
+        quad = (threadIdx.x >> 5) & 3;
+        half = ((threadIdx.x >> 5) - kF8FirstAdder) >> 2;
+    }
+    __device__ __forceinline__ const float *w_scales(const Tile &t) const {
+        const int nb = min((t.n0 + (TOKENS ? half * CPW : 0)) / kF8Depth, q.w_blocks - 1);
+        return q.p.w_scale + ((long long)t.e * q.w_blocks + nb) * q.chunks;
+    }
+    // x_scale of step c on its way to its slot: of this lane's row, or of the warp's columns.
+    __device__ __forceinline__ void ask(const Tile &t, int c) {
+        if (c < c1) {
+            const float *src = q.p.x_scale + c * q.xs_row + t.row0;
+            uint8_t *to = feed + ((c - c0) % kF8Ahead) * kSlot;
+            constexpr int COUNT = TOKENS ? 32 : CPW;
+#pragma unroll
+            for (int i = 0; i < COUNT; i += 32) {
+                const int row = TOKENS ? quad * 32 + lane : half * CPW + i + lane;
+                if (i + lane < COUNT && row < t.rows) cp_async_4(to + (i + lane) * 4, src + row, 4);
+            }
+        }
+        cp_async_commit();
+    }
+    // What a tile's first steps need, asked for before the tile before is finished.
+    __device__ __forceinline__ void begin(const Tile &t) {
+        const float *w = w_scales(t);
+        ws_next = c0 + lane < c1 ? load_ordered(w + c0 + lane) : 0.f;
+        if (!TOKENS) __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kF8Ahead; ++i) ask(t, c0 + i);
+    }
+    __device__ __forceinline__ bool add(const Tile &t) {
+        constexpr int CH = CPW < 32 ? CPW : 32;
+        const float *w = w_scales(t);
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) sum[i] = 0;
+        for (int c = c0; c < c1; ++c) {
+            const int at = (c - c0) & 31;
+            if (at == 0) {
+                ws = ws_next;
+                ws_next = c + 32 + lane < c1 ? load_ordered(w + c + 32 + lane) : 0.f;
+            }
+            if (!f8_wait(q, acc_full + 8 * acc.stage, acc.phase)) return false;
+            tc_fence_after();
+            const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16) + half * CPW;
+            uint32_t v[2][CH];
+            f8_load(d, v[0]);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kF8Ahead - 1) : "memory");
+            if (!TOKENS) __syncwarp();
+            const uint8_t *slot = feed + ((c - c0) % kF8Ahead) * kSlot;
+            const float w1 = __shfl_sync(0xFFFFFFFFu, ws, at);
+            float s = w1;
+            if (TOKENS) s *= *reinterpret_cast<const volatile float *>(slot + lane * 4);
+            const uint64_t ss = f8_two(s, s);
+#pragma unroll
+            for (int i = 0; i < CPW; i += CH) {
+                uint32_t(&now)[CH] = v[(i / CH) & 1];
+                f8_loaded(now);
+                if (i + CH < CPW) {
+                    f8_load(d + i + CH, v[(i / CH + 1) & 1]);
+                } else {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbarrier_arrive(acc_empty + 8 * acc.stage);
+                }
+#pragma unroll
+                for (int k = 0; k < CH; k += 4) {
+                    uint64_t s01 = ss, s23 = ss;
+                    if (!TOKENS) {
+                        const float4 xs = *reinterpret_cast<const float4 *>(slot + (i + k) * 4);
+                        s01 = f8_mul(f8_two(xs.x, xs.y), ss);
+                        s23 = f8_mul(f8_two(xs.z, xs.w), ss);
+                    }
+                    uint64_t *o = sum + (i + k) / 2;
+                    o[0] = f8_fma(f8_two(now[k], now[k + 1]), s01, o[0]);
+                    o[1] = f8_fma(f8_two(now[k + 2], now[k + 3]), s23, o[1]);
+                }
+            }
+            if (!TOKENS) __syncwarp();                  // all lanes have read the slot
+            ask(t, c + kF8Ahead);
+            acc.next(q.accs);
+        }
+        return true;
+    }
+    template <int ACT>
+    __device__ __forceinline__ void activate_as() {
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) sum[i] = f8_two(activate(f8_low(sum[i]), ACT), activate(f8_high(sum[i]), ACT));
+    }
+    __device__ __forceinline__ void activate_all() {
+        switch (q.p.act) {
+            case HIKONV_ACT_RELU: activate_as<HIKONV_ACT_RELU>(); break;
+            case HIKONV_ACT_SILU: activate_as<HIKONV_ACT_SILU>(); break;
+            case HIKONV_ACT_GELU: activate_as<HIKONV_ACT_GELU>(); break;
+            default: break;
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? f8_high(sum[i / 2]) : f8_low(sum[i / 2]); }
+
+    // Lanes are output columns: each row of x is written by neighbouring lanes.
+    template <typename T>
+    __device__ __forceinline__ void store_columns(const Tile &t) {
+        const LinearParams &p = q.p;
+        const int n = t.n0 + quad * 32 + lane;
+        if (n >= p.N) return;
+        const int left = t.rows - half * CPW;
+        const long long m = t.row0 + half * CPW;
+        T *o = (T *)p.out + m * p.out_row + n;
+        const T *r = (const T *)p.residual + m * p.res_row + n;
+#pragma unroll
+        for (int i0 = 0; i0 < CPW; i0 += 8) {
+            if (i0 >= left) break;
+            T res[8];
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i0 + i < left) res[i] = load_ordered(r + (i0 + i) * p.res_row);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < left) from_float(p.residual ? at(i0 + i) + to_float(res[i]) : at(i0 + i), o + (i0 + i) * p.out_row);
+        }
+    }
+    // Lanes are rows of x: 32 bytes of a row at a time where rows begin on such a boundary, else 16 columns of 32 rows, turned in shared
+    // memory so that neighbouring lanes write neighbouring columns.
+    template <typename T>
+    __device__ __forceinline__ void store_rows(const Tile &t, float *turn) {
+        const LinearParams &p = q.p;
+        const int row = quad * 32 + lane, n = t.n0 + half * CPW;
+        const long long m = t.row0 + row;
+        if (q.whole_stores && n + CPW <= p.N) {
+            constexpr int PER = 32 / sizeof(T);
+            if (row >= t.rows) return;
+            T *o = (T *)p.out + m * p.out_row + n;
+            const T *r = (const T *)p.residual + m * p.res_row + n;
+#pragma unroll
+            for (int i0 = 0; i0 < CPW; i0 += PER) {
+                union { uint32_t w[8]; T v[PER]; } y, x;
+                if (p.residual) load_global32(r + i0, x.w);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) from_float(p.residual ? at(i0 + i) + to_float(x.v[i]) : at(i0 + i), &y.v[i]);
+                store_global32(o + i0, y.w);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i0 = 0; i0 < CPW; i0 += 16) {
+            if (n + i0 >= p.N) break;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = at(i0 + i);
+            __syncwarp();
+            const int col = n + i0 + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
+                if (there >= t.rows || col >= p.N) continue;
+                float y = turn[mine * 17 + (lane & 15)];
+                if (p.residual) y += to_float(load_ordered((const T *)p.residual + (t.row0 + there) * p.res_row + col));
+                from_float(y, (T *)p.out + (t.row0 + there) * p.out_row + col);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(const Tile &t, float *turn) {
+        const LinearParams &p = q.p;
+        if (p.bias) {
+            const float *bias = (const float *)p.bias + (long long)t.e * p.N;
+            if (TOKENS) {
+                const int n = t.n0 + half * CPW;
+#pragma unroll
+                for (int i = 0; i < CPW; i += 2) {
+                    const float b0 = n + i < p.N ? load_ordered(bias + n + i) : 0.f, b1 = n + i + 1 < p.N ? load_ordered(bias + n + i + 1) : 0.f;
+                    sum[i / 2] = f8_two(f8_low(sum[i / 2]) + b0, f8_high(sum[i / 2]) + b1);
+                }
+            } else {
+                const int n = t.n0 + quad * 32 + lane;
+                const float b = n < p.N ? load_ordered(bias + n) : 0.f;
+#pragma unroll
+                for (int i = 0; i < CPW / 2; ++i) sum[i] = f8_two(f8_low(sum[i]) + b, f8_high(sum[i]) + b);
+            }
+        }
+        activate_all();
+        auto store = [&](auto type) {
+            using T = decltype(type);
+            if (TOKENS) store_rows<T>(t, turn);
+            else store_columns<T>(t);
+        };
+        switch (p.out_type) {
+            case HIKONV_OUT_F32: store(float()); break;
+            case HIKONV_OUT_F16: store(__half()); break;
+            default: store(__nv_bfloat16()); break;
+        }
+    }
+};
+
+// With a shared depth: this CTA's sums go to shared memory, [row of x][output column], over the stages (all that was loaded has been multiplied when
+// the last sums are there); after the cluster's barrier the CTA finishes its share of the columns, four of a row per thread at a time, adding the
+// parts in the order of the depth.
+template <typename T>
+__device__ __forceinline__ void finish_parts(const F8Params &q, const Tile &tile, int rank, uint32_t part) {
+    const LinearParams &p = q.p;
+    const int tid = threadIdx.x - kF8FirstAdder * 32;
+    const int lanes = (kF8Rows / 4) >> q.split_shift, own = (rank * lanes + (tid & (lanes - 1))) * 4, step = kF8Adders * 32 / lanes;
+    const int n = tile.n0 + own, inside = max(0, min(4, p.N - n));
+    uint32_t from[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) from[r] = remote_address(part + own * 4, r < q.splits ? r : 0);
+    float bias[4] = {};
+    if (p.bias) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < inside) bias[k] = load_ordered((const float *)p.bias + (long long)tile.e * p.N + n + k);
+    }
+    for (int i = tid / lanes; i < tile.rows; i += step) {
+        float res[4] = {};
+        if (p.residual) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < inside) res[k] = to_float(load_ordered((const T *)p.residual + (tile.row0 + i) * p.res_row + n + k));
+        }
+        float4 v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < q.splits) v[r] = load_cluster_float4(from[r] + i * kF8Rows * 4);
+        float s[4] = {};
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < q.splits) s[0] += v[r].x, s[1] += v[r].y, s[2] += v[r].z, s[3] += v[r].w;
+        T *o = (T *)p.out + (tile.row0 + i) * p.out_row + n;
+        T y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            s[k] = activate(s[k] + bias[k], p.act);
+            from_float(p.residual ? s[k] + res[k] : s[k], &y[k]);
+        }
+        if (inside == 4 && (uintptr_t)o % (4 * sizeof(T)) == 0) {
+            struct alignas(4 * sizeof(T)) Four { T v[4]; } four;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) four.v[k] = y[k];
+            *reinterpret_cast<Four *>(o) = four;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < inside) o[k] = y[k];
+        }
+    }
+}
+
+template <bool TOKENS, int CPW>
+__global__ void __launch_bounds__(kF8Threads, 1)
+    linear_f8_kernel(const __grid_constant__ F8Params q, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    F8Control &ctl = *reinterpret_cast<F8Control *>(dynamic);
+    const uint32_t control = smem_address(dynamic);
+#define HIKONV_BAR(name, i) (control + (uint32_t)offsetof(F8Control, name) + 8u * (uint32_t)(i))
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    const LinearParams &p = q.p;
+    const uint32_t stages = (control + (uint32_t)sizeof(F8Control) + 1023u) & ~1023u;
+    uint8_t *const area = dynamic + (stages - control);
+    int2 *group_row = reinterpret_cast<int2 *>(area + q.held);
+    int *group_tiles = reinterpret_cast<int *>(group_row + p.E);
+    const GroupTables tables{group_row, group_tiles};
+
+    if (warp == 0) {
+        if (lane < q.stages) {
+            mbarrier_init(HIKONV_BAR(full, lane), 1);
+            mbarrier_init(HIKONV_BAR(empty, lane), 1);
+        }
+        if (lane < q.accs) {
+            mbarrier_init(HIKONV_BAR(acc_full, lane), 1);
+            mbarrier_init(HIKONV_BAR(acc_empty, lane), kF8Adders);
+        }
+        if (lane == 0) {
+            mbarrier_init(HIKONV_BAR(drain, 0), 1);
+            ctl.whole = 1;
+        }
+        mbarrier_init_fence();
+        if (lane == 3) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        }
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(q.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl.tmem;
+    // Not before this CTA has its tensor memory: a CTA of the kernel behind that came to this SM first could take it, and wait for this
+    // one to end while this one waits for the memory.
+    grid_dependency_release();
+    grid_dependency_wait();
+    int tiles = q.m_tiles * q.n_blocks;
+    if (p.offsets) tiles = build_group_tables(q, group_row, group_tiles);
+    const int rank = blockIdx.x & (q.splits - 1), t0 = blockIdx.x >> q.split_shift, step = gridDim.x >> q.split_shift;
+    const int c0 = (int)(((long long)q.chunks * rank) >> q.split_shift), c1 = (int)(((long long)q.chunks * (rank + 1)) >> q.split_shift);
+
+    bool fine = true;
+    if (warp < kF8FirstAdder) {
+        if constexpr (CPW == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 0) {
+            Ring ring;
+            int loads = 0;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tile(q, tables, t, q.width);
+                const int w_row = tile.e * p.N + tile.n0;
+                for (int c = c0; c < c1; ++c) {
+                    fine = f8_wait(q, HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
+                    if (!fine) break;
+                    if (elect_one()) {
+                        const uint32_t at = stages + ring.stage * q.stage_bytes, bar = HIKONV_BAR(full, ring.stage);
+                        mbarrier_arrive_expect(bar, (uint32_t)(kF8Rows + (TOKENS ? q.width : q.nt)) * kF8Depth);
+                        tma_load_2d(at, &map_a, c * kF8Depth, TOKENS ? tile.row0 : w_row, bar);
+                        tma_load_2d(at + q.b_off, &map_b, c * kF8Depth, TOKENS ? w_row : tile.row0, bar);
+                    }
+                    ++loads;
+                    ring.next(q.stages);
+                }
+            }
+            // what is in flight has to land before the memory goes: the last load of every stage
+            for (int i = 0; i < q.stages && i < loads; ++i) {
+                ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+                if (ring.stage == q.stages - 1) ring.phase ^= 1;
+                fine &= f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+            }
+        } else if (warp == 1) {
+            Ring ring, acc;
+            const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + q.b_off);
+            const uint32_t stage_units = (uint32_t)q.stage_bytes >> 4;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tile(q, tables, t, q.width);
+                const int columns = TOKENS ? min(q.width, p.N - tile.n0) : tile.rows;
+                const uint32_t idesc = q.idesc | ((uint32_t)((columns + 15) & ~15) >> 3 << 17);
+                for (int c = c0; c < c1; ++c) {
+                    fine = f8_wait(q, HIKONV_BAR(acc_empty, acc.stage), acc.phase ^ 1) && f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+                    if (!fine) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t a = a0 + ring.stage * stage_units, b = b0 + ring.stage * stage_units;
+                        const uint32_t d = tmem + acc.stage * q.acc_cols;
+#pragma unroll
+                        for (int k = 0; k < kF8Depth / 32; ++k) f8_mma(d, a + k * 2, b + k * 2, idesc, k > 0);
+                        tc_commit(HIKONV_BAR(empty, ring.stage));
+                        tc_commit(HIKONV_BAR(acc_full, acc.stage));
+                    }
+                    ring.next(q.stages);
+                    acc.next(q.accs);
+                }
+            }
+            if (!fine) {                                // multiplies in flight read shared memory and write tensor memory
+                if (elect_one()) tc_commit(HIKONV_BAR(drain, 0));
+                f8_wait(q, HIKONV_BAR(drain, 0), 0);
+            }
+        }
+        if (q.splits > 1) {
+            if (!fine) ctl.whole = 0;
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();                         // the others may still read this CTA's part
+        }
+    } else {
+        if constexpr (CPW == 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        Adder<TOKENS, CPW> adder(q, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0), c0, c1, area + q.feed_off);
+        float *turn = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17);
+        Tile tile{0, 0, 0, 0};
+        if (t0 < tiles) {
+            tile = find_tile(q, tables, t0, q.width);
+            adder.begin(tile);
+        }
+        if (!TOKENS && q.splits > 1) {
+            if (t0 < tiles) fine = adder.add(tile);
+            if (t0 < tiles && fine) {
+#pragma unroll
+                for (int i = 0; i < CPW; ++i)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + ((adder.half * CPW + i) * kF8Rows + adder.quad * 32 + lane) * 4), "f"(adder.at(i)) : "memory");
+            }
+            if (!fine) ctl.whole = 0;
+            const uint32_t flag_at = remote_address(smem_address(&ctl.whole), lane & (q.splits - 1));
+            __syncwarp();
+            cluster_sync_all();
+            const int flag = load_cluster_s32(flag_at);
+            if (__all_sync(0xFFFFFFFFu, flag)) {
+                if (p.out_type == HIKONV_OUT_F32) finish_parts<float>(q, tile, rank, stages);
+                else if (p.out_type == HIKONV_OUT_F16) finish_parts<__half>(q, tile, rank, stages);
+                else finish_parts<__nv_bfloat16>(q, tile, rank, stages);
+            }
+            cluster_sync_all();                         // the others may still read this CTA's part
+        } else {
+            for (int t = t0; t < tiles; t += step) {
+                fine = adder.add(tile);
+                if (!fine) break;
+                const Tile now = tile;
+                if (t + step < tiles) {
+                    tile = find_tile(q, tables, t + step, q.width);
+                    adder.begin(tile);
+                }
+                adder.finish(now, turn);
+            }
+        }
+        cp_async_wait_all();
+    }
+    if (!fine && lane == 0) atomicAdd(&linear_f8_timeouts, 1u);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(q.tmem_cols));
+#undef HIKONV_BAR
+}
+
+// ---- host
+
+struct F8Shape {
+    bool tokens;
+    int nt, width, splits;
+};
+
+// The tile that a model of the time, in cycles, likes best.  A step costs the longest of its multiplies (2 per column of the instruction), its
+// way from the second-level cache (70 bytes per cycle and SM) and the exchange between the warps; a tile its set-up and its end.
+static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
+    const int chunks = ceil_div(p.K, kF8Depth), filled = p.E < p.M ? p.E : p.M;
+    F8Shape best{false, 16, kF8Rows, 1};
+    double least = 1e300;
+    auto consider = [&](bool tokens, int nt, int width, int splits) {
+        const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * ceil_div(p.N, width);
+        if (splits > 1 && (tiles * splits > sms - 20 || splits > chunks)) return;
+        const int columns = tokens ? width : nt;
+        const double bytes = (kF8Rows + columns) * (double)kF8Depth;
+        double step = 2.0 * columns > bytes / 70.0 ? 2.0 * columns : bytes / 70.0;
+        if (step < 300) step = 300;
+        const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
+        const double time = waves * (ceil_div(chunks, splits) * step + 800.0 + 10.0 * columns) + 3000.0 +
+                            (splits > 1 ? 2000.0 + 500.0 * splits + 62.0 * nt / splits + 8.0 * nt : 0.0);
+        if (time < least) {
+            least = time;
+            best = F8Shape{tokens, nt, width, splits};
+        }
+    };
+    for (int nt = 16; nt <= 128; nt *= 2)
+        for (int splits = 1; splits <= 8; splits *= 2) consider(false, nt, kF8Rows, splits);
+    consider(true, kF8Rows, 128, 1);
+    consider(true, kF8Rows, 256, 1);
+    return best;
+}
+
+static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long xs_row, cudaStream_t st) {
+    const int sms = sm_count_here();
+    const F8Shape shape = choose_f8_tile(p, sms);
+    F8Params q;
+    memset(&q, 0, sizeof(q));
+    q.p = p;
+    q.xs_row = xs_row;
+    q.nt = shape.nt;
+    q.width = shape.width;
+    q.splits = shape.splits;
+    while ((1 << q.split_shift) < q.splits) ++q.split_shift;
+    q.chunks = (p.K - 1) / kF8Depth + 1;
+    q.w_blocks = ceil_div(p.N, kF8Depth);
+    q.n_blocks = ceil_div(p.N, q.width);
+    q.m_tiles = ceil_div(p.M, q.nt);
+    q.tokens_first = p.offsets || (long long)p.M <= (long long)p.N;
+    const int columns = shape.tokens ? q.width : q.nt;
+    q.b_off = kF8Rows * kF8Depth;
+    q.stage_bytes = q.b_off + columns * kF8Depth;
+    q.acc_cols = columns < 32 ? 32 : columns;
+    q.accs = 512 / q.acc_cols < 4 ? 512 / q.acc_cols : 4;
+    q.tmem_cols = q.accs * q.acc_cols;                   // a power of two
+    const int slot = (shape.tokens || columns < 64 ? 32 : columns / 2) * 4, feeds = kF8Adders * kF8Ahead * slot;
+    const int turns = shape.tokens ? kF8Adders * 32 * 17 * 4 : 0;
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
+    q.stages = (int)((kF8MostSmem - 2048 - tables - feeds - turns) / q.stage_bytes);
+    if (q.stages > kF8MostStages) q.stages = kF8MostStages;
+    const int parts = q.splits > 1 ? ceil_div(q.nt * kF8Rows * 4, q.stage_bytes) : 1;
+    if (q.stages < parts || q.stages < 2) return HIKONV_ERR_UNSUPPORTED;
+    const long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
+    const int own = ceil_div(q.chunks, q.splits);
+    if (tiles * q.splits <= sms && q.stages > own) q.stages = own > parts ? own : parts;
+    q.feed_off = q.stages * q.stage_bytes;
+    q.turn_off = q.feed_off + feeds;
+    q.held = q.turn_off + turns;
+    const int elem = p.out_type == HIKONV_OUT_F32 ? 4 : 2;
+    q.whole_stores = (uintptr_t)p.out % 32 == 0 && (uintptr_t)p.residual % 32 == 0 && p.out_row * elem % 32 == 0 && (!p.residual || p.res_row * elem % 32 == 0);
+    // sums in 32 bits (1), the operands' types, 128 rows; the columns follow per tile
+    const int a_type = shape.tokens ? x_f8 : w_f8, b_type = shape.tokens ? w_f8 : x_f8;
+    q.idesc = (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(kF8Rows >> 4) << 24);
+    q.wait_cycles = kWaitCycles;
+    const size_t smem = (size_t)q.held + 2048 + tables;
+
+    CUtensorMap map_x, map_w;
+    if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, (uint64_t)p.x_row, kF8Depth, (uint32_t)q.nt) ||
+        !encode_map(&map_w, p.w, (uint64_t)p.K, (uint64_t)p.E * p.N, (uint64_t)p.w_row, kF8Depth, (uint32_t)q.width))
+        return HIKONV_ERR_CUDA;
+    const unsigned grid = (unsigned)(q.splits > 1 ? tiles * q.splits : tiles < sms ? tiles : sms);
+    auto launch = [&](auto kernel) {
+        return with_dynamic_smem((const void *)kernel, smem > 49 * 1024 ? smem : 49 * 1024, [&] {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(grid);
+            cfg.blockDim = dim3(kF8Threads);
+            cfg.dynamicSmemBytes = smem;
+            cfg.stream = st;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = (unsigned)q.splits;
+            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = q.splits > 1 ? 2 : 1;
+            const CUtensorMap &a = shape.tokens ? map_x : map_w, &b = shape.tokens ? map_w : map_x;
+            return cudaLaunchKernelEx(&cfg, kernel, q, a, b) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+        });
+    };
+    if (shape.tokens) return q.width == 256 ? launch(linear_f8_kernel<true, 128>) : launch(linear_f8_kernel<true, 64>);
+    switch (q.nt) {
+        case 16: return launch(linear_f8_kernel<false, 8>);
+        case 32: return launch(linear_f8_kernel<false, 16>);
+        case 64: return launch(linear_f8_kernel<false, 32>);
+        default: return launch(linear_f8_kernel<false, 64>);
+    }
+}
+
+int read_linear_f8_timeouts(unsigned int *h_count) {
+    return cudaMemcpyFromSymbol(h_count, linear_f8_timeouts, sizeof(*h_count)) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+}
+
+static int linear_f8_run(const void *d_x, int x_f8, long long x_row, const void *d_w, int w_f8, long long w_row, const int32_t *d_offsets, bool grouped, int E,
+                         int M, int N, int K, const float *d_x_scale, long long xs_row, const float *d_w_scale, void *d_out, long long out_row,
+                         const hikonv_epilogue_t *ep, void *stream) {
+    if (!ep || M < 0 || N < 1 || K < 1 || E < 1) return HIKONV_ERR_INVALID_ARG;
+    if ((x_f8 != HIKONV_F8_E4M3 && x_f8 != HIKONV_F8_E5M2) || (w_f8 != HIKONV_F8_E4M3 && w_f8 != HIKONV_F8_E5M2)) return HIKONV_ERR_INVALID_ARG;
+    const int type = ep->out_type;
+    if (type != HIKONV_OUT_F32 && type != HIKONV_OUT_F16 && type != HIKONV_OUT_BF16) return HIKONV_ERR_INVALID_ARG;
+    if (ep->activation < HIKONV_ACT_NONE || ep->activation > HIKONV_ACT_GELU) return HIKONV_ERR_INVALID_ARG;
+    if (ep->d_x_scale || ep->d_w_scale || ep->shift || ep->lo || ep->hi) return HIKONV_ERR_INVALID_ARG;
+    if (E > HIKONV_MAX_GROUPS || M > (1 << 30) || N > (1 << 30) || (long long)E * N > 0x7FFFFFFFll || K > (1 << 30)) return HIKONV_ERR_UNSUPPORTED;
+    // few enough tiles for 32-bit counts
+    if (((long long)M / 16 + (E < M ? E : M) + 1) * ceil_div(N, kF8Rows) >= 0x3FFFFFFFll) return HIKONV_ERR_UNSUPPORTED;
+    if (M == 0) return HIKONV_OK;
+    const int elem = type == HIKONV_OUT_F32 ? 4 : 2;
+    const long long blocks = (K - 1) / kF8Depth + 1, n_blocks = (N - 1) / kF8Depth + 1, wide = (long long)align_up(K, 16);
+    if (M == 1) x_row = wide, out_row = N;                       // there is no second row
+    if ((long long)E * N == 1) w_row = wide;
+    if (blocks == 1) xs_row = M;
+    const long long res_row = M == 1 || !ep->d_residual ? N : ep->residual_row_stride;
+    if (!d_x || !d_w || !d_out || !d_x_scale || !d_w_scale || (grouped && !d_offsets)) return HIKONV_ERR_INVALID_ARG;
+    if (x_row < K || w_row < K || xs_row < M || out_row < N || res_row < N) return HIKONV_ERR_INVALID_ARG;
+    constexpr long long most = 1ll << 39;                        // bytes from row to row: what a tensor map takes, and offsets stay in 64 bits
+    if (x_row >= most || w_row >= most || xs_row >= most || out_row >= most || res_row >= most) return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_out % elem || (uintptr_t)ep->d_residual % elem || (uintptr_t)ep->d_bias % 4 || (uintptr_t)d_x_scale % 4 || (uintptr_t)d_w_scale % 4 ||
+        (uintptr_t)d_offsets % 4)
+        return HIKONV_ERR_INVALID_ARG;
+    if ((uintptr_t)d_x % 16 || x_row % 16 || (uintptr_t)d_w % 16 || w_row % 16) return HIKONV_ERR_UNSUPPORTED;
+    const size_t columns = (size_t)E * N * 4, w_scales = (size_t)(E * n_blocks * blocks) * 4;
+    if (rows_overlap(d_out, out_row * elem, N * elem, M, d_x, x_row, K, M) || rows_overlap(d_out, out_row * elem, N * elem, M, d_w, w_row, K, (size_t)E * N) ||
+        rows_overlap(d_out, out_row * elem, N * elem, M, d_x_scale, xs_row * 4, (size_t)M * 4, blocks) ||
+        rows_overlap(d_out, out_row * elem, N * elem, M, d_w_scale, w_scales, w_scales, 1) ||
+        rows_overlap(d_out, out_row * elem, N * elem, M, ep->d_bias, columns, columns, 1) ||
+        rows_overlap(d_out, out_row * elem, N * elem, M, d_offsets, (size_t)(E + 1) * 4, (size_t)(E + 1) * 4, 1))
+        return HIKONV_ERR_INVALID_ARG;
+    if (ep->d_residual && !(ep->d_residual == d_out && res_row == out_row) &&
+        rows_overlap(d_out, out_row * elem, N * elem, M, ep->d_residual, res_row * elem, N * elem, M))
+        return HIKONV_ERR_INVALID_ARG;
+    LinearParams k;
+    memset(&k, 0, sizeof(k));
+    k.x = (const uint8_t *)d_x; k.w = (const uint8_t *)d_w; k.offsets = d_offsets;
+    k.x_row = x_row; k.w_row = w_row;
+    k.M = M; k.N = N; k.K = K; k.E = E;
+    k.out_type = type; k.act = ep->activation;
+    k.out = d_out; k.residual = ep->d_residual; k.bias = ep->d_bias;
+    k.x_scale = d_x_scale; k.w_scale = d_w_scale;
+    k.out_row = out_row; k.res_row = res_row;
+    return launch_linear_f8(k, x_f8, w_f8, xs_row, (cudaStream_t)stream);
+}
+
+}  // namespace hikonv
+
+using namespace hikonv;
+
+extern "C" int hikonv_linear_f8(const void *d_x, int x_f8, long long x_row_stride, const void *d_w, int w_f8, long long w_row_stride, int M, int N, int K,
+                                const float *d_x_scale, long long x_scale_row_stride, const float *d_w_scale, void *d_out, long long out_row_stride,
+                                const hikonv_epilogue_t *epilogue, void *stream) {
+    return linear_f8_run(d_x, x_f8, x_row_stride, d_w, w_f8, w_row_stride, nullptr, false, 1, M, N, K, d_x_scale, x_scale_row_stride, d_w_scale, d_out,
+                         out_row_stride, epilogue, stream);
+}
+
+extern "C" int hikonv_grouped_linear_f8(const void *d_x, int x_f8, long long x_row_stride, const void *d_w, int w_f8, long long w_row_stride,
+                                        const int32_t *d_offsets, int E, int T, int N, int K, const float *d_x_scale, long long x_scale_row_stride,
+                                        const float *d_w_scale, void *d_out, long long out_row_stride, const hikonv_epilogue_t *epilogue, void *stream) {
+    return linear_f8_run(d_x, x_f8, x_row_stride, d_w, w_f8, w_row_stride, d_offsets, true, E, T, N, K, d_x_scale, x_scale_row_stride, d_w_scale, d_out,
+                         out_row_stride, epilogue, stream);
+}

@@ -30,6 +30,14 @@ decltype(&hikonv_quantize_rows) g_quantize_rows = nullptr;
 decltype(&hikonv_linear) g_linear = nullptr;
 decltype(&hikonv_grouped_linear) g_grouped_linear = nullptr;
 decltype(&hikonv_linear_workspace_bytes) g_linear_workspace_bytes = nullptr;
+decltype(&hikonv_sort_by_expert) g_sort_by_expert = nullptr;
+decltype(&hikonv_sort_by_expert_workspace_bytes) g_sort_workspace_bytes = nullptr;
+decltype(&hikonv_rows_to_experts) g_rows_to_experts = nullptr;
+decltype(&hikonv_rows_from_experts) g_rows_from_experts = nullptr;
+decltype(&hikonv_rows_from_experts_grad) g_rows_from_experts_grad = nullptr;
+decltype(&hikonv_quantize_blocks) g_quantize_blocks = nullptr;
+decltype(&hikonv_linear_f8) g_linear_f8 = nullptr;
+decltype(&hikonv_grouped_linear_f8) g_grouped_linear_f8 = nullptr;
 
 // Reads arguments one after the other; `ok` stays true while all are as expected.
 struct Args {
@@ -425,6 +433,241 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// What the calls of a mixture of experts share: the places of pairs, and two results.
+bool slots_ok(const at::Tensor *t, const at::Tensor &like, int64_t rows) {
+    return plain_cuda(t) && t->scalar_type() == at::kInt && t->dim() == 2 && t->device() == like.device() && (rows < 0 || t->size(0) == rows) &&
+           fits_int(t->size(0)) && fits_int(t->size(1));
+}
+PyObject *two(PyObject *a, PyObject *b) {
+    PyObject *both = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return both;
+}
+int f8_type(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? HIKONV_F8_E4M3 : t == at::kFloat8_e5m2 ? HIKONV_F8_E5M2 : -1; }
+// Rows on 16-byte boundaries.
+at::Tensor f8_rows(int64_t rows, int64_t K, at::ScalarType type, const at::Tensor &like) {
+    const int64_t wide = (K + 15) / 16 * 16;
+    const at::Tensor t = empty({rows, wide}, type, like);
+    return wide == K ? t : t.narrow(1, 0, K);
+}
+
+// sort_by_expert(experts, n_experts, offsets, slots, workspace)
+PyObject *sort_by_expert(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor();
+        const int E = in.int32();
+        const at::Tensor *offsets = in.optional_tensor(), *slots = in.optional_tensor(), *space = in.optional_tensor();
+        int64_t row;
+        if (!in.ok || !matrix(x, &row) || (x->scalar_type() != at::kInt && x->scalar_type() != at::kLong) || E < 1) return nullptr;
+        const int64_t T = x->size(0), k = x->size(1);
+        at::Tensor made_offsets, made_slots, made_space;
+        if (!offsets) made_offsets = empty({(int64_t)E + 1}, at::kInt, *x);
+        if (!slots) made_slots = empty({T, k}, at::kInt, *x);
+        const at::Tensor &o = offsets ? *offsets : made_offsets, &s = slots ? *slots : made_slots;
+        if (!vector_ok(&o, at::kInt, {(int64_t)E + 1}, *x) || !vector_ok(&s, at::kInt, {T, k}, *x)) return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const size_t need = g_sort_workspace_bytes((int)T, (int)k, E);
+        if (need && !space) {
+            made_space = empty({(int64_t)need}, at::kByte, *x);
+            space = &made_space;
+        }
+        if (space && (!plain_cuda(space) || space->device() != x->device())) return nullptr;
+        const void *x_ptr = x->data_ptr();
+        const int index_bytes = (int)x->element_size();
+        int32_t *o_ptr = (int32_t *)o.data_ptr(), *s_ptr = (int32_t *)s.data_ptr();
+        void *space_ptr = space ? space->data_ptr() : nullptr, *st = current_stream();
+        const size_t space_bytes = space ? (size_t)space->numel() * space->element_size() : 0;
+        if (unlocked([&] { return g_sort_by_expert(x_ptr, index_bytes, row, (int)T, (int)k, E, o_ptr, s_ptr, space_ptr, space_bytes, st); }) != HIKONV_OK)
+            return nullptr;
+        return two(result(a[2], made_offsets), result(a[3], made_slots));
+    });
+}
+
+// rows_to_experts(x, slots, out)
+PyObject *rows_to_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor(), *slots = in.tensor(), *given = in.optional_tensor();
+        int64_t x_row, out_row;
+        if (!in.ok || !matrix(x, &x_row) || x->is_complex() || !slots_ok(slots, *x, x->size(0))) return nullptr;
+        const int size = (int)x->element_size();
+        if (size != 1 && size != 2 && size != 4) return nullptr;
+        const int64_t T = x->size(0), H = x->size(1), k = slots->size(1);
+        at::Tensor made;
+        if (!given) made = empty({T * k, H}, x->scalar_type(), *x);
+        const at::Tensor &y = given ? *given : made;
+        if (y.dim() != 2 || !out_matrix(&y, y.size(0), H, x->scalar_type(), *x, &out_row)) return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const void *x_ptr = x->data_ptr();
+        const int32_t *s_ptr = (const int32_t *)slots->data_ptr();
+        void *y_ptr = y.data_ptr(), *st = current_stream();
+        const int R = (int)y.size(0);
+        if (unlocked([&] { return g_rows_to_experts(x_ptr, size, x_row, s_ptr, (int)T, (int)k, (int)H, y_ptr, out_row, R, st); }) != HIKONV_OK) return nullptr;
+        return result(a[2], made);
+    });
+}
+
+// rows_from_experts(y, slots, weights, residual, out)
+PyObject *rows_from_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *y = in.tensor(), *slots = in.tensor(), *weights = in.optional_tensor(), *residual = in.optional_tensor(), *given = in.optional_tensor();
+        int64_t y_row, out_row, res_row;
+        if (!in.ok || !matrix(y, &y_row) || !slots_ok(slots, *y, -1)) return nullptr;
+        const int type = float_type(y->scalar_type());
+        if (type < 0) return nullptr;
+        const int64_t R = y->size(0), H = y->size(1), T = slots->size(0), k = slots->size(1);
+        at::Tensor made;
+        if (!given) made = empty({T, H}, y->scalar_type(), *y);
+        const at::Tensor &o = given ? *given : made;
+        res_row = H;
+        if (!out_matrix(&o, T, H, y->scalar_type(), *y, &out_row) || !vector_ok(weights, at::kFloat, {T, k}, *y) ||
+            (residual && !out_matrix(residual, T, H, y->scalar_type(), *y, &res_row)))
+            return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(y->device());
+        const void *y_ptr = y->data_ptr(), *r_ptr = address(residual);
+        const int32_t *s_ptr = (const int32_t *)slots->data_ptr();
+        const float *w_ptr = (const float *)address(weights);
+        void *o_ptr = o.data_ptr(), *st = current_stream();
+        if (unlocked([&] {
+                return g_rows_from_experts(y_ptr, type, y_row, (int)R, s_ptr, w_ptr, (int)T, (int)k, (int)H, r_ptr, res_row, o_ptr, out_row, st);
+            }) != HIKONV_OK)
+            return nullptr;
+        return result(a[4], made);
+    });
+}
+
+// rows_from_experts_grad(grad, y, slots, weights, grad_y, grad_weights)
+PyObject *rows_from_experts_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *grad = in.tensor(), *y = in.optional_tensor(), *slots = in.tensor(), *weights = in.optional_tensor(),
+                         *given_y = in.optional_tensor(), *given_w = in.optional_tensor();
+        int64_t grad_row, y_row, grad_y_row;
+        if (!in.ok || !matrix(grad, &grad_row) || !slots_ok(slots, *grad, grad->size(0)) || (given_w && !weights) || (weights && !y)) return nullptr;
+        const at::ScalarType type = grad->scalar_type();
+        if (float_type(type) < 0 || (y && y->dim() != 2)) return nullptr;
+        const int64_t T = grad->size(0), H = grad->size(1), k = slots->size(1);
+        at::Tensor made_y, made_w;
+        if (!given_y) made_y = empty({y ? y->size(0) : T * k, H}, type, *grad);
+        if (weights && !given_w) made_w = empty({T, k}, at::kFloat, *grad);
+        const at::Tensor &gy = given_y ? *given_y : made_y;
+        const at::Tensor *gw = given_w ? given_w : weights ? &made_w : nullptr;
+        if (gy.dim() != 2 || !out_matrix(&gy, gy.size(0), H, type, *grad, &grad_y_row)) return nullptr;
+        const int64_t R = gy.size(0);
+        y_row = H;
+        if (weights && !out_matrix(y, R, H, type, *grad, &y_row)) return nullptr;
+        if (!vector_ok(weights, at::kFloat, {T, k}, *grad) || !vector_ok(gw, at::kFloat, {T, k}, *grad)) return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(grad->device());
+        const void *g_ptr = grad->data_ptr(), *y_ptr = weights ? y->data_ptr() : nullptr;
+        const int32_t *s_ptr = (const int32_t *)slots->data_ptr();
+        const float *w_ptr = (const float *)address(weights);
+        void *gy_ptr = gy.data_ptr(), *st = current_stream();
+        float *gw_ptr = (float *)address(gw);
+        if (unlocked([&] {
+                return g_rows_from_experts_grad(g_ptr, float_type(type), grad_row, y_ptr, y_row, (int)R, s_ptr, w_ptr, (int)T, (int)k, (int)H, gy_ptr,
+                                                grad_y_row, gw_ptr, st);
+            }) != HIKONV_OK)
+            return nullptr;
+        PyObject *second = nullptr;
+        if (gw) {
+            second = result(a[5], made_w);
+        } else {
+            Py_INCREF(Py_None);
+            second = Py_None;
+        }
+        return two(result(a[4], made_y), second);
+    });
+}
+
+// quantize_blocks(x, dtype, slots, values, scale)
+PyObject *quantize_blocks(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor();
+        PyObject *dtype = in.next();
+        const at::Tensor *slots = in.optional_tensor(), *given_v = in.optional_tensor(), *given_s = in.optional_tensor();
+        int64_t x_row, v_row, s_row;
+        if (!in.ok || !matrix(x, &x_row) || !THPDtype_Check(dtype)) return nullptr;
+        const int type = float_type(x->scalar_type());
+        const at::ScalarType f8 = ((THPDtype *)dtype)->scalar_type;
+        if (type < 0 || f8_type(f8) < 0 || (slots && !slots_ok(slots, *x, x->size(0)))) return nullptr;
+        const int64_t M = x->size(0), K = x->size(1), k = slots ? slots->size(1) : 0, blocks = (K + 127) / 128;
+        if (K < 1 || (given_v && given_v->dim() != 2)) return nullptr;
+        const int64_t rows = !slots ? M : given_v ? given_v->size(0) : M * k;
+        at::Tensor made_v, made_s;
+        if (!given_v) made_v = f8_rows(rows, K, f8, *x);
+        if (!given_s) made_s = empty({blocks, rows}, at::kFloat, *x);
+        const at::Tensor &v = given_v ? *given_v : made_v, &s = given_s ? *given_s : made_s;
+        if (!out_matrix(&v, rows, K, f8, *x, &v_row) || !out_matrix(&s, blocks, rows, at::kFloat, *x, &s_row)) return nullptr;
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const void *x_ptr = x->data_ptr();
+        const int32_t *slots_ptr = (const int32_t *)address(slots);
+        uint8_t *v_ptr = (uint8_t *)v.data_ptr();
+        float *s_ptr = (float *)s.data_ptr();
+        void *st = current_stream();
+        if (unlocked([&] {
+                return g_quantize_blocks(x_ptr, type, x_row, (int)M, (int)K, f8_type(f8), slots_ptr, (int)k, slots ? (int)rows : 0, v_ptr, v_row, s_ptr, s_row, st);
+            }) != HIKONV_OK)
+            return nullptr;
+        return two(result(a[3], made_v), result(a[4], made_s));
+    });
+}
+
+// linear_f8(x, w, offsets or None, x_scale, w_scale, bias, activation, residual, out_dtype, out)
+PyObject *linear_f8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Args in{a, n};
+        const at::Tensor *x = in.tensor(), *w = in.tensor(), *offsets = in.optional_tensor(), *x_scale = in.tensor(), *w_scale = in.tensor(),
+                         *bias = in.optional_tensor();
+        hikonv_epilogue_t ep{};
+        ep.activation = in.int32();
+        const at::Tensor *residual = in.optional_tensor();
+        PyObject *dtype = in.next();
+        const at::Tensor *given = in.optional_tensor();
+        int64_t x_row, xs_row, out_row, res_row;
+        if (!in.ok || !matrix(x, &x_row) || f8_type(x->scalar_type()) < 0 || (dtype != Py_None && !THPDtype_Check(dtype))) return nullptr;
+        const int dims = offsets ? 3 : 2;
+        if (!w->is_cuda() || w->layout() != at::kStrided || f8_type(w->scalar_type()) < 0 || w->device() != x->device() || w->dim() != dims) return nullptr;
+        const int64_t M = x->size(0), K = x->size(1), E = offsets ? w->size(0) : 1, N = w->size(dims - 2), blocks = (K + 127) / 128, n_blocks = (N + 127) / 128;
+        if (K < 1 || N < 1 || E < 1 || !fits_int(N) || !fits_int(E) || w->size(dims - 1) != K || (K > 1 && w->stride(dims - 1) != 1)) return nullptr;
+        const int64_t w_row = N > 1 ? w->stride(dims - 2) : E > 1 ? w->stride(0) : K;
+        if (E > 1 && w->stride(0) != N * w_row) return nullptr;
+        const at::ScalarType type = dtype != Py_None ? ((THPDtype *)dtype)->scalar_type : given ? given->scalar_type() : at::kBFloat16;
+        ep.out_type = float_type(type);
+        if (ep.out_type < 0) return nullptr;
+        at::Tensor made;
+        if (!given) made = empty({M, N}, type, *x);
+        const at::Tensor &y = given ? *given : made;
+        if (!out_matrix(&y, M, N, type, *x, &out_row) || !out_matrix(x_scale, blocks, M, at::kFloat, *x, &xs_row)) return nullptr;
+        const int64_t per_column[2] = {E, N}, per_tile[3] = {E, n_blocks, blocks};
+        if (!vector_ok(w_scale, at::kFloat, at::IntArrayRef(per_tile + (offsets ? 0 : 1), dims), *x) ||
+            !vector_ok(bias, at::kFloat, at::IntArrayRef(per_column + (offsets ? 0 : 1), dims - 1), *x) || !vector_ok(offsets, at::kInt, {E + 1}, *x))
+            return nullptr;
+        if (residual) {
+            if (!out_matrix(residual, M, N, type, *x, &res_row)) return nullptr;
+            ep.residual_row_stride = res_row;
+        }
+        ep.d_bias = address(bias);
+        ep.d_residual = address(residual);
+        const c10::cuda::OptionalCUDAGuard guard(x->device());
+        const void *x_ptr = x->data_ptr(), *w_ptr = w->data_ptr();
+        const int x_f8 = f8_type(x->scalar_type()), w_f8 = f8_type(w->scalar_type());
+        const int32_t *off_ptr = (const int32_t *)address(offsets);
+        const float *xs_ptr = (const float *)x_scale->data_ptr(), *ws_ptr = (const float *)w_scale->data_ptr();
+        void *y_ptr = y.data_ptr(), *st = current_stream();
+        const int status = unlocked([&] {
+            return offsets ? g_grouped_linear_f8(x_ptr, x_f8, x_row, w_ptr, w_f8, w_row, off_ptr, (int)E, (int)M, (int)N, (int)K, xs_ptr, xs_row, ws_ptr, y_ptr,
+                                                 out_row, &ep, st)
+                           : g_linear_f8(x_ptr, x_f8, x_row, w_ptr, w_f8, w_row, (int)M, (int)N, (int)K, xs_ptr, xs_row, ws_ptr, y_ptr, out_row, &ep, st);
+        });
+        if (status != HIKONV_OK) return nullptr;
+        return result(a[9], made);
+    });
+}
+
 // bind(name, address): the entry points of the library that is loaded.
 PyObject *bind(PyObject *, PyObject *args) {
     const char *name;
@@ -442,6 +685,14 @@ PyObject *bind(PyObject *, PyObject *args) {
     else if (s == "hikonv_linear") g_linear = (decltype(g_linear))ptr;
     else if (s == "hikonv_grouped_linear") g_grouped_linear = (decltype(g_grouped_linear))ptr;
     else if (s == "hikonv_linear_workspace_bytes") g_linear_workspace_bytes = (decltype(g_linear_workspace_bytes))ptr;
+    else if (s == "hikonv_sort_by_expert") g_sort_by_expert = (decltype(g_sort_by_expert))ptr;
+    else if (s == "hikonv_sort_by_expert_workspace_bytes") g_sort_workspace_bytes = (decltype(g_sort_workspace_bytes))ptr;
+    else if (s == "hikonv_rows_to_experts") g_rows_to_experts = (decltype(g_rows_to_experts))ptr;
+    else if (s == "hikonv_rows_from_experts") g_rows_from_experts = (decltype(g_rows_from_experts))ptr;
+    else if (s == "hikonv_rows_from_experts_grad") g_rows_from_experts_grad = (decltype(g_rows_from_experts_grad))ptr;
+    else if (s == "hikonv_quantize_blocks") g_quantize_blocks = (decltype(g_quantize_blocks))ptr;
+    else if (s == "hikonv_linear_f8") g_linear_f8 = (decltype(g_linear_f8))ptr;
+    else if (s == "hikonv_grouped_linear_f8") g_grouped_linear_f8 = (decltype(g_grouped_linear_f8))ptr;
     else {
         PyErr_Format(PyExc_ValueError, "no entry point %s", name);
         return nullptr;
@@ -458,6 +709,12 @@ PyMethodDef methods[] = {
     {"conv2d_dense", (PyCFunction)(void (*)(void))conv2d_dense, METH_FASTCALL, nullptr},
     {"quantize_rows", (PyCFunction)(void (*)(void))quantize_rows, METH_FASTCALL, nullptr},
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, nullptr},
+    {"sort_by_expert", (PyCFunction)(void (*)(void))sort_by_expert, METH_FASTCALL, nullptr},
+    {"rows_to_experts", (PyCFunction)(void (*)(void))rows_to_experts, METH_FASTCALL, nullptr},
+    {"rows_from_experts", (PyCFunction)(void (*)(void))rows_from_experts, METH_FASTCALL, nullptr},
+    {"rows_from_experts_grad", (PyCFunction)(void (*)(void))rows_from_experts_grad, METH_FASTCALL, nullptr},
+    {"quantize_blocks", (PyCFunction)(void (*)(void))quantize_blocks, METH_FASTCALL, nullptr},
+    {"linear_f8", (PyCFunction)(void (*)(void))linear_f8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
