@@ -61,6 +61,11 @@ __device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[32]) {
                    "=r"(v[30]), "=r"(v[31])
                  : "r"(taddr));
 }
+__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[64]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+                 : "r"(taddr));
+}
 // The wait for tcgen05.ld, which what it loaded goes through: no arithmetic on it can be moved in front.
 template <int N>
 __device__ __forceinline__ void f8_loaded(uint32_t (&v)[N]) {
@@ -101,10 +106,135 @@ __device__ __forceinline__ void store_global32(void *a, const uint32_t (&v)[8]) 
 }
 
 __device__ __forceinline__ bool f8_wait(const F8Params &q, uint32_t bar, uint32_t parity) {
+    if (__all_sync(0xFFFFFFFFu, mbarrier_try_wait(bar, parity))) return true;
     return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
 
-// A warp that adds up: the 32 lanes of its quarter, CPW of the columns.  Sums are pairs of floats.
+// The sums of a thread, CPW neighbouring columns of its lane as pairs of floats, and what becomes of them: a few at a time, which are then
+// shifted out, so that the code for them is there once and nothing else has to be in registers beside the rest.
+template <int CPW>
+struct Sums {
+    uint64_t sum[CPW / 2];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) sum[i] = 0;
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? f8_high(sum[i / 2]) : f8_low(sum[i / 2]); }
+    template <int COUNT>
+    __device__ __forceinline__ void shift_out() {
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) sum[i] = i + COUNT / 2 < CPW / 2 ? sum[i + COUNT / 2] : 0;
+    }
+    template <int ACT, int COUNT>
+    __device__ __forceinline__ void activate_as(float (&v)[COUNT]) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = activate(v[i], ACT);
+    }
+    template <int COUNT>
+    __device__ __forceinline__ void activate_all(int act, float (&v)[COUNT]) {
+        switch (act) {
+            case HIKONV_ACT_RELU: activate_as<HIKONV_ACT_RELU>(v); break;
+            case HIKONV_ACT_SILU: activate_as<HIKONV_ACT_SILU>(v); break;
+            case HIKONV_ACT_GELU: activate_as<HIKONV_ACT_GELU>(v); break;
+            default: break;
+        }
+    }
+    // Lanes are rows of x from row0 + quad 32 on, `rows` of them in all; columns from n on, 16 at a time.  32 bytes of a row at once where rows begin
+    // on such a boundary, else turned in shared memory so that neighbouring lanes write neighbouring columns.
+    template <typename T>
+    __device__ __forceinline__ void store_rows(const F8Params &q, const float (&v)[16], long long row0, int rows, int n, float *turn) {
+        const LinearParams &p = q.p;
+        const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
+        if (q.whole_stores && n + 16 <= p.N) {
+            constexpr int PER = 32 / sizeof(T);
+            if (row < rows) {
+                T *o = (T *)p.out + (row0 + row) * p.out_row + n;
+                const T *r = (const T *)p.residual + (row0 + row) * p.res_row + n;
+#pragma unroll
+                for (int i0 = 0; i0 < 16; i0 += PER) {
+                    union { uint32_t w[8]; T v[PER]; } y, x;
+                    if (p.residual) load_global32(r + i0, x.w);
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) from_float(p.residual ? v[i0 + i] + to_float(x.v[i]) : v[i0 + i], &y.v[i]);
+                    store_global32(o + i0, y.w);
+                }
+            }
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = v[i];
+        __syncwarp();
+        const int col = n + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
+            if (there >= rows || col >= p.N) continue;
+            float y = turn[mine * 17 + (lane & 15)];
+            if (p.residual) y += to_float(load_ordered((const T *)p.residual + (row0 + there) * p.res_row + col));
+            from_float(y, (T *)p.out + (row0 + there) * p.out_row + col);
+        }
+    }
+    __device__ __forceinline__ void finish_rows(const F8Params &q, int e, int row0, int rows, int n, float *turn) {
+        const LinearParams &p = q.p;
+        const float *bias = (const float *)p.bias + (long long)e * p.N;
+#pragma unroll 1
+        for (int i0 = 0; i0 < CPW && n < p.N; i0 += 16, n += 16) {
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = at(i);
+            shift_out<16>();
+            if (p.bias) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] += n + i < p.N ? load_ordered(bias + n + i) : 0.f;
+            }
+            activate_all(p.act, v);
+            switch (p.out_type) {
+                case HIKONV_OUT_F32: store_rows<float>(q, v, row0, rows, n, turn); break;
+                case HIKONV_OUT_F16: store_rows<__half>(q, v, row0, rows, n, turn); break;
+                default: store_rows<__nv_bfloat16>(q, v, row0, rows, n, turn); break;
+            }
+        }
+    }
+    // Lanes are output columns from n0 + quad 32 on: each of `rows` rows of x from row0 on is written by neighbouring lanes, eight rows at a time.
+    template <typename T>
+    __device__ __forceinline__ void store_columns(const F8Params &q, const float (&v)[8], long long row0, int rows, int n) {
+        const LinearParams &p = q.p;
+        T *o = (T *)p.out + row0 * p.out_row + n;
+        const T *r = (const T *)p.residual + row0 * p.res_row + n;
+        T res[8];
+        if (p.residual) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < rows) res[i] = load_ordered(r + i * p.res_row);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < rows) from_float(p.residual ? v[i] + to_float(res[i]) : v[i], o + i * p.out_row);
+    }
+    __device__ __forceinline__ void finish_columns(const F8Params &q, int e, int row0, int rows, int n0) {
+        const LinearParams &p = q.p;
+        const int n = n0 + ((threadIdx.x >> 5) & 3) * 32 + (threadIdx.x & 31);
+        if (n >= p.N) return;
+        const float b = p.bias ? load_ordered((const float *)p.bias + (long long)e * p.N + n) : 0.f;
+#pragma unroll 1
+        for (int i0 = 0; i0 < CPW && rows > 0; i0 += 8, rows -= 8, row0 += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p.bias ? at(i) + b : at(i);
+            shift_out<8>();
+            activate_all(p.act, v);
+            switch (p.out_type) {
+                case HIKONV_OUT_F32: store_columns<float>(q, v, row0, rows, n); break;
+                case HIKONV_OUT_F16: store_columns<__half>(q, v, row0, rows, n); break;
+                default: store_columns<__nv_bfloat16>(q, v, row0, rows, n); break;
+            }
+        }
+    }
+};
+
+// A warp that adds up: the 32 lanes of its quarter, CPW of the columns.
 template <bool TOKENS, int CPW>
 struct Adder {
     const F8Params &q;
@@ -113,7 +243,7 @@ struct Adder {
     uint8_t *const feed;                 // this warp's: kF8Ahead slots of scales
     int lane, quad, half;
     Ring acc;
-    uint64_t sum[CPW / 2];
+    Sums<CPW> sums;
     float ws, ws_next;                   // w_scale of 32 steps, a lane each
 
     static constexpr int kSlot = (TOKENS ? 32 : CPW < 32 ? 32 : CPW) * 4;
@@ -154,8 +284,7 @@ struct Adder {
     __device__ __forceinline__ bool add(const Tile &t) {
         constexpr int CH = CPW < 32 ? CPW : 32;
         const float *w = w_scales(t);
-#pragma unroll
-        for (int i = 0; i < CPW / 2; ++i) sum[i] = 0;
+        sums.clear();
         for (int c = c0; c < c1; ++c) {
             const int at = (c - c0) & 31;
             if (at == 0) {
@@ -193,7 +322,7 @@ struct Adder {
                         s01 = f8_mul(f8_two(xs.x, xs.y), ss);
                         s23 = f8_mul(f8_two(xs.z, xs.w), ss);
                     }
-                    uint64_t *o = sum + (i + k) / 2;
+                    uint64_t *o = sums.sum + (i + k) / 2;
                     o[0] = f8_fma(f8_two(now[k], now[k + 1]), s01, o[0]);
                     o[1] = f8_fma(f8_two(now[k + 2], now[k + 3]), s23, o[1]);
                 }
@@ -204,114 +333,9 @@ struct Adder {
         }
         return true;
     }
-    template <int ACT>
-    __device__ __forceinline__ void activate_as() {
-#pragma unroll
-        for (int i = 0; i < CPW / 2; ++i) sum[i] = f8_two(activate(f8_low(sum[i]), ACT), activate(f8_high(sum[i]), ACT));
-    }
-    __device__ __forceinline__ void activate_all() {
-        switch (q.p.act) {
-            case HIKONV_ACT_RELU: activate_as<HIKONV_ACT_RELU>(); break;
-            case HIKONV_ACT_SILU: activate_as<HIKONV_ACT_SILU>(); break;
-            case HIKONV_ACT_GELU: activate_as<HIKONV_ACT_GELU>(); break;
-            default: break;
-        }
-    }
-    __device__ __forceinline__ float at(int i) const { return i & 1 ? f8_high(sum[i / 2]) : f8_low(sum[i / 2]); }
-
-    // Lanes are output columns: each row of x is written by neighbouring lanes.
-    template <typename T>
-    __device__ __forceinline__ void store_columns(const Tile &t) {
-        const LinearParams &p = q.p;
-        const int n = t.n0 + quad * 32 + lane;
-        if (n >= p.N) return;
-        const int left = t.rows - half * CPW;
-        const long long m = t.row0 + half * CPW;
-        T *o = (T *)p.out + m * p.out_row + n;
-        const T *r = (const T *)p.residual + m * p.res_row + n;
-#pragma unroll
-        for (int i0 = 0; i0 < CPW; i0 += 8) {
-            if (i0 >= left) break;
-            T res[8];
-            if (p.residual) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i0 + i < left) res[i] = load_ordered(r + (i0 + i) * p.res_row);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i0 + i < left) from_float(p.residual ? at(i0 + i) + to_float(res[i]) : at(i0 + i), o + (i0 + i) * p.out_row);
-        }
-    }
-    // Lanes are rows of x: 32 bytes of a row at a time where rows begin on such a boundary, else 16 columns of 32 rows, turned in shared
-    // memory so that neighbouring lanes write neighbouring columns.
-    template <typename T>
-    __device__ __forceinline__ void store_rows(const Tile &t, float *turn) {
-        const LinearParams &p = q.p;
-        const int row = quad * 32 + lane, n = t.n0 + half * CPW;
-        const long long m = t.row0 + row;
-        if (q.whole_stores && n + CPW <= p.N) {
-            constexpr int PER = 32 / sizeof(T);
-            if (row >= t.rows) return;
-            T *o = (T *)p.out + m * p.out_row + n;
-            const T *r = (const T *)p.residual + m * p.res_row + n;
-#pragma unroll
-            for (int i0 = 0; i0 < CPW; i0 += PER) {
-                union { uint32_t w[8]; T v[PER]; } y, x;
-                if (p.residual) load_global32(r + i0, x.w);
-#pragma unroll
-                for (int i = 0; i < PER; ++i) from_float(p.residual ? at(i0 + i) + to_float(x.v[i]) : at(i0 + i), &y.v[i]);
-                store_global32(o + i0, y.w);
-            }
-            return;
-        }
-#pragma unroll
-        for (int i0 = 0; i0 < CPW; i0 += 16) {
-            if (n + i0 >= p.N) break;
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = at(i0 + i);
-            __syncwarp();
-            const int col = n + i0 + (lane & 15);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
-                if (there >= t.rows || col >= p.N) continue;
-                float y = turn[mine * 17 + (lane & 15)];
-                if (p.residual) y += to_float(load_ordered((const T *)p.residual + (t.row0 + there) * p.res_row + col));
-                from_float(y, (T *)p.out + (t.row0 + there) * p.out_row + col);
-            }
-        }
-    }
     __device__ __forceinline__ void finish(const Tile &t, float *turn) {
-        const LinearParams &p = q.p;
-        if (p.bias) {
-            const float *bias = (const float *)p.bias + (long long)t.e * p.N;
-            if (TOKENS) {
-                const int n = t.n0 + half * CPW;
-#pragma unroll
-                for (int i = 0; i < CPW; i += 2) {
-                    const float b0 = n + i < p.N ? load_ordered(bias + n + i) : 0.f, b1 = n + i + 1 < p.N ? load_ordered(bias + n + i + 1) : 0.f;
-                    sum[i / 2] = f8_two(f8_low(sum[i / 2]) + b0, f8_high(sum[i / 2]) + b1);
-                }
-            } else {
-                const int n = t.n0 + quad * 32 + lane;
-                const float b = n < p.N ? load_ordered(bias + n) : 0.f;
-#pragma unroll
-                for (int i = 0; i < CPW / 2; ++i) sum[i] = f8_two(f8_low(sum[i]) + b, f8_high(sum[i]) + b);
-            }
-        }
-        activate_all();
-        auto store = [&](auto type) {
-            using T = decltype(type);
-            if (TOKENS) store_rows<T>(t, turn);
-            else store_columns<T>(t);
-        };
-        switch (p.out_type) {
-            case HIKONV_OUT_F32: store(float()); break;
-            case HIKONV_OUT_F16: store(__half()); break;
-            default: store(__nv_bfloat16()); break;
-        }
+        if (TOKENS) sums.finish_rows(q, t.e, t.row0, t.rows, t.n0 + half * CPW, turn);
+        else sums.finish_columns(q, t.e, t.row0 + half * CPW, t.rows - half * CPW, t.n0);
     }
 };
 
@@ -422,7 +446,6 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 
     bool fine = true;
     if (warp < kF8FirstAdder) {
-        if constexpr (CPW == 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             Ring ring;
             int loads = 0;
@@ -484,7 +507,6 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             cluster_sync_all();                         // the others may still read this CTA's part
         }
     } else {
-        if constexpr (CPW == 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         Adder<TOKENS, CPW> adder(q, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0), c0, c1, area + q.feed_off);
         float *turn = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17);
         Tile tile{0, 0, 0, 0};
@@ -497,7 +519,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             if (t0 < tiles && fine) {
 #pragma unroll
                 for (int i = 0; i < CPW; ++i)
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + ((adder.half * CPW + i) * kF8Rows + adder.quad * 32 + lane) * 4), "f"(adder.at(i)) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stages + ((adder.half * CPW + i) * kF8Rows + adder.quad * 32 + lane) * 4), "f"(adder.sums.at(i)) : "memory");
             }
             if (!fine) ctl.whole = 0;
             const uint32_t flag_at = remote_address(smem_address(&ctl.whole), lane & (q.splits - 1));
@@ -532,10 +554,271 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 #undef HIKONV_BAR
 }
 
+// ---- pairs of CTAs
+//
+// The two CTAs of a cluster take a tile of 256 rows of x by 256 output columns: each brings its 128 rows of x and half of the rows of w, and the
+// first one's multiplies (cta_group::2) read both shared memories and write each CTA's 128 lanes in its own tensor memory.  That halves what an SM
+// fetches of w and reads of it from shared memory: 32 KB per step of 128 instead of 48.
+// A step is two multiplies of 128 columns each, which four warps each add up (every thread 128 sums): while one four load from tensor memory, the
+// other four add.
+constexpr int kPairRows = 256, kPairWidth = 256, kPairHalf = 128, kPairStages = 6, kPairStage = 2 * kF8Rows * kF8Depth;
+constexpr int kPairAdders = 8, kPairThreads = (kF8FirstAdder + kPairAdders) * 32;
+// The sums take more registers than an even share: those of a thread that adds up, and of one that does not.  Together no more than the launch's,
+// which takes all that 384 threads can have.
+constexpr int kPairAdderRegs = 216, kPairOtherRegs = 64, kPairLaunchRegs = 168;
+static_assert(kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32 <= kPairLaunchRegs * kPairThreads, "registers of the launch");
+
+struct PairControl {
+    uint64_t full[kPairStages], empty[kPairStages], acc_full[4], acc_empty[4], drain[2];
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                 "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// Arrives at the barrier of this offset in both CTAs when the multiplies so far are done.
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+// A warp that adds up: a quarter of the lanes, 128 columns, 32 at a time.  Scales of x come by asynchronous copies, kF8Ahead steps ahead, those of w
+// 32 steps at a time.  While 32 columns are added the next ones are on their way from tensor memory, those of the next step among them, whose barrier
+// is waited for before the last ones of a step are added.
+struct PairAdder {
+    static constexpr int kChunk = 32;
+    const F8Params &q;
+    Sums<kPairHalf> sums;
+    const float *xs, *ws;                // the next scale to ask for, of this lane's row; of this warp's columns
+    const uint32_t feed;                 // kF8Ahead slots of 32 scales of x
+    float w_now, w_next;                 // scales of w, a lane each
+
+    __device__ __forceinline__ PairAdder(const F8Params &q_, uint32_t feed_) : q(q_), feed(feed_) {}
+    __device__ __forceinline__ void ask(int c) {
+        if (c < q.chunks) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(feed + c % kF8Ahead * 128), "l"(xs) : "memory");
+        xs += q.xs_row;
+        cp_async_commit();
+    }
+    // A tile's first scales, asked for before the tile before is finished.  row: of this lane, or one that there is.
+    __device__ __forceinline__ void begin(int e, int row, int block) {
+        const int lane = threadIdx.x & 31;
+        xs = q.p.x_scale + row;
+        ws = q.p.w_scale + ((long long)e * q.w_blocks + block) * q.chunks + lane;
+        w_next = lane < q.chunks ? load_ordered(ws) : 0.f;
+#pragma unroll 1
+        for (int i = 0; i < kF8Ahead; ++i) ask(i);
+    }
+    // The scale of step c, and that of kF8Ahead steps later asked for.
+    __device__ __forceinline__ float scale(int c) {
+        if ((c & 31) == 0) {
+            w_now = w_next;
+            w_next = c + 32 + (int)(threadIdx.x & 31) < q.chunks ? load_ordered(ws + c + 32) : 0.f;
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kF8Ahead - 1) : "memory");
+        float x;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(feed + c % kF8Ahead * 128) : "memory");
+        const float s = x * __shfl_sync(0xFFFFFFFFu, w_now, c & 31);
+        ask(c + kF8Ahead);
+        return s;
+    }
+    // taddr, bars: of the first of this warp's two accumulators, the second's 256 columns and two barriers on; empty: the cluster's address.
+    __device__ __forceinline__ bool add(uint32_t taddr, uint32_t full, uint32_t empty, uint32_t &turn) {
+        sums.clear();
+        float s = scale(0);
+#pragma unroll 1
+        for (int c = 1; c <= q.chunks; ++c) {
+            const uint64_t ss = f8_two(s, s);
+            const uint32_t which = turn & 1, d = taddr + which * 2 * kPairHalf;
+            if (!f8_wait(q, full + 16 * which, turn >> 1 & 1)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int i = 0; i < kPairHalf; i += kChunk) {
+                uint32_t v[kChunk];
+                f8_load(d + i, v);
+                f8_loaded(v);
+                if (i + kChunk == kPairHalf) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if ((threadIdx.x & 31) == 0) arrive_at(empty + 16 * which);
+                    if (c < q.chunks) s = scale(c);
+                }
+#pragma unroll
+                for (int k = 0; k < kChunk; k += 2) sums.sum[(i + k) / 2] = f8_fma(f8_two(v[k], v[k + 1]), ss, sums.sum[(i + k) / 2]);
+            }
+            ++turn;
+        }
+        return true;
+    }
+};
+
+__global__ void __launch_bounds__(kPairThreads, 1)
+    linear_f8_pair_kernel(const __grid_constant__ F8Params q, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    PairControl &ctl = *reinterpret_cast<PairControl *>(dynamic);
+    const uint32_t control = smem_address(dynamic);
+#define HIKONV_BAR(name, i) (control + (uint32_t)offsetof(PairControl, name) + 8u * (uint32_t)(i))
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    const uint32_t rank = blockIdx.x & 1;
+    const LinearParams &p = q.p;
+    const uint32_t stages = (control + (uint32_t)sizeof(PairControl) + 1023u) & ~1023u;
+    uint8_t *const area = dynamic + (stages - control);
+    int2 *group_row = reinterpret_cast<int2 *>(area + q.held);
+    int *group_tiles = reinterpret_cast<int *>(group_row + p.E);
+    const GroupTables tables{group_row, group_tiles};
+
+    if (warp == 0) {
+        if (lane < q.stages) {
+            mbarrier_init(HIKONV_BAR(full, lane), 1);
+            mbarrier_init(HIKONV_BAR(empty, lane), 2);                     // a warp for each half of the columns
+        }
+        if (lane < 4) {
+            mbarrier_init(HIKONV_BAR(acc_full, lane), 1);
+            mbarrier_init(HIKONV_BAR(acc_empty, lane), kPairAdders);       // four warps of each CTA
+        }
+        if (lane < 2) mbarrier_init(HIKONV_BAR(drain, lane), 1);
+        mbarrier_init_fence();
+        if (lane == 3) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
+        }
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl.tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                 // the other CTA's barriers are there
+    tc_fence_after();
+    const uint32_t tmem = ctl.tmem;
+    // Not before this CTA has its tensor memory: a CTA of the kernel behind that came to this SM first could take it, and wait for this
+    // one to end while this one waits for the memory.
+    grid_dependency_release();
+    grid_dependency_wait();
+    int tiles = q.m_tiles * q.n_blocks;
+    if (p.offsets) tiles = build_group_tables(q, group_row, group_tiles);
+    const int t0 = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+    bool fine = true;
+    if (warp < kF8FirstAdder) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPairOtherRegs));
+        if (warp == 0) {
+            Ring ring;
+            int loads = 0;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tile(q, tables, t, kPairWidth);
+                const int x_row = tile.row0 + (int)rank * kF8Rows, w_row = tile.e * p.N + tile.n0 + (int)rank * (kPairHalf / 2);
+                for (int c = 0; c < q.chunks; ++c) {
+                    fine = f8_wait(q, HIKONV_BAR(empty, ring.stage), ring.phase ^ 1);
+                    if (!fine) break;
+                    if (elect_one()) {
+                        const uint32_t at = stages + ring.stage * kPairStage, bar = remote_address(HIKONV_BAR(full, ring.stage), 0);
+                        if (rank == 0) mbarrier_arrive_expect(HIKONV_BAR(full, ring.stage), 2 * kPairStage);
+                        pair_load(at, &map_x, c * kF8Depth, x_row, bar);
+                        pair_load(at + kF8Rows * kF8Depth, &map_w, c * kF8Depth, w_row, bar);
+                        pair_load(at + (kF8Rows + kPairHalf / 2) * kF8Depth, &map_w, c * kF8Depth, w_row + kPairHalf, bar);
+                    }
+                    ++loads;
+                    ring.next(q.stages);
+                }
+            }
+            // what is in flight, of both CTAs, has to land before the memory goes: the last load of every stage
+            if (rank == 0) {
+                for (int i = 0; i < q.stages && i < loads; ++i) {
+                    ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+                    if (ring.stage == q.stages - 1) ring.phase ^= 1;
+                    fine &= f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+                }
+            }
+        } else if (warp <= 2 && rank == 0) {
+            // a warp for each half of the columns
+            const int h = warp - 1;
+            Ring ring;
+            uint32_t turn = 0;
+            const uint64_t a0 = smem_descriptor(stages), b0 = smem_descriptor(stages + (kF8Rows + h * (kPairHalf / 2)) * kF8Depth);
+            for (int t = t0; fine && t < tiles; t += step) {
+                const bool there = p.N - find_tile(q, tables, t, kPairWidth).n0 > h * kPairHalf;
+                for (int c = 0; c < q.chunks; ++c) {
+                    const uint32_t acc = (turn & 1) * 2 + h;
+                    fine = (!there || f8_wait(q, HIKONV_BAR(acc_empty, acc), turn >> 1 & 1 ^ 1)) && f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+                    if (!fine) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        if (there) {
+                            const uint64_t a = a0 + ring.stage * (kPairStage >> 4), b = b0 + ring.stage * (kPairStage >> 4);
+#pragma unroll
+                            for (int k = 0; k < kF8Depth / 32; ++k) pair_mma(tmem + acc * kPairHalf, a + k * 2, b + k * 2, q.idesc, k > 0);
+                            pair_commit(HIKONV_BAR(acc_full, acc));
+                        }
+                        pair_commit(HIKONV_BAR(empty, ring.stage));
+                    }
+                    turn += there;
+                    ring.next(q.stages);
+                }
+            }
+            if (!fine) {                                // multiplies in flight read shared memory and write tensor memory
+                if (elect_one())
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(HIKONV_BAR(drain, h)) : "memory");
+                f8_wait(q, HIKONV_BAR(drain, h), 0);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairAdderRegs));
+        PairAdder adder(q, stages + q.feed_off + (warp - kF8FirstAdder) * (kF8Ahead * 128) + lane * 4);
+        float *turn_area = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17 + 4);
+        float *kept = turn_area + 32 * 17;
+        const int quad = warp & 3, half = (warp - kF8FirstAdder) >> 2;
+        const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + half * kPairHalf, full = HIKONV_BAR(acc_full, half);
+        const uint32_t empty = remote_address(HIKONV_BAR(acc_empty, half), 0);
+        uint32_t turn = 0;
+        // tiles of which this warp has columns
+        auto next_tile = [&](int t, Tile &tile) {
+            for (; t < tiles; t += step) {
+                tile = find_tile(q, tables, t, kPairWidth);
+                if (tile.n0 + half * kPairHalf < p.N) break;
+            }
+            return t;
+        };
+        auto begin = [&](const Tile &tile) {
+            const int row = min(tile.row0 + (int)rank * kF8Rows + quad * 32 + lane, p.M - 1);
+            adder.begin(tile.e, row, tile.n0 / kF8Depth + half);
+        };
+        Tile tile{0, 0, 0, 0};
+        int t = next_tile(t0, tile);
+        if (t < tiles) begin(tile);
+        while (t < tiles) {
+            fine = adder.add(taddr, full, empty, turn);
+            if (!fine) break;
+            const Tile now = tile;
+            t = next_tile(t + step, tile);
+            if (t < tiles) begin(tile);
+            adder.sums.finish_rows(q, now.e, now.row0 + (int)rank * kF8Rows, now.rows - (int)rank * kF8Rows, now.n0 + half * kPairHalf, turn_area);
+        }
+        cp_async_wait_all();
+    }
+    if (!fine && lane == 0) atomicAdd(&linear_f8_timeouts, 1u);
+    __syncwarp();
+    tc_fence_before();
+    cluster_sync_all();                                 // the other CTA's multiplies, copies and arrivals are over
+    __syncthreads();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+#undef HIKONV_BAR
+}
+
 // ---- host
 
 struct F8Shape {
-    bool tokens;
+    bool tokens, pair;
     int nt, width, splits;
 };
 
@@ -543,28 +826,66 @@ struct F8Shape {
 // way from the second-level cache (70 bytes per cycle and SM) and the exchange between the warps; a tile its set-up and its end.
 static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
     const int chunks = ceil_div(p.K, kF8Depth), filled = p.E < p.M ? p.E : p.M;
-    F8Shape best{false, 16, kF8Rows, 1};
+    F8Shape best{false, false, 16, kF8Rows, 1};
     double least = 1e300;
     auto consider = [&](bool tokens, int nt, int width, int splits) {
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * ceil_div(p.N, width);
         if (splits > 1 && (tiles * splits > sms - 20 || splits > chunks)) return;
+        const bool pair = nt == kPairRows;
         const int columns = tokens ? width : nt;
-        const double bytes = (kF8Rows + columns) * (double)kF8Depth;
+        const double bytes = pair ? kPairStage : (kF8Rows + columns) * (double)kF8Depth;
         double step = 2.0 * columns > bytes / 70.0 ? 2.0 * columns : bytes / 70.0;
         if (step < 300) step = 300;
-        const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > sms ? tiles / sms + 0.3 : 1.0) : (double)((long long)(tiles + sms - 1) / sms);
+        const int units = pair ? sms / 2 : sms;
+        const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > units ? tiles / units + 0.3 : 1.0) : (double)((long long)(tiles + units - 1) / units);
         const double time = waves * (ceil_div(chunks, splits) * step + 800.0 + 10.0 * columns) + 3000.0 +
                             (splits > 1 ? 2000.0 + 500.0 * splits + 62.0 * nt / splits + 8.0 * nt : 0.0);
         if (time < least) {
             least = time;
-            best = F8Shape{tokens, nt, width, splits};
+            best = F8Shape{tokens, nt == kPairRows, nt, width, splits};
         }
     };
     for (int nt = 16; nt <= 128; nt *= 2)
         for (int splits = 1; splits <= 8; splits *= 2) consider(false, nt, kF8Rows, splits);
     consider(true, kF8Rows, 128, 1);
-    consider(true, kF8Rows, 256, 1);
+    consider(true, kPairRows, kPairWidth, 1);
     return best;
+}
+
+static int launch_pair(F8Params q, int x_f8, int w_f8, cudaStream_t st) {
+    const LinearParams &p = q.p;
+    const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
+    const int feeds = kPairAdders * kF8Ahead * 32 * 4, turns = kPairAdders * (32 * 17 + 4) * 4;
+    q.stages = (int)((kF8MostSmem - 2048 - tables - feeds - turns) / kPairStage);          // six; five beside the tables of 600 groups and more
+    if (q.stages > kPairStages) q.stages = kPairStages;
+    q.feed_off = q.stages * kPairStage;
+    q.turn_off = q.feed_off + feeds;
+    q.held = q.turn_off + turns;
+    // sums in 32 bits (1), the operands' types, 128 columns, 256 rows
+    q.idesc = (1u << 4) | ((uint32_t)x_f8 << 7) | ((uint32_t)w_f8 << 10) | ((uint32_t)(kPairHalf >> 3) << 17) | ((uint32_t)(kPairRows >> 4) << 24);
+    CUtensorMap map_x, map_w;
+    if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, (uint64_t)p.x_row, kF8Depth, kF8Rows) ||
+        !encode_map(&map_w, p.w, (uint64_t)p.K, (uint64_t)p.E * p.N, (uint64_t)p.w_row, kF8Depth, kPairHalf / 2))
+        return HIKONV_ERR_CUDA;
+    const int pairs = sm_count_here() / 2;
+    const long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
+    const size_t smem = (size_t)q.held + 2048 + tables;
+    return with_dynamic_smem((const void *)linear_f8_pair_kernel, smem, [&] {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
+        cfg.blockDim = dim3(kPairThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = 2;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, linear_f8_pair_kernel, q, map_x, map_w) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+    });
 }
 
 static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long xs_row, cudaStream_t st) {
@@ -580,9 +901,13 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     while ((1 << q.split_shift) < q.splits) ++q.split_shift;
     q.chunks = (p.K - 1) / kF8Depth + 1;
     q.w_blocks = ceil_div(p.N, kF8Depth);
+    q.wait_cycles = kWaitCycles;
     q.n_blocks = ceil_div(p.N, q.width);
     q.m_tiles = ceil_div(p.M, q.nt);
     q.tokens_first = p.offsets || (long long)p.M <= (long long)p.N;
+    const int elem = p.out_type == HIKONV_OUT_F32 ? 4 : 2;
+    q.whole_stores = (uintptr_t)p.out % 32 == 0 && (uintptr_t)p.residual % 32 == 0 && p.out_row * elem % 32 == 0 && (!p.residual || p.res_row * elem % 32 == 0);
+    if (shape.pair) return launch_pair(q, x_f8, w_f8, st);
     const int columns = shape.tokens ? q.width : q.nt;
     q.b_off = kF8Rows * kF8Depth;
     q.stage_bytes = q.b_off + columns * kF8Depth;
@@ -602,12 +927,9 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     q.feed_off = q.stages * q.stage_bytes;
     q.turn_off = q.feed_off + feeds;
     q.held = q.turn_off + turns;
-    const int elem = p.out_type == HIKONV_OUT_F32 ? 4 : 2;
-    q.whole_stores = (uintptr_t)p.out % 32 == 0 && (uintptr_t)p.residual % 32 == 0 && p.out_row * elem % 32 == 0 && (!p.residual || p.res_row * elem % 32 == 0);
     // sums in 32 bits (1), the operands' types, 128 rows; the columns follow per tile
     const int a_type = shape.tokens ? x_f8 : w_f8, b_type = shape.tokens ? w_f8 : x_f8;
     q.idesc = (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(kF8Rows >> 4) << 24);
-    q.wait_cycles = kWaitCycles;
     const size_t smem = (size_t)q.held + 2048 + tables;
 
     CUtensorMap map_x, map_w;
@@ -634,7 +956,7 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
             return cudaLaunchKernelEx(&cfg, kernel, q, a, b) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
         });
     };
-    if (shape.tokens) return q.width == 256 ? launch(linear_f8_kernel<true, 128>) : launch(linear_f8_kernel<true, 64>);
+    if (shape.tokens) return launch(linear_f8_kernel<true, 64>);
     switch (q.nt) {
         case 16: return launch(linear_f8_kernel<false, 8>);
         case 32: return launch(linear_f8_kernel<false, 16>);
