@@ -8,7 +8,7 @@
 // neighbours in a row of the output) and output columns where rows are few (the number of rows is then that of the instruction's
 // columns, any multiple of 16, and the CTAs of a cluster may share the depth of a tile).
 //
-// One CTA per SM walks over the tiles.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 add up and finish.
+// One CTA per SM walks over the tiles.  Warp 0 loads, warp 1 multiplies, warp 2 brings the scales, warps 4 to 11 add up and finish.
 #include <cstddef>
 #include <cstring>
 
@@ -19,7 +19,6 @@ namespace hikonv {
 constexpr int kF8Rows = 128, kF8Depth = 128;
 constexpr int kF8MostStages = 12, kF8MostAccs = 8;
 constexpr int kF8FirstAdder = 4, kF8Adders = 8, kF8Threads = (kF8FirstAdder + kF8Adders) * 32;
-constexpr int kF8Ahead = 8;                             // steps whose scales of x are on their way
 constexpr size_t kF8MostSmem = 226 * 1024;
 
 struct F8Params {
@@ -37,11 +36,6 @@ struct F8Params {
     long long wait_cycles;
 };
 
-struct F8Control {
-    uint64_t full[kF8MostStages], empty[kF8MostStages], acc_full[kF8MostAccs], acc_empty[kF8MostAccs], drain;
-    uint32_t tmem;
-    int whole;                           // no wait of this CTA has run out
-};
 
 static __device__ unsigned int linear_f8_timeouts;
 
@@ -88,6 +82,9 @@ __device__ __forceinline__ uint64_t f8_mul(uint64_t a, uint64_t b) {
 }
 __device__ __forceinline__ float f8_low(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float f8_high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ void cp_async_4_at(uint32_t to, const float *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ float4 load_cluster_float4(uint32_t remote) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote));
@@ -110,8 +107,119 @@ __device__ __forceinline__ bool f8_wait(const F8Params &q, uint32_t bar, uint32_
     return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
 
-// The sums of a thread, CPW neighbouring columns of its lane as pairs of floats, and what becomes of them: a few at a time, which are then
-// shifted out, so that the code for them is there once and nothing else has to be in registers beside the rest.
+// ---- scales
+//
+// The scales of x and w that a tile's steps need come to shared memory by asynchronous copies of four bytes (rows of scales begin anywhere), a few steps at
+// a time, by a warp of their own, which runs ahead as far as the ring allows and waits for no copy: the copies themselves arrive at the slot's
+// barrier.  Asked for by the warps that add up, a step's scales took them 150 cycles.
+constexpr int kScaleBatch = 4, kScaleSlots = 4;         // steps of a slot; slots
+constexpr int kScaleBytes = (kScaleBatch * kF8Rows + 2 * kScaleBatch) * 4;       // of a slot: [step][row of x], [128-column block][step]
+struct ScaleBars {
+    uint64_t full[kScaleSlots], empty[kScaleSlots];
+};
+
+// `rows` rows of x from row0 on; `blocks` blocks of output columns, the first's scales at w, one block's behind the other's.
+__device__ __forceinline__ bool bring_scales(const F8Params &q, Ring &ring, uint32_t slots, uint32_t full, uint32_t empty, int row0, int rows, const float *w, int blocks,
+                                             int c0, int c1) {
+    const int lane = threadIdx.x & 31;
+    const float *xs = q.p.x_scale + c0 * q.xs_row + row0 + lane;
+    for (int c = c0; c < c1; c += kScaleBatch) {
+        if (!f8_wait(q, empty + 8 * ring.stage, ring.phase ^ 1)) return false;
+        const uint32_t slot = slots + ring.stage * kScaleBytes;
+#pragma unroll
+        for (int b = 0; b < kScaleBatch; ++b) {
+            if (c + b < c1) {
+#pragma unroll
+                for (int i = 0; i < kF8Rows; i += 32)
+                    if (i + lane < rows) cp_async_4_at(slot + (b * kF8Rows + i + lane) * 4, xs + i);
+            }
+            xs += q.xs_row;
+        }
+        const int block = lane / kScaleBatch, at = c + lane % kScaleBatch;
+        if (block < blocks && at < c1) cp_async_4_at(slot + (kScaleBatch * kF8Rows + lane) * 4, w + block * q.chunks + at);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * ring.stage) : "memory");
+        ring.next(kScaleSlots);
+    }
+    return true;
+}
+
+// The reader's side, one warp: which slot and step is next.
+struct ScaleRing {
+    const F8Params &q;
+    const uint32_t slots, full, empty;
+    uint32_t beat = 0;                   // steps that slots were there for
+
+    __device__ __forceinline__ ScaleRing(const F8Params &q_, uint32_t slots_, uint32_t full_, uint32_t empty_) : q(q_), slots(slots_), full(full_), empty(empty_) {}
+    // The slot of the next step, once it has been brought; null when the wait for it ran out.
+    __device__ __forceinline__ bool wait() {
+        return beat % kScaleBatch != 0 || f8_wait(q, full + 8 * (beat / kScaleBatch % kScaleSlots), beat / (kScaleBatch * kScaleSlots) & 1);
+    }
+    __device__ __forceinline__ uint32_t xs() const { return slots + beat / kScaleBatch % kScaleSlots * kScaleBytes + beat % kScaleBatch * (kF8Rows * 4); }
+    __device__ __forceinline__ uint32_t w(int block) const {
+        return slots + beat / kScaleBatch % kScaleSlots * kScaleBytes + (kScaleBatch * kF8Rows + block * kScaleBatch + beat % kScaleBatch) * 4;
+    }
+    // The step's scales have been read by this lane; `last`: of the tile.
+    __device__ __forceinline__ void next(bool last) {
+        const uint32_t slot = beat / kScaleBatch % kScaleSlots;
+        ++beat;
+        if (last) beat = (beat + kScaleBatch - 1) / kScaleBatch * kScaleBatch;
+        if (beat % kScaleBatch == 0) {
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbarrier_arrive(empty + 8 * slot);
+        }
+    }
+};
+__device__ __forceinline__ float load_shared_float(uint32_t at) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+struct F8Control {
+    uint64_t full[kF8MostStages], empty[kF8MostStages], acc_full[kF8MostAccs], acc_empty[kF8MostAccs], drain;
+    ScaleBars scales;
+    uint32_t tmem;
+    int whole;                           // no wait of this CTA has run out
+};
+
+// SiLU of two values for outputs of 16 bits, v / (1 + t) or v t / (1 + t) for v < 0 with t = exp(-|v|), as silu() has it.  t comes as a power of two
+// whose argument is rounded once, which moves it by less than 2^-17 of itself, and 2^32 times too large, so that normal results down to the smallest
+// keep their bits; both divisors, which lie in [1, 2], share a reciprocal (fminf: one value's NaN must not reach the other).  Eleven instructions a
+// value instead of 18, and the special-function unit, which does a quarter of a warp per cycle, is asked three times for two values instead of four.
+__device__ __forceinline__ void silu_short(float &v0, float &v1) {
+    float t0, t1, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t0) : "f"(fmaf(fabsf(v0), -1.44269504f, 32.f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t1) : "f"(fmaf(fabsf(v1), -1.44269504f, 32.f)));
+    const float d0 = fminf(fmaf(t0, 0x1p-32f, 1.f), 2.f), d1 = fminf(fmaf(t1, 0x1p-32f, 1.f), 2.f);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+    v0 = (v0 < 0.f ? v0 * t0 * 0x1p-32f : v0) * (r * d1);
+    v1 = (v1 < 0.f ? v1 * t1 * 0x1p-32f : v1) * (r * d0);
+}
+// The activation of neighbouring values in front of an output of type T.
+template <typename T, int COUNT>
+__device__ __forceinline__ void activate_some(float (&v)[COUNT], int act) {
+    switch (act) {
+        case HIKONV_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[i] = activate(v[i], HIKONV_ACT_RELU);
+            break;
+        case HIKONV_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < COUNT; i += 2) {
+                if constexpr (sizeof(T) == 2) silu_short(v[i], v[i + 1]);
+                else v[i] = activate(v[i], HIKONV_ACT_SILU), v[i + 1] = activate(v[i + 1], HIKONV_ACT_SILU);
+            }
+            break;
+        case HIKONV_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[i] = activate(v[i], HIKONV_ACT_GELU);
+            break;
+        default: break;
+    }
+}
+
+// The sums of a thread, CPW neighbouring columns of its lane as pairs of floats, and what becomes of them: some at a time, after which the rest is
+// moved down, so that the code for them is there once.
 template <int CPW>
 struct Sums {
     uint64_t sum[CPW / 2];
@@ -124,61 +232,46 @@ struct Sums {
     template <int COUNT>
     __device__ __forceinline__ void shift_out() {
 #pragma unroll
-        for (int i = 0; i < CPW / 2; ++i) sum[i] = i + COUNT / 2 < CPW / 2 ? sum[i + COUNT / 2] : 0;
+        for (int i = 0; i + COUNT / 2 < CPW / 2; ++i) sum[i] = sum[i + COUNT / 2];
     }
-    template <int ACT, int COUNT>
-    __device__ __forceinline__ void activate_as(float (&v)[COUNT]) {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = activate(v[i], ACT);
-    }
-    template <int COUNT>
-    __device__ __forceinline__ void activate_all(int act, float (&v)[COUNT]) {
-        switch (act) {
-            case HIKONV_ACT_RELU: activate_as<HIKONV_ACT_RELU>(v); break;
-            case HIKONV_ACT_SILU: activate_as<HIKONV_ACT_SILU>(v); break;
-            case HIKONV_ACT_GELU: activate_as<HIKONV_ACT_GELU>(v); break;
-            default: break;
-        }
-    }
-    // Lanes are rows of x from row0 + quad 32 on, `rows` of them in all; columns from n on, 16 at a time.  32 bytes of a row at once where rows begin
-    // on such a boundary, else turned in shared memory so that neighbouring lanes write neighbouring columns.
+    // Lanes are rows of x from row0 + quad 32 on, `rows` of them in all; columns from n on.  32 bytes of a row at once where rows begin on such a
+    // boundary, else turned in shared memory, 16 columns at a time, so that neighbouring lanes write neighbouring columns.
     template <typename T>
-    __device__ __forceinline__ void store_rows(const F8Params &q, const float (&v)[16], long long row0, int rows, int n, float *turn) {
+    __device__ __forceinline__ void finish_rows_as(const F8Params &q, int e, long long row0, int rows, int n, float *turn) {
+        constexpr int PER = 32 / sizeof(T), SOME = CPW < 64 ? CPW : 64;
         const LinearParams &p = q.p;
         const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
-        if (q.whole_stores && n + 16 <= p.N) {
-            constexpr int PER = 32 / sizeof(T);
-            if (row < rows) {
-                T *o = (T *)p.out + (row0 + row) * p.out_row + n;
-                const T *r = (const T *)p.residual + (row0 + row) * p.res_row + n;
+        const float *bias = (const float *)p.bias + (long long)e * p.N;
+        if (q.whole_stores && n + CPW <= p.N) {
+            T *o = (T *)p.out + (row0 + row) * p.out_row + n;
+            const T *r = (const T *)p.residual + (row0 + row) * p.res_row + n;
+            const bool there = row < rows;
+#pragma unroll 1
+            for (int i0 = 0; i0 < CPW; i0 += SOME) {
 #pragma unroll
-                for (int i0 = 0; i0 < 16; i0 += PER) {
+                for (int j = 0; j < SOME; j += PER) {
                     union { uint32_t w[8]; T v[PER]; } y, x;
-                    if (p.residual) load_global32(r + i0, x.w);
+                    float v[PER];
+                    if (p.residual && there) load_global32(r + i0 + j, x.w);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) from_float(p.residual ? v[i0 + i] + to_float(x.v[i]) : v[i0 + i], &y.v[i]);
-                    store_global32(o + i0, y.w);
+                    for (int i = 0; i < PER; ++i) v[i] = at(j + i);
+                    if (p.bias) {
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) v[i] += load_ordered(bias + n + i0 + j + i);
+                    }
+                    activate_some<T>(v, p.act);
+                    if (p.residual) {
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) v[i] += to_float(x.v[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) from_float(v[i], &y.v[i]);
+                    if (there) store_global32(o + i0 + j, y.w);
                 }
+                shift_out<SOME>();
             }
             return;
         }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = v[i];
-        __syncwarp();
-        const int col = n + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
-            if (there >= rows || col >= p.N) continue;
-            float y = turn[mine * 17 + (lane & 15)];
-            if (p.residual) y += to_float(load_ordered((const T *)p.residual + (row0 + there) * p.res_row + col));
-            from_float(y, (T *)p.out + (row0 + there) * p.out_row + col);
-        }
-    }
-    __device__ __forceinline__ void finish_rows(const F8Params &q, int e, int row0, int rows, int n, float *turn) {
-        const LinearParams &p = q.p;
-        const float *bias = (const float *)p.bias + (long long)e * p.N;
 #pragma unroll 1
         for (int i0 = 0; i0 < CPW && n < p.N; i0 += 16, n += 16) {
             float v[16];
@@ -189,47 +282,61 @@ struct Sums {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] += n + i < p.N ? load_ordered(bias + n + i) : 0.f;
             }
-            activate_all(p.act, v);
-            switch (p.out_type) {
-                case HIKONV_OUT_F32: store_rows<float>(q, v, row0, rows, n, turn); break;
-                case HIKONV_OUT_F16: store_rows<__half>(q, v, row0, rows, n, turn); break;
-                default: store_rows<__nv_bfloat16>(q, v, row0, rows, n, turn); break;
+            activate_some<T>(v, p.act);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = v[i];
+            __syncwarp();
+            const int col = n + (lane & 15);
+#pragma unroll 4
+            for (int i = 0; i < 16; ++i) {
+                const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
+                if (there >= rows || col >= p.N) continue;
+                float y = turn[mine * 17 + (lane & 15)];
+                if (p.residual) y += to_float(load_ordered((const T *)p.residual + (row0 + there) * p.res_row + col));
+                from_float(y, (T *)p.out + (row0 + there) * p.out_row + col);
             }
+        }
+    }
+    __device__ __forceinline__ void finish_rows(const F8Params &q, int e, int row0, int rows, int n, float *turn) {
+        switch (q.p.out_type) {
+            case HIKONV_OUT_F32: finish_rows_as<float>(q, e, row0, rows, n, turn); break;
+            case HIKONV_OUT_F16: finish_rows_as<__half>(q, e, row0, rows, n, turn); break;
+            default: finish_rows_as<__nv_bfloat16>(q, e, row0, rows, n, turn); break;
         }
     }
     // Lanes are output columns from n0 + quad 32 on: each of `rows` rows of x from row0 on is written by neighbouring lanes, eight rows at a time.
     template <typename T>
-    __device__ __forceinline__ void store_columns(const F8Params &q, const float (&v)[8], long long row0, int rows, int n) {
+    __device__ __forceinline__ void finish_columns_as(const F8Params &q, int e, long long row0, int rows, int n) {
         const LinearParams &p = q.p;
+        const float b = p.bias ? load_ordered((const float *)p.bias + (long long)e * p.N + n) : 0.f;
         T *o = (T *)p.out + row0 * p.out_row + n;
         const T *r = (const T *)p.residual + row0 * p.res_row + n;
-        T res[8];
-        if (p.residual) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < rows) res[i] = load_ordered(r + i * p.res_row);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < rows) from_float(p.residual ? v[i] + to_float(res[i]) : v[i], o + i * p.out_row);
-    }
-    __device__ __forceinline__ void finish_columns(const F8Params &q, int e, int row0, int rows, int n0) {
-        const LinearParams &p = q.p;
-        const int n = n0 + ((threadIdx.x >> 5) & 3) * 32 + (threadIdx.x & 31);
-        if (n >= p.N) return;
-        const float b = p.bias ? load_ordered((const float *)p.bias + (long long)e * p.N + n) : 0.f;
 #pragma unroll 1
-        for (int i0 = 0; i0 < CPW && rows > 0; i0 += 8, rows -= 8, row0 += 8) {
+        for (int i0 = 0; i0 < CPW && rows > 0; i0 += 8, rows -= 8, o += 8 * p.out_row, r += 8 * p.res_row) {
             float v[8];
+            T res[8];
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < rows) res[i] = load_ordered(r + i * p.res_row);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = p.bias ? at(i) + b : at(i);
             shift_out<8>();
-            activate_all(p.act, v);
-            switch (p.out_type) {
-                case HIKONV_OUT_F32: store_columns<float>(q, v, row0, rows, n); break;
-                case HIKONV_OUT_F16: store_columns<__half>(q, v, row0, rows, n); break;
-                default: store_columns<__nv_bfloat16>(q, v, row0, rows, n); break;
-            }
+            activate_some<T>(v, p.act);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < rows) from_float(p.residual ? v[i] + to_float(res[i]) : v[i], o + i * p.out_row);
+        }
+    }
+    __device__ __forceinline__ void finish_columns(const F8Params &q, int e, int row0, int rows, int n0) {
+        const int n = n0 + ((threadIdx.x >> 5) & 3) * 32 + (threadIdx.x & 31);
+        if (n >= q.p.N) return;
+        switch (q.p.out_type) {
+            case HIKONV_OUT_F32: finish_columns_as<float>(q, e, row0, rows, n); break;
+            case HIKONV_OUT_F16: finish_columns_as<__half>(q, e, row0, rows, n); break;
+            default: finish_columns_as<__nv_bfloat16>(q, e, row0, rows, n); break;
         }
     }
 };
@@ -239,70 +346,35 @@ template <bool TOKENS, int CPW>
 struct Adder {
     const F8Params &q;
     const uint32_t tmem, acc_full, acc_empty;
-    const int c0, c1;
-    uint8_t *const feed;                 // this warp's: kF8Ahead slots of scales
     int lane, quad, half;
+    ScaleRing scales;
     Ring acc;
     Sums<CPW> sums;
-    float ws, ws_next;                   // w_scale of 32 steps, a lane each
 
-    static constexpr int kSlot = (TOKENS ? 32 : CPW < 32 ? 32 : CPW) * 4;
-
-    __device__ __forceinline__ Adder(const F8Params &q_, uint32_t tmem_, uint32_t full, uint32_t empty, int c0_, int c1_, uint8_t *feeds)
-        : q(q_), tmem(tmem_), acc_full(full), acc_empty(empty), c0(c0_), c1(c1_),
-          feed(feeds + ((threadIdx.x >> 5) - kF8FirstAdder) * (kF8Ahead * kSlot)) {
+    __device__ __forceinline__ Adder(const F8Params &q_, uint32_t tmem_, uint32_t full, uint32_t empty, const ScaleRing &s)
+        : q(q_), tmem(tmem_), acc_full(full), acc_empty(empty), scales(s) {
         lane = threadIdx.x & 31;
         quad = (threadIdx.x >> 5) & 3;
         half = ((threadIdx.x >> 5) - kF8FirstAdder) >> 2;
     }
-    __device__ __forceinline__ const float *w_scales(const Tile &t) const {
-        const int nb = min((t.n0 + (TOKENS ? half * CPW : 0)) / kF8Depth, q.w_blocks - 1);
-        return q.p.w_scale + ((long long)t.e * q.w_blocks + nb) * q.chunks;
-    }
-    // x_scale of step c on its way to its slot: of this lane's row, or of the warp's columns.
-    __device__ __forceinline__ void ask(const Tile &t, int c) {
-        if (c < c1) {
-            const float *src = q.p.x_scale + c * q.xs_row + t.row0;
-            uint8_t *to = feed + ((c - c0) % kF8Ahead) * kSlot;
-            constexpr int COUNT = TOKENS ? 32 : CPW;
-#pragma unroll
-            for (int i = 0; i < COUNT; i += 32) {
-                const int row = TOKENS ? quad * 32 + lane : half * CPW + i + lane;
-                if (i + lane < COUNT && row < t.rows) cp_async_4(to + (i + lane) * 4, src + row, 4);
-            }
-        }
-        cp_async_commit();
-    }
-    // What a tile's first steps need, asked for before the tile before is finished.
-    __device__ __forceinline__ void begin(const Tile &t) {
-        const float *w = w_scales(t);
-        ws_next = c0 + lane < c1 ? load_ordered(w + c0 + lane) : 0.f;
-        if (!TOKENS) __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kF8Ahead; ++i) ask(t, c0 + i);
-    }
-    __device__ __forceinline__ bool add(const Tile &t) {
+    __device__ __forceinline__ bool add(int steps) {
         constexpr int CH = CPW < 32 ? CPW : 32;
-        const float *w = w_scales(t);
         sums.clear();
-        for (int c = c0; c < c1; ++c) {
-            const int at = (c - c0) & 31;
-            if (at == 0) {
-                ws = ws_next;
-                ws_next = c + 32 + lane < c1 ? load_ordered(w + c + 32 + lane) : 0.f;
+        for (int c = 0; c < steps; ++c) {
+            if (!scales.wait()) return false;
+            const float w = load_shared_float(scales.w(0));
+            const uint32_t xs = scales.xs();
+            float s = w;
+            if (TOKENS) {
+                s *= load_shared_float(xs + (quad * 32 + lane) * 4);
+                scales.next(c == steps - 1);
             }
+            const uint64_t ss = f8_two(s, s);
             if (!f8_wait(q, acc_full + 8 * acc.stage, acc.phase)) return false;
             tc_fence_after();
             const uint32_t d = tmem + acc.stage * q.acc_cols + ((uint32_t)(quad * 32) << 16) + half * CPW;
             uint32_t v[2][CH];
             f8_load(d, v[0]);
-            asm volatile("cp.async.wait_group %0;" ::"n"(kF8Ahead - 1) : "memory");
-            if (!TOKENS) __syncwarp();
-            const uint8_t *slot = feed + ((c - c0) % kF8Ahead) * kSlot;
-            const float w1 = __shfl_sync(0xFFFFFFFFu, ws, at);
-            float s = w1;
-            if (TOKENS) s *= *reinterpret_cast<const volatile float *>(slot + lane * 4);
-            const uint64_t ss = f8_two(s, s);
 #pragma unroll
             for (int i = 0; i < CPW; i += CH) {
                 uint32_t(&now)[CH] = v[(i / CH) & 1];
@@ -318,17 +390,16 @@ struct Adder {
                 for (int k = 0; k < CH; k += 4) {
                     uint64_t s01 = ss, s23 = ss;
                     if (!TOKENS) {
-                        const float4 xs = *reinterpret_cast<const float4 *>(slot + (i + k) * 4);
-                        s01 = f8_mul(f8_two(xs.x, xs.y), ss);
-                        s23 = f8_mul(f8_two(xs.z, xs.w), ss);
+                        const uint4 x = load_shared16(xs + (half * CPW + i + k) * 4);
+                        s01 = f8_mul(f8_two(x.x, x.y), ss);
+                        s23 = f8_mul(f8_two(x.z, x.w), ss);
                     }
                     uint64_t *o = sums.sum + (i + k) / 2;
                     o[0] = f8_fma(f8_two(now[k], now[k + 1]), s01, o[0]);
                     o[1] = f8_fma(f8_two(now[k + 2], now[k + 3]), s23, o[1]);
                 }
             }
-            if (!TOKENS) __syncwarp();                  // all lanes have read the slot
-            ask(t, c + kF8Ahead);
+            if (!TOKENS) scales.next(c == steps - 1);
             acc.next(q.accs);
         }
         return true;
@@ -417,6 +488,10 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             mbarrier_init(HIKONV_BAR(acc_full, lane), 1);
             mbarrier_init(HIKONV_BAR(acc_empty, lane), kF8Adders);
         }
+        if (lane < kScaleSlots) {
+            mbarrier_init(HIKONV_BAR(scales.full, lane), 32);
+            mbarrier_init(HIKONV_BAR(scales.empty, lane), kF8Adders);
+        }
         if (lane == 0) {
             mbarrier_init(HIKONV_BAR(drain, 0), 1);
             ctl.whole = 1;
@@ -500,6 +575,15 @@ __global__ void __launch_bounds__(kF8Threads, 1)
                 f8_wait(q, HIKONV_BAR(drain, 0), 0);
             }
         }
+        if (warp == 2) {
+            Ring ring;
+            for (int t = t0; fine && t < tiles; t += step) {
+                const Tile tile = find_tile(q, tables, t, q.width);
+                const float *w = p.w_scale + ((long long)tile.e * q.w_blocks + tile.n0 / kF8Depth) * q.chunks;
+                fine = bring_scales(q, ring, stages + q.feed_off, HIKONV_BAR(scales.full, 0), HIKONV_BAR(scales.empty, 0), tile.row0, tile.rows, w, 1, c0, c1);
+            }
+            cp_async_wait_all();
+        }
         if (q.splits > 1) {
             if (!fine) ctl.whole = 0;
             __syncwarp();
@@ -507,15 +591,15 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             cluster_sync_all();                         // the others may still read this CTA's part
         }
     } else {
-        Adder<TOKENS, CPW> adder(q, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0), c0, c1, area + q.feed_off);
+        Adder<TOKENS, CPW> adder(q, tmem, HIKONV_BAR(acc_full, 0), HIKONV_BAR(acc_empty, 0),
+                                   ScaleRing(q, stages + q.feed_off, HIKONV_BAR(scales.full, 0), HIKONV_BAR(scales.empty, 0)));
         float *turn = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17);
-        Tile tile{0, 0, 0, 0};
-        if (t0 < tiles) {
-            tile = find_tile(q, tables, t0, q.width);
-            adder.begin(tile);
-        }
         if (!TOKENS && q.splits > 1) {
-            if (t0 < tiles) fine = adder.add(tile);
+            Tile tile{0, 0, 0, 0};
+            if (t0 < tiles) {
+                tile = find_tile(q, tables, t0, q.width);
+                fine = adder.add(c1 - c0);
+            }
             if (t0 < tiles && fine) {
 #pragma unroll
                 for (int i = 0; i < CPW; ++i)
@@ -534,17 +618,11 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             cluster_sync_all();                         // the others may still read this CTA's part
         } else {
             for (int t = t0; t < tiles; t += step) {
-                fine = adder.add(tile);
+                fine = adder.add(c1 - c0);
                 if (!fine) break;
-                const Tile now = tile;
-                if (t + step < tiles) {
-                    tile = find_tile(q, tables, t + step, q.width);
-                    adder.begin(tile);
-                }
-                adder.finish(now, turn);
+                adder.finish(find_tile(q, tables, t, q.width), turn);
             }
         }
-        cp_async_wait_all();
     }
     if (!fine && lane == 0) atomicAdd(&linear_f8_timeouts, 1u);
     __syncwarp();
@@ -567,6 +645,8 @@ constexpr int kPairAdders = 8, kPairThreads = (kF8FirstAdder + kPairAdders) * 32
 // which takes all that 384 threads can have.
 constexpr int kPairAdderRegs = 216, kPairOtherRegs = 64, kPairLaunchRegs = 168;
 static_assert(kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32 <= kPairLaunchRegs * kPairThreads, "registers of the launch");
+
+constexpr int kPairAhead = 8;                           // steps whose scales of x are on their way
 
 struct PairControl {
     uint64_t full[kPairStages], empty[kPairStages], acc_full[4], acc_empty[4], drain[2];
@@ -591,7 +671,7 @@ __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// A warp that adds up: a quarter of the lanes, 128 columns, 32 at a time.  Scales of x come by asynchronous copies, kF8Ahead steps ahead, those of w
+// A warp that adds up: a quarter of the lanes, 128 columns, 32 at a time.  Scales of x come by asynchronous copies, kPairAhead steps ahead, those of w
 // 32 steps at a time.  While 32 columns are added the next ones are on their way from tensor memory, those of the next step among them, whose barrier
 // is waited for before the last ones of a step are added.
 struct PairAdder {
@@ -599,12 +679,12 @@ struct PairAdder {
     const F8Params &q;
     Sums<kPairHalf> sums;
     const float *xs, *ws;                // the next scale to ask for, of this lane's row; of this warp's columns
-    const uint32_t feed;                 // kF8Ahead slots of 32 scales of x
+    const uint32_t feed;                 // kPairAhead slots of 32 scales of x
     float w_now, w_next;                 // scales of w, a lane each
 
     __device__ __forceinline__ PairAdder(const F8Params &q_, uint32_t feed_) : q(q_), feed(feed_) {}
     __device__ __forceinline__ void ask(int c) {
-        if (c < q.chunks) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(feed + c % kF8Ahead * 128), "l"(xs) : "memory");
+        if (c < q.chunks) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(feed + c % kPairAhead * 128), "l"(xs) : "memory");
         xs += q.xs_row;
         cp_async_commit();
     }
@@ -614,20 +694,20 @@ struct PairAdder {
         xs = q.p.x_scale + row;
         ws = q.p.w_scale + ((long long)e * q.w_blocks + block) * q.chunks + lane;
         w_next = lane < q.chunks ? load_ordered(ws) : 0.f;
-#pragma unroll 1
-        for (int i = 0; i < kF8Ahead; ++i) ask(i);
+#pragma unroll
+        for (int i = 0; i < kPairAhead; ++i) ask(i);
     }
-    // The scale of step c, and that of kF8Ahead steps later asked for.
+    // The scale of step c, and that of kPairAhead steps later asked for.
     __device__ __forceinline__ float scale(int c) {
         if ((c & 31) == 0) {
             w_now = w_next;
             w_next = c + 32 + (int)(threadIdx.x & 31) < q.chunks ? load_ordered(ws + c + 32) : 0.f;
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(kF8Ahead - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kPairAhead - 1) : "memory");
         float x;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(feed + c % kF8Ahead * 128) : "memory");
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(feed + c % kPairAhead * 128) : "memory");
         const float s = x * __shfl_sync(0xFFFFFFFFu, w_now, c & 31);
-        ask(c + kF8Ahead);
+        ask(c + kPairAhead);
         return s;
     }
     // taddr, bars: of the first of this warp's two accumulators, the second's 256 columns and two barriers on; empty: the cluster's address.
@@ -774,9 +854,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairAdderRegs));
-        PairAdder adder(q, stages + q.feed_off + (warp - kF8FirstAdder) * (kF8Ahead * 128) + lane * 4);
-        float *turn_area = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17 + 4);
-        float *kept = turn_area + 32 * 17;
+        PairAdder adder(q, stages + q.feed_off + (warp - kF8FirstAdder) * (kPairAhead * 128) + lane * 4);
+        float *turn_area = reinterpret_cast<float *>(area + q.turn_off) + (warp - kF8FirstAdder) * (32 * 17);
         const int quad = warp & 3, half = (warp - kF8FirstAdder) >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + half * kPairHalf, full = HIKONV_BAR(acc_full, half);
         const uint32_t empty = remote_address(HIKONV_BAR(acc_empty, half), 0);
@@ -822,40 +901,41 @@ struct F8Shape {
     int nt, width, splits;
 };
 
-// The tile that a model of the time, in cycles, likes best.  A step costs the longest of its multiplies (2 per column of the instruction), its
-// way from the second-level cache (70 bytes per cycle and SM) and the exchange between the warps; a tile its set-up and its end.
+// The tile that a model of the time, in us, likes best: a set-up, and for each tile that a CTA or pair takes in turn its steps and its end, as measured
+// on weights from memory at depths of 512 to 16384.  A step of a tile of few rows is the round of its sums from the multiplies to the adding warps
+// and back, 0.265 us for 16 rows to 0.6 for 128; a shared depth has fewer steps and an exchange of sums.  4096 x 4096 weights: 16 rows 11.6 us,
+// in two parts 9.6, in four 8.5; 128 rows by tiles of 64 rows in two parts 12.4, by 128 x 128 15.6, by pairs 21; 512 rows 27, 16.3 and 20; 1024 rows
+// 50, 28.6 and 20.2; 4096 rows by 128 x 128 90, by pairs 70.
 static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
     const int chunks = ceil_div(p.K, kF8Depth), filled = p.E < p.M ? p.E : p.M;
     F8Shape best{false, false, 16, kF8Rows, 1};
     double least = 1e300;
-    auto consider = [&](bool tokens, int nt, int width, int splits) {
+    auto consider = [&](bool tokens, int nt, int width, int splits, double setup, double step, double end) {
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * ceil_div(p.N, width);
         if (splits > 1 && (tiles * splits > sms - 20 || splits > chunks)) return;
-        const bool pair = nt == kPairRows;
-        const int columns = tokens ? width : nt;
-        const double bytes = pair ? kPairStage : (kF8Rows + columns) * (double)kF8Depth;
-        double step = 2.0 * columns > bytes / 70.0 ? 2.0 * columns : bytes / 70.0;
-        if (step < 300) step = 300;
-        const int units = pair ? sms / 2 : sms;
-        const double waves = splits > 1 ? 1.0 : p.offsets ? (tiles > units ? tiles / units + 0.3 : 1.0) : (double)((long long)(tiles + units - 1) / units);
-        const double time = waves * (ceil_div(chunks, splits) * step + 800.0 + 10.0 * columns) + 3000.0 +
-                            (splits > 1 ? 2000.0 + 500.0 * splits + 62.0 * nt / splits + 8.0 * nt : 0.0);
+        const int units = nt == kPairRows ? sms / 2 : sms;
+        const double turns = splits > 1 ? 1.0 : p.offsets ? (tiles > units ? tiles / units + 0.3 : 1.0) : (double)((long long)(tiles + units - 1) / units);
+        const double time = setup + turns * (ceil_div(chunks, splits) * step + end) + (splits == 1 ? 0.0 : splits == 2 ? 2.3 : splits == 4 ? 2.6 : 2.9);
         if (time < least) {
             least = time;
             best = F8Shape{tokens, nt == kPairRows, nt, width, splits};
         }
     };
-    for (int nt = 16; nt <= 128; nt *= 2)
-        for (int splits = 1; splits <= 8; splits *= 2) consider(false, nt, kF8Rows, splits);
-    consider(true, kF8Rows, 128, 1);
-    consider(true, kPairRows, kPairWidth, 1);
+    for (int splits = 1; splits <= 8; splits *= 2) {
+        consider(false, 16, kF8Rows, splits, 2.6, 0.265, 0.4);
+        consider(false, 32, kF8Rows, splits, 2.6, 0.3, 0.5);
+        consider(false, 64, kF8Rows, splits, 2.6, 0.385, 0.7);
+        consider(false, 128, kF8Rows, splits, 2.6, 0.6, 1.1);
+    }
+    consider(true, kF8Rows, 128, 1, 3.0, 0.37, 0.9);
+    consider(true, kPairRows, kPairWidth, 1, 4.5, 0.46, 1.3);
     return best;
 }
 
 static int launch_pair(F8Params q, int x_f8, int w_f8, cudaStream_t st) {
     const LinearParams &p = q.p;
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
-    const int feeds = kPairAdders * kF8Ahead * 32 * 4, turns = kPairAdders * (32 * 17 + 4) * 4;
+    const int feeds = kPairAdders * kPairAhead * 32 * 4, turns = kPairAdders * 32 * 17 * 4;
     q.stages = (int)((kF8MostSmem - 2048 - tables - feeds - turns) / kPairStage);          // six; five beside the tables of 600 groups and more
     if (q.stages > kPairStages) q.stages = kPairStages;
     q.feed_off = q.stages * kPairStage;
@@ -870,22 +950,25 @@ static int launch_pair(F8Params q, int x_f8, int w_f8, cudaStream_t st) {
     const int pairs = sm_count_here() / 2;
     const long long tiles = (p.offsets ? p.M / q.nt + (p.E < p.M ? p.E : p.M) : (long long)q.m_tiles) * q.n_blocks;
     const size_t smem = (size_t)q.held + 2048 + tables;
-    return with_dynamic_smem((const void *)linear_f8_pair_kernel, smem, [&] {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
-        cfg.blockDim = dim3(kPairThreads);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = 2;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 2;
-        return cudaLaunchKernelEx(&cfg, linear_f8_pair_kernel, q, map_x, map_w) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
-    });
+    auto launch = [&](auto kernel) {
+        return with_dynamic_smem((const void *)kernel, smem, [&] {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
+            cfg.blockDim = dim3(kPairThreads);
+            cfg.dynamicSmemBytes = smem;
+            cfg.stream = st;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = 2;
+            attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+            return cudaLaunchKernelEx(&cfg, kernel, q, map_x, map_w) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+        });
+    };
+    return launch(linear_f8_pair_kernel);
 }
 
 static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long xs_row, cudaStream_t st) {
@@ -914,7 +997,7 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     q.acc_cols = columns < 32 ? 32 : columns;
     q.accs = 512 / q.acc_cols < 4 ? 512 / q.acc_cols : 4;
     q.tmem_cols = q.accs * q.acc_cols;                   // a power of two
-    const int slot = (shape.tokens || columns < 64 ? 32 : columns / 2) * 4, feeds = kF8Adders * kF8Ahead * slot;
+    const int feeds = kScaleSlots * kScaleBytes;
     const int turns = shape.tokens ? kF8Adders * 32 * 17 * 4 : 0;
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
     q.stages = (int)((kF8MostSmem - 2048 - tables - feeds - turns) / q.stage_bytes);
