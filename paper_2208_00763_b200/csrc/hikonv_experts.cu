@@ -17,7 +17,7 @@ namespace hikonv {
 
 // ---- sorting
 
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortSteps = 8;
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortSteps = 8;
 constexpr int kSortBlock = kSortThreads * kSortSteps;       // pairs whose experts the registers of a CTA hold
 constexpr int kSortMostCtas = 128;
 
@@ -27,41 +27,58 @@ struct SortParams {
     long long row;                       // elements from token to token
     long long pairs;
     int k, E, ctas;
-    long long per_cta;                   // pairs, a multiple of kSortBlock
+    long long per_cta;                   // pairs; a multiple of kSortBlock where there are several CTAs
     int32_t *offsets, *slots;
     uint32_t *counts;                    // [ctas][E + 1], null for one CTA
 };
 
-// The expert of a pair, E for none.
-__device__ __forceinline__ int expert_of(const SortParams &p, long long pair) {
-    long long at = pair;
-    if (p.row != p.k) {
-        const long long t = pair <= 0x7FFFFFFF ? (long long)((uint32_t)pair / (uint32_t)p.k) : pair / p.k;
-        at = t * p.row + (pair - t * p.k);
+// The experts of a stretch of pairs that begins at `from`: step s of a warp are 32 neighbours, the steps of a warp follow one another.  E for none,
+// -1 behind the end.
+__device__ __forceinline__ void read_experts(const SortParams &p, long long from, long long end, int steps, int (&key)[kSortSteps]) {
+    const long long first = from + (long long)((threadIdx.x >> 5) * steps) * 32 + (threadIdx.x & 31);
+    long long e[kSortSteps];
+#pragma unroll
+    for (int s = 0; s < kSortSteps; ++s) {
+        const long long i = first + s * 32;
+        e[s] = -1;
+        if (s >= steps || i >= end) continue;
+        long long at = i;
+        if (p.row != p.k) {
+            const long long t = i <= 0x7FFFFFFF ? (long long)((uint32_t)i / (uint32_t)p.k) : i / p.k;
+            at = t * p.row + (i - t * p.k);
+        }
+        e[s] = p.wide ? load_ordered((const long long *)p.experts + at) : (long long)load_ordered((const int32_t *)p.experts + at);
     }
-    const long long e = p.wide ? load_ordered((const long long *)p.experts + at) : (long long)load_ordered((const int32_t *)p.experts + at);
-    return e >= 0 && e < p.E ? (int)e : p.E;
+#pragma unroll
+    for (int s = 0; s < kSortSteps; ++s) key[s] = s >= steps || first + s * 32 >= end ? -1 : e[s] >= 0 && e[s] < p.E ? (int)e[s] : p.E;
 }
 
 // How many pairs of each expert a CTA's stretch has.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortParams p) {
     extern __shared__ uint32_t hist[];
     grid_dependency_release();
-    grid_dependency_wait();
     for (int e = threadIdx.x; e <= p.E; e += kSortThreads) hist[e] = 0;
+    grid_dependency_wait();
     __syncthreads();
-    const long long a = blockIdx.x * p.per_cta, b = min(a + p.per_cta, p.pairs);
-    for (long long i = a + threadIdx.x; i < b; i += kSortThreads) atomicAdd(hist + expert_of(p, i), 1u);
+    const long long begin = blockIdx.x * p.per_cta, end = min(begin + p.per_cta, p.pairs);
+    for (long long from = begin; from < end; from += kSortBlock) {
+        int key[kSortSteps];
+        read_experts(p, from, end, kSortSteps, key);
+#pragma unroll
+        for (int s = 0; s < kSortSteps; ++s)
+            if (key[s] >= 0) atomicAdd(hist + key[s], 1u);
+    }
     __syncthreads();
     for (int e = threadIdx.x; e <= p.E; e += kSortThreads) p.counts[(long long)blockIdx.x * (p.E + 1) + e] = hist[e];
 }
 
-// Places of a CTA's stretch.  Every warp takes neighbouring pairs, 32 at a time: the lanes of one expert find each other, and the place is
-// the expert's next one in this warp plus the lanes before.
+// Places of a CTA's stretch.  Every warp takes neighbouring pairs, 32 at a time: the lanes of one expert find each other, and a place is the
+// expert's next one, the pairs of warps before, of this warp so far, and of lanes before.
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortParams p) {
     extern __shared__ uint32_t shared[];
     const int E1 = p.E + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    uint32_t *hist = shared, *next = shared + kSortWarps * E1, *total = next + E1, *sums = total + E1;     // [warp][E1]: of each expert in each warp; next place; all pairs
+    // [warp][E1] pairs of each expert in each warp, then in the warps before; its next place; all its pairs; of this block; sums of warps
+    uint32_t *hist = shared, *next = hist + kSortWarps * E1, *total = next + E1, *block = total + E1, *sums = block + E1;
     grid_dependency_release();
     for (int i = tid; i < (kSortWarps + 2) * E1; i += kSortThreads) shared[i] = 0;
     grid_dependency_wait();
@@ -69,50 +86,55 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     const long long begin = blockIdx.x * p.per_cta, end = min(begin + p.per_cta, p.pairs);
     int key[kSortSteps];
     uint32_t same[kSortSteps];
-    auto read = [&](long long from) {                   // the block's experts, and how many each warp has
+    // The block's experts, in how many lanes of each step, and how many each warp has; then how many the warps before have.
+    auto read = [&](long long from) {
+        const int steps = (int)min((long long)kSortSteps, (end - from + kSortThreads - 1) / kSortThreads);
+        read_experts(p, from, end, steps, key);
 #pragma unroll
         for (int s = 0; s < kSortSteps; ++s) {
-            const long long i = from + (warp * kSortSteps + s) * 32 + lane;
-            key[s] = i < end ? expert_of(p, i) : -1;
-        }
-#pragma unroll
-        for (int s = 0; s < kSortSteps; ++s) {
-            if (from + (warp * kSortSteps + s) * 32 >= end) break;
+            if (s >= steps) break;
             same[s] = __match_any_sync(0xFFFFFFFFu, key[s]);
             if (key[s] >= 0 && lane == __ffs(same[s]) - 1) hist[warp * E1 + key[s]] += __popc(same[s]);
             __syncwarp();
         }
+        __syncthreads();
+        for (int e = warp; e < E1; e += kSortWarps) {
+            const uint32_t mine = hist[lane * E1 + e];
+            uint32_t upto = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+                if (lane >= d) upto += v;
+            }
+            hist[lane * E1 + e] = upto - mine;
+            if (lane == 31) block[e] = upto;
+        }
+        return steps;
     };
-    read(begin);
     if (p.counts) {
         // columns of the counts, by several threads each: what lies in front of this CTA, and all
-        int parts = 1;
-        while (parts * 2 * E1 <= kSortThreads && parts < p.ctas) parts *= 2;
+        const int parts = (p.ctas + 7) / 8;
         for (int i = tid; i < parts * E1; i += kSortThreads) {
-            const int e = i % E1;
-            uint32_t before = 0, all = 0;
-            for (int c = i / E1; c < p.ctas; c += parts) {
-                const uint32_t v = load_ordered(p.counts + (long long)c * E1 + e);
-                all += v;
-                if (c < (int)blockIdx.x) before += v;
+            const int part = i / E1, e = i - part * E1;
+            uint32_t v[8], before = 0, all = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = part * 8 + j < p.ctas ? load_ordered(p.counts + (long long)(part * 8 + j) * E1 + e) : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                all += v[j];
+                if (part * 8 + j < (int)blockIdx.x) before += v[j];
             }
-            atomicAdd(next + e, before);
-            atomicAdd(total + e, all);
+            if (before) atomicAdd(next + e, before);
+            if (all) atomicAdd(total + e, all);
         }
-        __syncthreads();
-    } else {
-        __syncthreads();
-        for (int e = tid; e < E1; e += kSortThreads) {
-            uint32_t all = 0;
-            for (int w = 0; w < kSortWarps; ++w) all += hist[w * E1 + e];
-            total[e] = all;
-        }
-        __syncthreads();
     }
+    int steps = read(begin);
+    __syncthreads();
     // where each expert begins
+    const uint32_t *all = p.counts ? total : block;
     const int items = (E1 + kSortThreads - 1) / kSortThreads;
     uint32_t mine = 0;
-    for (int i = 0; i < items; ++i) mine += tid * items + i < E1 ? total[tid * items + i] : 0;
+    for (int i = 0; i < items; ++i) mine += tid * items + i < E1 ? all[tid * items + i] : 0;
     uint32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -121,33 +143,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     }
     if (lane == 31) sums[warp] = upto;
     __syncthreads();
-    uint32_t start = upto - mine;
-    for (int w = 0; w < warp; ++w) start += sums[w];
+    uint32_t before = lane < warp ? sums[lane] : 0;
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    uint32_t start = before + upto - mine;
     for (int i = 0; i < items; ++i) {
         const int e = tid * items + i;
         if (e >= E1) break;
         if (blockIdx.x == 0) p.offsets[e] = (int32_t)start;
         next[e] += start;
-        start += total[e];
+        start += all[e];
     }
     __syncthreads();
     for (long long from = begin; from < end;) {
-        for (int e = tid; e < E1; e += kSortThreads) {
-            uint32_t at = next[e];
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t v = hist[w * E1 + e];
-                hist[w * E1 + e] = at;
-                at += v;
-            }
-            next[e] = at;
-        }
-        __syncthreads();
 #pragma unroll
         for (int s = 0; s < kSortSteps; ++s) {
-            const long long i = from + (warp * kSortSteps + s) * 32 + lane;
-            if (i - lane >= end) break;
+            if (s >= steps) break;
+            const long long i = from + (long long)(warp * steps + s) * 32 + lane;
             if (key[s] >= 0) {
-                const int place = (int)(hist[warp * E1 + key[s]] + __popc(same[s] & ((1u << lane) - 1)));
+                const int place = (int)(next[key[s]] + hist[warp * E1 + key[s]] + __popc(same[s] & ((1u << lane) - 1)));
                 p.slots[i] = key[s] < p.E ? place : -2 - place;
             }
             __syncwarp();
@@ -157,9 +170,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
         from += kSortBlock;
         if (from >= end) break;
         __syncthreads();
+        for (int e = tid; e < E1; e += kSortThreads) next[e] += block[e];
         for (int i = tid; i < kSortWarps * E1; i += kSortThreads) hist[i] = 0;
         __syncthreads();
-        read(from);
+        steps = read(from);
         __syncthreads();
     }
 }
@@ -191,57 +205,76 @@ template <> __device__ __forceinline__ float rows_round(float v) { return v; }
 template <> __device__ __forceinline__ __half rows_round(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 rows_round(float v) { return __float2bfloat16_rn(v); }
 
-// V neighbouring values of a row, loaded and stored as one.
-template <typename T, int V>
-struct alignas(sizeof(T) * V) Pack {
-    T v[V];
+// The V columns of a row that a thread takes: neighbours, loaded and stored as one, where rows begin on 16-byte boundaries (WIDE), else as far apart as
+// there are threads, so that neighbouring threads load and store neighbours.
+template <typename T, int V, bool WIDE>
+struct Columns {
+    struct alignas(WIDE ? sizeof(T) * V : sizeof(T)) Pack {
+        T v[V];
+    };
+    static __device__ __forceinline__ int first(int thread) { return WIDE ? thread * V : thread; }
+    static __device__ __forceinline__ Pack load(const T *row, int c, int apart, int H) {
+        if constexpr (WIDE) {
+            return load_ordered(reinterpret_cast<const Pack *>(row + c));
+        } else {
+            Pack o;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i * apart < H) o.v[i] = load_ordered(row + c + i * apart);
+                else o.v[i] = T();
+            return o;
+        }
+    }
+    static __device__ __forceinline__ void store(T *row, int c, int apart, int H, const Pack &o) {
+        if constexpr (WIDE) {
+            *reinterpret_cast<Pack *>(row + c) = o;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i * apart < H) row[c + i * apart] = o.v[i];
+        }
+    }
 };
-
-// A thread takes one column of packs of one token.  Block: (columns, tokens).
-struct Place {
-    int t;
-    long long c;
-};
-template <int V>
-__device__ __forceinline__ Place row_place() {
-    return {(int)(blockIdx.x * blockDim.y + threadIdx.y), ((long long)blockIdx.y * blockDim.x + threadIdx.x) * V};
-}
+// Block: (columns, tokens); a grid's second dimension goes on along the rows.
+__device__ __forceinline__ int row_token() { return blockIdx.x * blockDim.y + threadIdx.y; }
 
 // Copies: T stands for so many bytes.
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(256) rows_to_kernel(const RowsParams p) {
+    using C = Columns<T, V, false>;
     grid_dependency_release();
     grid_dependency_wait();
-    const Place at = row_place<1>();
-    if (at.t >= p.T || at.c >= p.H) return;
-    const T v = load_ordered((const T *)p.x + at.t * p.x_row + at.c);
-    const int32_t *slots = p.slots + (long long)at.t * p.k;
+    const int t = row_token(), c = blockIdx.y * blockDim.x * V + threadIdx.x;
+    if (t >= p.T || c >= p.H) return;
+    const typename C::Pack v = C::load((const T *)p.x + t * p.x_row, c, blockDim.x, p.H);
+    const int32_t *slots = p.slots + (long long)t * p.k;
 #pragma unroll 4
     for (int j = 0; j < p.k; ++j) {
         const int s = load_ordered(slots + j);
-        if (s >= 0 && s < p.R) ((T *)p.out)[s * p.out_row + at.c] = v;
+        if (s >= 0 && s < p.R) C::store((T *)p.out + s * p.out_row, c, blockDim.x, p.H, v);
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool WIDE>
 __global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
+    using C = Columns<T, V, WIDE>;
     constexpr int BATCH = 4;
     grid_dependency_release();
     grid_dependency_wait();
-    const Place at = row_place<V>();
-    if (at.t >= p.T || at.c >= p.H) return;
-    const int32_t *slots = p.slots + (long long)at.t * p.k;
-    const float *weights = p.weights ? p.weights + (long long)at.t * p.k : nullptr;
+    const int t = row_token(), apart = blockDim.x, c = blockIdx.y * blockDim.x * V + C::first(threadIdx.x);
+    if (t >= p.T || c >= p.H) return;
+    const int32_t *slots = p.slots + (long long)t * p.k;
+    const float *weights = p.weights ? p.weights + (long long)t * p.k : nullptr;
     float sum[V] = {};
     if (p.residual) {
-        const Pack<T, V> r = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.residual + at.t * p.res_row + at.c));
+        const typename C::Pack r = C::load((const T *)p.residual + t * p.res_row, c, apart, p.H);
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] = rows_float(r.v[i]);
     }
     for (int j0 = 0; j0 < p.k; j0 += BATCH) {
         int s[BATCH];
         float w[BATCH];
-        Pack<T, V> y[BATCH];
+        typename C::Pack y[BATCH];
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             s[b] = j0 + b < p.k ? load_ordered(slots + j0 + b) : -1;
@@ -250,7 +283,7 @@ __global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
         }
 #pragma unroll
         for (int b = 0; b < BATCH; ++b)
-            if (s[b] >= 0) y[b] = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.y + s[b] * p.y_row + at.c));
+            if (s[b] >= 0) y[b] = C::load((const T *)p.y + s[b] * p.y_row, c, apart, p.H);
 #pragma unroll
         for (int b = 0; b < BATCH; ++b)
             if (s[b] >= 0) {
@@ -258,20 +291,22 @@ __global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
                 for (int i = 0; i < V; ++i) sum[i] = fmaf(w[b], rows_float(y[b].v[i]), sum[i]);
             }
     }
-    Pack<T, V> o;
+    typename C::Pack o;
 #pragma unroll
     for (int i = 0; i < V; ++i) o.v[i] = rows_round<T>(sum[i]);
-    *reinterpret_cast<Pack<T, V> *>((T *)p.out + at.t * p.out_row + at.c) = o;
+    C::store((T *)p.out + t * p.out_row, c, apart, p.H, o);
 }
 
-// The gradient: a token by blockDim.x threads, which walk along its row; dot products of a batch of choices in registers.
-constexpr int kGradBatch = 8;
-template <typename T, int V>
-__global__ void __launch_bounds__(256) rows_from_grad_kernel(const RowsParams p) {
+// The gradient: a token by blockDim.x threads, which walk along its row; dot products of eight choices in registers, the rows of four of them on their
+// way at a time, so that three CTAs fit an SM (two where values are loaded one by one).
+constexpr int kGradBatch = 8, kGradLoads = 4;
+template <typename T, int V, bool WIDE>
+__global__ void __launch_bounds__(256, WIDE ? 3 : 2) rows_from_grad_kernel(const RowsParams p) {
+    using C = Columns<T, V, WIDE>;
     __shared__ float part[8][kGradBatch];
     grid_dependency_release();
     grid_dependency_wait();
-    const int t = blockIdx.x * blockDim.y + threadIdx.y;
+    const int t = row_token(), apart = blockDim.x;
     const bool inside = t < p.T;
     const int lane = threadIdx.x & 31, warp = threadIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5), warps = blockDim.x / 32;
     const T *g = (const T *)p.x + (inside ? t : 0) * p.x_row;
@@ -283,29 +318,34 @@ __global__ void __launch_bounds__(256) rows_from_grad_kernel(const RowsParams p)
 #pragma unroll
         for (int j = 0; j < kGradBatch; ++j) {
             s[j] = inside && j < some ? load_ordered(p.slots + pair + j) : -1;
+            if (s[j] >= p.R) s[j] = -1;
             w[j] = s[j] < 0 ? 0.f : p.weights ? load_ordered(p.weights + pair + j) : 1.f;
             dot[j] = 0.f;
         }
-        for (int c = threadIdx.x * V; c < p.H && inside; c += blockDim.x * V) {
-            const Pack<T, V> gv = load_ordered(reinterpret_cast<const Pack<T, V> *>(g + c));
-            Pack<T, V> y[kGradBatch];
-            if (p.weights) {
+        for (int c = C::first(threadIdx.x); c < p.H && inside; c += apart * V) {
+            const typename C::Pack gv = C::load(g, c, apart, p.H);
 #pragma unroll
-                for (int j = 0; j < kGradBatch; ++j)
-                    if (s[j] >= 0 && s[j] < p.R) y[j] = load_ordered(reinterpret_cast<const Pack<T, V> *>((const T *)p.y + s[j] * p.y_row + c));
-            }
+            for (int j1 = 0; j1 < kGradBatch; j1 += kGradLoads) {
+                if (j1 >= some) break;
+                typename C::Pack y[kGradLoads];
+                if (p.weights) {
 #pragma unroll
-            for (int j = 0; j < kGradBatch; ++j) {
-                const int row = s[j] >= 0 ? s[j] : -2 - s[j];          // -1: nowhere
-                if (row < 0 || row >= p.R) continue;
-                Pack<T, V> o;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float v = rows_float(gv.v[i]);
-                    o.v[i] = rows_round<T>(s[j] >= 0 ? w[j] * v : 0.f);
-                    if (p.weights && s[j] >= 0) dot[j] = fmaf(v, rows_float(y[j].v[i]), dot[j]);
+                    for (int j = 0; j < kGradLoads; ++j)
+                        if (s[j1 + j] >= 0) y[j] = C::load((const T *)p.y + s[j1 + j] * p.y_row, c, apart, p.H);
                 }
-                *reinterpret_cast<Pack<T, V> *>((T *)p.out_y + row * p.out_y_row + c) = o;
+#pragma unroll
+                for (int j = 0; j < kGradLoads; ++j) {
+                    const int at = s[j1 + j], row = at >= 0 ? at : -2 - at;         // -1: nowhere
+                    if (row < 0 || row >= p.R) continue;
+                    typename C::Pack o;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float v = rows_float(gv.v[i]);
+                        o.v[i] = rows_round<T>(at >= 0 ? w[j1 + j] * v : 0.f);
+                        if (p.weights && at >= 0) dot[j1 + j] = fmaf(v, rows_float(y[j].v[i]), dot[j1 + j]);
+                    }
+                    C::store((T *)p.out_y + row * p.out_y_row, c, apart, p.H, o);
+                }
             }
         }
         if (!p.weights) continue;
@@ -325,7 +365,7 @@ __global__ void __launch_bounds__(256) rows_from_grad_kernel(const RowsParams p)
     }
 }
 
-// Threads along a row and tokens per block, of 256 in all; at least `least` along the row.
+// Threads along a row (a power of two from `least` to 256) and tokens per block, of 256 threads in all; `columns`: threads that a row takes.
 static dim3 row_block(long long columns, int least) {
     int x = least;
     while (x < 256 && x < columns) x *= 2;
@@ -357,28 +397,29 @@ static bool meets(const Region &a, std::initializer_list<Region> others) {
 // Strides up to what keeps byte offsets in 64 bits.
 static bool row_ok(long long row, long long H) { return row >= H && row <= (1ll << 40); }
 
-template <typename T>
-static int launch_rows_to(RowsParams p, cudaStream_t st) {
-    const dim3 block = row_block(p.H, 1);
-    return launch_dependent(rows_to_kernel<T>, row_grid(block, p.T, p.H), block, 0, st, p);
-}
 template <typename T, int V>
-static int launch_rows_from(const RowsParams &p, cudaStream_t st) {
-    const long long columns = p.H / V;
+static int launch_rows_to(const RowsParams &p, cudaStream_t st) {
+    const int columns = ceil_div(p.H, V);
     const dim3 block = row_block(columns, 1);
-    return launch_dependent(rows_from_kernel<T, V>, row_grid(block, p.T, columns), block, 0, st, p);
+    return launch_dependent(rows_to_kernel<T, V>, row_grid(block, p.T, columns), block, 0, st, p);
 }
-template <typename T, int V>
-static int launch_rows_from_grad(const RowsParams &p, cudaStream_t st) {
-    const dim3 block = row_block(p.H / V, 32);
-    return launch_dependent(rows_from_grad_kernel<T, V>, dim3((unsigned)((p.T - 1) / block.y + 1)), block, 0, st, p);
-}
-// Calls f with the type and whether packs of 16 bytes fit.
+// Calls f with the type's Columns.
 template <typename F>
-static int with_rows_type(int type, int bytes, F f) {
-    if (type == HIKONV_OUT_F32) return bytes == 16 ? f(Pack<float, 4>()) : f(Pack<float, 1>());
-    if (type == HIKONV_OUT_F16) return bytes == 16 ? f(Pack<__half, 8>()) : f(Pack<__half, 1>());
-    return bytes == 16 ? f(Pack<__nv_bfloat16, 8>()) : f(Pack<__nv_bfloat16, 1>());
+static int with_columns(int type, int bytes, F f) {
+    if (type == HIKONV_OUT_F32) return bytes == 16 ? f(float(), Columns<float, 4, true>()) : f(float(), Columns<float, 4, false>());
+    if (type == HIKONV_OUT_F16) return bytes == 16 ? f(__half(), Columns<__half, 8, true>()) : f(__half(), Columns<__half, 8, false>());
+    return bytes == 16 ? f(__nv_bfloat16(), Columns<__nv_bfloat16, 8, true>()) : f(__nv_bfloat16(), Columns<__nv_bfloat16, 8, false>());
+}
+template <typename T, int V, bool WIDE>
+static int launch_rows_from(T, Columns<T, V, WIDE>, const RowsParams &p, cudaStream_t st) {
+    const int columns = ceil_div(p.H, V);
+    const dim3 block = row_block(columns, 1);
+    return launch_dependent(rows_from_kernel<T, V, WIDE>, row_grid(block, p.T, columns), block, 0, st, p);
+}
+template <typename T, int V, bool WIDE>
+static int launch_rows_from_grad(T, Columns<T, V, WIDE>, const RowsParams &p, cudaStream_t st) {
+    const dim3 block = row_block(ceil_div(p.H, V), 32);
+    return launch_dependent(rows_from_grad_kernel<T, V, WIDE>, dim3((unsigned)((p.T - 1) / block.y + 1)), block, 0, st, p);
 }
 static bool is_float_type(int type) { return type == HIKONV_OUT_F32 || type == HIKONV_OUT_F16 || type == HIKONV_OUT_BF16; }
 static bool pairs_ok(int T, int k) { return T >= 0 && k >= 1 && (long long)T * k <= (1 << 30); }
@@ -418,7 +459,7 @@ extern "C" int hikonv_sort_by_expert(const void *d_experts, int index_bytes, lon
         const int rc = launch_dependent(sort_count_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), (size_t)(E + 1) * 4, st, p);
         if (rc != HIKONV_OK) return rc;
     }
-    const size_t smem = ((size_t)(kSortWarps + 2) * (E + 1) + kSortWarps) * 4;
+    const size_t smem = ((size_t)(kSortWarps + 3) * (E + 1) + kSortWarps) * 4;
     return with_dynamic_smem((const void *)sort_place_kernel, smem,
                              [&] { return launch_dependent(sort_place_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), smem, st, p); });
 }
@@ -444,11 +485,11 @@ extern "C" int hikonv_rows_to_experts(const void *d_x, int element_bytes, long l
     p.T = T; p.k = k; p.H = H / per; p.R = R;
     cudaStream_t st = (cudaStream_t)stream;
     switch (bytes) {
-        case 16: return launch_rows_to<uint4>(p, st);
-        case 8: return launch_rows_to<uint2>(p, st);
-        case 4: return launch_rows_to<uint32_t>(p, st);
-        case 2: return launch_rows_to<uint16_t>(p, st);
-        default: return launch_rows_to<uint8_t>(p, st);
+        case 16: return launch_rows_to<uint4, 1>(p, st);
+        case 8: return launch_rows_to<uint2, 2>(p, st);
+        case 4: return launch_rows_to<uint32_t, 4>(p, st);
+        case 2: return launch_rows_to<uint16_t, 8>(p, st);
+        default: return launch_rows_to<uint8_t, 8>(p, st);
     }
 }
 
@@ -475,9 +516,7 @@ extern "C" int hikonv_rows_from_experts(const void *d_y, int type, long long y_r
     p.T = T; p.k = k; p.H = H; p.R = R;
     const int bytes = common_bytes(size, {(long long)(uintptr_t)d_y, (long long)(uintptr_t)d_out, (long long)(uintptr_t)d_residual, y.row, residual.row, out.row, y.bytes});
     cudaStream_t st = (cudaStream_t)stream;
-    return with_rows_type(type, bytes, [&](auto pack) {
-        return launch_rows_from<std::remove_reference_t<decltype(pack.v[0])>, sizeof(pack) / sizeof(pack.v[0])>(p, st);
-    });
+    return with_columns(type, bytes, [&](auto t, auto columns) { return launch_rows_from(t, columns, p, st); });
 }
 
 extern "C" int hikonv_rows_from_experts_grad(const void *d_grad, int type, long long grad_row_stride, const void *d_y, long long y_row_stride, int R,
@@ -511,7 +550,5 @@ extern "C" int hikonv_rows_from_experts_grad(const void *d_grad, int type, long 
     const int bytes = common_bytes(size, {(long long)(uintptr_t)grad.at, (long long)(uintptr_t)y.at, (long long)(uintptr_t)grad_y.at, grad.row, y.row, grad_y.row,
                                           bytes_of_row});
     cudaStream_t st = (cudaStream_t)stream;
-    return with_rows_type(type, bytes, [&](auto pack) {
-        return launch_rows_from_grad<std::remove_reference_t<decltype(pack.v[0])>, sizeof(pack) / sizeof(pack.v[0])>(p, st);
-    });
+    return with_columns(type, bytes, [&](auto t, auto columns) { return launch_rows_from_grad(t, columns, p, st); });
 }

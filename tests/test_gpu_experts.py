@@ -47,7 +47,7 @@ def check_sort(experts, E, dtype=torch.int32, **kw):
 
 @pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
 @pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 64), (3, 2, 5), (31, 1, 4), (64, 8, 64), (100, 7, 33), (512, 8, 256), (4096, 1, 1024), (4097, 1, 16),
-                                   (513, 8, 1024), (1000, 6, 511), (2048, 8, 512), (20000, 8, 256), (70001, 8, 20)])
+                                   (513, 8, 1024), (1000, 6, 511), (1024, 8, 300), (1025, 8, 300), (8193, 1, 1024), (9000, 3, 1024), (2048, 8, 512), (20000, 8, 256), (70001, 8, 20)])
 def test_sort(T, k, E, dtype):
     check_sort(route(T, k, E, T + E), E, dtype)
 
@@ -82,7 +82,7 @@ def test_sort_of_columns_of_a_wider_matrix(T):
 
 
 def test_sort_of_many_blocks_per_cta():
-    T = 200000
+    T = 200000                                           # 196 blocks on 98 CTAs
     check_sort(route(T, 8, 77, 5), 77, torch.int32)
 
 
