@@ -550,7 +550,7 @@ int hikonv_linear_wait_check(long long cycles, void *stream);
  *   slots:   [T][k], the place of each pair.  Pairs whose expert is outside 0 .. E - 1 have none: their slots are -2 - place, with places
  *            behind offsets[E], so that every place below T k belongs to one pair.
  * T k <= 2^30, 1 <= E <= HIKONV_MAX_GROUPS; T == 0 makes all offsets 0.  The outputs must not overlap the input or each other.
- * d_workspace: hikonv_sort_by_expert_workspace_bytes of it (0 for up to 8192 pairs), 4-byte aligned, for one call at a time.
+ * d_workspace: hikonv_sort_by_expert_workspace_bytes of it (0 for up to 4096 pairs), 4-byte aligned, for one call at a time.
  */
 int hikonv_sort_by_expert(const void *d_experts, int index_bytes, long long experts_row_stride, int T, int k, int E, int32_t *d_offsets,
                           int32_t *d_slots, void *d_workspace, size_t workspace_bytes, void *stream);

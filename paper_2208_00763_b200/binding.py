@@ -735,7 +735,7 @@ def sort_by_expert(experts: torch.Tensor, n_experts: int, offsets: Optional[torc
 
 
 def sort_by_expert_workspace_bytes(tokens: int, choices: int, n_experts: int) -> int:
-    """Bytes that ``sort_by_expert`` needs between its launches: 0 for up to 8192 pairs."""
+    """Bytes that ``sort_by_expert`` needs between its launches: 0 for up to 4096 pairs."""
     return int(lib().hikonv_sort_by_expert_workspace_bytes(tokens, choices, n_experts))
 
 

@@ -17,6 +17,8 @@ namespace hikonv {
 
 // ---- sorting
 
+static_assert(HIKONV_MAX_GROUPS + 1 < 1 << 11, "bits of a key");
+
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortSteps = 8;
 constexpr int kSortBlock = kSortThreads * kSortSteps;       // pairs whose experts the registers of a CTA hold
 constexpr int kSortMostCtas = 128;
@@ -27,7 +29,7 @@ struct SortParams {
     long long row;                       // elements from token to token
     long long pairs;
     int k, E, ctas;
-    long long per_cta;                   // pairs; a multiple of kSortBlock where there are several CTAs
+    long long per_cta;                   // pairs
     int32_t *offsets, *slots;
     uint32_t *counts;                    // [ctas][E + 1], null for one CTA
 };
@@ -53,6 +55,19 @@ __device__ __forceinline__ void read_experts(const SortParams &p, long long from
     for (int s = 0; s < kSortSteps; ++s) key[s] = s >= steps || first + s * 32 >= end ? -1 : e[s] >= 0 && e[s] < p.E ? (int)e[s] : p.E;
 }
 
+// The lanes whose key is this lane's, bit by bit: the instruction that finds them at once (match.any) took a CTA of 32 warps 2000 cycles.
+__device__ __forceinline__ uint32_t lanes_with(int key, int bits) {
+    uint32_t same = 0xFFFFFFFFu;
+#pragma unroll
+    for (int b = 0; b < 11; ++b) {                      // keys are at most HIKONV_MAX_GROUPS + 1
+        if (b >= bits) break;
+        const bool set = key >> b & 1;
+        const uint32_t those = __ballot_sync(0xFFFFFFFFu, set);
+        same &= set ? those : ~those;
+    }
+    return same;
+}
+
 // How many pairs of each expert a CTA's stretch has.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortParams p) {
     extern __shared__ uint32_t hist[];
@@ -76,7 +91,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortPara
 // expert's next one, the pairs of warps before, of this warp so far, and of lanes before.
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortParams p) {
     extern __shared__ uint32_t shared[];
-    const int E1 = p.E + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int E1 = p.E + 1, bits = 32 - __clz(E1), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // [warp][E1] pairs of each expert in each warp, then in the warps before; its next place; all its pairs; of this block; sums of warps
     uint32_t *hist = shared, *next = hist + kSortWarps * E1, *total = next + E1, *block = total + E1, *sums = block + E1;
     grid_dependency_release();
@@ -93,7 +108,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
 #pragma unroll
         for (int s = 0; s < kSortSteps; ++s) {
             if (s >= steps) break;
-            same[s] = __match_any_sync(0xFFFFFFFFu, key[s]);
+            same[s] = lanes_with(key[s] < 0 ? E1 : key[s], bits);
             if (key[s] >= 0 && lane == __ffs(same[s]) - 1) hist[warp * E1 + key[s]] += __popc(same[s]);
             __syncwarp();
         }
@@ -113,16 +128,18 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     };
     if (p.counts) {
         // columns of the counts, by several threads each: what lies in front of this CTA, and all
-        const int parts = (p.ctas + 7) / 8;
+        constexpr int ROWS = 16;
+        const int parts = (p.ctas + ROWS - 1) / ROWS;
         for (int i = tid; i < parts * E1; i += kSortThreads) {
             const int part = i / E1, e = i - part * E1;
-            uint32_t v[8], before = 0, all = 0;
+            const uint32_t *at = p.counts + (part * ROWS * E1 + e);
+            uint32_t v[ROWS], before = 0, all = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = part * 8 + j < p.ctas ? load_ordered(p.counts + (long long)(part * 8 + j) * E1 + e) : 0;
+            for (int j = 0; j < ROWS; ++j) v[j] = part * ROWS + j < p.ctas ? load_ordered(at + j * E1) : 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < ROWS; ++j) {
                 all += v[j];
-                if (part * 8 + j < (int)blockIdx.x) before += v[j];
+                if (part * ROWS + j < (int)blockIdx.x) before += v[j];
             }
             if (before) atomicAdd(next + e, before);
             if (all) atomicAdd(total + e, all);
@@ -178,10 +195,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     }
 }
 
+// CTAs for so many pairs, and the pairs of each.  One up to four steps (the launch that counts costs 2 us); then two steps each, since a CTA's matches
+// take longer than its reading of the others' counts, until there are 128.
 static int sort_ctas(long long pairs, long long *per_cta) {
-    const long long blocks = (pairs + kSortBlock - 1) / kSortBlock, per = (blocks + kSortMostCtas - 1) / kSortMostCtas;
-    *per_cta = (per > 0 ? per : 1) * kSortBlock;
-    return blocks > 0 ? (int)((blocks + per - 1) / per) : 1;
+    constexpr long long step = kSortThreads;
+    const long long steps = (pairs + step - 1) / step, per = (steps + kSortMostCtas - 1) / kSortMostCtas;
+    *per_cta = (steps <= 4 ? 4 : per > 2 ? per : 2) * step;
+    return pairs > 0 ? (int)((pairs + *per_cta - 1) / *per_cta) : 1;
 }
 
 // ---- rows
@@ -297,71 +317,81 @@ __global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
     C::store((T *)p.out + t * p.out_row, c, apart, p.H, o);
 }
 
-// The gradient: a token by blockDim.x threads, which walk along its row; dot products of eight choices in registers, the rows of four of them on their
-// way at a time, so that three CTAs fit an SM (two where values are loaded one by one).
-constexpr int kGradBatch = 8, kGradLoads = 4;
+// The gradient: a token by blockDim.x threads, which walk along its row; dot products of eight choices in registers, the rows of LOADS of them on their
+// way at a time.  Bound by the loads of all threads of an SM together: places and weights lie in shared memory, so that four CTAs fit one.  4096 tokens,
+// eight rows of 4096 bf16 values each: 103 us (5.5 TB/s); with four rows on their way, 136 registers and one CTA 201, 80 and three 111.
+constexpr int kGradBatch = 8;
 template <typename T, int V, bool WIDE>
-__global__ void __launch_bounds__(256, WIDE ? 3 : 2) rows_from_grad_kernel(const RowsParams p) {
+__global__ void __launch_bounds__(256, 4) rows_from_grad_kernel(const RowsParams p) {
     using C = Columns<T, V, WIDE>;
+    constexpr int LOADS = WIDE ? 2 : 4;
     __shared__ float part[8][kGradBatch];
+    __shared__ int slot[8][kGradBatch];
+    __shared__ float weight[8][kGradBatch];
     grid_dependency_release();
     grid_dependency_wait();
-    const int t = row_token(), apart = blockDim.x;
+    const int t = row_token(), apart = blockDim.x, y = threadIdx.y;
     const bool inside = t < p.T;
-    const int lane = threadIdx.x & 31, warp = threadIdx.y * (blockDim.x / 32) + (threadIdx.x >> 5), warps = blockDim.x / 32;
+    const int lane = threadIdx.x & 31, warp = y * (blockDim.x / 32) + (threadIdx.x >> 5), warps = blockDim.x / 32;
     const T *g = (const T *)p.x + (inside ? t : 0) * p.x_row;
     for (int j0 = 0; j0 < p.k; j0 += kGradBatch) {
         const int some = min(kGradBatch, p.k - j0);
-        const long long pair = (long long)(inside ? t : 0) * p.k + j0;
-        int s[kGradBatch];
-        float w[kGradBatch], dot[kGradBatch];
-#pragma unroll
-        for (int j = 0; j < kGradBatch; ++j) {
-            s[j] = inside && j < some ? load_ordered(p.slots + pair + j) : -1;
-            if (s[j] >= p.R) s[j] = -1;
-            w[j] = s[j] < 0 ? 0.f : p.weights ? load_ordered(p.weights + pair + j) : 1.f;
-            dot[j] = 0.f;
+        const long long pair = (long long)(inside ? t : 0) * p.k + j0 + threadIdx.x;
+        if (threadIdx.x < kGradBatch) {
+            int s = -1;
+            float w = 1.f;
+            if (inside && (int)threadIdx.x < some) {
+                s = load_ordered(p.slots + pair);
+                if (p.weights) w = load_ordered(p.weights + pair);
+            }
+            slot[y][threadIdx.x] = s < p.R ? s : -1;
+            weight[y][threadIdx.x] = w;
         }
+        __syncthreads();
+        float dot[kGradBatch] = {};
         for (int c = C::first(threadIdx.x); c < p.H && inside; c += apart * V) {
             const typename C::Pack gv = C::load(g, c, apart, p.H);
 #pragma unroll
-            for (int j1 = 0; j1 < kGradBatch; j1 += kGradLoads) {
+            for (int j1 = 0; j1 < kGradBatch; j1 += LOADS) {
                 if (j1 >= some) break;
-                typename C::Pack y[kGradLoads];
+                typename C::Pack rows[LOADS];
                 if (p.weights) {
 #pragma unroll
-                    for (int j = 0; j < kGradLoads; ++j)
-                        if (s[j1 + j] >= 0) y[j] = C::load((const T *)p.y + s[j1 + j] * p.y_row, c, apart, p.H);
+                    for (int j = 0; j < LOADS; ++j) {
+                        const int s = slot[y][j1 + j];
+                        if (s >= 0) rows[j] = C::load((const T *)p.y + s * p.y_row, c, apart, p.H);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < kGradLoads; ++j) {
-                    const int at = s[j1 + j], row = at >= 0 ? at : -2 - at;         // -1: nowhere
+                for (int j = 0; j < LOADS; ++j) {
+                    const int s = slot[y][j1 + j], row = s >= 0 ? s : -2 - s;       // -1: nowhere
                     if (row < 0 || row >= p.R) continue;
+                    const float w = weight[y][j1 + j];
                     typename C::Pack o;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float v = rows_float(gv.v[i]);
-                        o.v[i] = rows_round<T>(at >= 0 ? w[j1 + j] * v : 0.f);
-                        if (p.weights && at >= 0) dot[j1 + j] = fmaf(v, rows_float(y[j].v[i]), dot[j1 + j]);
+                        o.v[i] = rows_round<T>(s >= 0 ? w * v : 0.f);
+                        if (p.weights && s >= 0) dot[j1 + j] = fmaf(v, rows_float(rows[j].v[i]), dot[j1 + j]);
                     }
                     C::store((T *)p.out_y + row * p.out_y_row, c, apart, p.H, o);
                 }
             }
         }
-        if (!p.weights) continue;
+        if (p.weights) {
 #pragma unroll
-        for (int j = 0; j < kGradBatch; ++j) {
+            for (int j = 0; j < kGradBatch; ++j) {
 #pragma unroll
-            for (int d = 16; d; d /= 2) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], d);
-            if (lane == 0) part[warp][j] = dot[j];
+                for (int d = 16; d; d /= 2) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], d);
+                if (lane == 0) part[warp][j] = dot[j];
+            }
         }
         __syncthreads();
-        if ((int)threadIdx.x < some && inside) {
+        if (p.weights && (int)threadIdx.x < some && inside) {
             float sum = 0.f;
-            for (int i = 0; i < warps; ++i) sum += part[threadIdx.y * warps + i][threadIdx.x];
-            p.out_weights[pair + threadIdx.x] = sum;
+            for (int i = 0; i < warps; ++i) sum += part[y * warps + i][threadIdx.x];
+            p.out_weights[pair] = sum;
         }
-        __syncthreads();
     }
 }
 
@@ -407,8 +437,8 @@ static int launch_rows_to(const RowsParams &p, cudaStream_t st) {
 template <typename F>
 static int with_columns(int type, int bytes, F f) {
     if (type == HIKONV_OUT_F32) return bytes == 16 ? f(float(), Columns<float, 4, true>()) : f(float(), Columns<float, 4, false>());
-    if (type == HIKONV_OUT_F16) return bytes == 16 ? f(__half(), Columns<__half, 8, true>()) : f(__half(), Columns<__half, 8, false>());
-    return bytes == 16 ? f(__nv_bfloat16(), Columns<__nv_bfloat16, 8, true>()) : f(__nv_bfloat16(), Columns<__nv_bfloat16, 8, false>());
+    if (type == HIKONV_OUT_F16) return bytes == 16 ? f(__half(), Columns<__half, 8, true>()) : f(__half(), Columns<__half, 4, false>());
+    return bytes == 16 ? f(__nv_bfloat16(), Columns<__nv_bfloat16, 8, true>()) : f(__nv_bfloat16(), Columns<__nv_bfloat16, 4, false>());
 }
 template <typename T, int V, bool WIDE>
 static int launch_rows_from(T, Columns<T, V, WIDE>, const RowsParams &p, cudaStream_t st) {

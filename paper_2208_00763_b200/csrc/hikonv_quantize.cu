@@ -15,6 +15,7 @@
 
 #include "hikonv_cuda.cuh"
 #include "hikonv_linear.h"
+#include "hikonv_pairs.cuh"
 
 namespace hikonv {
 
@@ -44,31 +45,14 @@ __device__ __forceinline__ uint32_t quantize_exactly(float v, float scale, float
     const float q = __fdiv_rn(v, scale);
     return q != q ? 0u : (uint32_t)__float2int_rn(fminf(fmaxf(q, lo), hi)) & 255u;
 }
-// The same by the rounded reciprocal, two values at a time, for a finite row and a scale in the range that RowScale names.  Two steps
-// after Markstein (Computation of elementary functions on the IBM RISC System/6000 processor, 1990): q' = q + (v - q s) / s, with the
-// remainder by a fused multiply-add and 1 / s by its rounded value y.  The product v y is within 1.5 steps of v / s; after the first step
-// q is off by at most 1/2 + 2^-22 steps u, its remainder is exact, and the second rounds v / s + e with |e| <= (1/2 + 2^-22) u s |1/s - y|.
-// For s in [1, 2) that is below (1/2 + 2^-22) u s 2^-25, while v / s, a quotient of 24-bit numbers, lies at least u 2^-24 / s from any
-// point between two floats: the same rounding for s^2 (1/2 + 2^-22) < 2, that is for all but the last few mantissas.
+// The same by quotient_pair, two values at a time, for a finite row and a scale that divides_quickly.
 // Adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves the code in the low byte.  Bounds are needed below zero
 // for unsigned codes alone: the largest value's quotient rounds to hi or to a float next to it.
-__device__ __forceinline__ uint64_t pair(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
 template <bool SIGNED>
 __device__ __forceinline__ void quantize_two(float v0, float v1, uint64_t minus_scale, uint64_t inverse, uint32_t &o0, uint32_t &o1) {
     const uint64_t v = SIGNED ? pair(v0, v1) : pair(fmaxf(v0, 0.f), fmaxf(v1, 0.f));
-    uint64_t q, lifted;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(v), "l"(inverse));
-    q = fma_pair(fma_pair(q, minus_scale, v), inverse, q);
-    q = fma_pair(fma_pair(q, minus_scale, v), inverse, q);
+    const uint64_t q = quotient_pair(v, minus_scale, inverse);
+    uint64_t lifted;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(lifted) : "l"(q), "l"(pair(12582912.f, 12582912.f)));
     asm("mov.b64 {%0, %1}, %2;" : "=r"(o0), "=r"(o1) : "l"(lifted));
 }
@@ -82,8 +66,7 @@ struct RowScale {
         inverse = __frcp_rn(scale);
         lo = (float)p.lo;
         hi = (float)p.hi;
-        // remainders far from underflow, and a mantissa at least sixteen steps below 2
-        quick = scale >= 0x1p-64f && scale <= 0x1p64f && (__float_as_uint(scale) & 0x7FFFF0u) != 0x7FFFF0u;
+        quick = divides_quickly(scale);
     }
 };
 

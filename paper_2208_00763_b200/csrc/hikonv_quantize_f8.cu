@@ -11,6 +11,7 @@
 
 #include "hikonv_cuda.cuh"
 #include "hikonv_linear.h"
+#include "hikonv_pairs.cuh"
 
 namespace hikonv {
 
@@ -66,10 +67,22 @@ __device__ __forceinline__ void f8_read(const T *row, int k, int K, float (&v)[k
 template <bool E5M2>
 __device__ __forceinline__ uint4 f8_codes(const float (&v)[kF8PerLane], float scale) {
     uint32_t o[4];
+    if (divides_quickly(scale)) {
+        const float y = __frcp_rn(scale);
+        const uint64_t minus = pair(-scale, -scale), inverse = pair(y, y);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        o[i] = f8_pair<E5M2>(f8_quotient(v[4 * i], scale), f8_quotient(v[4 * i + 1], scale)) |
-               f8_pair<E5M2>(f8_quotient(v[4 * i + 2], scale), f8_quotient(v[4 * i + 3], scale)) << 16;
+        for (int i = 0; i < 4; ++i) {
+            float a, b, c, d;
+            unpair(quotient_pair(pair(v[4 * i], v[4 * i + 1]), minus, inverse), a, b);
+            unpair(quotient_pair(pair(v[4 * i + 2], v[4 * i + 3]), minus, inverse), c, d);
+            o[i] = f8_pair<E5M2>(a, b) | f8_pair<E5M2>(c, d) << 16;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = f8_pair<E5M2>(f8_quotient(v[4 * i], scale), f8_quotient(v[4 * i + 1], scale)) |
+                   f8_pair<E5M2>(f8_quotient(v[4 * i + 2], scale), f8_quotient(v[4 * i + 3], scale)) << 16;
+    }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 // Sixteen bytes of a row from k on (a multiple of 16), without those behind its end.

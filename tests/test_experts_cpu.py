@@ -119,9 +119,10 @@ def test_columns_of_one_buffer_are_taken(which, change):
 
 
 def test_workspace_of_the_sort():
-    assert hk.sort_by_expert_workspace_bytes(1024, 8, 64) == 0
-    assert hk.sort_by_expert_workspace_bytes(1025, 8, 64) == 2 * 65 * 4
+    assert hk.sort_by_expert_workspace_bytes(512, 8, 64) == 0
+    assert hk.sort_by_expert_workspace_bytes(513, 8, 64) == 3 * 65 * 4
     assert hk.sort_by_expert_workspace_bytes(1 << 27, 8, 1024) == 128 * 1025 * 4
+    assert hk.sort_by_expert_workspace_bytes(32768, 8, 256) == 128 * 257 * 4
     assert hk.sort_by_expert_workspace_bytes(0, 8, 64) == 0
 
 

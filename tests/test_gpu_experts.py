@@ -82,7 +82,7 @@ def test_sort_of_columns_of_a_wider_matrix(T):
 
 
 def test_sort_of_many_blocks_per_cta():
-    T = 200000                                           # 196 blocks on 98 CTAs
+    T = 200000                                           # two blocks a CTA
     check_sort(route(T, 8, 77, 5), 77, torch.int32)
 
 
