@@ -12,6 +12,7 @@
 #include <cstddef>
 #include <cstring>
 
+#include "hikonv_linear_f8.h"
 #include "hikonv_linear_tiles.cuh"
 
 namespace hikonv {
@@ -912,7 +913,8 @@ static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
     double least = 1e300;
     auto consider = [&](bool tokens, int nt, int width, int splits, double setup, double step, double end) {
         const double tiles = (p.offsets ? (double)p.M / nt + 0.5 * filled : (double)ceil_div(p.M, nt)) * ceil_div(p.N, width);
-        if (splits > 1 && (tiles * splits > sms - 20 || splits > chunks)) return;
+        // clusters of four and more do not fill every SM: their CTAs share one part of the GPU (16 clusters of eight took two turns)
+        if (splits > 1 && (tiles * splits > (splits == 8 ? 96 : sms - 20) || splits > chunks)) return;
         const int units = nt == kPairRows ? sms / 2 : sms;
         const double turns = splits > 1 ? 1.0 : p.offsets ? (tiles > units ? tiles / units + 0.3 : 1.0) : (double)((long long)(tiles + units - 1) / units);
         const double time = setup + turns * (ceil_div(chunks, splits) * step + end) + (splits == 1 ? 0.0 : splits == 2 ? 2.3 : splits == 4 ? 2.6 : 2.9);
@@ -1098,6 +1100,7 @@ static int linear_f8_run(const void *d_x, int x_f8, long long x_row, const void 
     k.out = d_out; k.residual = ep->d_residual; k.bias = ep->d_bias;
     k.x_scale = d_x_scale; k.w_scale = d_w_scale;
     k.out_row = out_row; k.res_row = res_row;
+    if (linear_f8_rows_takes(k)) return launch_linear_f8_rows(k, x_f8, w_f8, xs_row, (cudaStream_t)stream);
     return launch_linear_f8(k, x_f8, w_f8, xs_row, (cudaStream_t)stream);
 }
 

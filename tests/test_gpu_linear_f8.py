@@ -67,7 +67,8 @@ def operands(M, N, K, seed, xt=E4M3, wt=E4M3, E=0):
 
 
 SIZES = [(1, 1, 1), (1, 128, 128), (3, 5, 7), (16, 64, 128), (17, 130, 200), (2, 4096, 4096), (31, 257, 1000), (33, 96, 2048), (64, 128, 8192), (65, 1001, 300),
-         (128, 128, 128), (129, 255, 129), (200, 512, 384), (257, 384, 640), (500, 1501, 1001), (1024, 1024, 512), (3000, 520, 260), (1, 20000, 512), (130, 33, 6000)]
+         (128, 128, 128), (129, 255, 129), (200, 512, 384), (257, 384, 640), (500, 1501, 1001), (1024, 1024, 512), (3000, 520, 260), (1, 20000, 512), (130, 33, 6000), (8, 4096, 4096), (9, 300, 700), (3, 5000, 6000), (8, 17, 20000),
+         (300, 256, 128), (700, 2304, 1920)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -127,7 +128,8 @@ def groups(counts, first=0, tail=0):
 
 @pytest.mark.parametrize("N,K", [(128, 128), (200, 300), (1024, 512), (257, 129)])
 @pytest.mark.parametrize("counts,first,tail", [([3], 0, 0), ([0, 5, 0, 1], 2, 3), ([0, 0, 0], 0, 4), ([200, 0, 17, 128, 1], 0, 5), ([1] * 40, 0, 0),
-                                               ([700, 300, 650], 1, 2), ([2, 0, 1000] + [0] * 61, 0, 0)])
+                                               ([700, 300, 650], 1, 2), ([2, 0, 1000] + [0] * 61, 0, 0),
+                                               ([0] * 30 + [50] + [1] * 9, 0, 3), ([0, 300, 0, 0, 257, 0, 0, 130], 5, 5)])
 def test_groups(counts, first, tail, N, K):
     off, offsets, M = groups(counts, first, tail)
     x, w, xs, ws, g = operands(M, N, K, sum(counts), E=len(counts))
