@@ -628,7 +628,7 @@ int hikonv_quantize_tiles(const void *d_w, int w_type, long long w_row_stride, i
  *
  * hikonv_grouped_linear_f8 - with a matrix per group of rows: w: [E][N][K] (rows equally far apart throughout), w_scale: [E][..][..],
  *   d_bias: [E][N]; rows offsets[e] .. offsets[e + 1] - 1 belong to matrix e.  Offsets as for hikonv_grouped_linear; rows of no group are
- *   left as they were.  M, N <= 2^30, E N < 2^31.
+ *   left as they were.  M, N, K <= 2^30, E <= HIKONV_MAX_GROUPS, E N <= 2^31 - 256.
  */
 int hikonv_linear_f8(const void *d_x, int x_f8, long long x_row_stride, const void *d_w, int w_f8, long long w_row_stride, int M, int N, int K,
                      const float *d_x_scale, long long x_scale_row_stride, const float *d_w_scale, void *d_out, long long out_row_stride,

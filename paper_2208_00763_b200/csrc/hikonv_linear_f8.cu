@@ -934,7 +934,16 @@ static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
     return best;
 }
 
+// Whether the kernel was given the registers that its warps ask for: one that waits for registers which are not there waits for good.
+static bool pair_has_registers() {
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, linear_f8_pair_kernel) != cudaSuccess) return false;
+    return (a.numRegs + 7) / 8 * 8 * kPairThreads >= kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32;
+}
+
 static int launch_pair(F8Params q, int x_f8, int w_f8, cudaStream_t st) {
+    static const bool enough = pair_has_registers();
+    if (!enough) return HIKONV_ERR_CUDA;
     const LinearParams &p = q.p;
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
     const int feeds = kPairAdders * kPairAhead * 32 * 4, turns = kPairAdders * 32 * 17 * 4;
@@ -1015,7 +1024,10 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     // sums in 32 bits (1), the operands' types, 128 rows; the columns follow per tile
     const int a_type = shape.tokens ? x_f8 : w_f8, b_type = shape.tokens ? w_f8 : x_f8;
     q.idesc = (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(kF8Rows >> 4) << 24);
-    const size_t smem = (size_t)q.held + 2048 + tables;
+    // CTAs of a cluster wait for one another, and for tensor memory.  With two such kernels at once (two streams), each could hold the memory that the
+    // other's CTA waits for; with this much shared memory none shares its SM with another CTA that takes tensor memory.
+    size_t smem = (size_t)q.held + 2048 + tables;
+    if (q.splits > 1 && smem < 184 * 1024) smem = 184 * 1024;
 
     CUtensorMap map_x, map_w;
     if (!encode_map(&map_x, p.x, (uint64_t)p.K, (uint64_t)p.M, (uint64_t)p.x_row, kF8Depth, (uint32_t)q.nt) ||
@@ -1063,7 +1075,7 @@ static int linear_f8_run(const void *d_x, int x_f8, long long x_row, const void 
     if (type != HIKONV_OUT_F32 && type != HIKONV_OUT_F16 && type != HIKONV_OUT_BF16) return HIKONV_ERR_INVALID_ARG;
     if (ep->activation < HIKONV_ACT_NONE || ep->activation > HIKONV_ACT_GELU) return HIKONV_ERR_INVALID_ARG;
     if (ep->d_x_scale || ep->d_w_scale || ep->shift || ep->lo || ep->hi) return HIKONV_ERR_INVALID_ARG;
-    if (E > HIKONV_MAX_GROUPS || M > (1 << 30) || N > (1 << 30) || (long long)E * N > 0x7FFFFFFFll || K > (1 << 30)) return HIKONV_ERR_UNSUPPORTED;
+    if (E > HIKONV_MAX_GROUPS || M > (1 << 30) || N > (1 << 30) || (long long)E * N > 0x7FFFFF00ll || K > (1 << 30)) return HIKONV_ERR_UNSUPPORTED;
     // few enough tiles for 32-bit counts
     if (((long long)M / 16 + (E < M ? E : M) + 1) * ceil_div(N, kF8Rows) >= 0x3FFFFFFFll) return HIKONV_ERR_UNSUPPORTED;
     if (M == 0) return HIKONV_OK;

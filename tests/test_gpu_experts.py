@@ -323,3 +323,45 @@ def test_shapes_that_do_not_fit_are_refused():
         hk.quantize_blocks(x[:, :20], values=torch.zeros(4, 20, dtype=torch.float8_e4m3fn, device="cuda"))
     with pytest.raises(hk.HikonvError):
         hk.rows_to_experts(x, slots, out=x)
+
+
+def test_in_a_graph_replayed_with_other_choices():
+    T, k, E, H = 900, 8, 16, 72                            # two launches of the sort
+    experts = torch.randint(-1, E, (T, k), device="cuda")
+    x, grad = torch.randn(T, H, device="cuda"), torch.randn(T, H, device="cuda")
+    w = torch.rand(T, k, device="cuda")
+
+    def step():
+        offsets, slots = hk.sort_by_expert(experts, E)
+        y = hk.rows_to_experts(x, slots, out=torch.zeros(T * k, H, device="cuda"))
+        return (offsets, slots, y, hk.rows_from_experts(y, slots, w), *hk.rows_from_experts_grad(grad, y, slots, w), *hk.quantize_blocks(x))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in (1, 2):
+        torch.manual_seed(seed)
+        experts.copy_(torch.randint(-1, E, (T, k), device="cuda")), x.normal_(), w.uniform_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, step()):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) if a.element_size() == 1 else torch.equal(a, b)
+
+
+def test_a_sort_on_several_streams():
+    cases = [torch.randint(-1, 64, (T, 8), device="cuda") for T in (40, 3000, 700)]
+    want = [hk.sort_by_expert(c, 64) for c in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cases], []
+    for _ in range(20):
+        for s, c in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(hk.sort_by_expert(c, 64))
+    torch.cuda.synchronize()
+    for i, (o, s) in enumerate(got):
+        assert torch.equal(o, want[i % 3][0]) and torch.equal(s, want[i % 3][1])

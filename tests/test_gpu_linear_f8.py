@@ -170,6 +170,33 @@ def test_infinities_and_nan_stay_in_their_rows_and_columns():
         assert torch.isnan(got[1]).all() and not torch.isfinite(got[2]).any() and torch.equal(got[keep], clean[keep])
 
 
+@pytest.mark.parametrize("act", [hk.ACT_RELU, hk.ACT_SILU, hk.ACT_GELU])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("M", [3, 40, 300])
+def test_activations_at_the_ends_of_their_range(M, dtype, act):
+    # sums of a power of two each: one value of x, one of w
+    N, K = 256, 128
+    x, w = torch.zeros(M, K, device="cuda").to(E4M3), torch.zeros(N, K, device="cuda").to(E4M3)
+    x[:, 0], w[:, 0] = 1.0, 1.0
+    scale = torch.linspace(-95, 95, M, device="cuda")
+    scale[0], scale[1] = float("nan"), 1e-30
+    bias = torch.zeros(N, device="cuda")
+    bias[1::2] = -1.0                                      # neighbours of other size
+    bias[7] = float("inf")
+    got = hk.linear_f8(x, w, scale[None], torch.ones(2, 1, device="cuda"), bias, act, out_dtype=dtype)
+    v = (scale[:, None] + bias).double()
+    want = act64(v, act)
+    assert torch.isnan(got[0]).all() and torch.isinf(got[1:, 7]).all()
+    rows = torch.ones(M, N, dtype=torch.bool, device="cuda")
+    rows[0], rows[:, 7] = False, False
+    # SiLU: every normal result to 2^-16 of itself, and the rounding; GELU is 2^-21 |v| off at most; both after an addition in 32 bits.
+    # For outputs in 32 bits SiLU multiplies v by exp(-|v|), which is a multiple of 2^-149 where it is subnormal: half of that off, |v| 2^-150 in the product.
+    eps, tiny = torch.finfo(dtype).eps, torch.finfo(dtype).smallest_normal
+    bound = want.abs() * (eps / 2 + (2.0 ** -16 if act == hk.ACT_SILU else 2.0 ** -24)) + tiny * eps + (2.0 ** -21 * v.abs() if act == hk.ACT_GELU else 0.0)
+    bound = bound + (v.abs() * 2.0 ** -150 if act == hk.ACT_SILU and dtype == torch.float32 else 0.0)
+    assert ((got.double() - want).abs() <= bound)[rows & (want.abs() < torch.finfo(dtype).max)].all()
+
+
 def test_zero_scales_and_rows_of_nothing():
     x, w, xs, ws, _ = operands(5, 130, 256, 4)
     assert not hk.linear_f8(x, w, torch.zeros_like(xs), ws).any()
@@ -306,3 +333,50 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for i, g in enumerate(got):
         assert torch.equal(g, want[i % 2])
+
+
+def test_training_step_of_experts():
+    """Forward and backward of experts on float32 rows, by these calls around plain products, against automatic differentiation in 64 bits."""
+    T, E, k, H = 60, 5, 2, 48
+    g = torch.Generator("cuda").manual_seed(0)
+    x, up = (torch.randn(T, H, generator=g, device="cuda") for _ in range(2))
+    w = torch.randn(E, H, H, generator=g, device="cuda") / H ** 0.5
+    top, experts = torch.topk(torch.randn(T, E, generator=g, device="cuda"), k, dim=1)
+    experts[3, 1] = experts[7, 0] = experts[7, 1] = -1
+    weights = torch.softmax(top, 1)
+    offsets, slots = hk.sort_by_expert(experts, E)
+    ends = offsets.tolist()
+    rows = hk.rows_to_experts(x, slots, out=torch.zeros(T * k, H, device="cuda"))
+    y = torch.zeros_like(rows)
+    for e in range(E):
+        y[ends[e]:ends[e + 1]] = rows[ends[e]:ends[e + 1]] @ w[e].T
+    out = hk.rows_from_experts(y, slots, weights, residual=x)
+    grad_y, grad_weights = hk.rows_from_experts_grad(up, y, slots, weights)
+    grad_rows, grad_w = torch.zeros_like(rows), torch.zeros_like(w)
+    for e in range(E):
+        at = slice(ends[e], ends[e + 1])
+        grad_rows[at], grad_w[e] = grad_y[at] @ w[e], grad_y[at].T @ rows[at]
+    grad_x = hk.rows_from_experts(grad_rows, slots, residual=up)
+    x64, w64, r64 = (t.double().requires_grad_() for t in (x, w, weights))
+    want = x64
+    for j in range(k):
+        there = (experts[:, j] >= 0)[:, None]
+        want = want + torch.where(there, torch.einsum("th,tnh->tn", x64, w64[experts[:, j].clamp(min=0)]) * r64[:, j:j + 1], 0.0)
+    (want * up.double()).sum().backward()
+    # sums of H = 48 products and of some dozens of rows in 32 bits, of values of order one: 2^-24 times a few hundred
+    for got, ref in ((out, want), (grad_x, x64.grad), (grad_w, w64.grad), (grad_weights, torch.where(experts >= 0, r64.grad, 0.0))):
+        assert (got.double() - ref).abs().max() < 400 * 2.0 ** -24 * max(1.0, ref.abs().max().item())
+
+
+def test_clusters_at_once_on_two_streams():
+    # layers whose depth is shared by clusters, many at once
+    cases = [operands(M, N, 4096, M) for M, N in ((9, 512), (100, 1024), (12, 2048), (60, 640))]
+    want = [hk.linear_f8(*c[:4]) for c in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(4)], []
+    for _ in range(50):
+        for s, c in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(hk.linear_f8(*c[:4]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 4]) for i, y in enumerate(got)) and hk.linear_wait_timeouts() == 0
