@@ -72,61 +72,60 @@ __global__ void __launch_bounds__(kF8RowsThreads, 3) linear_f8_rows_kernel(const
     grid_dependency_wait();
     const int2 range = group_rows(p, e);
     const float *ws = p.w_scale + ((long long)e * q.w_blocks + min(n0 / 128, q.w_blocks - 1)) * q.chunks;
-    for (int m0 = range.x; m0 < range.y; m0 += kF8RowsAtOnce) {
-        const int rows = min(kF8RowsAtOnce, range.y - m0);
-        const uint8_t *x = g < rows ? p.x + (m0 + g) * p.x_row : nullptr;
-        float sum[4] = {};
-        for (int b = b0; b < b1; ++b) {
-            const int k = b * 128 + t * 16;
-            uint4 wv[2][2], xv[2];
-            float s[2], c[4] = {};
+    const int m0 = range.x, rows = min(kF8RowsAtOnce, range.y - m0);
+    if (rows <= 0) return;
+    const uint8_t *x = g < rows ? p.x + (m0 + g) * p.x_row : nullptr;
+    float sum[4] = {};
+    for (int b = b0; b < b1; ++b) {
+        const int k = b * 128 + t * 16;
+        uint4 wv[2][2], xv[2];
+        float s[2], c[4] = {};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                wv[h][0] = f8_piece(w[0], k + 64 * h, p.K);
-                wv[h][1] = f8_piece(w[1], k + 64 * h, p.K);
-                xv[h] = f8_piece(x, k + 64 * h, p.K);
-            }
-            const float sw = load_ordered(ws + b);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s[i] = 2 * t + i < rows ? load_ordered(p.x_scale + b * q.xs_row + m0 + 2 * t + i) * sw : 0.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f8_mma_rows<X5, W5>(c, wv[h][0].x, wv[h][1].x, wv[h][0].y, wv[h][1].y, xv[h].x, xv[h].y);
-                f8_mma_rows<X5, W5>(c, wv[h][0].z, wv[h][1].z, wv[h][0].w, wv[h][1].w, xv[h].z, xv[h].w);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = fmaf(c[i], s[i & 1], sum[i]);
+        for (int h = 0; h < 2; ++h) {
+            wv[h][0] = f8_piece(w[0], k + 64 * h, p.K);
+            wv[h][1] = f8_piece(w[1], k + 64 * h, p.K);
+            xv[h] = f8_piece(x, k + 64 * h, p.K);
         }
-        if (m0 > range.x) __syncthreads();              // the parts of the rows before have been read
-        // rows g and g + 8 of the tile, rows 2 t and 2 t + 1 of x
+        const float sw = load_ordered(ws + b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[warp][(2 * t + (i & 1)) * 16 + g + (i >> 1) * 8] = sum[i];
-        __syncthreads();
-        const int threads = q.ksplit * 32, who = tid % threads, n = n0 + (who & 15);
-        for (int i = who; i < rows * 16 && n < p.N; i += threads) {
-            float v = 0.f;
-            for (int k = 0; k < q.ksplit; ++k) v += part[local * q.ksplit + k][i];
-            const long long m = m0 + (i >> 4);
-            if (p.bias) v += load_ordered((const float *)p.bias + (long long)e * p.N + n);
-            v = activate(v, p.act);
-            auto put = [&](auto zero) {
-                using T = decltype(zero);
-                if (p.residual) v += to_float(load_ordered((const T *)p.residual + m * p.res_row + n));
-                from_float(v, (T *)p.out + m * p.out_row + n);
-            };
-            if (p.out_type == HIKONV_OUT_F32) put(float());
-            else if (p.out_type == HIKONV_OUT_F16) put(__half());
-            else put(__nv_bfloat16());
+        for (int i = 0; i < 2; ++i) s[i] = 2 * t + i < rows ? load_ordered(p.x_scale + b * q.xs_row + m0 + 2 * t + i) * sw : 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f8_mma_rows<X5, W5>(c, wv[h][0].x, wv[h][1].x, wv[h][0].y, wv[h][1].y, xv[h].x, xv[h].y);
+            f8_mma_rows<X5, W5>(c, wv[h][0].z, wv[h][1].z, wv[h][0].w, wv[h][1].w, xv[h].z, xv[h].w);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(c[i], s[i & 1], sum[i]);
+    }
+    // rows g and g + 8 of the tile, rows 2 t and 2 t + 1 of x
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[warp][(2 * t + (i & 1)) * 16 + g + (i >> 1) * 8] = sum[i];
+    __syncthreads();
+    const int threads = q.ksplit * 32, who = tid % threads, n = n0 + (who & 15);
+    for (int i = who; i < rows * 16 && n < p.N; i += threads) {
+        float v = 0.f;
+        for (int k = 0; k < q.ksplit; ++k) v += part[local * q.ksplit + k][i];
+        const long long m = m0 + (i >> 4);
+        if (p.bias) v += load_ordered((const float *)p.bias + (long long)e * p.N + n);
+        v = activate(v, p.act);
+        auto put = [&](auto zero) {
+            using T = decltype(zero);
+            if (p.residual) v += to_float(load_ordered((const T *)p.residual + m * p.res_row + n));
+            from_float(v, (T *)p.out + m * p.out_row + n);
+        };
+        if (p.out_type == HIKONV_OUT_F32) put(float());
+        else if (p.out_type == HIKONV_OUT_F16) put(__half());
+        else put(__nv_bfloat16());
     }
 }
 
-// Where this kernel is the faster one, by what was measured on weights from memory, up to eight rows: 1024 x 1024 weights 2.2 us here, 4.7 by tiles;
-// 2048 x 2048 3.8 and 6; 4096 x 4096 6.8 and 8.0; eight groups of 2048 x 2048 12 and 10.6; 8192 x 8192 20 and 16.5, where the copies of the tiles keep
-// more bytes on their way than the registers here.
+// Where this kernel is the faster one, by what was measured on weights from memory.  Up to eight rows in all, so that a weight is read once however rows
+// fall to groups (512 rows of 64 groups took 8 us here spread evenly and 248 in one group, 64 times eight of them; tiles take 9 and 6).  Plain: 1024 x 1024
+// weights 2.2 us here, 4.7 by tiles; 2048 x 2048 3.8 and 6; 4096 x 4096 6.8 and 8.0; 4096 x 5632 9.2 and 9.7; 8192 x 8192 20 and 16.5, where the copies of
+// the tiles keep more bytes on their way than the registers here.  Groups, eight rows: four of 2048 x 2048 7.1 and 8.7, five 10.9 and 9.1; 64 of 512 x 512 4.9
+// and 5.4; 16 of 1024 x 1024 6.6 and 6.8, 32 9.4 and 6.8.
 bool linear_f8_rows_takes(const LinearParams &p) {
-    const int rows = p.offsets ? ceil_div(p.M, p.E) : p.M;          // of a group, on average
-    return rows <= kF8RowsAtOnce && (double)p.E * p.N * p.K <= 1.4 * (1 << 24);
+    return p.M <= kF8RowsAtOnce && (double)p.E * p.N * p.K <= (p.offsets ? 1.0 : 1.4) * (1 << 24);
 }
 
 int launch_linear_f8_rows(const LinearParams &p, int x_f8, int w_f8, long long xs_row, cudaStream_t st) {

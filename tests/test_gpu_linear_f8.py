@@ -146,6 +146,34 @@ def test_groups(counts, first, tail, N, K):
     assert hk.linear_wait_timeouts() == 0
 
 
+@pytest.mark.parametrize("xt,wt", [(E4M3, E4M3), (E5M2, E4M3)])
+@pytest.mark.parametrize("N,K", [(64, 128), (259, 300), (512, 513), (1024, 2048)])
+@pytest.mark.parametrize("counts,first,tail", [([1], 0, 0), ([0, 5, 0, 1], 1, 1), ([1] * 8, 0, 0), ([0] * 5 + [8], 0, 0), ([0] * 5 + [9], 0, 0), ([0, 0, 0], 0, 8),
+                                               ([3, 0, 0, 0, 0, 0, 4], 1, 0)])
+def test_few_rows_however_they_fall_to_groups(counts, first, tail, N, K, xt, wt):
+    off, offsets, M = groups(counts, first, tail)
+    x, w, xs, ws, g = operands(M, N, K, sum(counts) + N, xt, wt, E=len(counts))
+    bias = torch.randn(len(counts), N, generator=g, device="cuda")
+    out = torch.full((M, N), 3.0, dtype=torch.float32, device="cuda")
+    x.view(torch.uint8)[:first], x.view(torch.uint8)[off[-1]:] = 0x7F, 0x7F
+    hk.grouped_linear_f8(x, w, offsets, xs, ws, bias, out=out)
+    assert (out[:first] == 3).all() and (out[off[-1]:] == 3).all()
+    for e in range(len(counts)):
+        at = slice(off[e], off[e + 1])
+        if counts[e]:
+            near(out[at], *reference(x[at], w[e], xs[:, at], ws[e], bias[e], hk.ACT_NONE, None))
+
+
+def test_few_rows_with_offsets_that_are_not_in_order_stay_in_bounds():
+    M, N, K = 8, 130, 256
+    x, w, xs, ws, _ = operands(M, N, K, 3, E=3)
+    guard = torch.full((M + 20, N), 3.0, dtype=torch.bfloat16, device="cuda")
+    for off in ([-5, 1, 3, 2000], [6, 2, 4, 8], [8, 0, 8, 0]):
+        guard.fill_(3.0)
+        hk.grouped_linear_f8(x, w, torch.tensor(off, dtype=torch.int32, device="cuda"), xs, ws, out=guard[10:M + 10])
+        assert (guard[:10] == 3).all() and (guard[M + 10:] == 3).all()
+
+
 def test_offsets_that_are_not_in_order_stay_in_bounds():
     M, N, K = 64, 128, 128
     x, w, xs, ws, _ = operands(M, N, K, 3, E=3)
