@@ -365,3 +365,51 @@ def test_a_sort_on_several_streams():
     torch.cuda.synchronize()
     for i, (o, s) in enumerate(got):
         assert torch.equal(o, want[i % 3][0]) and torch.equal(s, want[i % 3][1])
+
+
+# ---- offsets beyond 32 bits
+
+def far(t, stride):
+    """The same rows, `stride` elements apart, behind one another in memory of their own."""
+    buf = torch.empty((t.shape[0] - 1) * stride + t.shape[1], dtype=t.dtype, device="cuda")
+    view = buf.as_strided(t.shape, (stride, 1))
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("H", [64, 37])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_far_apart(dtype, H):
+    T, k = 3, 2
+    _, slots, d_slots = places(T, k, 4, 5, 0.2)
+    g = torch.Generator("cuda").manual_seed(H)
+    x, r = (torch.randn(T, H, generator=g, device="cuda").to(dtype) for _ in range(2))
+    y = torch.randn(T * k, H, generator=g, device="cuda").to(dtype)
+    w = torch.rand(T, k, generator=g, device="cuda")
+    by_token, by_pair = (1 << 30) + 64, (1 << 29) - 64                 # the last rows lie 2^31 elements and more behind the first
+    zero = torch.zeros_like(y)
+    named = torch.tensor(slots[slots >= 0], device="cuda")
+    assert torch.equal(hk.rows_to_experts(far(x, by_token), d_slots, out=far(zero, by_pair))[named], hk.rows_to_experts(x, d_slots)[named])
+    want = hk.rows_from_experts(y, d_slots, w, r)
+    assert torch.equal(hk.rows_from_experts(far(y, by_pair), d_slots, w, far(r, by_token)), want)
+    assert torch.equal(hk.rows_from_experts(y, d_slots, w, r, out=far(torch.zeros_like(r), by_token)), want)
+    grad_y, grad_w = hk.rows_from_experts_grad(x, y, d_slots, w)
+    far_y, far_w = hk.rows_from_experts_grad(far(x, by_token), far(y, by_pair), d_slots, w, grad_y=far(zero, by_pair))
+    assert torch.equal(far_y, grad_y)
+    # products in another order where rows begin elsewhere
+    assert torch.allclose(far_w, grad_w, rtol=0, atol=H * 2.0 ** -24 * (x.float().abs() @ y.float().abs().T).max().item() * 2)
+
+
+def test_blocks_far_apart():
+    T, k, K = 3, 2, 300
+    _, slots, d_slots = places(T, k, 4, 5, 0.2)
+    x = hidden(T, K, torch.bfloat16, 0)
+    named = torch.tensor(slots[slots >= 0], device="cuda")
+    values, scale = hk.quantize_blocks(x, slots=d_slots)
+    row = 1 << 30
+    out = torch.empty(5 * row + K, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).as_strided((T * k, K), (row, 1))
+    out_scale = torch.empty(2 * row + T * k, device="cuda").as_strided((3, T * k), (row, 1))
+    hk.quantize_blocks(far(x, row + 64), slots=d_slots, values=out, scale=out_scale)
+    assert torch.equal(out.view(torch.uint8)[named], values.view(torch.uint8)[named]) and torch.equal(out_scale[:, named], scale[:, named])
+    w = hidden(131, K, torch.float32, 1)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(hk.quantize_tiles(far(w, 1 << 25)), hk.quantize_tiles(w)))

@@ -408,3 +408,42 @@ def test_clusters_at_once_on_two_streams():
                 got.append(hk.linear_f8(*c[:4]))
     torch.cuda.synchronize()
     assert all(torch.equal(y, want[i % 4]) for i, y in enumerate(got)) and hk.linear_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("M,N", [(3, 40), (40, 140), (300, 130), (300, 2048), (2048, 2048), (4096, 2048)])
+def test_operands_far_apart(M, N):
+    # rows of x, w, the scales and the output reach beyond 2^32 bytes
+    K = 384
+    x, w, xs, ws, g = operands(M, N, K, M)
+    residual = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    want = hk.linear_f8(x, w, xs, ws, residual=residual)
+
+    def far(t, span):
+        step = span // (t.shape[0] - 1) // 16 * 16 + 16
+        view = torch.empty((t.shape[0] - 1) * step + (t.shape[1] + 15) // 16 * 16, dtype=t.dtype, device="cuda").as_strided(t.shape, (step, 1))
+        view.copy_(t)
+        return view
+
+    out = far(torch.zeros_like(residual), 1 << 31)
+    hk.linear_f8(far(x, 1 << 32), far(w, 1 << 32), far(xs, 1 << 31), ws, residual=far(residual, 1 << 31), out=out)
+    assert torch.equal(out, want)
+
+
+def test_weights_of_many_bytes():
+    # the last matrices begin 2^32 bytes and more behind the first
+    E, N, K = 33, 8192, 16384
+    w = torch.zeros(E, N, K, dtype=torch.uint8, device="cuda").view(E4M3)
+    ws = torch.ones(E, N // 128, K // 128, device="cuda")
+    for counts in ([0] * 31 + [3, 4], [0] * 31 + [40, 300], [1] * 33):
+        off, offsets, M = groups(counts)
+        x, small, xs, small_ws, _ = operands(M, N, 128, len(counts) + M, E=2)
+        w[31:, :, -128:].view(torch.uint8).copy_(small.view(torch.uint8))
+        ws[31:, :, -1] = small_ws[..., 0]
+        wide_x, wide_xs = torch.zeros(M, K, dtype=torch.uint8, device="cuda").view(E4M3), torch.zeros(K // 128, M, device="cuda")
+        wide_x[:, -128:].view(torch.uint8).copy_(x.view(torch.uint8))
+        wide_xs[-1] = xs[0]
+        got = hk.grouped_linear_f8(wide_x, w, offsets, wide_xs, ws, out_dtype=torch.float32)
+        assert not got[:off[31]].any()
+        for i in range(2):
+            at = slice(off[31 + i], off[32 + i])
+            near(got[at], *reference(x[at], small[i], xs[:, at], small_ws[i], None, hk.ACT_NONE, None))
