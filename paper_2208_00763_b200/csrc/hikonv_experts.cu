@@ -6,8 +6,9 @@
 // give back to a token is summed in registers, in the order of its choices.
 //
 // 512 pairs over 64 experts are sorted in 4.3 us, 262144 over 256 in 12.8 (two launches; the second's CTAs each read the counts of all).  Rows are bound by
-// memory: 8192 tokens with eight rows of 4096 bf16 values each come back in 115 us (5.9 TB/s), and rows that start anywhere by the two or four
-// bytes of a load (5003 x 3 rows of 1333 fp16 values go out in 15 us, 3.3 TB/s; by one column a thread 32).
+// memory: 8192 tokens with eight rows of 4096 bf16 values each come back in 114 us (5.9 TB/s), and rows that start anywhere by the two or four
+// bytes of a load or store (5003 x 3 rows of 1333 fp16 values go out in 12.3 us, 4.0 TB/s, by words of four bytes; 15.2 by elements, four a thread; by one 32.
+// 8-bit ones 6.1 and 14).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -279,6 +280,56 @@ __global__ void __launch_bounds__(256) rows_to_kernel(const RowsParams p) {
     }
 }
 
+// Copies of rows that begin anywhere (p.x_row, p.out_row and p.H: bytes).  A thread's V words of four bytes of an output row come out of two neighbouring
+// words of x's row each, moved by a funnel shift: unit q has the words q - 1 and q of x's row (words count from the one that its first byte lies in)
+// and gives the output row's word q - 1, or q where the output row begins later in its first word than x's does.  The up to three bytes in front of
+// an output row's first whole word and behind its last are a thread's each.
+template <int V>
+__global__ void __launch_bounds__(256) rows_to_bytes_kernel(const RowsParams p) {
+    constexpr int BATCH = 4;
+    grid_dependency_release();
+    grid_dependency_wait();
+    const int t = row_token(), apart = blockDim.x, first = blockIdx.y * blockDim.x * V + threadIdx.x;
+    if (t >= p.T) return;
+    const uint8_t *x = (const uint8_t *)p.x + t * p.x_row;
+    const int32_t *slots = p.slots + (long long)t * p.k;
+    const int m = (int)((uintptr_t)x & 3), words = (m + p.H + 3) / 4;
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(x - m);
+    uint32_t low[V], high[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int q = first + i * apart;
+        low[i] = q >= 1 && q <= words ? load_ordered(from + q - 1) : 0;
+        high[i] = q < words ? load_ordered(from + q) : 0;
+    }
+    for (int j0 = 0; j0 < p.k; j0 += BATCH) {
+        int s[BATCH];
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) s[j] = j0 + j < p.k ? load_ordered(slots + j0 + j) : -1;
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+            if (s[j] < 0 || s[j] >= p.R) continue;
+            uint8_t *row = (uint8_t *)p.out + s[j] * p.out_row;
+            const int a = (int)((uintptr_t)row & 3), later = m < a, shift = 8 * (m - a + 4 * later);
+            const int b0 = (first - 1 + later) * 4 - a;                     // the row's byte that the first word begins with
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int b = b0 + i * apart * 4;
+                if (b >= 0 && b + 4 <= p.H) *reinterpret_cast<uint32_t *>(row + b) = __funnelshift_r(low[i], high[i], shift);
+            }
+        }
+    }
+    if (blockIdx.y > 0) return;
+    for (int i = threadIdx.x; i < 8 * p.k; i += apart) {
+        const int s = load_ordered(slots + i / 8), n = i & 3;
+        if (s < 0 || s >= p.R) continue;
+        uint8_t *row = (uint8_t *)p.out + s * p.out_row;
+        const int a = (int)((uintptr_t)row & 3), head = -a & 3, tail = ((a + p.H) & ~3) - a;
+        const int b = i & 4 ? (tail >= head ? tail + n : p.H) : (n < head ? n : p.H);
+        if (b < p.H) row[b] = load_ordered(x + b);
+    }
+}
+
 template <typename T, int V, bool WIDE>
 __global__ void __launch_bounds__(256) rows_from_kernel(const RowsParams p) {
     using C = Columns<T, V, WIDE>;
@@ -399,10 +450,15 @@ __global__ void __launch_bounds__(256, 4) rows_from_grad_kernel(const RowsParams
     }
 }
 
-// Threads along a row (a power of two from `least` to 256) and tokens per block, of 256 threads in all; `columns`: threads that a row takes.
+// Threads along a row and tokens per block, of 256 threads at most; `columns`: threads that a row takes.  Along a row a power of two from `least` on, or
+// whole warps, as many as share the row evenly between as few blocks as will do (168 columns: 192 threads, not 256 of which a third has nothing to do).
 static dim3 row_block(long long columns, int least) {
-    int x = least;
-    while (x < 256 && x < columns) x *= 2;
+    long long x = least;
+    while (x < 32 && x < columns) x *= 2;
+    if (columns > 32) {
+        const long long blocks = (columns + 255) / 256;
+        x = ((columns + blocks - 1) / blocks + 31) / 32 * 32;
+    }
     return dim3((unsigned)x, (unsigned)(256 / x));
 }
 static dim3 row_grid(const dim3 &block, int T, long long columns) {
@@ -522,9 +578,12 @@ extern "C" int hikonv_rows_to_experts(const void *d_x, int element_bytes, long l
         case 16: return launch_rows_to<uint4, 1>(p, st);
         case 8: return launch_rows_to<uint2, 2>(p, st);
         case 4: return launch_rows_to<uint32_t, 4>(p, st);
-        case 2: return launch_rows_to<uint16_t, 8>(p, st);
-        default: return launch_rows_to<uint8_t, 8>(p, st);
     }
+    p.x_row = x_row_stride * size; p.out_row = out_row_stride * size; p.H = (int)(H * size);
+    constexpr int V = 4;
+    const int columns = ceil_div((p.H + 6) / 4 + 1, V);
+    const dim3 block = row_block(columns, 1);
+    return launch_dependent(rows_to_bytes_kernel<V>, row_grid(block, T, columns), block, 0, st, p);
 }
 
 extern "C" int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, int R, const int32_t *d_slots, const float *d_weights, int T, int k,

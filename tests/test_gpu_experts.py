@@ -413,3 +413,35 @@ def test_blocks_far_apart():
     assert torch.equal(out.view(torch.uint8)[named], values.view(torch.uint8)[named]) and torch.equal(out_scale[:, named], scale[:, named])
     w = hidden(131, K, torch.float32, 1)
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(hk.quantize_tiles(far(w, 1 << 25)), hk.quantize_tiles(w)))
+
+
+# ---- rows at every address
+
+@pytest.mark.parametrize("dtype", [torch.int8, torch.float16])
+@pytest.mark.parametrize("H", [1, 2, 3, 4, 5, 6, 7, 8, 9, 31, 33, 127, 530, 1333])
+def test_rows_to_from_and_to_every_address(dtype, H):
+    T, k = 5, 3
+    _, slots, d_slots = places(T, k, 4, H, 0.2)
+    x = torch.randint(-100, 100, (T, H), device="cuda").to(dtype)
+    for shift in range(4):
+        for pitch in (H, H + 1, H + 2, H + 3):
+            source = torch.full((shift + T * pitch + 4,), 55, device="cuda").to(dtype)
+            rows = source[shift:shift + T * pitch].view(T, pitch)[:, :H]
+            rows.copy_(x)
+            for out_shift in range(4):
+                for out_pitch in (H, H + 1, H + 3):
+                    buf = torch.full((out_shift + T * k * out_pitch + 4,), 77, device="cuda").to(dtype)
+                    want = buf.clone()
+                    view = lambda b: b[out_shift:out_shift + T * k * out_pitch].view(T * k, out_pitch)[:, :H]
+                    named = d_slots >= 0
+                    view(want)[d_slots[named].long()] = x[:, None].expand(T, k, H)[named]
+                    hk.rows_to_experts(rows, d_slots, out=view(buf))
+                    assert torch.equal(buf, want), (shift, pitch, out_shift, out_pitch)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("T,k,H", [(9, 3, 1333), (6, 2, 264), (5, 2, 700), (11, 3, 2600), (3, 9, 4104)])
+def test_rows_of_widths_between_powers_of_two(T, k, H, dtype):
+    test_rows_to(T, k, H, torch.bfloat16 if dtype != torch.float32 else torch.float32)
+    test_rows_from(T, k, H, dtype)
+    test_rows_from_grad(T, k, H, dtype)
