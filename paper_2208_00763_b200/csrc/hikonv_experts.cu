@@ -118,16 +118,20 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
             __syncwarp();
         }
         __syncthreads();
-        for (int e = warp; e < E1; e += kSortWarps) {
-            const uint32_t mine = hist[lane * E1 + e];
-            uint32_t upto = mine;
+        for (int e = tid; e < E1; e += kSortThreads) {
+            uint32_t upto = 0;
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-                if (lane >= d) upto += v;
+            for (int w0 = 0; w0 < kSortWarps; w0 += 16) {
+                uint32_t of[16];
+#pragma unroll
+                for (int w = 0; w < 16; ++w) of[w] = hist[(w0 + w) * E1 + e];
+#pragma unroll
+                for (int w = 0; w < 16; ++w) {
+                    hist[(w0 + w) * E1 + e] = upto;
+                    upto += of[w];
+                }
             }
-            hist[lane * E1 + e] = upto - mine;
-            if (lane == 31) block[e] = upto;
+            block[e] = upto;
         }
         return steps;
     };
