@@ -5,7 +5,7 @@
 // in which warps run.  Rows are moved by token: a token's row is read once however many experts it goes to, and what an expert's rows
 // give back to a token is summed in registers, in the order of its choices.
 //
-// 512 pairs over 64 experts are sorted in 4.3 us, 262144 over 256 in 12.8 (two launches; the second's CTAs each read the counts of all).  Rows are bound by
+// 512 pairs over 64 experts are sorted in 2.5 us, 262144 over 256 in 11 (two launches; the second's CTAs each read the counts of all).  Rows are bound by
 // memory: 8192 tokens with eight rows of 4096 bf16 values each come back in 114 us (5.9 TB/s), and rows that start anywhere by the two or four
 // bytes of a load or store (5003 x 3 rows of 1333 fp16 values go out in 12.3 us, 4.0 TB/s, by words of four bytes; 15.2 by elements, four a thread; by one 32.
 // 8-bit ones 6.1 and 14).
@@ -24,8 +24,7 @@ namespace hikonv {
 
 static_assert(HIKONV_MAX_GROUPS + 1 < 1 << 11, "bits of a key");
 
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortSteps = 8;
-constexpr int kSortBlock = kSortThreads * kSortSteps;       // pairs whose experts the registers of a CTA hold
+constexpr int kSortSteps = 8;            // pairs of a thread whose experts its registers hold
 constexpr int kSortMostCtas = 128;
 
 struct SortParams {
@@ -74,14 +73,15 @@ __device__ __forceinline__ uint32_t lanes_with(int key, int bits) {
 }
 
 // How many pairs of each expert a CTA's stretch has.
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortParams p) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) sort_count_kernel(const SortParams p) {
     extern __shared__ uint32_t hist[];
     grid_dependency_release();
-    for (int e = threadIdx.x; e <= p.E; e += kSortThreads) hist[e] = 0;
+    for (int e = threadIdx.x; e <= p.E; e += THREADS) hist[e] = 0;
     grid_dependency_wait();
     __syncthreads();
     const long long begin = blockIdx.x * p.per_cta, end = min(begin + p.per_cta, p.pairs);
-    for (long long from = begin; from < end; from += kSortBlock) {
+    for (long long from = begin; from < end; from += THREADS * kSortSteps) {
         int key[kSortSteps];
         read_experts(p, from, end, kSortSteps, key);
 #pragma unroll
@@ -89,18 +89,20 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortPara
             if (key[s] >= 0) atomicAdd(hist + key[s], 1u);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e <= p.E; e += kSortThreads) p.counts[(long long)blockIdx.x * (p.E + 1) + e] = hist[e];
+    for (int e = threadIdx.x; e <= p.E; e += THREADS) p.counts[(long long)blockIdx.x * (p.E + 1) + e] = hist[e];
 }
 
 // Places of a CTA's stretch.  Every warp takes neighbouring pairs, 32 at a time: the lanes of one expert find each other, and a place is the
 // expert's next one, the pairs of warps before, of this warp so far, and of lanes before.
-__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortParams p) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) sort_place_kernel(const SortParams p) {
+    constexpr int WARPS = THREADS / 32, AT_ONCE = WARPS < 16 ? WARPS : 16;
     extern __shared__ uint32_t shared[];
     const int E1 = p.E + 1, bits = 32 - __clz(E1), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // [warp][E1] pairs of each expert in each warp, then in the warps before; its next place; all its pairs; of this block; sums of warps
-    uint32_t *hist = shared, *next = hist + kSortWarps * E1, *total = next + E1, *block = total + E1, *sums = block + E1;
+    uint32_t *hist = shared, *next = hist + WARPS * E1, *total = next + E1, *block = total + E1, *sums = block + E1;
     grid_dependency_release();
-    for (int i = tid; i < (kSortWarps + 2) * E1; i += kSortThreads) shared[i] = 0;
+    for (int i = tid; i < (WARPS + 2) * E1; i += THREADS) shared[i] = 0;
     grid_dependency_wait();
     __syncthreads();
     const long long begin = blockIdx.x * p.per_cta, end = min(begin + p.per_cta, p.pairs);
@@ -108,7 +110,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     uint32_t same[kSortSteps];
     // The block's experts, in how many lanes of each step, and how many each warp has; then how many the warps before have.
     auto read = [&](long long from) {
-        const int steps = (int)min((long long)kSortSteps, (end - from + kSortThreads - 1) / kSortThreads);
+        const int steps = (int)min((long long)kSortSteps, (end - from + THREADS - 1) / THREADS);
         read_experts(p, from, end, steps, key);
 #pragma unroll
         for (int s = 0; s < kSortSteps; ++s) {
@@ -118,15 +120,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
             __syncwarp();
         }
         __syncthreads();
-        for (int e = tid; e < E1; e += kSortThreads) {
+        for (int e = tid; e < E1; e += THREADS) {
             uint32_t upto = 0;
 #pragma unroll
-            for (int w0 = 0; w0 < kSortWarps; w0 += 16) {
-                uint32_t of[16];
+            for (int w0 = 0; w0 < WARPS; w0 += AT_ONCE) {
+                uint32_t of[AT_ONCE];
 #pragma unroll
-                for (int w = 0; w < 16; ++w) of[w] = hist[(w0 + w) * E1 + e];
+                for (int w = 0; w < AT_ONCE; ++w) of[w] = hist[(w0 + w) * E1 + e];
 #pragma unroll
-                for (int w = 0; w < 16; ++w) {
+                for (int w = 0; w < AT_ONCE; ++w) {
                     hist[(w0 + w) * E1 + e] = upto;
                     upto += of[w];
                 }
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
         // columns of the counts, by several threads each: what lies in front of this CTA, and all
         constexpr int ROWS = 16;
         const int parts = (p.ctas + ROWS - 1) / ROWS;
-        for (int i = tid; i < parts * E1; i += kSortThreads) {
+        for (int i = tid; i < parts * E1; i += THREADS) {
             const int part = i / E1, e = i - part * E1;
             const uint32_t *at = p.counts + (part * ROWS * E1 + e);
             uint32_t v[ROWS], before = 0, all = 0;
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
     __syncthreads();
     // where each expert begins
     const uint32_t *all = p.counts ? total : block;
-    const int items = (E1 + kSortThreads - 1) / kSortThreads;
+    const int items = (E1 + THREADS - 1) / THREADS;
     uint32_t mine = 0;
     for (int i = 0; i < items; ++i) mine += tid * items + i < E1 ? all[tid * items + i] : 0;
     uint32_t upto = mine;
@@ -193,11 +195,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
             if (key[s] >= 0 && lane == __ffs(same[s]) - 1) hist[warp * E1 + key[s]] += __popc(same[s]);
             __syncwarp();
         }
-        from += kSortBlock;
+        from += THREADS * kSortSteps;
         if (from >= end) break;
         __syncthreads();
-        for (int e = tid; e < E1; e += kSortThreads) next[e] += block[e];
-        for (int i = tid; i < kSortWarps * E1; i += kSortThreads) hist[i] = 0;
+        for (int e = tid; e < E1; e += THREADS) next[e] += block[e];
+        for (int i = tid; i < WARPS * E1; i += THREADS) hist[i] = 0;
         __syncthreads();
         steps = read(from);
         __syncthreads();
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortPara
 // CTAs for so many pairs, and the pairs of each.  One up to four steps (the launch that counts costs 2 us); then two steps each, since a CTA's matches
 // take longer than its reading of the others' counts, until there are 128.
 static int sort_ctas(long long pairs, long long *per_cta) {
-    constexpr long long step = kSortThreads;
+    constexpr long long step = 1024;
     const long long steps = (pairs + step - 1) / step, per = (steps + kSortMostCtas - 1) / kSortMostCtas;
     *per_cta = (steps <= 4 ? 4 : per > 2 ? per : 2) * step;
     return pairs > 0 ? (int)((pairs + *per_cta - 1) / *per_cta) : 1;
@@ -549,13 +551,22 @@ extern "C" int hikonv_sort_by_expert(const void *d_experts, int index_bytes, lon
         p.counts = (uint32_t *)d_workspace;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (p.counts) {
-        const int rc = launch_dependent(sort_count_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), (size_t)(E + 1) * 4, st, p);
-        if (rc != HIKONV_OK) return rc;
-    }
-    const size_t smem = ((size_t)(kSortWarps + 3) * (E + 1) + kSortWarps) * 4;
-    return with_dynamic_smem((const void *)sort_place_kernel, smem,
-                             [&] { return launch_dependent(sort_place_kernel, dim3((unsigned)p.ctas), dim3(kSortThreads), smem, st, p); });
+    // Threads of a CTA: each warp has a row of counts to clear and to add up, each step of a warp comes after the one before, and CTAs of 1024 threads begin
+    // after those of the kernel before have left.  8 pairs of 64 experts take 1.9 us with 256 threads, 2.3 with 512, 3.6 with 1024; 512 pairs 2.4, 2.5 and
+    // 3.7; 2048 pairs 4.8, 3.9 and 4.4; 4104 pairs 6.1 with 512 and 7.2 with 1024; 65536 of 256 experts 8.3 and 8.2, 262144 15.9 and 11.0.
+    auto sort = [&](auto threads) {
+        constexpr int THREADS = decltype(threads)::value;
+        if (p.counts) {
+            const int rc = launch_dependent(sort_count_kernel<THREADS>, dim3((unsigned)p.ctas), dim3(THREADS), (size_t)(E + 1) * 4, st, p);
+            if (rc != HIKONV_OK) return rc;
+        }
+        const size_t smem = ((size_t)(THREADS / 32 + 3) * (E + 1) + THREADS / 32) * 4;
+        return with_dynamic_smem((const void *)sort_place_kernel<THREADS>, smem,
+                                 [&] { return launch_dependent(sort_place_kernel<THREADS>, dim3((unsigned)p.ctas), dim3(THREADS), smem, st, p); });
+    };
+    if (pairs <= 512) return sort(std::integral_constant<int, 256>());
+    if (pairs <= 1 << 16) return sort(std::integral_constant<int, 512>());
+    return sort(std::integral_constant<int, 1024>());
 }
 
 extern "C" int hikonv_rows_to_experts(const void *d_x, int element_bytes, long long x_row_stride, const int32_t *d_slots, int T, int k, int H, void *d_out,
