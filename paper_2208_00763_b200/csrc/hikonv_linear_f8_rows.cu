@@ -50,7 +50,7 @@ __device__ __forceinline__ uint4 f8_piece(const uint8_t *row, int k, int K) {
 }
 
 template <bool X5, bool W5>
-__global__ void __launch_bounds__(kF8RowsThreads, 3) linear_f8_rows_kernel(const __grid_constant__ F8RowsParams q) {
+__global__ void __launch_bounds__(kF8RowsThreads, 2) linear_f8_rows_kernel(const __grid_constant__ F8RowsParams q) {
     __shared__ float part[kF8RowsWarps][16 * kF8RowsAtOnce];
     const LinearParams &p = q.p;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, e = blockIdx.y;
@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(kF8RowsThreads, 3) linear_f8_rows_kernel(const
     if (rows <= 0) return;
     const uint8_t *x = g < rows ? p.x + (m0 + g) * p.x_row : nullptr;
     float sum[4] = {};
+    // blocks whose loads are on their way at once: 4096 x 4096 weights 6.2 us with four, 6.3 with two, 6.6 with one and three CTAs per SM
+#pragma unroll 4
     for (int b = b0; b < b1; ++b) {
         const int k = b * 128 + t * 16;
         uint4 wv[2][2], xv[2];
@@ -120,13 +122,11 @@ __global__ void __launch_bounds__(kF8RowsThreads, 3) linear_f8_rows_kernel(const
 }
 
 // Where this kernel is the faster one, by what was measured on weights from memory.  Up to eight rows in all, so that a weight is read once however rows
-// fall to groups (512 rows of 64 groups took 8 us here spread evenly and 248 in one group, 64 times eight of them; tiles take 9 and 6).  Plain: 1024 x 1024
-// weights 2.2 us here, 4.7 by tiles; 2048 x 2048 3.8 and 6; 4096 x 4096 6.8 and 8.0; 4096 x 5632 9.2 and 9.7; 8192 x 8192 20 and 16.5, where the copies of
-// the tiles keep more bytes on their way than the registers here.  Groups, eight rows: four of 2048 x 2048 7.1 and 8.7, five 10.9 and 9.1; 64 of 512 x 512 4.9
-// and 5.4; 16 of 1024 x 1024 6.6 and 6.8, 32 9.4 and 6.8.
-bool linear_f8_rows_takes(const LinearParams &p) {
-    return p.M <= kF8RowsAtOnce && (double)p.E * p.N * p.K <= (p.offsets ? 1.0 : 1.4) * (1 << 24);
-}
+// fall to groups (512 rows of 64 groups took 8 us here spread evenly and 248 in one group, 64 times eight of them; tiles take 9 and 6).  Plain, eight rows: 1024 x
+// 1024 weights 2.2 us here, 4.7 by tiles; 2048 x 2048 3.5 and 6; 4096 x 4096 6.6 and 8.0; 4608 x 4096, whose CTAs are all that the GPU holds at once, 9.2 and
+// 9.2; 5632 x 4096 10.0 and 9.7; 8192 x 8192 20 and 16.5, where the copies of the tiles keep more bytes on their way than the registers here.  Groups, eight
+// rows: four of 2048 x 2048 6.7 and 8.7, five 10.9 and 9.1; 64 of 512 x 512 4.8 and 5.4; 16 of 1024 x 1024 6.1 and 6.8, 32 9.4 and 6.8.
+bool linear_f8_rows_takes(const LinearParams &p) { return p.M <= kF8RowsAtOnce && (double)p.E * p.N * p.K <= 1 << 24; }
 
 int launch_linear_f8_rows(const LinearParams &p, int x_f8, int w_f8, long long xs_row, cudaStream_t st) {
     F8RowsParams q;
