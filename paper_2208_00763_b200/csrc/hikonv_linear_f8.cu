@@ -236,10 +236,12 @@ struct Sums {
         for (int i = 0; i + COUNT / 2 < CPW / 2; ++i) sum[i] = sum[i + COUNT / 2];
     }
     // Lanes are rows of x from row0 + quad 32 on, `rows` of them in all; columns from n on.  32 bytes of a row at once where rows begin on such a
-    // boundary, else turned in shared memory, 16 columns at a time, so that neighbouring lanes write neighbouring columns.
+    // boundary, else turned in shared memory, 16 columns at a time, so that neighbouring lanes write neighbouring columns.  A residual is asked for
+    // before the columns in front of it are stored, or several rows at once (939 x 5002 x 3013 with bias and residual 50 us; a row at a time 76, without either
+    // 36); whole rows' bias comes by a column a lane, through shared memory.
     template <typename T>
     __device__ __forceinline__ void finish_rows_as(const F8Params &q, int e, long long row0, int rows, int n, float *turn) {
-        constexpr int PER = 32 / sizeof(T), SOME = CPW < 64 ? CPW : 64;
+        constexpr int PER = 32 / sizeof(T), SOME = CPW < 64 ? CPW : 64, ROWS = CPW < 128 ? 8 : 4;
         const LinearParams &p = q.p;
         const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
         const float *bias = (const float *)p.bias + (long long)e * p.N;
@@ -247,23 +249,32 @@ struct Sums {
             T *o = (T *)p.out + (row0 + row) * p.out_row + n;
             const T *r = (const T *)p.residual + (row0 + row) * p.res_row + n;
             const bool there = row < rows;
+            if (p.bias) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < CPW; i += 32) turn[i + lane] = load_ordered(bias + n + i + lane);
+                __syncwarp();
+            }
+            union { uint32_t w[8]; T v[PER]; } x;
+            const bool adds = p.residual && there;
+            if (adds) load_global32(r, x.w);
 #pragma unroll 1
             for (int i0 = 0; i0 < CPW; i0 += SOME) {
 #pragma unroll
                 for (int j = 0; j < SOME; j += PER) {
-                    union { uint32_t w[8]; T v[PER]; } y, x;
+                    union { uint32_t w[8]; T v[PER]; } y;
                     float v[PER];
-                    if (p.residual && there) load_global32(r + i0 + j, x.w);
 #pragma unroll
                     for (int i = 0; i < PER; ++i) v[i] = at(j + i);
                     if (p.bias) {
 #pragma unroll
-                        for (int i = 0; i < PER; ++i) v[i] += load_ordered(bias + n + i0 + j + i);
+                        for (int i = 0; i < PER; ++i) v[i] += turn[i0 + j + i];
                     }
                     activate_some<T>(v, p.act);
                     if (p.residual) {
 #pragma unroll
                         for (int i = 0; i < PER; ++i) v[i] += to_float(x.v[i]);
+                        if (adds && i0 + j + PER < CPW) load_global32(r + i0 + j + PER, x.w);
                     }
 #pragma unroll
                     for (int i = 0; i < PER; ++i) from_float(v[i], &y.v[i]);
@@ -288,14 +299,21 @@ struct Sums {
 #pragma unroll
             for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = v[i];
             __syncwarp();
-            const int col = n + (lane & 15);
-#pragma unroll 4
-            for (int i = 0; i < 16; ++i) {
-                const int mine = 2 * i + (lane >> 4), there = quad * 32 + mine;
-                if (there >= rows || col >= p.N) continue;
-                float y = turn[mine * 17 + (lane & 15)];
-                if (p.residual) y += to_float(load_ordered((const T *)p.residual + (row0 + there) * p.res_row + col));
-                from_float(y, (T *)p.out + (row0 + there) * p.out_row + col);
+            const int col = n + (lane & 15), first = quad * 32 + (lane >> 4), left = col < p.N ? rows - first : 0;      // this lane's rows: first, first + 2, ..
+#pragma unroll 1
+            for (int i = 0; 2 * i < left && i < 16; i += ROWS) {
+                T res[ROWS];
+                if (p.residual) {
+                    const T *r = (const T *)p.residual + (row0 + first + 2 * i) * p.res_row + col;
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j)
+                        if (2 * (i + j) < left) res[j] = load_ordered(r + 2 * j * p.res_row);
+                }
+                T *o = (T *)p.out + (row0 + first + 2 * i) * p.out_row + col;
+                const float *mine = turn + (2 * i + (lane >> 4)) * 17 + (lane & 15);
+#pragma unroll
+                for (int j = 0; j < ROWS; ++j)
+                    if (2 * (i + j) < left) from_float(p.residual ? mine[2 * j * 17] + to_float(res[j]) : mine[2 * j * 17], o + 2 * j * p.out_row);
             }
         }
     }
@@ -646,7 +664,7 @@ constexpr int kPairRows = 256, kPairWidth = 256, kPairHalf = 128, kPairStages = 
 constexpr int kPairAdders = 8, kPairThreads = (kF8FirstAdder + kPairAdders) * 32;
 // The sums take more registers than an even share: those of a thread that adds up, and of one that does not.  Together no more than the launch's,
 // which takes all that 384 threads can have.
-constexpr int kPairAdderRegs = 216, kPairOtherRegs = 64, kPairLaunchRegs = 168;
+constexpr int kPairAdderRegs = 232, kPairOtherRegs = 40, kPairLaunchRegs = 168;
 static_assert(kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32 <= kPairLaunchRegs * kPairThreads, "registers of the launch");
 
 constexpr int kPairAhead = 8;                           // steps whose scales of x are on their way

@@ -447,3 +447,19 @@ def test_weights_of_many_bytes():
         for i in range(2):
             at = slice(off[31 + i], off[32 + i])
             near(got[at], *reference(x[at], small[i], xs[:, at], small_ws[i], None, hk.ACT_NONE, None))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K,act", [(4096, 2048, 384, hk.ACT_SILU), (4096, 2049, 384, hk.ACT_NONE), (4100, 2064, 300, hk.ACT_GELU), (4096, 2200, 200, hk.ACT_SILU),
+                                       (500, 1501, 256, hk.ACT_NONE), (500, 1536, 256, hk.ACT_RELU), (130, 1009, 640, hk.ACT_SILU)])
+def test_bias_and_residual_of_large_outputs(M, N, K, act, dtype):
+    x, w, xs, ws, g = operands(M, N, K, N)
+    bias = torch.randn(N, generator=g, device="cuda")
+    residual = torch.randn(M, N, generator=g, device="cuda").to(dtype)
+    for b, r in ((bias, None), (None, residual), (bias, residual)):
+        want, off = reference(x, w, xs, ws, b, act, r)
+        near(hk.linear_f8(x, w, xs, ws, b, act, r, out_dtype=dtype), want, off)
+    both = residual.clone()                                # in place
+    hk.linear_f8(x, w, xs, ws, bias, act, both, out=both)
+    near(both, want, off)
+    assert hk.linear_wait_timeouts() == 0
