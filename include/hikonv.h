@@ -578,7 +578,8 @@ int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, 
 /*
  * hikonv_rows_from_experts_grad - its gradient for y and the weights from the one for out (which the residual's is, too).
  *   grad_y[slots[t][j]] = weights[t][j] grad[t]; zeros in row -2 - slots[t][j] for slots below -1, so that every row is written when
- *      slots come from hikonv_sort_by_expert and R = T k.  Rows outside 0 .. R - 1 are left out.
+ *      slots come from hikonv_sort_by_expert and R = T k.  Other rows of grad_y (of padding, of pairs whose slot was set to -1) are left as
+ *      they were: where there are any, grad_y is zeroed before the call.  Rows outside 0 .. R - 1 are left out.
  *   grad_weights[t][j] = sum_h grad[t][h] y[slots[t][j]][h], 32-bit sums in an order that depends on the sizes alone; 0 without a row
  *   weights and grad_weights: [T][k] float, or both NULL (then y is not read).
  * Outputs must overlap neither inputs nor each other.

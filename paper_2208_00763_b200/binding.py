@@ -542,12 +542,12 @@ def _stream_of(t: torch.Tensor, stream) -> int:
     return _raw_stream(t.device.index) if stream is None else int(stream.cuda_stream)
 
 
-def _empty(shape, dtype, like: torch.Tensor, stream) -> torch.Tensor:
+def _empty(shape, dtype, like: torch.Tensor, stream, make=torch.empty) -> torch.Tensor:
     """Memory that a call on `stream` may write at once: the allocator's for that stream, which nothing on another one still uses."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return make(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return make(shape, dtype=dtype, device=like.device)
 
 
 def quantize_rows(x: torch.Tensor, bits: int, is_signed: bool = True, codes: Optional[torch.Tensor] = None,
@@ -791,8 +791,10 @@ def rows_from_experts_grad(grad: torch.Tensor, y: Optional[torch.Tensor], slots:
                            grad_y: Optional[torch.Tensor] = None, grad_weights: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """The gradient of ``rows_from_experts``, from the one for its output: (grad_y, grad_weights).  ``grad_y[slots[t, j]]`` is
     ``weights[t, j] * grad[t]``, zeros in the places of pairs without expert; ``grad_weights[t, j]`` the product of ``grad[t]`` with the
-    pair's row of ``y``, 0 without one.  Without weights ``y`` is not read (it may be None) and there is no grad_weights.  ``grad_y`` has a row for
-    each pair unless it is given; then rows that no slot names are left as they were.  The residual's gradient is ``grad`` itself."""
+    pair's row of ``y``, 0 without one.  Without weights ``y`` is not read (it may be None) and there is no grad_weights.  ``grad_y`` has the rows of
+    ``y``, or one for each pair without it, and zeros where no slot names a row (padding of ``y``, a row whose pair was dropped by a slot of
+    -1): the call sets it to zero first.  In a ``grad_y`` that is given such rows are left as they were, and nothing is set to zero first: with
+    the slots of ``sort_by_expert`` every row of T k is written.  The residual's gradient is ``grad`` itself."""
     if stream is None:
         done = (_fast or _load_fast()).rows_from_experts_grad(grad, y, slots, weights, grad_y, grad_weights)
         if done is not None:
@@ -807,7 +809,8 @@ def rows_from_experts_grad(grad: torch.Tensor, y: Optional[torch.Tensor], slots:
     if weights is not None and y is None:
         raise ValueError("the gradient of weights needs y")
     if grad_y is None:
-        grad_y = _empty((T * k if y is None else y.shape[0], H), grad.dtype, grad, stream)
+        # the kernel writes the rows that slots name
+        grad_y = _empty((T * k if y is None else y.shape[0], H), grad.dtype, grad, stream, torch.zeros)
     grad_y_row = _rows(grad_y, "grad_y", (grad.dtype,), grad, (grad_y.shape[0] if grad_y.dim() == 2 else T * k, H))
     R = grad_y.shape[0]
     y_row = H if weights is None else _rows(y, "y", (grad.dtype,), grad, (R, H))

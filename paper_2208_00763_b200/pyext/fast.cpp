@@ -551,7 +551,8 @@ PyObject *rows_from_experts_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (float_type(type) < 0 || (y && y->dim() != 2)) return nullptr;
         const int64_t T = grad->size(0), H = grad->size(1), k = slots->size(1);
         at::Tensor made_y, made_w;
-        if (!given_y) made_y = empty({y ? y->size(0) : T * k, H}, type, *grad);
+        // zeros: the kernel writes the rows that slots name
+        if (!given_y) made_y = at::zeros({y ? y->size(0) : T * k, H}, at::TensorOptions().dtype(type).device(grad->device()));
         if (weights && !given_w) made_w = empty({T, k}, at::kFloat, *grad);
         const at::Tensor &gy = given_y ? *given_y : made_y;
         const at::Tensor *gw = given_w ? given_w : weights ? &made_w : nullptr;
