@@ -464,7 +464,7 @@ typedef enum {
 typedef enum {
     HIKONV_ACT_NONE = 0,
     HIKONV_ACT_RELU = 1, /* max(v, 0)                         */
-    HIKONV_ACT_SILU = 2, /* v / (1 + exp(-v)); every normal result keeps its bits; NaN for -infinity */
+    HIKONV_ACT_SILU = 2, /* v / (1 + exp(-v)): every normal result within 2^-21 of itself (v < -87: 2^-17); NaN for -infinity */
     HIKONV_ACT_GELU = 3  /* v (1 + erf(v / sqrt(2))) / 2 in just these steps: within 2^-22 |v|, also where the result is far smaller */
 } hikonv_activation;
 

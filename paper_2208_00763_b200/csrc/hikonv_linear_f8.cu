@@ -183,18 +183,20 @@ struct F8Control {
     int whole;                           // no wait of this CTA has run out
 };
 
-// SiLU of two values for outputs of 16 bits, v / (1 + t) or v t / (1 + t) for v < 0 with t = exp(-|v|), as silu() has it.  t comes as a power of two
-// whose argument is rounded once, which moves it by less than 2^-17 of itself, and 2^32 times too large, so that normal results down to the smallest
-// keep their bits; both divisors, which lie in [1, 2], share a reciprocal (fminf: one value's NaN must not reach the other).  Eleven instructions a
-// value instead of 18, and the special-function unit, which does a quarter of a warp per cycle, is asked three times for two values instead of four.
-__device__ __forceinline__ void silu_short(float &v0, float &v1) {
-    float t0, t1, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t0) : "f"(fmaf(fabsf(v0), -1.44269504f, 32.f)));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t1) : "f"(fmaf(fabsf(v1), -1.44269504f, 32.f)));
-    const float d0 = fminf(fmaf(t0, 0x1p-32f, 1.f), 2.f), d1 = fminf(fmaf(t1, 0x1p-32f, 1.f), 2.f);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
-    v0 = (v0 < 0.f ? v0 * t0 * 0x1p-32f : v0) * (r * d1);
-    v1 = (v1 < 0.f ? v1 * t1 * 0x1p-32f : v1) * (r * d0);
+// SiLU in front of outputs of 16 bits, as v / (1 + exp(-v)) for either sign.  -v log2(e) is rounded to z, a multiple of 2^-13 (by the sum with 1536);
+// exp(-v) is 2^z (1 + e) with the rest e = -v - z ln 2, whose square is below 2^-29.  All of it is taken 2^-14 times, so that the divisor is finite and its
+// reciprocal normal for every result that an output could hold, and |v| counts as 98 beyond that (the sign's and the minimum's instruction is one), which
+// leaves infinite and NaN values to the last product.  Off by 2^-21.2 of the result at most over all values from -87 on (silu(): 2^-21.6), by 2^-17.4
+// below, where the reciprocal times 2^-14 is subnormal (silu(): the same); measured on every one of them.  Eleven instructions a value against silu()'s
+// 18, and one rounding of the whole exponent, two values to a reciprocal, has eleven, too, but is off by 2^-18 at -80: 32 groups of 16384 x 2048 x 4096 258 us
+// (silu() 265, the coarse form 251).
+__device__ __forceinline__ float silu_short(float v) {
+    float a, t, r;
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(a) : "f"(v), "f"(98.f));
+    const float lifted = fmaf(a, -1.44269504f, 1536.f), e = fmaf(lifted - 1536.f, -0.693147182f, -a);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(lifted - 1550.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(t, e, t) + 0x1p-14f));
+    return v * (r * 0x1p-14f);
 }
 // The activation of neighbouring values in front of an output of type T.
 template <typename T, int COUNT>
@@ -206,10 +208,7 @@ __device__ __forceinline__ void activate_some(float (&v)[COUNT], int act) {
             break;
         case HIKONV_ACT_SILU:
 #pragma unroll
-            for (int i = 0; i < COUNT; i += 2) {
-                if constexpr (sizeof(T) == 2) silu_short(v[i], v[i + 1]);
-                else v[i] = activate(v[i], HIKONV_ACT_SILU), v[i + 1] = activate(v[i + 1], HIKONV_ACT_SILU);
-            }
+            for (int i = 0; i < COUNT; ++i) v[i] = sizeof(T) == 2 ? silu_short(v[i]) : activate(v[i], HIKONV_ACT_SILU);
             break;
         case HIKONV_ACT_GELU:
 #pragma unroll
