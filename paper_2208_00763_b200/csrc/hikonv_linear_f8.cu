@@ -108,6 +108,17 @@ __device__ __forceinline__ bool f8_wait(const F8Params &q, uint32_t bar, uint32_
     return __all_sync(0xFFFFFFFFu, mbarrier_wait(bar, parity, q.wait_cycles));
 }
 
+// Waits until every stage that the loads up to here, of which the ring holds the next, have filled is free again: all copies have landed and all
+// multiplies of them have ended and arrived.  A stage that was never filled counts as free.
+__device__ __forceinline__ bool f8_stages_free(const F8Params &q, Ring ring, uint32_t empty) {
+    bool fine = true;
+    for (int i = 0; fine && i < q.stages; ++i) {
+        fine = f8_wait(q, empty + 8 * ring.stage, ring.phase ^ 1);
+        ring.next(q.stages);
+    }
+    return fine;
+}
+
 // ---- scales
 //
 // The scales of x and w that a tile's steps need come to shared memory by asynchronous copies of four bytes (rows of scales begin anywhere), a few steps at
@@ -558,11 +569,14 @@ __global__ void __launch_bounds__(kF8Threads, 1)
                     ring.next(q.stages);
                 }
             }
-            // what is in flight has to land before the memory goes: the last load of every stage
-            for (int i = 0; i < q.stages && i < loads; ++i) {
-                ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
-                if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                fine &= f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+            fine = fine && f8_stages_free(q, ring, HIKONV_BAR(empty, 0));
+            if (!fine) {
+                // what is in flight has to land before the memory goes: the last load of every stage
+                for (int i = 0; i < q.stages && i < loads; ++i) {
+                    ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+                    if (ring.stage == q.stages - 1) ring.phase ^= 1;
+                    f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+                }
             }
         } else if (warp == 1) {
             Ring ring, acc;
@@ -832,12 +846,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                     ring.next(q.stages);
                 }
             }
-            // what is in flight, of both CTAs, has to land before the memory goes: the last load of every stage
-            if (rank == 0) {
+            // both CTAs' copies and multiplies, and the multiplies' arrivals at this CTA's barriers
+            fine = fine && f8_stages_free(q, ring, HIKONV_BAR(empty, 0));
+            if (!fine && rank == 0) {
+                // what is in flight, of both CTAs, has to land before the memory goes: the last load of every stage
                 for (int i = 0; i < q.stages && i < loads; ++i) {
                     ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
                     if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                    fine &= f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+                    f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
                 }
             }
         } else if (warp <= 2 && rank == 0) {
@@ -908,7 +924,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (!fine && lane == 0) atomicAdd(&linear_f8_timeouts, 1u);
     __syncwarp();
     tc_fence_before();
-    cluster_sync_all();                                 // the other CTA's multiplies, copies and arrivals are over
+    // The other CTA's copies, multiplies and arrivals are over: its own warps' by the barrier, the multiplies' arrivals by the waits for them in front
+    // of it, of the adding warps for full accumulators and of each CTA's loading warp for free stages.
+    cluster_sync_all();
     __syncthreads();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 #undef HIKONV_BAR

@@ -40,3 +40,25 @@ def test_silu_less_a_residual_that_cancels_it(M, N, dtype, most):
     bound = bound + torch.finfo(dtype).eps / 2 * (left.abs() + bound) + torch.finfo(dtype).tiny * torch.finfo(dtype).eps / 2
     assert ((got.double() - left).abs() <= bound).all(), ((got.double() - left).abs() / bound).max().item()
     assert hk.linear_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("N", [2048, 2176])                # the last tile of 256 columns whole, and half of one
+@pytest.mark.parametrize("K", [16, 128, 640, 768, 896, 1500])    # fewer steps than there are stages, as many, and more
+def test_pairs_of_ctas_one_call_after_the_other(K, N):
+    # each call's CTAs come to where the ones of the call before have just left
+    g = torch.Generator("cuda").manual_seed(K)
+    M = 4096
+    x, w = (torch.randn(r, (K + 15) // 16 * 16, generator=g, device="cuda").mul_(100).clamp_(-448, 448).to(E4M3)[:, :K] for r in (M, N))
+    xs, ws = torch.rand(-(-K // 128), M, generator=g, device="cuda"), torch.rand(-(-N // 128), -(-K // 128), generator=g, device="cuda")
+    out = [torch.empty(M, N, dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    for i in range(64):
+        hk.linear_f8(x, w, xs, ws, out=out[i % 8])
+        if i % 3 == 0:
+            hk.linear_f8(x[: 40 * (i % 5) + 1], w, xs[:, : 40 * (i % 5) + 1], ws)
+    xv = x.float() * xs.T.repeat_interleave(128, 1)[:, :K]
+    wv = w.float() * ws.repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
+    want, size = xv.double() @ wv.double().T, xv.double().abs() @ wv.double().abs().T
+    # a block's sum by the tensor cores, 2^-23 of its magnitudes each; the scales' products and the blocks, half a step each; and the rounding
+    bound = size * (128 * 2.0 ** -23 + (K // 128 + 8) * 2.0 ** -24)
+    assert ((out[0].double() - want).abs() <= bound + 2.0 ** -8 * (want.abs() + bound)).all()
+    assert all(torch.equal(o, out[0]) for o in out) and hk.linear_wait_timeouts() == 0
