@@ -683,8 +683,9 @@ static_assert(kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder
 constexpr int kPairAhead = 8;                           // steps whose scales of x are on their way
 
 struct PairControl {
-    uint64_t full[kPairStages], empty[kPairStages], acc_full[4], acc_empty[4], drain[2];
+    uint64_t full[kPairStages], empty[kPairStages], acc_full[4], acc_empty[4], drain[2], peer;
     uint32_t tmem;
+    int peer_loads;                      // of the second CTA, in the first one's memory, once that has arrived at peer
 };
 
 __device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -703,6 +704,12 @@ __device__ __forceinline__ void pair_commit(uint32_t bar) {
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ void store_then_arrive_at(uint32_t cluster_address, int v, uint32_t cluster_bar) {
+    asm volatile("st.shared::cluster.s32 [%0], %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [%2];" ::"r"(cluster_address), "r"(v),
+                 "r"(cluster_bar)
+                 : "memory");
 }
 
 // A warp that adds up: a quarter of the lanes, 128 columns, 32 at a time.  Scales of x come by asynchronous copies, kPairAhead steps ahead, those of w
@@ -800,6 +807,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             mbarrier_init(HIKONV_BAR(acc_empty, lane), kPairAdders);       // four warps of each CTA
         }
         if (lane < 2) mbarrier_init(HIKONV_BAR(drain, lane), 1);
+        if (lane == 2) mbarrier_init(HIKONV_BAR(peer, 0), 1);
         mbarrier_init_fence();
         if (lane == 3) {
             asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
@@ -848,13 +856,30 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
             // both CTAs' copies and multiplies, and the multiplies' arrivals at this CTA's barriers
             fine = fine && f8_stages_free(q, ring, HIKONV_BAR(empty, 0));
-            if (!fine && rank == 0) {
-                // what is in flight, of both CTAs, has to land before the memory goes: the last load of every stage
-                for (int i = 0; i < q.stages && i < loads; ++i) {
-                    ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
-                    if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                    f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
+            // Where a wait ran out, the two may have loaded different stages; both CTAs' copies end at the first one's barriers.
+            if (rank == 1) {
+                if (elect_one()) store_then_arrive_at(remote_address(control + (uint32_t)offsetof(PairControl, peer_loads), 0), loads, remote_address(HIKONV_BAR(peer, 0), 0));
+            } else if (!fine) {
+                // the second CTA's loading warp ends after one wait that runs out at most
+                bool told = false;
+                for (int i = 0; i < 4 && !told; ++i) told = f8_wait(q, HIKONV_BAR(peer, 0), 0);
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");
+                const int theirs = told ? *(volatile int *)&ctl.peer_loads : loads, most = max(loads, theirs);
+                // a step that one of them alone has loaded: the first counts the second's bytes, or brings as many in their place
+                for (int u = min(loads, theirs); u < most; ++u) {
+                    const uint32_t at = stages + u % q.stages * kPairStage, bar = HIKONV_BAR(full, u % q.stages);
+                    if (elect_one()) {
+                        if (u >= loads) {
+                            mbarrier_arrive_expect(bar, kPairStage);
+                        } else {
+                            pair_load(at, &map_x, 0, 0, remote_address(bar, 0));
+                            pair_load(at + kF8Rows * kF8Depth, &map_w, 0, 0, remote_address(bar, 0));
+                            pair_load(at + (kF8Rows + kPairHalf / 2) * kF8Depth, &map_w, 0, 0, remote_address(bar, 0));
+                        }
+                    }
                 }
+                // what is in flight, of both CTAs, has to land before the memory goes: the last load of every stage
+                for (int u = max(0, most - q.stages); u < most; ++u) f8_wait(q, HIKONV_BAR(full, u % q.stages), u / q.stages & 1);
             }
         } else if (warp <= 2 && rank == 0) {
             // a warp for each half of the columns
