@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
                 const float *w = p.w_scale + ((long long)tile.e * q.w_blocks + tile.n0 / kF8Depth) * q.chunks;
                 fine = bring_scales(q, ring, stages + q.feed_off, HIKONV_BAR(scales.full, 0), HIKONV_BAR(scales.empty, 0), tile.row0, tile.rows, w, 1, c0, c1);
             }
-            cp_async_wait_all();
+            asm volatile("cp.async.wait_all;" ::: "memory");        // these copies are in no group that is waited for
         }
         if (q.splits > 1) {
             if (!fine) ctl.whole = 0;
