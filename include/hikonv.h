@@ -535,10 +535,12 @@ int hikonv_grouped_linear(const void *d_x, long long x_row_stride, const void *d
  * hikonv_linear_wait_timeouts - warps of linear-layer kernels on the current device whose wait for their own copies or multiplies ran
  * out (after a second) since the last call of any thread; 0 unless the device is at fault.  What such a CTA had left to write stays
  * unwritten.  Synchronises the device, all its streams.
- * hikonv_linear_wait_check - a debug aid for the above, as hikonv_conv2d_wait_check.
+ * hikonv_linear_wait_check, hikonv_linear_f8_wait_check - debug aids for the above, as hikonv_conv2d_wait_check: one wait each that runs
+ * out in a kernel of the file of hikonv_linear, or of hikonv_linear_f8 (whose waits are counted with them).
  */
 int hikonv_linear_wait_timeouts(unsigned int *h_count);
 int hikonv_linear_wait_check(long long cycles, void *stream);
+int hikonv_linear_f8_wait_check(long long cycles, void *stream);
 
 /*
  * A mixture of experts: hikonv_sort_by_expert, hikonv_rows_to_experts (or hikonv_quantize_blocks), products of groups of rows,

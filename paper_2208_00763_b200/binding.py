@@ -103,6 +103,7 @@ _SIGNATURES = {
     "hikonv_linear_workspace_bytes": (_sz, [_vp, _ll, _vp] + [_i] * 5),
     "hikonv_linear_wait_timeouts": (_i, [_vp]),
     "hikonv_linear_wait_check": (_i, [_ll, _vp]),
+    "hikonv_linear_f8_wait_check": (_i, [_ll, _vp]),
     "hikonv_sort_by_expert": (_i, [_vp, _i, _ll, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "hikonv_sort_by_expert_workspace_bytes": (_sz, [_i, _i, _i]),
     "hikonv_rows_to_experts": (_i, [_vp, _i, _ll, _vp, _i, _i, _i, _vp, _ll, _i, _vp]),
@@ -684,6 +685,11 @@ def linear_wait_timeouts() -> int:
 def linear_wait_check(cycles: int, stream=None) -> None:
     """One thread waits `cycles` for a barrier that nothing completes, gives up and is counted."""
     _check(lib().hikonv_linear_wait_check(int(cycles), _stream(stream)), "hikonv_linear_wait_check")
+
+
+def linear_f8_wait_check(cycles: int, stream=None) -> None:
+    """The same for the products of 8-bit floating point numbers, whose waits that ran out ``linear_wait_timeouts`` counts, too."""
+    _check(lib().hikonv_linear_f8_wait_check(int(cycles), _stream(stream)), "hikonv_linear_f8_wait_check")
 
 
 # ------------------------------------------------------------------ a mixture of experts

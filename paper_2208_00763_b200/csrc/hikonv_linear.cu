@@ -133,3 +133,8 @@ extern "C" int hikonv_linear_wait_check(long long cycles, void *stream) {
     if (cycles < 0 || cycles > kWaitCycles) return HIKONV_ERR_INVALID_ARG;
     return launch_linear_wait_check(cycles, (cudaStream_t)stream);
 }
+
+extern "C" int hikonv_linear_f8_wait_check(long long cycles, void *stream) {
+    if (cycles < 0 || cycles > kWaitCycles) return HIKONV_ERR_INVALID_ARG;
+    return launch_linear_f8_wait_check(cycles, (cudaStream_t)stream);
+}

@@ -40,5 +40,6 @@ int launch_linear_tc(LinearParams p, void *workspace, size_t workspace_bytes, cu
 int read_linear_timeouts(unsigned int *h_count);             // on the current device, since it was loaded
 int read_linear_f8_timeouts(unsigned int *h_count);          // likewise, of hikonv_linear_f8.cu
 int launch_linear_wait_check(long long cycles, cudaStream_t st);
+int launch_linear_f8_wait_check(long long cycles, cudaStream_t st);
 
 }  // namespace hikonv

@@ -957,6 +957,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 #undef HIKONV_BAR
 }
 
+// A warp that waits as those above do, for a barrier that nothing completes, gives up and is counted.
+__global__ void linear_f8_wait_check_kernel(const __grid_constant__ F8Params q) {
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        mbarrier_init(smem_address(&bar), 1);
+        mbarrier_init_fence();
+    }
+    __syncwarp();
+    if (!f8_wait(q, smem_address(&bar), 0) && threadIdx.x == 0) atomicAdd(&linear_f8_timeouts, 1u);
+}
+
 // ---- host
 
 struct F8Shape {
@@ -1126,6 +1137,13 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
 
 int read_linear_f8_timeouts(unsigned int *h_count) {
     return cudaMemcpyFromSymbol(h_count, linear_f8_timeouts, sizeof(*h_count)) == cudaSuccess ? HIKONV_OK : HIKONV_ERR_CUDA;
+}
+
+int launch_linear_f8_wait_check(long long cycles, cudaStream_t st) {
+    F8Params q;
+    memset(&q, 0, sizeof(q));
+    q.wait_cycles = cycles;
+    return launch_plain(linear_f8_wait_check_kernel, dim3(1), dim3(32), 0, st, q);
 }
 
 static int linear_f8_run(const void *d_x, int x_f8, long long x_row, const void *d_w, int w_f8, long long w_row, const int32_t *d_offsets, bool grouped, int E,

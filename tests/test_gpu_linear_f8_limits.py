@@ -62,3 +62,19 @@ def test_pairs_of_ctas_one_call_after_the_other(K, N):
     bound = size * (128 * 2.0 ** -23 + (K // 128 + 8) * 2.0 ** -24)
     assert ((out[0].double() - want).abs() <= bound + 2.0 ** -8 * (want.abs() + bound)).all()
     assert all(torch.equal(o, out[0]) for o in out) and hk.linear_wait_timeouts() == 0
+
+
+def test_waits_that_run_out_are_counted():
+    assert hk.linear_wait_timeouts() == 0
+    side = torch.cuda.Stream()
+    for n in (1, 2):
+        for _ in range(n):
+            hk.linear_f8_wait_check(2000000, stream=side)
+        assert hk.linear_wait_timeouts() == n
+        assert hk.linear_wait_timeouts() == 0
+    hk.linear_f8_wait_check(2000000)
+    hk.linear_wait_check(2000000)
+    assert hk.linear_wait_timeouts() == 2 and hk.linear_wait_timeouts() == 0
+    for cycles in (1 << 40, -1):
+        with pytest.raises(hk.HikonvError):
+            hk.linear_f8_wait_check(cycles)
