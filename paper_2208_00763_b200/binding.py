@@ -512,6 +512,12 @@ def conv2d_multiplies(B, Ci, H, W, Co, K, pad, p, q, x_signed, w_signed, algo=AL
 _FLOAT_TYPES = {torch.float32: OUT_F32, torch.float16: OUT_F16, torch.bfloat16: OUT_BF16}
 
 
+def _fits(name: str, *sizes: int) -> None:
+    """The library takes sizes as 32-bit integers, which ctypes makes of larger ones without a word."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise ValueError("%s: a size of %d, above 2^31 - 1" % (name, max(sizes)))
+
+
 def _rows(t: torch.Tensor, name: str, dtypes, like: Optional[torch.Tensor] = None, shape=None) -> int:
     """Checks a matrix whose rows may lie apart; returns the elements from one row to the next."""
     if not getattr(t, "is_cuda", False) or t.layout != torch.strided or t.dim() != 2:
@@ -524,6 +530,7 @@ def _rows(t: torch.Tensor, name: str, dtypes, like: Optional[torch.Tensor] = Non
         raise ValueError("%s has shape %s, the call needs %s" % (name, tuple(t.shape), tuple(shape)))
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError("%s must have contiguous rows" % name)
+    _fits(name, *t.shape)
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -705,6 +712,7 @@ def _slots(slots: torch.Tensor, like: torch.Tensor, rows: Optional[int] = None) 
     T, k = slots.shape
     if rows is not None and T != rows:
         raise ValueError("slots has %d rows, there are %d tokens" % (T, rows))
+    _fits("slots", T, k)
     return _vector(slots, "slots", torch.int32, (T, k), like), T, k
 
 
@@ -721,6 +729,7 @@ def sort_by_expert(experts: torch.Tensor, n_experts: int, offsets: Optional[torc
     if getattr(experts, "dtype", None) not in _INDEX_TYPES:
         raise ValueError("experts must be an int32 or int64 matrix")
     row = _rows(experts, "experts", (experts.dtype,))
+    _fits("n_experts", n_experts)
     T, k = experts.shape
     if offsets is None:
         offsets = _empty(n_experts + 1, torch.int32, experts, stream)
@@ -742,6 +751,7 @@ def sort_by_expert(experts: torch.Tensor, n_experts: int, offsets: Optional[torc
 
 def sort_by_expert_workspace_bytes(tokens: int, choices: int, n_experts: int) -> int:
     """Bytes that ``sort_by_expert`` needs between its launches: 0 for up to 4096 pairs."""
+    _fits("sort_by_expert", tokens, choices, n_experts)
     return int(lib().hikonv_sort_by_expert_workspace_bytes(tokens, choices, n_experts))
 
 
@@ -911,6 +921,7 @@ def _weight_rows(w: torch.Tensor, name: str, dtypes, like: Optional[torch.Tensor
     row = w.stride(-2) if N > 1 else w.stride(0) if w.dim() == 3 and w.shape[0] > 1 else K
     if w.dim() == 3 and w.shape[0] > 1 and w.stride(0) != N * row:
         raise ValueError("%s must have its matrices one behind the other" % name)
+    _fits(name, *w.shape)
     return row
 
 
