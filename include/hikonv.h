@@ -562,7 +562,8 @@ size_t hikonv_sort_by_expert_workspace_bytes(int T, int k, int E);
  * hikonv_rows_to_experts - rows of tokens to the places of their pairs: out[slots[t][j]] = x[t] for every slot in 0 .. R - 1.
  *   x: [T][H] elements of 1, 2 or 4 bytes, rows x_row_stride elements apart (0 when all rows are one); out: [R][H], out_row_stride >= H.
  * Rows of out that no slot names are left as they were; a row that two slots name is undefined.  Its gradient is
- * hikonv_rows_from_experts without weights.  T k <= 2^30, H <= 2^23.  out must not overlap x or slots.
+ * hikonv_rows_from_experts without weights.  T k <= 2^30, H <= 2^23.  out must not overlap x or slots.  The bytes around a row of x that
+ * lie in the same four aligned bytes as part of it may be read, nothing else outside the operands.
  */
 int hikonv_rows_to_experts(const void *d_x, int element_bytes, long long x_row_stride, const int32_t *d_slots, int T, int k, int H, void *d_out,
                            long long out_row_stride, int R, void *stream);
@@ -601,7 +602,9 @@ int hikonv_rows_from_experts_grad(const void *d_grad, int type, long long grad_r
  *   scale: [ceil(K / 128)][rows], scale_row_stride elements from block to block.
  *   slots: NULL (k and R are 0), or [M][k]: row m goes to the rows slots[m][j] in 0 .. R - 1 of values and of scale; others are left as they were.
  * A block of zeros has scale 0 and values 0.  A block with a NaN has scale NaN and values NaN; one whose largest magnitude is infinite has
- * scale infinity, values 0 and, for the infinite ones, NaN (so what is computed from such a block is NaN).  Subnormals are kept.
+ * scale infinity, values 0 and, for the infinite ones, NaN (so what is computed from such a block is NaN).  Subnormal inputs and
+ * scales are kept, but a scale below 2^-126 has fewer bits: quotients by one that was rounded down saturate at max(type), and a block whose
+ * largest magnitude is at most max(type) 2^-150 has scale 0 and values 0, as one of zeros has.  A zero among the values may have either sign.
  * M k <= 2^30.  Outputs must overlap neither x, slots nor each other.
  */
 typedef enum {
@@ -627,7 +630,10 @@ int hikonv_quantize_tiles(const void *d_w, int w_type, long long w_row_stride, i
  *   epilogue: out_type F32, F16 or BF16, activation, d_bias (float) and d_residual as for hikonv_linear; d_x_scale and d_w_scale, shift, lo
  *      and hi NULL or 0
  * Products of a block are summed by the tensor cores in 32-bit arithmetic; blocks are added in 32 bits in an order that depends on
- * sizes and alignment alone.  out must overlap no input but the residual (same address and stride).
+ * sizes and alignment alone.  A block's two scales are multiplied with each other first, in 32 bits: a product below 2^-126 has fewer bits
+ * (2^-150 of the block's sum is added to the error), and one beyond 3.4e38 is infinite (NaN for a sum of 0).
+ * out must overlap no input but the residual (same address and stride).  The bytes behind a row of x or w that lie in the same 16
+ * aligned bytes as its end may be read, nothing else outside the operands.
  *
  * hikonv_grouped_linear_f8 - with a matrix per group of rows: w: [E][N][K] (rows equally far apart throughout), w_scale: [E][..][..],
  *   d_bias: [E][N]; rows offsets[e] .. offsets[e + 1] - 1 belong to matrix e.  Offsets as for hikonv_grouped_linear; rows of no group are

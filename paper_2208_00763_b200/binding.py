@@ -6,6 +6,9 @@ library.  Loading fails loudly when the library has not been built: there is no 
 The calls of every step (``conv1d``, ``conv1d_dense``, ``pack``, ``conv2d``, ``conv2d_dense`` without tuning record and
 explicit stream, ``quantize_rows``, ``linear``, ``grouped_linear`` and the calls of a mixture of experts without explicit stream) go through the extension module ``_fast`` first, which makes the same checks on the tensors natively and
 returns None where anything is amiss; the Python code below then raises the error.
+
+No call records gradients: what it returns does not require one, whether its inputs do or not.  ``rows_from_experts`` has its gradient in
+``rows_from_experts_grad``, ``rows_to_experts`` in ``rows_from_experts``.
 """
 from __future__ import annotations
 

@@ -41,7 +41,8 @@ __device__ __forceinline__ float f8_max(float a, float b) {
 }
 template <bool E5M2> constexpr float kF8Most = E5M2 ? 57344.f : 448.f;
 
-// Two quotients to two bytes, the first in the low one.  Quotients are at most the type's largest number and one step of 2^-24, which rounds to it.
+// Two quotients to two bytes, the first in the low one.  Quotients are at most the type's largest number and one step of 2^-24, which rounds to it; more
+// where the scale is subnormal and was rounded down (the smallest bf16 number, 2^-133, to E5M2 has scale 2^-149 and quotient 65536), and then saturate.
 template <bool E5M2>
 __device__ __forceinline__ uint32_t f8_pair(float a, float b) {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);

@@ -78,3 +78,41 @@ def test_waits_that_run_out_are_counted():
     for cycles in (1 << 40, -1):
         with pytest.raises(hk.HikonvError):
             hk.linear_f8_wait_check(cycles)
+
+
+@pytest.mark.parametrize("M,N", [(3, 130), (12, 128), (40, 130), (100, 256), (300, 257), (4096, 2048)])
+def test_scales_whose_product_leaves_the_normal_numbers(M, N):
+    # two blocks: a sum of 128 * 64 each
+    x, w = torch.full((M, 256), 8.0, device="cuda").to(E4M3), torch.full((N, 256), 8.0, device="cuda").to(E4M3)
+    xs, ws = torch.full((2, M), 1.3 * 2.0 ** -80, device="cuda"), torch.full((-(-N // 128), 2), 1.7 * 2.0 ** -66, device="cuda")
+    got = hk.linear_f8(x, w, xs, ws, out_dtype=torch.float32).double()
+    want = 2 * 128 * 64 * xs[0, 0].double() * ws[0, 0].double()
+    # each product of scales is a multiple of 2^-149, half of that off; the sum of two terms is rounded once
+    assert ((got - want).abs() <= 2 * 128 * 64 * 2.0 ** -150 + 2.0 ** -24 * want).all()
+    xs.fill_(2.0 ** 70), ws.fill_(2.0 ** 60)
+    assert torch.isinf(hk.linear_f8(x, w, xs, ws, out_dtype=torch.float32)).all()
+    x[:, :] = torch.zeros_like(x)
+    assert torch.isnan(hk.linear_f8(x, w, xs, ws, out_dtype=torch.float32)).all()
+
+
+@pytest.mark.parametrize("f8,most", [(E4M3, 448.0), (torch.float8_e5m2, 57344.0)])
+@pytest.mark.parametrize("K", [128, 200])
+def test_blocks_of_the_smallest_numbers(f8, most, K):
+    def blocks(v):
+        v = torch.tensor(v, dtype=torch.float64).float()   # subnormal numbers on the host, kept by a copy
+        x = torch.zeros(1, K)
+        x[0, : len(v)] = v
+        values, scale = hk.quantize_blocks(x.cuda(), f8)
+        return values.float().cpu()[0, : len(v)].tolist(), scale.cpu()[0, 0].item()
+
+    # a scale that rounds to one step of 2^-149 for up to one and a half: quotients above the largest number saturate
+    step = 2.0 ** -149
+    values, scale = blocks([1.4 * most * step, -1.4 * most * step, most * step / 2])
+    assert scale == step and values == [most, -most, most / 2]
+    # half a step and less: zeros, as for a block of zeros
+    for top in (most * step / 2, step, 0.0):
+        values, scale = blocks([top, -top])
+        assert scale == 0.0 and values == [0.0, 0.0]
+    # -0 is a zero of either sign
+    values, scale = blocks([-0.0, most])
+    assert scale == 1.0 and values == [0.0, most]
