@@ -18,7 +18,7 @@
 namespace hikonv {
 
 constexpr int kF8Rows = 128, kF8Depth = 128;
-constexpr int kF8MostStages = 12, kF8MostAccs = 8;
+constexpr int kF8MostStages = 12, kF8MostAccs = 4;
 constexpr int kF8FirstAdder = 4, kF8Adders = 8, kF8Threads = (kF8FirstAdder + kF8Adders) * 32;
 constexpr size_t kF8MostSmem = 226 * 1024;
 
@@ -54,11 +54,6 @@ __device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[32]) {
                    "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]),
                    "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]),
                    "=r"(v[30]), "=r"(v[31])
-                 : "r"(taddr));
-}
-__device__ __forceinline__ void f8_load(uint32_t taddr, uint32_t (&v)[64]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
                  : "r"(taddr));
 }
 // The wait for tcgen05.ld, which what it loaded goes through: no arithmetic on it can be moved in front.
@@ -125,14 +120,14 @@ __device__ __forceinline__ bool f8_stages_free(const F8Params &q, Ring ring, uin
 // a time, by a warp of their own, which runs ahead as far as the ring allows and waits for no copy: the copies themselves arrive at the slot's
 // barrier.  Asked for by the warps that add up, a step's scales took them 150 cycles.
 constexpr int kScaleBatch = 4, kScaleSlots = 4;         // steps of a slot; slots
-constexpr int kScaleBytes = (kScaleBatch * kF8Rows + 2 * kScaleBatch) * 4;       // of a slot: [step][row of x], [128-column block][step]
+constexpr int kScaleBytes = (kScaleBatch * kF8Rows + kScaleBatch) * 4;           // of a slot: [step][row of x], then [step] of w
 struct ScaleBars {
     uint64_t full[kScaleSlots], empty[kScaleSlots];
 };
 
-// `rows` rows of x from row0 on; `blocks` blocks of output columns, the first's scales at w, one block's behind the other's.
-__device__ __forceinline__ bool bring_scales(const F8Params &q, Ring &ring, uint32_t slots, uint32_t full, uint32_t empty, int row0, int rows, const float *w, int blocks,
-                                             int c0, int c1) {
+// `rows` rows of x from row0 on; the scales of the tile's output columns at w.
+__device__ __forceinline__ bool bring_scales(const F8Params &q, Ring &ring, uint32_t slots, uint32_t full, uint32_t empty, int row0, int rows, const float *w, int c0,
+                                             int c1) {
     const int lane = threadIdx.x & 31;
     const float *xs = q.p.x_scale + c0 * q.xs_row + row0 + lane;
     for (int c = c0; c < c1; c += kScaleBatch) {
@@ -147,8 +142,7 @@ __device__ __forceinline__ bool bring_scales(const F8Params &q, Ring &ring, uint
             }
             xs += q.xs_row;
         }
-        const int block = lane / kScaleBatch, at = c + lane % kScaleBatch;
-        if (block < blocks && at < c1) cp_async_4_at(slot + (kScaleBatch * kF8Rows + lane) * 4, w + block * q.chunks + at);
+        if (lane < kScaleBatch && c + lane < c1) cp_async_4_at(slot + (kScaleBatch * kF8Rows + lane) * 4, w + c + lane);
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * ring.stage) : "memory");
         ring.next(kScaleSlots);
     }
@@ -167,8 +161,8 @@ struct ScaleRing {
         return beat % kScaleBatch != 0 || f8_wait(q, full + 8 * (beat / kScaleBatch % kScaleSlots), beat / (kScaleBatch * kScaleSlots) & 1);
     }
     __device__ __forceinline__ uint32_t xs() const { return slots + beat / kScaleBatch % kScaleSlots * kScaleBytes + beat % kScaleBatch * (kF8Rows * 4); }
-    __device__ __forceinline__ uint32_t w(int block) const {
-        return slots + beat / kScaleBatch % kScaleSlots * kScaleBytes + (kScaleBatch * kF8Rows + block * kScaleBatch + beat % kScaleBatch) * 4;
+    __device__ __forceinline__ uint32_t w() const {
+        return slots + beat / kScaleBatch % kScaleSlots * kScaleBytes + (kScaleBatch * kF8Rows + beat % kScaleBatch) * 4;
     }
     // The step's scales have been read by this lane; `last`: of the tile.
     __device__ __forceinline__ void next(bool last) {
@@ -391,7 +385,7 @@ struct Adder {
         sums.clear();
         for (int c = 0; c < steps; ++c) {
             if (!scales.wait()) return false;
-            const float w = load_shared_float(scales.w(0));
+            const float w = load_shared_float(scales.w());
             const uint32_t xs = scales.xs();
             float s = w;
             if (TOKENS) {
@@ -612,7 +606,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             for (int t = t0; fine && t < tiles; t += step) {
                 const Tile tile = find_tile(q, tables, t, q.width);
                 const float *w = p.w_scale + ((long long)tile.e * q.w_blocks + tile.n0 / kF8Depth) * q.chunks;
-                fine = bring_scales(q, ring, stages + q.feed_off, HIKONV_BAR(scales.full, 0), HIKONV_BAR(scales.empty, 0), tile.row0, tile.rows, w, 1, c0, c1);
+                fine = bring_scales(q, ring, stages + q.feed_off, HIKONV_BAR(scales.full, 0), HIKONV_BAR(scales.empty, 0), tile.row0, tile.rows, w, c0, c1);
             }
             asm volatile("cp.async.wait_all;" ::: "memory");        // these copies are in no group that is waited for
         }
@@ -1079,7 +1073,7 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     q.b_off = kF8Rows * kF8Depth;
     q.stage_bytes = q.b_off + columns * kF8Depth;
     q.acc_cols = columns < 32 ? 32 : columns;
-    q.accs = 512 / q.acc_cols < 4 ? 512 / q.acc_cols : 4;
+    q.accs = 512 / q.acc_cols < kF8MostAccs ? 512 / q.acc_cols : kF8MostAccs;
     q.tmem_cols = q.accs * q.acc_cols;                   // a power of two
     const int feeds = kScaleSlots * kScaleBytes;
     const int turns = shape.tokens ? kF8Adders * 32 * 17 * 4 : 0;
@@ -1098,7 +1092,9 @@ static int launch_linear_f8(const LinearParams &p, int x_f8, int w_f8, long long
     const int a_type = shape.tokens ? x_f8 : w_f8, b_type = shape.tokens ? w_f8 : x_f8;
     q.idesc = (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(kF8Rows >> 4) << 24);
     // CTAs of a cluster wait for one another, and for tensor memory.  With two such kernels at once (two streams), each could hold the memory that the
-    // other's CTA waits for; with this much shared memory none shares its SM with another CTA that takes tensor memory.
+    // other's CTA waits for.  Registers keep them apart: 384 threads with 113 of them and more, those of hikonv_linear's tiles 60000 in all, so that
+    // no two CTAs with tensor memory are on one SM.  Should a compiler give them fewer, this much shared memory still keeps two with clusters apart; one
+    // without waits for nobody once it has its memory, but for the kernels before its own, whose CTAs all have theirs.
     size_t smem = (size_t)q.held + 2048 + tables;
     if (q.splits > 1 && smem < 184 * 1024) smem = 184 * 1024;
 
