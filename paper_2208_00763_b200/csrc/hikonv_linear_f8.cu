@@ -9,6 +9,7 @@
 // columns, any multiple of 16, and the CTAs of a cluster may share the depth of a tile).
 //
 // One CTA per SM walks over the tiles.  Warp 0 loads, warp 1 multiplies, warp 2 brings the scales, warps 4 to 11 add up and finish.
+#include <atomic>
 #include <cstddef>
 #include <cstring>
 
@@ -969,6 +970,20 @@ struct F8Shape {
     int nt, width, splits;
 };
 
+// Whether the kernel of pairs was given the registers that its warps ask for: one that waits for registers which are not there waits for good.  Pairs are no
+// choice where it was not, or where that cannot be asked.
+static bool pair_has_registers() {
+    static std::atomic<int> known{0};                    // 1: no, 2: yes
+    int k = known.load(std::memory_order_relaxed);
+    if (k == 0) {
+        cudaFuncAttributes a;
+        if (cudaFuncGetAttributes(&a, linear_f8_pair_kernel) != cudaSuccess) return false;
+        k = (a.numRegs + 7) / 8 * 8 * kPairThreads >= kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32 ? 2 : 1;
+        known.store(k, std::memory_order_relaxed);
+    }
+    return k == 2;
+}
+
 // The tile that a model of the time, in us, likes best: a set-up, and for each tile that a CTA or pair takes in turn its steps and its end, as measured
 // on weights from memory at depths of 512 to 16384.  A step of a tile of few rows is the round of its sums from the multiplies to the adding warps
 // and back, 0.265 us for 16 rows to 0.6 for 128; a shared depth has fewer steps and an exchange of sums.  4096 x 4096 weights: 16 rows 11.6 us,
@@ -997,20 +1012,12 @@ static F8Shape choose_f8_tile(const LinearParams &p, int sms) {
         consider(false, 128, kF8Rows, splits, 2.6, 0.6, 1.1);
     }
     consider(true, kF8Rows, 128, 1, 3.0, 0.37, 0.9);
+    const F8Shape single = best;
     consider(true, kPairRows, kPairWidth, 1, 4.5, 0.46, 1.3);
-    return best;
-}
-
-// Whether the kernel was given the registers that its warps ask for: one that waits for registers which are not there waits for good.
-static bool pair_has_registers() {
-    cudaFuncAttributes a;
-    if (cudaFuncGetAttributes(&a, linear_f8_pair_kernel) != cudaSuccess) return false;
-    return (a.numRegs + 7) / 8 * 8 * kPairThreads >= kPairAdderRegs * kPairAdders * 32 + kPairOtherRegs * kF8FirstAdder * 32;
+    return best.pair && !pair_has_registers() ? single : best;
 }
 
 static int launch_pair(F8Params q, int x_f8, int w_f8, cudaStream_t st) {
-    static const bool enough = pair_has_registers();
-    if (!enough) return HIKONV_ERR_CUDA;
     const LinearParams &p = q.p;
     const size_t tables = p.offsets ? (size_t)p.E * 12 : 0;
     const int feeds = kPairAdders * kPairAhead * 32 * 4, turns = kPairAdders * 32 * 17 * 4;
