@@ -582,7 +582,7 @@ int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, 
  * hikonv_rows_from_experts_grad - its gradient for y and the weights from the one for out (which the residual's is, too).
  *   grad_y[slots[t][j]] = weights[t][j] grad[t]; zeros in row -2 - slots[t][j] for slots below -1, so that every row is written when
  *      slots come from hikonv_sort_by_expert and R = T k.  Other rows of grad_y (of padding, of pairs whose slot was set to -1) are left as
- *      they were: where there are any, grad_y is zeroed before the call.  Rows outside 0 .. R - 1 are left out.
+ *      they were: hikonv_zero_other_rows makes them zeros.  Rows outside 0 .. R - 1 are left out.
  *   grad_weights[t][j] = sum_h grad[t][h] y[slots[t][j]][h], 32-bit sums in an order that depends on the sizes alone; 0 without a row
  *   weights and grad_weights: [T][k] float, or both NULL (then y is not read).
  * Outputs must overlap neither inputs nor each other.
@@ -590,6 +590,15 @@ int hikonv_rows_from_experts(const void *d_y, int type, long long y_row_stride, 
 int hikonv_rows_from_experts_grad(const void *d_grad, int type, long long grad_row_stride, const void *d_y, long long y_row_stride, int R,
                                   const int32_t *d_slots, const float *d_weights, int T, int k, int H, void *d_grad_y,
                                   long long grad_y_row_stride, float *d_grad_weights, void *stream);
+
+/*
+ * hikonv_zero_other_rows - zeros in the rows of a matrix that slots do not name, neither as a place nor as -2 - place; the other rows are left as
+ * they were.  In front of or behind hikonv_rows_from_experts_grad with the same slots, every row of grad_y is written.
+ *   rows: [R][H] elements of 2 or 4 bytes, row_stride (>= H) elements apart; it must not overlap slots.
+ * d_workspace: R bytes, which overlap neither, for one call at a time.  T k <= 2^30, H <= 2^23.
+ */
+int hikonv_zero_other_rows(const int32_t *d_slots, int T, int k, void *d_rows, int element_bytes, long long row_stride, int R, int H, void *d_workspace,
+                           size_t workspace_bytes, void *stream);
 
 /*
  * Matrix products of 8-bit floating point numbers with a scale for each block of 128 along the depth.

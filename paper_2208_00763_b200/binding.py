@@ -112,6 +112,7 @@ _SIGNATURES = {
     "hikonv_rows_to_experts": (_i, [_vp, _i, _ll, _vp, _i, _i, _i, _vp, _ll, _i, _vp]),
     "hikonv_rows_from_experts": (_i, [_vp, _i, _ll, _i, _vp, _vp, _i, _i, _i, _vp, _ll, _vp, _ll, _vp]),
     "hikonv_rows_from_experts_grad": (_i, [_vp, _i, _ll, _vp, _ll, _i, _vp, _vp, _i, _i, _i, _vp, _ll, _vp, _vp]),
+    "hikonv_zero_other_rows": (_i, [_vp, _i, _i, _vp, _i, _ll, _i, _i, _vp, _sz, _vp]),
     "hikonv_quantize_blocks": (_i, [_vp, _i, _ll, _i, _i, _i, _vp, _i, _i, _vp, _ll, _vp, _ll, _vp]),
     "hikonv_quantize_tiles": (_i, [_vp, _i, _ll, _i, _i, _i, _i, _vp, _ll, _vp, _vp]),
     "hikonv_linear_f8": (_i, [_vp, _i, _ll, _vp, _i, _ll, _i, _i, _i, _vp, _ll, _vp, _vp, _ll, ctypes.POINTER(EpilogueT), _vp]),
@@ -123,7 +124,8 @@ _SIGNATURES = {
 _FAST_ENTRY_POINTS = ("hikonv_conv1d", "hikonv_conv1d_dense", "hikonv_pack", "hikonv_conv2d", "hikonv_conv2d_dense",
                       "hikonv_conv2d_workspace_bytes", "hikonv_quantize_rows", "hikonv_linear", "hikonv_grouped_linear",
                       "hikonv_linear_workspace_bytes", "hikonv_sort_by_expert", "hikonv_sort_by_expert_workspace_bytes",
-                      "hikonv_rows_to_experts", "hikonv_rows_from_experts", "hikonv_rows_from_experts_grad", "hikonv_quantize_blocks",
+                      "hikonv_rows_to_experts", "hikonv_rows_from_experts", "hikonv_rows_from_experts_grad", "hikonv_zero_other_rows",
+                      "hikonv_quantize_blocks",
                       "hikonv_linear_f8", "hikonv_grouped_linear_f8")
 
 
@@ -806,14 +808,18 @@ def rows_from_experts(y: torch.Tensor, slots: torch.Tensor, weights: Optional[to
     return out
 
 
+# As in pyext/fast.cpp.  Zeros to 8 MB take 3 us, to 256 MB 70; finding the rows that no slot names 5.
+_ZERO_ALL_BYTES = 8 << 20
+
+
 def rows_from_experts_grad(grad: torch.Tensor, y: Optional[torch.Tensor], slots: torch.Tensor, weights: Optional[torch.Tensor] = None,
                            grad_y: Optional[torch.Tensor] = None, grad_weights: Optional[torch.Tensor] = None, stream=None) -> tuple:
     """The gradient of ``rows_from_experts``, from the one for its output: (grad_y, grad_weights).  ``grad_y[slots[t, j]]`` is
     ``weights[t, j] * grad[t]``, zeros in the places of pairs without expert; ``grad_weights[t, j]`` the product of ``grad[t]`` with the
     pair's row of ``y``, 0 without one.  Without weights ``y`` is not read (it may be None) and there is no grad_weights.  ``grad_y`` has the rows of
     ``y``, or one for each pair without it, and zeros where no slot names a row (padding of ``y``, a row whose pair was dropped by a slot of
-    -1): the call sets it to zero first.  In a ``grad_y`` that is given such rows are left as they were, and nothing is set to zero first: with
-    the slots of ``sort_by_expert`` every row of T k is written.  The residual's gradient is ``grad`` itself."""
+    -1).  In a ``grad_y`` that is given such rows are left as they were: with the slots of ``sort_by_expert`` there are none among T k rows.  The
+    residual's gradient is ``grad`` itself."""
     if stream is None:
         done = (_fast or _load_fast()).rows_from_experts_grad(grad, y, slots, weights, grad_y, grad_weights)
         if done is not None:
@@ -827,15 +833,22 @@ def rows_from_experts_grad(grad: torch.Tensor, y: Optional[torch.Tensor], slots:
         raise ValueError("grad_weights without weights")
     if weights is not None and y is None:
         raise ValueError("the gradient of weights needs y")
+    others = None
     if grad_y is None:
-        # the kernel writes the rows that slots name
-        grad_y = _empty((T * k if y is None else y.shape[0], H), grad.dtype, grad, stream, torch.zeros)
+        # rows that no slot names are zeros: all rows beforehand where that is cheap, else those alone
+        rows = T * k if y is None else y.shape[0]
+        small = rows * H * grad.element_size() <= _ZERO_ALL_BYTES
+        grad_y = _empty((rows, H), grad.dtype, grad, stream, torch.zeros if small else torch.empty)
+        others = None if small else _empty(rows, torch.uint8, grad, stream)
     grad_y_row = _rows(grad_y, "grad_y", (grad.dtype,), grad, (grad_y.shape[0] if grad_y.dim() == 2 else T * k, H))
     R = grad_y.shape[0]
     y_row = H if weights is None else _rows(y, "y", (grad.dtype,), grad, (R, H))
     if weights is not None and grad_weights is None:
         grad_weights = _empty((T, k), torch.float32, grad, stream)
     with torch.cuda.device(grad.device):
+        if others is not None:
+            _check(lib().hikonv_zero_other_rows(places, T, k, grad_y.data_ptr(), grad.element_size(), grad_y_row, R, H, others.data_ptr(), R,
+                                                _stream_of(grad, stream)), "hikonv_zero_other_rows")
         _check(lib().hikonv_rows_from_experts_grad(grad.data_ptr(), _FLOAT_TYPES[grad.dtype], grad_row, None if weights is None else y.data_ptr(),
                                                    y_row, R, places, _vector(weights, "weights", torch.float32, (T, k), grad), T, k, H,
                                                    grad_y.data_ptr(), grad_y_row,

@@ -35,6 +35,7 @@ decltype(&hikonv_sort_by_expert_workspace_bytes) g_sort_workspace_bytes = nullpt
 decltype(&hikonv_rows_to_experts) g_rows_to_experts = nullptr;
 decltype(&hikonv_rows_from_experts) g_rows_from_experts = nullptr;
 decltype(&hikonv_rows_from_experts_grad) g_rows_from_experts_grad = nullptr;
+decltype(&hikonv_zero_other_rows) g_zero_other_rows = nullptr;
 decltype(&hikonv_quantize_blocks) g_quantize_blocks = nullptr;
 decltype(&hikonv_linear_f8) g_linear_f8 = nullptr;
 decltype(&hikonv_grouped_linear_f8) g_grouped_linear_f8 = nullptr;
@@ -539,6 +540,8 @@ PyObject *rows_from_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+constexpr int64_t kZeroAllBytes = 8 << 20;             // as in binding.py
+
 // rows_from_experts_grad(grad, y, slots, weights, grad_y, grad_weights)
 PyObject *rows_from_experts_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&]() -> PyObject * {
@@ -550,9 +553,14 @@ PyObject *rows_from_experts_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::ScalarType type = grad->scalar_type();
         if (float_type(type) < 0 || (y && y->dim() != 2)) return nullptr;
         const int64_t T = grad->size(0), H = grad->size(1), k = slots->size(1);
-        at::Tensor made_y, made_w;
-        // zeros: the kernel writes the rows that slots name
-        if (!given_y) made_y = at::zeros({y ? y->size(0) : T * k, H}, at::TensorOptions().dtype(type).device(grad->device()));
+        at::Tensor made_y, made_w, others;
+        if (!given_y) {
+            // rows that no slot names are zeros: all rows beforehand where that is cheap, else those alone
+            const int64_t rows = y ? y->size(0) : T * k;
+            const bool small = rows * H * (int64_t)grad->element_size() <= kZeroAllBytes;
+            made_y = small ? at::zeros({rows, H}, at::TensorOptions().dtype(type).device(grad->device())) : empty({rows, H}, type, *grad);
+            if (!small) others = empty({rows}, at::kByte, *grad);
+        }
         if (weights && !given_w) made_w = empty({T, k}, at::kFloat, *grad);
         const at::Tensor &gy = given_y ? *given_y : made_y;
         const at::Tensor *gw = given_w ? given_w : weights ? &made_w : nullptr;
@@ -567,7 +575,11 @@ PyObject *rows_from_experts_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const float *w_ptr = (const float *)address(weights);
         void *gy_ptr = gy.data_ptr(), *st = current_stream();
         float *gw_ptr = (float *)address(gw);
+        void *others_ptr = others.defined() ? others.data_ptr() : nullptr;
+        const int size = (int)grad->element_size();
         if (unlocked([&] {
+                const int rc = others_ptr ? g_zero_other_rows(s_ptr, (int)T, (int)k, gy_ptr, size, grad_y_row, (int)R, (int)H, others_ptr, (size_t)R, st) : HIKONV_OK;
+                if (rc != HIKONV_OK) return rc;
                 return g_rows_from_experts_grad(g_ptr, float_type(type), grad_row, y_ptr, y_row, (int)R, s_ptr, w_ptr, (int)T, (int)k, (int)H, gy_ptr,
                                                 grad_y_row, gw_ptr, st);
             }) != HIKONV_OK)
@@ -691,6 +703,7 @@ PyObject *bind(PyObject *, PyObject *args) {
     else if (s == "hikonv_rows_to_experts") g_rows_to_experts = (decltype(g_rows_to_experts))ptr;
     else if (s == "hikonv_rows_from_experts") g_rows_from_experts = (decltype(g_rows_from_experts))ptr;
     else if (s == "hikonv_rows_from_experts_grad") g_rows_from_experts_grad = (decltype(g_rows_from_experts_grad))ptr;
+    else if (s == "hikonv_zero_other_rows") g_zero_other_rows = (decltype(g_zero_other_rows))ptr;
     else if (s == "hikonv_quantize_blocks") g_quantize_blocks = (decltype(g_quantize_blocks))ptr;
     else if (s == "hikonv_linear_f8") g_linear_f8 = (decltype(g_linear_f8))ptr;
     else if (s == "hikonv_grouped_linear_f8") g_grouped_linear_f8 = (decltype(g_grouped_linear_f8))ptr;

@@ -65,3 +65,18 @@ def test_workspace_of_a_sort():
 def test_sizes_beyond_32_bits(call):
     with pytest.raises(ValueError, match="2\\^31"):
         call(Matrix)
+
+
+A, B, C = (0x100000000000 + (i << 40) for i in range(3))
+OTHER = dict(slots=A, T=5, k=3, rows=B, size=2, row=64, R=15, H=64, ws=C, ws_bytes=15)
+
+
+@pytest.mark.parametrize("status,change", [
+    (hk.ERR_INVALID_ARG, dict(T=-1)), (hk.ERR_INVALID_ARG, dict(k=0)), (hk.ERR_INVALID_ARG, dict(size=1)), (hk.ERR_INVALID_ARG, dict(size=8)),
+    (hk.ERR_INVALID_ARG, dict(H=0)), (hk.ERR_INVALID_ARG, dict(R=-1)), (hk.ERR_INVALID_ARG, dict(slots=None)), (hk.ERR_INVALID_ARG, dict(rows=None)),
+    (hk.ERR_INVALID_ARG, dict(row=63)), (hk.ERR_INVALID_ARG, dict(row=1 << 50)), (hk.ERR_INVALID_ARG, dict(rows=B + 1)), (hk.ERR_INVALID_ARG, dict(slots=A + 2)),
+    (hk.ERR_UNSUPPORTED, dict(T=1 << 29)), (hk.ERR_UNSUPPORTED, dict(H=(1 << 23) + 1, row=1 << 24)), (hk.ERR_WORKSPACE, dict(ws=None)),
+    (hk.ERR_WORKSPACE, dict(ws_bytes=14)), (hk.ERR_INVALID_ARG, dict(ws=A + 59)), (hk.ERR_INVALID_ARG, dict(ws=B - 14)), (hk.ERR_INVALID_ARG, dict(rows=A + 8)),
+    (hk.OK, dict(R=0))])
+def test_refusals_of_zeros_in_other_rows(status, change):
+    assert hk.lib().hikonv_zero_other_rows(*{**OTHER, **change}.values(), None) == status

@@ -112,3 +112,67 @@ def test_rows_of_a_given_gradient_that_no_slot_names_stay():
     rest = torch.ones(R, dtype=torch.bool, device="cuda")
     rest[named] = False
     assert (given[rest] == 7.0).all() and not (given[~rest] == 7.0).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,k,R,H", [(300, 4, 1200, 4096), (300, 4, 1300, 4001), (1, 1, 9, 1 << 20), (2000, 2, 100000, 50), (70000, 2, 140000, 33), (0, 2, 3000, 2048), (500, 1, 100000, 133)])
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_gradient_of_large_rows_that_no_slot_names_is_zero(T, k, R, H, dtype, own_stream):
+    # beyond 8 MB the rows that no slot names are found
+    g = torch.Generator().manual_seed(T + R)
+    slots = torch.randperm(R, generator=g)[: T * k].reshape(T, k).int()
+    if T > 1:
+        slots[T // 2, 0], slots[T // 3, k - 1], slots[T - 1, 0] = -1, R + 3, -2 - slots[T - 1, 0]
+        slots[5:9, 0] = torch.tensor([-(1 << 31), (1 << 31) - 1, -2 - R, R], dtype=torch.int32)
+    slots, stream = slots.cuda(), torch.cuda.Stream() if own_stream else None
+    grad, y = torch.randn(T, H, device="cuda").to(dtype), torch.randn(R, H, device="cuda").to(dtype)
+    want, _ = hk.rows_from_experts_grad(grad, y, slots, grad_y=torch.zeros_like(y))
+    torch.cuda.synchronize()
+    nan_behind(R, H, dtype, stream)
+    for _ in range(2):
+        got, _ = hk.rows_from_experts_grad(grad, y, slots, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        got.fill_(float("nan"))
+        del got
+
+
+def test_large_gradient_in_a_graph_replayed_with_other_slots():
+    T, k, R, H = 400, 2, 1000, 4100
+    g = torch.Generator().manual_seed(0)
+    grad, y, weights = torch.randn(T, H, device="cuda"), torch.randn(R, H, device="cuda"), torch.rand(T, k, device="cuda")
+    slots = some_slots(T, k, R, g).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        hk.rows_from_experts_grad(grad, y, slots, weights)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, got_w = hk.rows_from_experts_grad(grad, y, slots, weights)
+    for _ in range(3):
+        slots.copy_(some_slots(T, k, R, g))
+        graph.replay()
+        want, want_w = hk.rows_from_experts_grad(grad, y, slots, weights, grad_y=torch.zeros_like(y))
+        assert torch.equal(got, want) and torch.equal(got_w, want_w)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,row,first", [(1, 1, 0), (3, 5, 1), (7, 7, 1), (8, 8, 0), (9, 24, 3), (64, 64, 0), (133, 140, 5), (4096, 4096, 1)])
+def test_zeros_in_other_rows_alone(H, row, first, dtype):
+    T, k, R = 50, 3, 400
+    slots = some_slots(T, k, R, torch.Generator().manual_seed(H)).cuda()
+    buf = torch.full((R * row + first + 8,), 7.0, dtype=dtype, device="cuda")
+    rows = buf[first:first + R * row].view(R, row)[:, :H]
+    space = torch.full((R + 1,), 1, dtype=torch.uint8, device="cuda")[1:]
+    status = hk.lib().hikonv_zero_other_rows(slots.data_ptr(), T, k, rows.data_ptr(), buf.element_size(), row, R, H, space.data_ptr(), R,
+                                             torch.cuda.current_stream().cuda_stream)
+    assert status == hk.OK
+    named = torch.where(slots >= 0, slots, -2 - slots).flatten()
+    named = named[(named >= 0) & (named < R)].long()
+    want = torch.full_like(buf, 7.0)
+    inner = want[first:first + R * row].view(R, row)
+    rest = torch.ones(R, dtype=torch.bool, device="cuda")
+    rest[named] = False
+    inner[:, :H][rest] = 0.0
+    assert torch.equal(buf, want)
