@@ -194,8 +194,8 @@ struct F8Control {
 // reciprocal normal for every result that an output could hold, and |v| counts as 98 beyond that (the sign's and the minimum's instruction is one), which
 // leaves infinite and NaN values to the last product.  Off by 2^-21.2 of the result at most over all values from -87 on (silu(): 2^-21.6), by 2^-17.4
 // below, where the reciprocal times 2^-14 is subnormal (silu(): the same); measured on every one of them.  Eleven instructions a value against silu()'s
-// 18, and one rounding of the whole exponent, two values to a reciprocal, has eleven, too, but is off by 2^-18 at -80: 32 groups of 16384 x 2048 x 4096 258 us
-// (silu() 265, the coarse form 251).
+// 18, and one rounding of the whole exponent, two values to a reciprocal, has eleven, too, but is off by 2^-18 at -80: 32 groups of 16384 x 2048 x 4096 260 us
+// (silu() 270, the coarse form 256).
 __device__ __forceinline__ float silu_short(float v) {
     float a, t, r;
     asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(a) : "f"(v), "f"(98.f));
@@ -667,7 +667,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 // A step is two multiplies of 128 columns each, which four warps each add up (every thread 128 sums): while one four load from tensor memory, the
 // other four add.  4096 x 16384 x 4096: 250 us in a burst, 300 back to back (1.8 P operations per second at 1.4 GHz by the power limit; 249
 // without reading tensor memory, 266 without additions).  A step takes 860 cycles, of which the tensor cores multiply for 512; a tile's begin and end 4900, with
-// SiLU 8300.  The adding warps ask for their scales themselves: a warp that brings them, as below 256 rows a tile, made no difference (298 us).
+// SiLU 8700.  The adding warps ask for their scales themselves: a warp that brings them, as below 256 rows a tile, made no difference (298 us).
 constexpr int kPairRows = 256, kPairWidth = 256, kPairHalf = 128, kPairStages = 6, kPairStage = 2 * kF8Rows * kF8Depth;
 constexpr int kPairAdders = 8, kPairThreads = (kF8FirstAdder + kPairAdders) * 32;
 // The sums take more registers than an even share: those of a thread that adds up, and of one that does not.  Together no more than the launch's,
@@ -708,8 +708,8 @@ __device__ __forceinline__ void store_then_arrive_at(uint32_t cluster_address, i
 }
 
 // A warp that adds up: a quarter of the lanes, 128 columns, 32 at a time.  Scales of x come by asynchronous copies, kPairAhead steps ahead, those of w
-// 32 steps at a time.  While 32 columns are added the next ones are on their way from tensor memory, those of the next step among them, whose barrier
-// is waited for before the last ones of a step are added.
+// 32 steps at a time.  A warp waits for 32 columns from tensor memory, then adds them; the other warp of its quarter of the SM, which has the other half
+// of the columns, adds meanwhile.  The scale of the next step is made before the last columns of a step are added.
 struct PairAdder {
     static constexpr int kChunk = 32;
     const F8Params &q;
