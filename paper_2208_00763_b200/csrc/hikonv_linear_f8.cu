@@ -564,14 +564,12 @@ __global__ void __launch_bounds__(kF8Threads, 1)
                     ring.next(q.stages);
                 }
             }
-            fine = fine && f8_stages_free(q, ring, HIKONV_BAR(empty, 0));
-            if (!fine) {
-                // what is in flight has to land before the memory goes: the last load of every stage
-                for (int i = 0; i < q.stages && i < loads; ++i) {
-                    ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
-                    if (ring.stage == q.stages - 1) ring.phase ^= 1;
-                    f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
-                }
+            // what is in flight has to land before the memory goes: the last load of every stage.  (The multiplies' last arrivals are at this CTA's own
+            // barriers, committed in front of those that the adding warps wait for.)
+            for (int i = 0; i < q.stages && i < loads; ++i) {
+                ring.stage = ring.stage ? ring.stage - 1 : q.stages - 1;
+                if (ring.stage == q.stages - 1) ring.phase ^= 1;
+                fine &= f8_wait(q, HIKONV_BAR(full, ring.stage), ring.phase);
             }
         } else if (warp == 1) {
             Ring ring, acc;

@@ -94,8 +94,12 @@ def test_no_copy_is_in_flight_behind_the_last_wait_of_a_pair():
 
 def test_the_source_has_these_waits():
     text = open(SOURCE).read()
-    # each kernel's loading warp waits for free stages behind its last load
-    assert len(re.findall(r"fine = fine && f8_stages_free\(q, ring, HIKONV_BAR\(empty, 0\)\);", text)) == 2
+    # in the kernel of pairs, whose multiplies arrive at both CTAs' barriers, each loading warp waits for free stages behind its last load
+    pairs = text[text.index("linear_f8_pair_kernel(const"):]
+    assert len(re.findall(r"fine = fine && f8_stages_free\(q, ring, HIKONV_BAR\(empty, 0\)\);", pairs)) == 1
+    # ... in the one of single CTAs the stages' arrivals are committed in front of the accumulators', which the adding warps wait for
+    single = text[text.index("linear_f8_kernel(const"):text.index("linear_f8_pair_kernel(const")]
+    assert single.index("tc_commit(HIKONV_BAR(empty, ring.stage));") < single.index("tc_commit(HIKONV_BAR(acc_full, acc.stage));")
     # the scales' copies are in no group: the wait behind them is the one that counts those
     scales = text[text.index("fine = bring_scales("):]
     assert scales.index('"cp.async.wait_all;"') < scales.index("if (q.splits > 1)")
